@@ -69,7 +69,8 @@ enum {
     BRA_ERR_WORKSPACE = -5,   /* ws is NULL, misaligned (256 B) or too small */
     BRA_ERR_UNSUPPORTED = -6, /* valid shape outside what the kernels are built for */
     BRA_ERR_LAUNCH = -7,      /* the HIP runtime reported an error at enqueue time */
-    BRA_ERR_TOO_LARGE = -8    /* bra_forward_static: the shape needs more than BRA_STATIC_SCRATCH_BYTES */
+    BRA_ERR_TOO_LARGE = -8,   /* bra_forward_static: the shape needs more than BRA_STATIC_SCRATCH_BYTES */
+    BRA_ERR_ALIGN = -9        /* bra_ffn_*, bra_norm_*, bra_adamw_step: a pointer is not aligned as its entry point asks */
 };
 
 typedef struct bra_shape {
@@ -205,6 +206,43 @@ int bra_backward_workspace_bytes(const bra_shape *shape, size_t *out_bytes);
 int bra_backward(const bra_shape *shape, const void *X, const void *Wqkv, const void *Wo,
                  const void *Wlce, const int32_t *Ir, const void *dY, void *dX, float *dWqkv,
                  float *dWo, float *dWlce, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gated feed-forward block, the gated form of the MLP half of a block:
+ *     G | U = X W1 + b1,   A = act(G) * U (elementwise),   Y = A W2 + b2
+ * X [M, C], W1 [C, 2 hidden] = [W^g | W^u] column blocks, b1 [2 hidden], W2 [hidden, C], b2 [C], Y [M, C];
+ * act: SILU g / (1 + e^-g) or GELU g Phi(g) (the exact form).  X, W1, W2, Y and `pre` have shape->dtype, the
+ * biases are float32; b1, b2 may be NULL (no bias).  pre_opt (or NULL) [M, 2 hidden] receives G | U, which the
+ * backward pass can be given.  M = 0 is allowed and does nothing.
+ * Any sizes; rows that are no multiple of 8 elements, and float32, take one more pass over the operands.  bf16: A is
+ * rounded to bf16 between the products, the rest is float32.  float32: products of three bf16 terms per operand
+ * (relative error of a product 2^-23); a value that is not finite, or above 3.3e38, makes NaN of what depends on it.
+ * Alignment: where C and hidden are multiples of 8 (4 for float32 outputs) all of X, W1, W2, Y, pre, dY, dX and the weight
+ * gradients must lie on 16 bytes, else on their element's size; BRA_ERR_ALIGN otherwise.
+ * Errors: NULL; SHAPE (M < 0, C or hidden < 1 or above 2^20, M above 2^30); DTYPE (dtype or act); WORKSPACE; ALIGN; LAUNCH. */
+enum { BRA_SILU = 0, BRA_GELU = 1 };                /* bra_ffn_shape.act */
+typedef struct bra_ffn_shape {
+    int64_t M;                /* tokens */
+    int32_t C, hidden;
+    int32_t dtype;            /* BRA_F32 or BRA_BF16 */
+    int32_t act;
+} bra_ffn_shape;
+
+int bra_ffn_workspace_bytes(const bra_ffn_shape *shape, size_t *out_bytes);
+int bra_ffn_forward(const bra_ffn_shape *shape, const void *X, const void *W1, const float *b1_opt, const void *W2,
+                    const float *b2_opt, void *Y, void *pre_opt, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of it.  With dY = dLoss/dY [M, C]:
+ *     dA = dY W2^T,  dG = dA * U * act'(G),  dU = dA * act(G),  dX = [dG|dU] W1^T,
+ *     dW1 = X^T [dG|dU],  dW2 = A^T dY,  db1 = column sums of dG|dU,  db2 = column sums of dY.
+ * pre_opt: G | U as the forward returned them; NULL: they are formed again from X, W1 and b1_opt, without being rounded (b1_opt is
+ * read in that case only).  dX has shape->dtype.  dW1 [C, 2 hidden], dW2 [hidden, C] and, if wanted, db1_opt [2 hidden] and
+ * db2_opt [C] have grad_dtype (BRA_F32 or BRA_BF16) and are OVERWRITTEN (with zeros where M = 0).  bf16: A, dG and dU
+ * are rounded to bf16 between the products.  No atomic adds: a repeat gives the same bits.
+ * Workspace: with or without `pre` the same size.  Errors as above. */
+int bra_ffn_backward_workspace_bytes(const bra_ffn_shape *shape, size_t *out_bytes);
+int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, const float *b1_opt, const void *W2,
+                     const void *pre_opt, const void *dY, void *dX, void *dW1, void *dW2, void *db1_opt, void *db2_opt,
+                     int32_t grad_dtype, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Optional per-launch timing, for benchmarks (Sec. "Limitation": the paper locates
  * BRA's cost in kernel launches and memory transactions, so the benchmark reports

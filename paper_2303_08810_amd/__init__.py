@@ -19,13 +19,16 @@ NATIVE_PATH = os.path.join(_HERE, "_native.so")
 
 BRA_F32, BRA_BF16 = 0, 1
 PATH_AUTO, PATH_GENERIC, PATH_MFMA = 0, 1, 2
+SILU, GELU = 0, 1
+_ACTS = {"silu": SILU, "gelu": GELU}
 _PATHS = {"auto": PATH_AUTO, "generic": PATH_GENERIC, "mfma": PATH_MFMA}
 
 STATIC_SCRATCH_BYTES = 32 << 20
 
 EXPORTS = ("bra_workspace_bytes", "bra_route", "bra_forward", "bra_forward_static", "bra_padded_workspace_bytes",
            "bra_forward_padded", "bra_backward_workspace_bytes", "bra_backward", "bra_block_workspace_bytes",
-           "bra_block_forward", "bra_strerror", "bra_version",
+           "bra_block_forward", "bra_ffn_workspace_bytes", "bra_ffn_forward", "bra_ffn_backward_workspace_bytes",
+           "bra_ffn_backward", "bra_strerror", "bra_version",
            "bra_profile_begin", "bra_profile_end", "bra_kernel_name", "bra_util_copy",
            "bra_util_read", "bra_util_mfma", "bra_util_mfma32")
 
@@ -35,6 +38,12 @@ class BraShape(ctypes.Structure):
                 ("C", ctypes.c_int32), ("heads", ctypes.c_int32), ("S", ctypes.c_int32),
                 ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("path", ctypes.c_int32)]
+
+
+class BraFfnShape(ctypes.Structure):
+    """bra_ffn_shape."""
+    _fields_ = [("M", ctypes.c_int64), ("C", ctypes.c_int32), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32)]
 
 
 class BraBlockParams(ctypes.Structure):
@@ -83,6 +92,14 @@ def lib() -> ctypes.CDLL:
         L.bra_block_forward.restype = ctypes.c_int
         L.bra_block_forward.argtypes = [ctypes.POINTER(BraShape), ctypes.c_int32, ctypes.c_float, vp,
                                         ctypes.POINTER(BraBlockParams), vp, vp, vp, vp, sz, vp]
+        L.bra_ffn_workspace_bytes.restype = ctypes.c_int
+        L.bra_ffn_workspace_bytes.argtypes = [ctypes.POINTER(BraFfnShape), ctypes.POINTER(sz)]
+        L.bra_ffn_forward.restype = ctypes.c_int
+        L.bra_ffn_forward.argtypes = [ctypes.POINTER(BraFfnShape)] + [vp] * 8 + [sz, vp]
+        L.bra_ffn_backward_workspace_bytes.restype = ctypes.c_int
+        L.bra_ffn_backward_workspace_bytes.argtypes = [ctypes.POINTER(BraFfnShape), ctypes.POINTER(sz)]
+        L.bra_ffn_backward.restype = ctypes.c_int
+        L.bra_ffn_backward.argtypes = [ctypes.POINTER(BraFfnShape)] + [vp] * 11 + [ctypes.c_int32, vp, sz, vp]
         L.bra_strerror.restype = ctypes.c_char_p
         L.bra_strerror.argtypes = [ctypes.c_int]
         L.bra_version.restype = ctypes.c_int
@@ -205,6 +222,32 @@ def bra_block_forward(X, params, S, k, heads, *, eps=1e-6, scale=None, Ir_in=Non
     the matrices in X's dtype, the vectors float32."""
     return (_native_module or _load_native()).block_forward(X, tuple(map(params.__getitem__, BraBlockParams.FIELDS)), S, k,
                                                        heads, eps, scale, Ir_in, want_Ir, _PATHS[path], ws, out)
+
+
+def make_ffn_shape(M, C, hidden, dtype, act="silu") -> BraFfnShape:
+    dt = {torch.float32: BRA_F32, torch.bfloat16: BRA_BF16}.get(dtype, dtype)
+    return BraFfnShape(M, C, hidden, int(dt), _ACTS[act])
+
+
+def ffn_workspace_bytes(shape: BraFfnShape, backward: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    query = lib().bra_ffn_backward_workspace_bytes if backward else lib().bra_ffn_workspace_bytes
+    _check(query(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def bra_ffn_forward(X, W1, W2, *, b1=None, b2=None, act="silu", want_pre=False, ws=None, out=None):
+    """Gated feed-forward block Y [.., C] = (act(G) * U) W2 + b2 with G | U = X W1 + b1; act: "silu" or "gelu".
+    X [.., C], W1 [C, 2 hidden] = [W^g | W^u] and W2 [hidden, C] of one dtype, b1 [2 hidden] and b2 [C] float32 or None.
+    want_pre: also G | U [.., 2 hidden], for the backward pass (see include/bra.h)."""
+    return (_native_module or _load_native()).ffn_forward(X, W1, W2, b1, b2, _ACTS[act], want_pre, ws, out)
+
+
+def bra_ffn_backward(X, W1, W2, dY, *, b1=None, pre=None, act="silu", bias_grads=False, grad_dtype=None, ws=None):
+    """Gradients of bra_ffn_forward: (dX, dW1, dW2), with bias_grads also db1 and db2.  dX has X's dtype, the others
+    grad_dtype (None: X's dtype).  pre: G | U as the forward returned them; without it they are formed again from X, W1 and b1."""
+    grads = -1 if grad_dtype is None else {torch.float32: BRA_F32, torch.bfloat16: BRA_BF16}[grad_dtype]
+    return (_native_module or _load_native()).ffn_backward(X, W1, W2, dY, b1, pre, _ACTS[act], bias_grads, grads, ws)
 
 
 def profile_begin(max_records: int) -> None:

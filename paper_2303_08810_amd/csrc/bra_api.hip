@@ -1,8 +1,10 @@
 // C-ABI entry points of libbra: argument checks and dispatch to a kernel family.
 #include "bra_common.h"
+#include "bra_ffn.h"
 
 #include <math.h>
 
+#include <initializer_list>
 #include <mutex>
 
 // Scratch memory of bra_forward_static: one copy per GPU, held by the code object until the
@@ -71,6 +73,32 @@ static int make_padded_dims(const bra_shape *s, Dims &Dp)
     p.H = (s->H + s->S - 1) / s->S * s->S;
     p.W = (s->W + s->S - 1) / s->S * s->S;
     return make_dims(&p, Dp);
+}
+
+static int make_ffn_sizes(const bra_ffn_shape *s, ffn::Sizes &S)
+{
+    if (!s) return BRA_ERR_NULL;
+    if (s->M < 0 || s->M > (1L << 30) || s->C < 1 || s->hidden < 1 || s->C > (1 << 20) || s->hidden > (1 << 20)) return BRA_ERR_SHAPE;
+    if (s->dtype != BRA_F32 && s->dtype != BRA_BF16) return BRA_ERR_DTYPE;
+    if (s->act != BRA_SILU && s->act != BRA_GELU) return BRA_ERR_DTYPE;
+    S.M = s->M; S.C = s->C; S.h = s->hidden; S.act = s->act;
+    S.f32 = s->dtype == BRA_F32;
+    S.Cp = (S.C + 7) / 8 * 8; S.hp = (S.h + 7) / 8 * 8;
+    return BRA_OK;
+}
+
+// Whether every pointer that is not NULL is a multiple of `bytes`.
+static bool aligned(size_t bytes, std::initializer_list<const void *> pointers)
+{
+    for (const void *p : pointers)
+        if ((uintptr_t)p % bytes != 0) return false;
+    return true;
+}
+
+// Alignment of the block's matrices: whole 16-byte pieces where the rows are, else elements.
+static size_t ffn_alignment(const ffn::Sizes &S)
+{
+    return S.C % 8 == 0 && S.h % 8 == 0 ? 16 : S.f32 ? 4 : 2;
 }
 
 static bool ws_ok(const void *ws, size_t have, size_t need)
@@ -268,6 +296,53 @@ int bra_block_forward(const bra_shape *shape, int32_t hidden, float eps, const v
                          (hipStream_t)hip_stream);
 }
 
+int bra_ffn_workspace_bytes(const bra_ffn_shape *shape, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    ffn::Sizes S;
+    const int rc = make_ffn_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = ffn_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_ffn_forward(const bra_ffn_shape *shape, const void *X, const void *W1, const float *b1, const void *W2, const float *b2, void *Y, void *pre, void *ws,
+                    size_t ws_bytes, void *hip_stream)
+{
+    ffn::Sizes S;
+    const int rc = make_ffn_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    if (S.M == 0) return BRA_OK;
+    if (!X || !W1 || !W2 || !Y) return BRA_ERR_NULL;
+    if (!aligned(ffn_alignment(S), {X, W1, W2, Y, pre}) || !aligned(4, {b1, b2})) return BRA_ERR_ALIGN;
+    if (!ws_ok(ws, ws_bytes, ffn_workspace_bytes(S))) return BRA_ERR_WORKSPACE;
+    return ffn_forward(S, X, W1, b1, W2, b2, Y, pre, ws, (hipStream_t)hip_stream);
+}
+
+int bra_ffn_backward_workspace_bytes(const bra_ffn_shape *shape, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    ffn::Sizes S;
+    const int rc = make_ffn_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = ffn_backward_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, const float *b1, const void *W2, const void *pre, const void *dY, void *dX, void *dW1,
+                     void *dW2, void *db1, void *db2, int32_t grad_dtype, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    ffn::Sizes S;
+    const int rc = make_ffn_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    if (grad_dtype != BRA_F32 && grad_dtype != BRA_BF16) return BRA_ERR_DTYPE;
+    if (!dW1 || !dW2 || (S.M > 0 && (!X || !W1 || !W2 || !dY || !dX))) return BRA_ERR_NULL;
+    if (!aligned(ffn_alignment(S), {X, W1, W2, pre, dY, dX}) || !aligned(4, {b1})) return BRA_ERR_ALIGN;
+    if (!aligned(ffn_alignment(S) == 16 ? 16 : grad_dtype == BRA_F32 ? 4 : 2, {dW1, dW2, db1, db2})) return BRA_ERR_ALIGN;
+    if (!ws_ok(ws, ws_bytes, ffn_backward_workspace_bytes(S))) return BRA_ERR_WORKSPACE;
+    return ffn_backward(S, X, W1, b1, W2, pre, dY, dX, dW1, dW2, db1, db2, grad_dtype == BRA_F32, ws, (hipStream_t)hip_stream);
+}
+
 const char *bra_strerror(int code)
 {
     switch (code) {
@@ -280,6 +355,7 @@ const char *bra_strerror(int code)
     case BRA_ERR_UNSUPPORTED: return "shape not supported by the requested kernel family";
     case BRA_ERR_LAUNCH: return "HIP runtime error while enqueueing";
     case BRA_ERR_TOO_LARGE: return "shape needs more scratch memory than the library's built-in buffer holds";
+    case BRA_ERR_ALIGN: return "a tensor is not aligned as its entry point asks";
     default: return "unknown error code";
     }
 }

@@ -1,0 +1,243 @@
+// Gated feed-forward block: Y = (act(X Wg + bg) * (X Wu + bu)) Wd + bd, W1 = [Wg | Wu].
+//
+//   k_operands    float32 operands as three bf16 terms, operands of odd sizes padded to multiples of 8 (other calls skip it)
+//   k_gated       A = act(G) * U with G | U = X W1 + b1: the tile's columns are half of G and half of U, so that a lane holds both of a
+//                 hidden unit and nothing but A (and, where the caller wants it, G | U) is written
+//   k_product     Y = A W2 + b2
+#include "bra_ffn.h"
+#include "bra_ffn_dev.h"
+
+namespace bra {
+namespace ffn {
+
+namespace {
+
+template <typename E>
+__global__ __launch_bounds__(256) void k_operands(Layouts J)
+{
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    int j = 0;
+    while (j < J.count && i >= J.end[j]) ++j;
+    if (j == J.count) return;
+    const Layout L = J.job[j];
+    const long p = i - (j ? J.end[j - 1] : 0);
+    const int per = L.cols_p / 8, piece = (int)(p % per);
+    const long line = p / per;                       // row * blocks + block
+    float v[8];
+    load8((const E *)L.src + line * L.cols + 8 * piece, v, L.cols - 8 * piece, false);
+    store_operand<sizeof(E) == 4 ? 3 : 1>(L.dst + line * L.cols_p + 8 * piece, L.plane, v);
+}
+
+template <class T, int TERMS, int ACT, typename E>
+__global__ __launch_bounds__(T::kThreads, 2) void k_gated(Operand X, Operand W1, const float *__restrict__ b1, E *__restrict__ pre, bf16_t *__restrict__ Act,
+                                                         long plane, long M, int h, int hp)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *lds = (bf16_t *)smem;
+    constexpr int BJ = T::BN / 2, PW = 16 * T::NT;       // hidden units of a tile, of a wavefront
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    int mt0, nt0;
+    tile_of(blockIdx.x, (int)((M + T::BM - 1) / T::BM), (hp + BJ - 1) / BJ, mt0, nt0);
+    const long m0 = (long)mt0 * T::BM;
+    const int j0 = nt0 * BJ, last = hp - 8 - j0, rows = (int)min((long)T::BM, M - m0);
+    const Loads<T, T::BM, false, false> la(wave, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, true, true> lb(wave, lane, W1.ld, [&](int col) {
+        const int w = col / (2 * PW), in = col % (2 * PW);
+        return (long)(min(w * PW + in % PW, last) + (in >= PW ? hp : 0));
+    });
+    f32x16 acc[T::NT][T::MT];
+    clear<T>(acc);
+    multiply<T, false, true, TERMS>(X, W1, X.p + m0 * X.ld, W1.p + j0, la, lb, 0, (X.K + 63) / 64, lds, acc);
+    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wj = (wave % T::WC) * PW;
+    const bool vec = h % 8 == 0;
+#pragma unroll
+    for (int nt = 0; nt < T::NT / 2; ++nt)
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
+            const int j = j0 + wj + 32 * nt + 16 * run + 8 * hi, n = h - j;
+            if (j >= hp) continue;
+            float bg[8], bu[8];
+            if (b1) {
+                load8(b1 + j, bg, n, false);
+                load8(b1 + h + j, bu, n, false);
+            } else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bg[e] = bu[e] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < T::MT; ++mt) {
+                const int row = wm + 32 * mt + c;
+                if (row >= rows) continue;
+                const size_t m = (size_t)(m0 + row);
+                float g[8], u[8], a[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g[e] = acc[nt][mt][8 * run + e] + bg[e];
+                    u[e] = acc[T::NT / 2 + nt][mt][8 * run + e] + bu[e];
+                    a[e] = e < n ? activation<ACT>(g[e]) * u[e] : 0.f;
+                }
+                if (pre) {
+                    store8(pre + m * 2 * h + j, g, n, vec);
+                    store8(pre + m * 2 * h + h + j, u, n, vec);
+                }
+                store_operand<TERMS>(Act + m * hp + j, plane, a);
+            }
+        }
+}
+
+template <class T, bool BO, int TERMS, typename E>
+__global__ __launch_bounds__(T::kThreads, 2) void k_product(Operand A, Operand Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *lds = (bf16_t *)smem;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    int mt0, nt0;
+    tile_of(blockIdx.x, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
+    const long m0 = (long)mt0 * T::BM;
+    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), last = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
+    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, last); });
+    f32x16 acc[T::NT][T::MT];
+    clear<T>(acc);
+    multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, 0, (A.K + 63) / 64, lds, acc);
+    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
+    const bool vec = N % 8 == 0;
+#pragma unroll
+    for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
+            const int col = n0 + wn + 32 * nt + 16 * run + 8 * hi, n = N - col;
+            if (n <= 0) continue;
+            float b[8];
+            if (bias) load8(bias + col, b, n, false);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[e] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < T::MT; ++mt) {
+                const int row = wm + 32 * mt + c;
+                if (row >= rows) continue;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e] + b[e];
+                store8(Out + (size_t)(m0 + row) * N + col, v, n, vec);
+            }
+        }
+}
+
+template <class T, bool BO, int TERMS, typename E>
+int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
+{
+    if (allow_lds<k_product<T, BO, TERMS, E>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
+    const long tiles = ((M + T::BM - 1) / T::BM) * ((N + T::BN - 1) / T::BN);
+    k_product<T, BO, TERMS, E><<<(unsigned)tiles, T::kThreads, T::kLds, st>>>(A, Bm, bias, (E *)Out, M, N);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+template <bool BO, int TERMS, typename E>
+int pick_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
+{
+    switch (tile_size(M, N)) {
+    case 256: return launch_product<Tile<256, 256, 2, 4>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 128: return launch_product<Tile<128, 128, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    default: return launch_product<Tile<64, 64, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    }
+}
+
+template <class T, int TERMS, int ACT, typename E>
+int launch_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, hipStream_t st)
+{
+    if (allow_lds<k_gated<T, TERMS, ACT, E>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
+    const long tiles = ((S.M + T::BM - 1) / T::BM) * ((S.hp + T::BN / 2 - 1) / (T::BN / 2));
+    k_gated<T, TERMS, ACT, E><<<(unsigned)tiles, T::kThreads, T::kLds, st>>>(X, W1, b1, (E *)pre, Act, plane, S.M, S.h, S.hp);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+template <int TERMS, int ACT, typename E>
+int pick_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, hipStream_t st)
+{
+    switch (tile_size(S.M, 2L * S.hp)) {
+    case 256: return launch_gated<Tile<256, 256, 2, 4>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    case 128: return launch_gated<Tile<128, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    default: return launch_gated<Tile<64, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    }
+}
+
+}  // namespace
+
+int product(const Operand &A, const Operand &Bm, bool outer, long M, int N, void *Out, const float *bias, bool f32, int kernel_id, hipStream_t st)
+{
+    ProfScope prof(st, kernel_id);
+    if (f32) return outer ? pick_product<true, 3, float>(A, Bm, M, N, Out, bias, st) : pick_product<false, 3, float>(A, Bm, M, N, Out, bias, st);
+    return outer ? pick_product<true, 1, bf16_t>(A, Bm, M, N, Out, bias, st) : pick_product<false, 1, bf16_t>(A, Bm, M, N, Out, bias, st);
+}
+
+int lay_out(const Layouts &J, bool f32, hipStream_t st)
+{
+    const long pieces = J.count ? J.end[J.count - 1] : 0;
+    if (!pieces) return BRA_OK;
+    ProfScope prof(st, K_FFN_OPERANDS);
+    const unsigned blocks = (unsigned)((pieces + 255) / 256);
+    if (f32) k_operands<float><<<blocks, 256, 0, st>>>(J);
+    else k_operands<bf16_t><<<blocks, 256, 0, st>>>(J);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+}  // namespace ffn
+
+using namespace ffn;
+
+namespace {
+
+// What the forward keeps in the workspace.
+struct ForwardPlan {
+    size_t X, W1, W2, Act, total;
+    ForwardPlan(const Sizes &S)
+    {
+        size_t at = 0;
+        auto take = [&](size_t elements) {
+            const size_t here = at;
+            at += align256(elements * S.terms() * sizeof(bf16_t));
+            return here;
+        };
+        X = S.copies() ? take((size_t)S.M * S.Cp) : 0;
+        W1 = S.copies() ? take((size_t)S.C * 2 * S.hp) : 0;
+        W2 = S.copies() ? take((size_t)S.h * S.Cp) : 0;
+        Act = take((size_t)S.M * S.hp);
+        total = at;
+    }
+};
+
+}  // namespace
+
+size_t ffn_workspace_bytes(const Sizes &S) { return ForwardPlan(S).total; }
+
+int ffn_forward(const Sizes &S, const void *X, const void *W1, const float *b1, const void *W2, const float *b2, void *Y, void *pre, void *ws, hipStream_t st)
+{
+    if (S.M == 0) return BRA_OK;
+    const ForwardPlan P(S);
+    auto at = [&](size_t offset) { return (bf16_t *)((char *)ws + offset); };
+    const long pX = S.M * S.Cp, pW1 = (long)S.C * 2 * S.hp, pW2 = (long)S.h * S.Cp, pA = S.M * S.hp;
+    if (S.copies()) {
+        Layouts J{};
+        add_layout(J, X, at(P.X), S.M, 1, S.C, S.Cp, pX);
+        add_layout(J, W1, at(P.W1), S.C, 2, S.h, S.hp, pW1);
+        add_layout(J, W2, at(P.W2), S.h, 1, S.C, S.Cp, pW2);
+        const int rc = lay_out(J, S.f32, st);
+        if (rc != BRA_OK) return rc;
+        X = at(P.X); W1 = at(P.W1); W2 = at(P.W2);
+    }
+    const Operand oX{(const bf16_t *)X, S.Cp, pX, S.Cp}, oW1{(const bf16_t *)W1, 2L * S.hp, pW1, S.C}, oW2{(const bf16_t *)W2, S.Cp, pW2, S.h},
+        oA{at(P.Act), S.hp, pA, S.hp};
+    int rc;
+    {
+        ProfScope prof(st, K_FFN_GATED);
+        if (S.f32) rc = S.act == BRA_SILU ? pick_gated<3, BRA_SILU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, st)
+                                          : pick_gated<3, BRA_GELU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, st);
+        else rc = S.act == BRA_SILU ? pick_gated<1, BRA_SILU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, st)
+                                    : pick_gated<1, BRA_GELU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, st);
+    }
+    if (rc != BRA_OK) return rc;
+    return product(oA, oW2, true, S.M, S.C, Y, b2, S.f32, K_FFN_PRODUCT, st);
+}
+
+}  // namespace bra

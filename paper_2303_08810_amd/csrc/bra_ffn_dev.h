@@ -1,0 +1,302 @@
+// Building blocks of the gated feed-forward block's products (internal).
+//
+// A tile of BM rows m x BN columns n of a product, the contraction in chunks of 64 that direct loads bring into one of two
+// buffers in LDS while the other is multiplied.  Either operand may lie with the contraction axis inside (rows of k) or
+// outside (rows of m or n): the second kind is read by the transposing LDS read, so that no product of the forward or the
+// backward pass needs a transposed copy.  The product is formed transposed (rows n, columns m of the 32x32x16 instruction), the two
+// middle bits of n exchanged, so that a lane ends up with 8 consecutive columns of one row.
+// float32 operands enter as three exact bf16 terms hi + mid + lo, each a plane of its own in memory; the six products of terms whose
+// sizes matter (2^-24 of the product is left out) are further rounds over the contraction into the same accumulators, the small
+// ones first.  On the float32 matrix instruction a product would take 16 bf16 ones' time, this way it takes 6.
+#pragma once
+
+#include "bra_attn_dev.h"
+#include "bra_ffn.h"
+
+#include <atomic>
+
+namespace bra {
+namespace ffn {
+
+using namespace mfma;
+
+// What chunks read beyond the contraction's end.
+alignas(16) static __device__ bf16_t zeros[8];
+
+// BM x BN outputs by WR x WC wavefronts, MT x NT 32 x 32 tiles each.
+template <int BM_, int BN_, int WR_, int WC_>
+struct Tile {
+    static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, kWaves = WR * WC, kThreads = 64 * kWaves;
+    static constexpr int MT = BM / (32 * WR), NT = BN / (32 * WC);
+    static constexpr int kChunkA = BM * 64, kChunkB = BN * 64;                  // elements of a chunk
+    static constexpr size_t kLds = 2 * (size_t)(kChunkA + kChunkB) * 2;
+};
+
+// Swizzle of the 16-byte pieces of a row: by rows of k where the contraction is outside (the four rows that a transposing
+// read touches lie in different quarters of the banks), else differently for the 8 rows that 8 lanes next to each other read.
+template <int B>
+__device__ __forceinline__ int turn_outer(int k) { return B >= 128 ? 4 * (k % 4) : 4 * (k / 2 % 2); }
+template <bool PERMUTED>
+__device__ __forceinline__ int turn_inner(int row) { return PERMUTED ? row % 4 + row / 8 % 2 * 4 : row % 8; }
+
+// A wavefront's direct loads of one operand's chunks: B rows (or columns) of the tile, OUTER: contraction outside.
+template <class T, int B, bool OUTER, bool PERMUTED>
+struct Loads {
+    static constexpr int L = B / 8 / T::kWaves, CH = B / 8, RPI = 64 / CH;
+    static_assert(L * 8 * T::kWaves == B, "a chunk is a whole number of loads per wavefront");
+    unsigned off[L];                    // bytes from the chunk's origin
+    // at(i): where row (column) i of the tile lies, relative to the origin; for OUTER asked for multiples of 8
+    template <class F>
+    __device__ __forceinline__ Loads(int wave, int lane, long ld, F at)
+    {
+#pragma unroll
+        for (int u = 0; u < L; ++u) {
+            if (OUTER) {
+                const int k = RPI * (wave * L + u) + lane / CH;
+                off[u] = 2u * (unsigned)(k * ld + at(8 * ((lane % CH) ^ turn_outer<B>(k))));
+            } else {
+                const int row = 8 * (wave * L + u) + lane / 8;
+                off[u] = 2u * (unsigned)(at(row) * ld + 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row)));
+            }
+        }
+    }
+    // chunk whose first element is `origin` (the same for all lanes), `left` of the contraction from there on, to LDS address `at`
+    __device__ __forceinline__ void request(const bf16_t *origin, int left, unsigned at, int wave, int lane) const
+    {
+        if (left >= 64) {
+#pragma unroll
+            for (int u = 0; u < L; ++u) load_to_lds_untracked(origin, off[u], at + 1024 * (wave * L + u));
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < L; ++u) {
+            const int row = 8 * (wave * L + u) + lane / 8;
+            const int k = OUTER ? RPI * (wave * L + u) + lane / CH : 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row));
+            const bf16_t *p = (const bf16_t *)((const char *)origin + off[u]);
+            load_to_lds_untracked(k < left ? p : zeros, at + 1024 * (wave * L + u));
+        }
+    }
+};
+
+// Operand of the matrix instruction: 32 rows (columns) from `first` on of the chunk, step ks of 16.
+template <int B, bool OUTER, bool PERMUTED>
+__device__ __forceinline__ bf16x8 fragment(const bf16_t *S, int first, int ks, int lane)
+{
+    const int h = lane / 32, c = lane % 32;
+    if (!OUTER) {
+        const int row = first + (PERMUTED ? (c & 0x13) + ((c & 4) << 1) + ((c & 8) >> 1) : c);
+        return *(const bf16x8 *)(S + row * 64 + 8 * ((2 * ks + h) ^ turn_inner<PERMUTED>(row)));
+    }
+    // lane s of a 16-lane group q gives the address of 4 columns of row k
+    const int s = lane % 16, q = lane / 16, col4 = PERMUTED ? (s % 2) * 2 + s % 4 / 2 : s % 4;
+    u32x2 r[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int k = 16 * ks + 8 * (q / 2) + 4 * half + s / 4, o = first + 16 * (q % 2) + 4 * col4;
+        r[half] = __builtin_bit_cast(u32x2, lds_read_tr16(S + k * B + 8 * ((o / 8) ^ turn_outer<B>(k)) + o % 8));
+    }
+    return __builtin_bit_cast(bf16x8, u32x4{r[0][0], r[0][1], r[1][0], r[1][1]});
+}
+
+template <class T>
+__device__ __forceinline__ void clear(f32x16 (&acc)[T::NT][T::MT])
+{
+#pragma unroll
+    for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[nt][mt][e] = 0.f;
+}
+
+// acc += A^T-or-A B over the contraction's chunks [first, end).  a0, b0: origins of the tile at k = 0 in the first plane.
+// One barrier per chunk: it stands in the middle of the chunk's last quarter, whose operands are in registers by then, so that
+// the buffer just read is free for the chunk after next, and the next chunk, requested one chunk's time ago, is there; the quarter's
+// second half of products runs while the next chunk's first operands are read.
+template <class T, bool AO, bool BO, int TERMS>
+__device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, const bf16_t *a0, const bf16_t *b0, const Loads<T, T::BM, AO, false> &la,
+                                         const Loads<T, T::BN, BO, true> &lb, int first, int end, bf16_t *lds, f32x16 (&acc)[T::NT][T::MT])
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
+    const unsigned base = lds_address(lds);
+    constexpr unsigned kBuffer = 2 * (T::kChunkA + T::kChunkB);
+    const int rounds = end - first, total = TERMS == 1 ? rounds : 6 * rounds;
+    auto request = [&](int chunk, int buffer) {
+        long pa = 0, pb = 0;
+        int c = chunk;
+        if (TERMS > 1) {
+            const int round = chunk / rounds;
+            c -= round * rounds;
+            // (lo, hi), (hi, lo), (mid, mid), (mid, hi), (hi, mid), (hi, hi)
+            pa = ((0x001102 >> (4 * round)) & 3) * A.plane;
+            pb = ((0x010120 >> (4 * round)) & 3) * Bm.plane;
+        }
+        const int k0 = 64 * (first + c);
+        la.request(a0 + pa + (AO ? k0 * A.ld : (long)k0), A.K - k0, base + buffer * kBuffer, wave, lane);
+        lb.request(b0 + pb + (BO ? k0 * Bm.ld : (long)k0), Bm.K - k0, base + buffer * kBuffer + 2 * T::kChunkA, wave, lane);
+    };
+    bf16x8 xf[2][T::MT], wf[2][T::NT];
+    auto read = [&](int buffer, int ks, int to) {
+        const bf16_t *As = lds + buffer * (T::kChunkA + T::kChunkB), *Bs = As + T::kChunkA;
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt) wf[to][nt] = fragment<T::BN, BO, true>(Bs, wn + 32 * nt, ks, lane);
+#pragma unroll
+        for (int mt = 0; mt < T::MT; ++mt) xf[to][mt] = fragment<T::BM, AO, false>(As, wm + 32 * mt, ks, lane);
+    };
+    auto products = [&](int from, int mt0, int mt1) {
+#pragma unroll
+        for (int mt = mt0; mt < mt1; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < T::NT; ++nt) acc[nt][mt] = mfma32(wf[from][nt], xf[from][mt], acc[nt][mt]);
+    };
+    constexpr int kHalf = (T::MT + 1) / 2;
+    constexpr int kLoads = Loads<T, T::BM, AO, false>::L + Loads<T, T::BN, BO, true>::L;
+    __builtin_amdgcn_s_barrier();                  // the buffers are free
+    request(0, 0);
+    if (total > 1) {
+        request(1, 1);
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read(0, 0, 0);
+    for (int i = 0; i < total; ++i) {
+        const int buffer = i & 1;
+#pragma unroll
+        for (int ks = 0; ks < 3; ++ks) {
+            read(buffer, ks + 1, (ks + 1) & 1);
+            __builtin_amdgcn_sched_barrier(0);
+            products(ks & 1, 0, T::MT);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        products(1, 0, kHalf);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + 1 < total) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (i + 2 < total) request(i + 2, buffer);
+            read(buffer ^ 1, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        products(1, kHalf, T::MT);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // the wait between the last products and the first use of their results, spelled out: where a branch lies between them the
+    // compiler has left it short
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tile (m, n) of workgroup `block`: an XCD takes neighbouring tiles, in groups of 4 tiles along m, so that what its workgroups read at the
+// same time fits its L2.
+__device__ __forceinline__ void tile_of(int block, int mtiles, int ntiles, int &m, int &n)
+{
+    const int tiles = mtiles * ntiles, xcd = block % 8, per = tiles / 8, rest = tiles % 8;
+    const int i = xcd * per + min(xcd, rest) + block / 8;
+    const int group = 4 * ntiles, g = i / group, m0 = 4 * g, ms = min(4, mtiles - m0), r = i - g * group;
+    m = m0 + r % ms;
+    n = r / ms;
+}
+
+// 8 consecutive values; `n` of them exist, `vec`: in whole 16-byte pieces.
+__device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8], int n, bool vec)
+{
+    if (vec && n >= 8) {
+        *(u32x4 *)p = __builtin_bit_cast(u32x4, pack8(v));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = f32_to_bf16(v[e]);
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8], int n, bool vec)
+{
+    if (vec && n >= 8) {
+        *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = v[e];
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8], int n, bool vec)
+{
+    if (vec && n >= 8) {
+        const u32x4 t = *(const u32x4 *)p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[2 * e] = bf16_lo(t[e]); v[2 * e + 1] = bf16_hi(t[e]); }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? bf16_to_f32(p[e]) : 0.f;
+}
+__device__ __forceinline__ void load8(const float *p, float (&v)[8], int n, bool vec)
+{
+    if (vec && n >= 8) {
+        const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+}
+
+// 8 values of an operand that a later product reads: one bf16 rounding, or three terms.
+template <int TERMS>
+__device__ __forceinline__ void store_operand(bf16_t *p, long plane, const float (&v)[8])
+{
+    if (TERMS == 1) {
+        *(bf16x8 *)p = pack8(v);
+        return;
+    }
+    bf16x8 t[3];
+    split3(v, t);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *(bf16x8 *)(p + q * plane) = t[q];
+}
+
+// The activations' distribution functions: act(g) = g F(g), act'(g) = F(g) + g F'(g).
+//   silu: F = 1 / (1 + e^-g), F' = F (1 - F);  gelu: F = Phi, F' = e^(-g^2 / 2) / sqrt(2 pi).
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)); }
+
+template <int ACT>
+__device__ __forceinline__ float activation(float g)
+{
+    return ACT == BRA_SILU ? g * sigmoid(g) : gelu_f32(g);
+}
+
+template <int ACT>
+__device__ __forceinline__ void activation_slope(float g, float &a, float &slope)
+{
+    if (ACT == BRA_SILU) {
+        const float f = sigmoid(g);
+        a = g * f;
+        slope = f + a * (1.f - f);
+    } else {
+        const float f = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+        a = g * f;
+        slope = f + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
+    }
+}
+
+// Allows a kernel's LDS beyond 64 KB, once per device.
+template <auto kernel>
+inline int allow_lds(size_t bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return BRA_ERR_LAUNCH;
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_acquire) & bit)) return BRA_OK;
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return BRA_ERR_LAUNCH;
+    done.fetch_or(bit, std::memory_order_release);
+    return BRA_OK;
+}
+
+}  // namespace ffn
+}  // namespace bra

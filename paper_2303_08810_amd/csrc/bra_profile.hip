@@ -17,6 +17,8 @@ const char *const kNames[K_COUNT] = {
     "gen_gemm_wo", "mfma_prep", "mfma_qkv", "mfma_attention", "mfma_pool_qk", "mfma_route_rows",
     "mfma_fused_k1", "mfma_attn_small", "mfma_lce_add", "mfma_wo",
     "block_pos_ln", "block_add_ln", "block_mlp_in", "block_mlp_out", "block_mlp_fused", "gen_backward",
+    "ffn_operands", "ffn_gated", "ffn_product", "ffn_few", "ffn_hidden_grads", "ffn_weight_grads", "ffn_sums",
+    "norm", "norm_backward", "norm_sums", "adamw",
 };
 }  // namespace
 

@@ -5,6 +5,7 @@
 // Functions here take every argument by position; the Python functions of the package give them their names and
 // defaults.  No kernel lives here and nothing is computed.
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
@@ -384,6 +385,108 @@ PyObject *py_block_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// A matrix or vector of the operators below, if it is there: on X's GPU, dense, of the type and the shape.
+void same_place(const at::Tensor *t, const at::Tensor &X, at::ScalarType type, std::initializer_list<int64_t> dims, const char *text)
+{
+    if (t && !(t->is_cuda() && t->is_contiguous() && t->device() == X.device() && t->scalar_type() == type && dims_are(*t, dims))) value_error(text);
+}
+
+bool like(const at::Tensor &t, const at::Tensor &X)
+{
+    return t.is_cuda() && t.is_contiguous() && t.device() == X.device() && t.scalar_type() == X.scalar_type() && t.sizes().equals(X.sizes());
+}
+
+// The caller's workspace, or one of `bytes` on X's GPU.
+const at::Tensor *workspace(const at::Tensor *ws, size_t bytes, const at::Tensor &X, at::Tensor &own)
+{
+    if (!ws) {
+        own = scratch(bytes, X);
+        return &own;
+    }
+    if (!(ws->is_cuda() && ws->is_contiguous() && ws->device() == X.device() && ws->scalar_type() == at::kByte)) value_error("ws must be a contiguous uint8 tensor on X's GPU");
+    return ws;
+}
+
+// The gated block's operands; X [.., C].
+bra_ffn_shape ffn_shape(const at::Tensor &X, const at::Tensor &W1, const at::Tensor &W2, const at::Tensor *b1, const at::Tensor *b2, PyObject *act)
+{
+    if (X.dim() < 1) value_error("X must be [.., C]");
+    same_kind(X, X);
+    const int64_t C = X.size(-1), h = W2.dim() == 2 ? W2.size(0) : 0;
+    same_kind(W1, X);
+    same_kind(W2, X);
+    if (!dims_are(W2, {h, C})) value_error("W2 must be [hidden, C]");
+    if (!dims_are(W1, {C, 2 * h})) value_error("W1 must be [C, 2 hidden]");
+    same_place(b1, X, at::kFloat, {2 * h}, "b1 must be a contiguous float32 [2 hidden] tensor on X's GPU");
+    same_place(b2, X, at::kFloat, {C}, "b2 must be a contiguous float32 [C] tensor on X's GPU");
+    if (C < 1 || h < 1 || C > INT32_MAX || h > INT32_MAX) check(BRA_ERR_SHAPE);
+    return bra_ffn_shape{X.numel() / C, (int32_t)C, (int32_t)h, dtype_of(X), integer(act)};
+}
+
+// ffn_forward(X, W1, W2, b1, b2, act, want_pre, ws, out)
+PyObject *py_ffn_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 9, [&]() -> PyObject * {
+        const at::Tensor &X = need(a[0]), &W1 = need(a[1]), &W2 = need(a[2]);
+        const at::Tensor *b1 = tensor(a[3]), *b2 = tensor(a[4]), *out = tensor(a[8]);
+        const bra_ffn_shape s = ffn_shape(X, W1, W2, b1, b2, a[5]);
+        if (out && !like(*out, X)) value_error("out must be a contiguous tensor of X's shape and dtype on X's GPU");
+        const c10::DeviceGuard guard(X.device());
+        size_t bytes = 0;
+        check(bra_ffn_workspace_bytes(&s, &bytes));
+        at::Tensor own, Y = out ? *out : at::empty_like(X), pre;
+        const at::Tensor *ws = workspace(tensor(a[7]), bytes, X, own);
+        const bool want_pre = PyObject_IsTrue(a[6]);
+        if (want_pre) {
+            auto sizes = X.sizes().vec();
+            sizes.back() = 2 * (int64_t)s.hidden;
+            pre = at::empty(sizes, X.options());
+        }
+        void *st = stream_of(X);
+        run([&] {
+            return bra_ffn_forward(&s, X.data_ptr(), W1.data_ptr(), (const float *)data(b1), W2.data_ptr(), (const float *)data(b2), Y.data_ptr(),
+                                   want_pre ? pre.data_ptr() : nullptr, ws->data_ptr(), (size_t)ws->numel(), st);
+        });
+        PyObject *y;
+        if (out) Py_INCREF(y = a[8]);
+        else y = wrap(Y);
+        return want_pre ? tuple({y, wrap(pre)}) : y;
+    });
+}
+
+// ffn_backward(X, W1, W2, dY, b1, pre, act, bias_grads, grad_dtype or -1, ws)
+PyObject *py_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&]() -> PyObject * {
+        const at::Tensor &X = need(a[0]), &W1 = need(a[1]), &W2 = need(a[2]), &dY = need(a[3]);
+        const at::Tensor *b1 = tensor(a[4]), *pre = tensor(a[5]);
+        const bra_ffn_shape s = ffn_shape(X, W1, W2, b1, nullptr, a[6]);
+        if (!like(dY, X)) value_error("dY must be a contiguous tensor of X's shape and dtype on X's GPU");
+        if (pre && !(pre->is_cuda() && pre->is_contiguous() && pre->device() == X.device() && pre->scalar_type() == X.scalar_type() && pre->dim() >= 1 &&
+                     pre->size(-1) == 2 * (int64_t)s.hidden && pre->numel() == 2 * s.hidden * s.M))
+            value_error("pre must be what bra_ffn_forward returned: contiguous [.., 2 hidden] of X's dtype on X's GPU");
+        const c10::DeviceGuard guard(X.device());
+        size_t bytes = 0;
+        check(bra_ffn_backward_workspace_bytes(&s, &bytes));
+        const int asked = integer(a[8]), kind = asked < 0 ? s.dtype : asked;
+        const auto options = X.options().dtype(kind == BRA_F32 ? at::kFloat : at::kBFloat16);
+        const bool biases = PyObject_IsTrue(a[7]);
+        at::Tensor own, dX = at::empty_like(X), dW1 = at::empty(W1.sizes(), options), dW2 = at::empty(W2.sizes(), options), db1, db2;
+        if (biases) {
+            db1 = at::empty({2 * (int64_t)s.hidden}, options);
+            db2 = at::empty({(int64_t)s.C}, options);
+        }
+        const at::Tensor *ws = workspace(tensor(a[9]), bytes, X, own);
+        void *st = stream_of(X);
+        run([&] {
+            return bra_ffn_backward(&s, X.data_ptr(), W1.data_ptr(), (const float *)data(b1), W2.data_ptr(), data(pre), dY.data_ptr(), dX.data_ptr(), dW1.data_ptr(),
+                                    dW2.data_ptr(), biases ? db1.data_ptr() : nullptr, biases ? db2.data_ptr() : nullptr, kind, ws->data_ptr(), (size_t)ws->numel(), st);
+        });
+        if (biases) return tuple({wrap(dX), wrap(dW1), wrap(dW2), wrap(db1), wrap(db2)});
+        return tuple({wrap(dX), wrap(dW1), wrap(dW2)});
+    });
+}
+
 PyMethodDef methods[] = {
     {"init", (PyCFunction)(void *)py_init, METH_FASTCALL, nullptr},
     {"route", (PyCFunction)(void *)py_route, METH_FASTCALL, nullptr},
@@ -392,6 +495,8 @@ PyMethodDef methods[] = {
     {"forward_padded", (PyCFunction)(void *)py_forward_padded, METH_FASTCALL, nullptr},
     {"backward", (PyCFunction)(void *)py_backward, METH_FASTCALL, nullptr},
     {"block_forward", (PyCFunction)(void *)py_block_forward, METH_FASTCALL, nullptr},
+    {"ffn_forward", (PyCFunction)(void *)py_ffn_forward, METH_FASTCALL, nullptr},
+    {"ffn_backward", (PyCFunction)(void *)py_ffn_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
