@@ -70,6 +70,7 @@ enum {
     BRA_ERR_UNSUPPORTED = -6, /* valid shape outside what the kernels are built for */
     BRA_ERR_LAUNCH = -7,      /* the HIP runtime reported an error at enqueue time */
     BRA_ERR_TOO_LARGE = -8,   /* bra_forward_static: the shape needs more than BRA_STATIC_SCRATCH_BYTES */
+    BRA_ERR_OVERLAP = -10,    /* bra_adamw_step: parameters that share memory */
     BRA_ERR_ALIGN = -9        /* bra_ffn_*, bra_norm_*, bra_adamw_step: a pointer is not aligned as its entry point asks */
 };
 
@@ -243,6 +244,92 @@ int bra_ffn_backward_workspace_bytes(const bra_ffn_shape *shape, size_t *out_byt
 int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, const float *b1_opt, const void *W2,
                      const void *pre_opt, const void *dY, void *dX, void *dW1, void *dW2, void *db1_opt, void *db2_opt,
                      int32_t grad_dtype, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Norms before and after a block, fused with its gate, its residual scale and the residual sum: with a residual stream X
+ * and a block's output Y,
+ *     R = X + scale * gate[row / (rows / groups)] * post(Y),   N = norm(R)
+ *     norm(t)  = (t - mean) / sqrt(variance + eps) * gamma + beta          BRA_LAYERNORM (biased variance, over the C channels)
+ *              = t / sqrt(mean of squares + eps) * gamma + beta            BRA_RMSNORM
+ *     post(t)  = the same with post_gamma, post_beta; the identity where post_gamma is NULL
+ * R goes on as the residual stream, N into the next block.  X, Y, R, N [rows, C] and gate [groups, C] have shape->dtype, the vectors are
+ * float32 [C].  Any of them may be absent (NULL): scale and gate (factors 1), beta and post_beta (0); Y (then R is X: pass R = NULL,
+ * only N is written); gamma (then N is not formed: pass N = NULL).  Statistics and sums are float32, N is that of the float32 sum,
+ * not of the rounded R.  R may be X or Y.  groups divides rows.  Rows of zeros give N = beta.
+ * Any C up to 8192; rows that are no multiple of 16 bytes are read by elements.  Alignment: elements.
+ * Errors: NULL; SHAPE (rows < 0 or above 2^30, C < 1, groups < 1 or not a divisor of rows, eps < 0); DTYPE (dtype or kind);
+ * UNSUPPORTED (C > 8192); ALIGN; LAUNCH. */
+enum { BRA_LAYERNORM = 0, BRA_RMSNORM = 1 };        /* bra_norm_shape.kind */
+typedef struct bra_norm_shape {
+    int64_t rows;
+    int32_t groups;           /* rows of the gate; 1 where there is none */
+    int32_t C;
+    int32_t dtype;            /* BRA_F32 or BRA_BF16 */
+    int32_t kind;
+    float eps;
+} bra_norm_shape;
+typedef struct bra_norm_params {        /* a HOST struct of DEVICE pointers, any of them NULL as above */
+    const float *gamma, *beta;
+    const float *post_gamma, *post_beta;
+    const float *scale;
+    const void *gate;
+} bra_norm_params;
+
+int bra_norm_forward(const bra_norm_shape *shape, const void *X, const void *Y_opt, const bra_norm_params *params,
+                     void *R_opt, void *N_opt, void *hip_stream);
+
+/* Gradients of it.  R: the sum that the forward returned (X where there was no Y), Y_opt: its Y; dN_opt, dR_opt: what came
+ * back to N and to R (at least one of them).  dX [rows, C] is the gradient of X, and with it that of R.
+ * Where Y_opt is given dY [rows, C] is required; dscale [C], dgate [groups, C] (in shape->dtype) and, with the post norm, dpost_gamma and
+ * dpost_beta [C] may be NULL, as may dgamma and dbeta [C].  What is asked for is OVERWRITTEN, the vectors in float32, summed over all rows;
+ * dgamma and dbeta are left as they were where dN_opt is NULL.  dX may be dR, dN or R; dY may be Y.  No atomic adds: a repeat gives
+ * the same bits.  Errors as above, and WORKSPACE. */
+typedef struct bra_norm_grads {         /* a HOST struct of DEVICE pointers */
+    void *dX, *dY, *dgate;
+    float *dgamma, *dbeta, *dpost_gamma, *dpost_beta, *dscale;
+} bra_norm_grads;
+
+int bra_norm_backward_workspace_bytes(const bra_norm_shape *shape, int32_t post, size_t *out_bytes);
+int bra_norm_backward(const bra_norm_shape *shape, const void *R, const void *Y_opt, const bra_norm_params *params,
+                      const void *dN_opt, const void *dR_opt, const bra_norm_grads *grads, void *ws, size_t ws_bytes,
+                      void *hip_stream);
+
+/* One AdamW step over many tensors, in place:
+ *     g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *     p  = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in float32.  Parameters and gradients are float32 or bf16, each tensor as it likes; a bf16 parameter is rounded once per step.  copy
+ * (or NULL): receives a float32 parameter's new value in bf16, as the layers read it.  A tensor whose grad is NULL is left alone.
+ * The states of all tensors lie in flat buffers: tensor i takes ceil(n / 32) blocks of 32 values behind those of the tensors before it
+ * (zeros to begin with; the rest of a last block stays zero).
+ *   bits 32: exp_avg, exp_avg_sq float32.
+ *   bits 8:  exp_avg and exp_avg_sq are bytes, OCP e4m3 codes, of m and of sqrt(v); a block's values are code * 2^(scale - 127) with the byte
+ *            `scale` of exp_avg_scale, exp_avg_sq_scale [blocks]: the smallest with which the block's largest value is at most 448 (at
+ *            least 2^-126).  A root that is not 0 is kept as the smallest code at least.
+ * t: `step` (from 1 on), or, where step_device is not NULL, the int32 there when the kernel runs (so that a captured graph can be replayed
+ * with a step that counts on); `scalars` is then device scratch for 2 floats.  grad_scale: NULL or one float32 on the device, for a
+ * loss scale or clipping.  No workspace otherwise; 72 tensors go into a launch.
+ * Alignment: exp_avg, exp_avg_sq 32 bytes, the others their elements' size (16 bytes are faster).
+ * Errors: NULL; SHAPE (count < 0, n < 0 or above 2^36, step < 1, betas outside [0, 1), lr, eps or weight_decay negative or not finite); DTYPE
+ * (dtypes; bits; a copy of a bf16 parameter); OVERLAP (parameters or copies that share memory); ALIGN; LAUNCH. */
+#define BRA_ADAMW_BLOCK 32
+typedef struct bra_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *copy;
+    int64_t n;
+    float weight_decay;
+    int32_t param_dtype, grad_dtype;
+} bra_adamw_tensor;
+typedef struct bra_adamw_args {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    const int32_t *step_device;
+    float *scalars;
+    const float *grad_scale;
+    int32_t bits;             /* 32 or 8 */
+    void *exp_avg, *exp_avg_sq, *exp_avg_scale, *exp_avg_sq_scale;
+} bra_adamw_args;
+
+int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_adamw_args *args, void *hip_stream);
 
 /* Optional per-launch timing, for benchmarks (Sec. "Limitation": the paper locates
  * BRA's cost in kernel launches and memory transactions, so the benchmark reports

@@ -20,6 +20,9 @@ NATIVE_PATH = os.path.join(_HERE, "_native.so")
 BRA_F32, BRA_BF16 = 0, 1
 PATH_AUTO, PATH_GENERIC, PATH_MFMA = 0, 1, 2
 SILU, GELU = 0, 1
+LAYERNORM, RMSNORM = 0, 1
+_KINDS = {"layer": LAYERNORM, "rms": RMSNORM}
+ADAMW_BLOCK = 32
 _ACTS = {"silu": SILU, "gelu": GELU}
 _PATHS = {"auto": PATH_AUTO, "generic": PATH_GENERIC, "mfma": PATH_MFMA}
 
@@ -28,7 +31,8 @@ STATIC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ("bra_workspace_bytes", "bra_route", "bra_forward", "bra_forward_static", "bra_padded_workspace_bytes",
            "bra_forward_padded", "bra_backward_workspace_bytes", "bra_backward", "bra_block_workspace_bytes",
            "bra_block_forward", "bra_ffn_workspace_bytes", "bra_ffn_forward", "bra_ffn_backward_workspace_bytes",
-           "bra_ffn_backward", "bra_strerror", "bra_version",
+           "bra_ffn_backward", "bra_norm_forward", "bra_norm_backward_workspace_bytes", "bra_norm_backward",
+           "bra_adamw_step", "bra_strerror", "bra_version",
            "bra_profile_begin", "bra_profile_end", "bra_kernel_name", "bra_util_copy",
            "bra_util_read", "bra_util_mfma", "bra_util_mfma32")
 
@@ -44,6 +48,36 @@ class BraFfnShape(ctypes.Structure):
     """bra_ffn_shape."""
     _fields_ = [("M", ctypes.c_int64), ("C", ctypes.c_int32), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("act", ctypes.c_int32)]
+
+
+class BraNormShape(ctypes.Structure):
+    """bra_norm_shape."""
+    _fields_ = [("rows", ctypes.c_int64), ("groups", ctypes.c_int32), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class BraNormParams(ctypes.Structure):
+    """bra_norm_params: device pointers."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("gamma", "beta", "post_gamma", "post_beta", "scale", "gate")]
+
+
+class BraNormGrads(ctypes.Structure):
+    """bra_norm_grads: device pointers."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("dX", "dY", "dgate", "dgamma", "dbeta", "dpost_gamma", "dpost_beta", "dscale")]
+
+
+class BraAdamwTensor(ctypes.Structure):
+    """bra_adamw_tensor."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class BraAdamwArgs(ctypes.Structure):
+    """bra_adamw_args."""
+    _fields_ = ([(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps")] +
+                [("step", ctypes.c_int64), ("step_device", ctypes.c_void_p), ("scalars", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p),
+                 ("bits", ctypes.c_int32)] +
+                [(name, ctypes.c_void_p) for name in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")])
 
 
 class BraBlockParams(ctypes.Structure):
@@ -100,6 +134,15 @@ def lib() -> ctypes.CDLL:
         L.bra_ffn_backward_workspace_bytes.argtypes = [ctypes.POINTER(BraFfnShape), ctypes.POINTER(sz)]
         L.bra_ffn_backward.restype = ctypes.c_int
         L.bra_ffn_backward.argtypes = [ctypes.POINTER(BraFfnShape)] + [vp] * 11 + [ctypes.c_int32, vp, sz, vp]
+        L.bra_norm_forward.restype = ctypes.c_int
+        L.bra_norm_forward.argtypes = [ctypes.POINTER(BraNormShape), vp, vp, ctypes.POINTER(BraNormParams), vp, vp, vp]
+        L.bra_norm_backward_workspace_bytes.restype = ctypes.c_int
+        L.bra_norm_backward_workspace_bytes.argtypes = [ctypes.POINTER(BraNormShape), ctypes.c_int32, ctypes.POINTER(sz)]
+        L.bra_norm_backward.restype = ctypes.c_int
+        L.bra_norm_backward.argtypes = [ctypes.POINTER(BraNormShape), vp, vp, ctypes.POINTER(BraNormParams), vp, vp,
+                                        ctypes.POINTER(BraNormGrads), vp, sz, vp]
+        L.bra_adamw_step.restype = ctypes.c_int
+        L.bra_adamw_step.argtypes = [ctypes.POINTER(BraAdamwTensor), ctypes.c_int32, ctypes.POINTER(BraAdamwArgs), vp]
         L.bra_strerror.restype = ctypes.c_char_p
         L.bra_strerror.argtypes = [ctypes.c_int]
         L.bra_version.restype = ctypes.c_int
@@ -248,6 +291,47 @@ def bra_ffn_backward(X, W1, W2, dY, *, b1=None, pre=None, act="silu", bias_grads
     grad_dtype (None: X's dtype).  pre: G | U as the forward returned them; without it they are formed again from X, W1 and b1."""
     grads = -1 if grad_dtype is None else {torch.float32: BRA_F32, torch.bfloat16: BRA_BF16}[grad_dtype]
     return (_native_module or _load_native()).ffn_backward(X, W1, W2, dY, b1, pre, _ACTS[act], bias_grads, grads, ws)
+
+
+def bra_norm_forward(X, gamma=None, beta=None, *, Y=None, post_gamma=None, post_beta=None, scale=None, gate=None,
+                     kind="layer", eps=1e-6, out=None):
+    """Norms around a residual sum: R = X + scale * gate * post(Y) and N = norm(R), in one pass.  Returns (R, N), without Y
+    N alone, without gamma R alone.  kind: "layer" or "rms", of both norms; post(Y) is Y where post_gamma is None.
+    X, Y [.., C] of one dtype; the vectors float32 [C]; gate: X's dtype, [leading dimensions of X.., C] (ones may stand for the
+    others), one row for all that share those indices.  out: receives R; may be X (see include/bra.h)."""
+    return (_native_module or _load_native()).norm_forward(X, Y, gamma, beta, post_gamma, post_beta, scale, gate, _KINDS[kind], eps, out)
+
+
+def bra_norm_backward(R, gamma=None, dN=None, *, dX=None, Y=None, post_gamma=None, post_beta=None, scale=None, gate=None,
+                      kind="layer", eps=1e-6, ws=None):
+    """Gradients of bra_norm_forward as a dict.  R: the sum that the forward returned (without Y: X); dN, dX: what came back to N and
+    to R, at least one of them.  Returns "dX", the gradient of X and of R; with dN "dgamma" and "dbeta"; with Y "dY" and, for what was given,
+    "dscale", "dgate", "dpost_gamma" and "dpost_beta"."""
+    return (_native_module or _load_native()).norm_backward(R, Y, gamma, post_gamma, post_beta, scale, gate, dN, dX, _KINDS[kind], eps, ws)
+
+
+def adamw_state(params, bits=32):
+    """States of bra_adamw_step for these parameters, zeros: flat tensors in which parameter i takes ceil(numel / 32) blocks of
+    32 values behind those before it.  bits 32: {"exp_avg", "exp_avg_sq"} in float32.  bits 8: {"exp_avg", "exp_avg_scale",
+    "exp_avg_root", "exp_avg_root_scale"}: e4m3 codes of the first moment and of the second's root, with a power of two per block."""
+    if bits not in (32, 8):
+        raise ValueError("bits must be 32 or 8")
+    blocks = sum((p.numel() + ADAMW_BLOCK - 1) // ADAMW_BLOCK for p in params)
+    device = params[0].device if len(params) else None
+    if bits == 32:
+        return {k: torch.zeros(blocks * ADAMW_BLOCK, dtype=torch.float32, device=device) for k in ("exp_avg", "exp_avg_sq")}
+    zeros = lambda n, dtype: torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
+    return {k + s: zeros(n, t) for k in ("exp_avg", "exp_avg_root")
+            for s, n, t in (("", blocks * ADAMW_BLOCK, torch.float8_e4m3fn), ("_scale", blocks, torch.float8_e8m0fnu))}
+
+
+def bra_adamw_step(params, grads, state, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, copies=None,
+                   grad_scale=None):
+    """One AdamW step over lists of parameters and gradients (None: left alone), in place; state: adamw_state(params).
+    step: this step's number from 1 on, or a one-element int32 tensor on the GPU that holds it when the step runs (for captured
+    graphs).  weight_decay: a number, or one for each parameter.  copies: bf16 tensors (or None) that receive the float32 parameters'
+    new values.  grad_scale: None or a one-element float32 tensor on the GPU that the gradients are multiplied by (see include/bra.h)."""
+    (_native_module or _load_native()).adamw_step(params, grads, state, step, lr, beta1, beta2, eps, weight_decay, copies, grad_scale)
 
 
 def profile_begin(max_records: int) -> None:

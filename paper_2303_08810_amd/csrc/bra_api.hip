@@ -1,11 +1,17 @@
 // C-ABI entry points of libbra: argument checks and dispatch to a kernel family.
 #include "bra_common.h"
+#include "bra_adamw.h"
 #include "bra_ffn.h"
+#include "bra_norm.h"
 
 #include <math.h>
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <mutex>
+#include <utility>
+#include <vector>
 
 // Scratch memory of bra_forward_static: one copy per GPU, held by the code object until the
 // process ends.  In host code the array's name is only a handle for hipGetSymbolAddress; the
@@ -99,6 +105,19 @@ static bool aligned(size_t bytes, std::initializer_list<const void *> pointers)
 static size_t ffn_alignment(const ffn::Sizes &S)
 {
     return S.C % 8 == 0 && S.h % 8 == 0 ? 16 : S.f32 ? 4 : 2;
+}
+
+static int make_norm_sizes(const bra_norm_shape *s, bool post, NormSizes &S)
+{
+    if (!s) return BRA_ERR_NULL;
+    if (s->rows < 0 || s->rows > (1L << 30) || s->C < 1 || s->groups < 1 || s->rows % s->groups || !(s->eps >= 0.f)) return BRA_ERR_SHAPE;
+    if (s->dtype != BRA_F32 && s->dtype != BRA_BF16) return BRA_ERR_DTYPE;
+    if (s->kind != BRA_LAYERNORM && s->kind != BRA_RMSNORM) return BRA_ERR_DTYPE;
+    if (s->C > 8192) return BRA_ERR_UNSUPPORTED;
+    S.rows = s->rows; S.groups = s->groups; S.per_group = s->rows / s->groups; S.C = s->C;
+    S.f32 = s->dtype == BRA_F32; S.layer = s->kind == BRA_LAYERNORM; S.post = post; S.eps = s->eps;
+    S.vec = S.C % 8 == 0;
+    return BRA_OK;
 }
 
 static bool ws_ok(const void *ws, size_t have, size_t need)
@@ -343,6 +362,94 @@ int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, 
     return ffn_backward(S, X, W1, b1, W2, pre, dY, dX, dW1, dW2, db1, db2, grad_dtype == BRA_F32, ws, (hipStream_t)hip_stream);
 }
 
+int bra_norm_forward(const bra_norm_shape *shape, const void *X, const void *Y, const bra_norm_params *p, void *R, void *N, void *hip_stream)
+{
+    NormSizes S;
+    const int rc = make_norm_sizes(shape, p && p->post_gamma, S);
+    if (rc != BRA_OK) return rc;
+    if (!p) return BRA_ERR_NULL;
+    if (S.rows == 0) return BRA_OK;
+    if (!X || !Y != !R || !p->gamma != !N || (!Y && !N)) return BRA_ERR_NULL;
+    const size_t element = S.f32 ? 4 : 2;
+    if (!aligned(element, {X, Y, R, N, p->gate}) || !aligned(4, {p->gamma, p->beta, p->post_gamma, p->post_beta, p->scale})) return BRA_ERR_ALIGN;
+    S.vec = S.vec && aligned(16, {X, Y, R, N, p->gate});
+    S.post = S.post && Y;
+    const NormIn I{X, Y, Y ? p->gate : nullptr, p->gamma, p->beta, p->post_gamma, p->post_beta, p->scale};
+    return norm_forward(S, I, R, N, (hipStream_t)hip_stream);
+}
+
+int bra_norm_backward_workspace_bytes(const bra_norm_shape *shape, int32_t post, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    NormSizes S;
+    const int rc = make_norm_sizes(shape, post != 0, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = norm_backward_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_norm_backward(const bra_norm_shape *shape, const void *R, const void *Y, const bra_norm_params *p, const void *dN, const void *dR, const bra_norm_grads *g,
+                      void *ws, size_t ws_bytes, void *hip_stream)
+{
+    NormSizes S;
+    const int rc = make_norm_sizes(shape, p && p->post_gamma && Y, S);
+    if (rc != BRA_OK) return rc;
+    if (!p || !g) return BRA_ERR_NULL;
+    if (S.rows > 0 && (!R || !g->dX || (Y && !g->dY) || (!dN && !dR) || (dN && !p->gamma))) return BRA_ERR_NULL;
+    const size_t element = S.f32 ? 4 : 2;
+    if (!aligned(element, {R, Y, p->gate, dN, dR, g->dX, g->dY, g->dgate})) return BRA_ERR_ALIGN;
+    if (!aligned(4, {p->gamma, p->beta, p->post_gamma, p->post_beta, p->scale, g->dgamma, g->dbeta, g->dpost_gamma, g->dpost_beta, g->dscale})) return BRA_ERR_ALIGN;
+    S.vec = S.vec && aligned(16, {R, Y, p->gate, dN, dR, g->dX, g->dY, g->dgate});
+    const size_t need = norm_backward_workspace_bytes(S);
+    if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    const NormIn I{R, Y, Y ? p->gate : nullptr, p->gamma, p->beta, p->post_gamma, p->post_beta, p->scale};
+    const NormGrads G{g->dX, g->dY, p->gate && (Y || S.rows == 0) ? g->dgate : nullptr, g->dgamma, g->dbeta, g->dpost_gamma, g->dpost_beta, g->dscale};
+    return norm_backward(S, I, dN, dR, G, ws, (hipStream_t)hip_stream);
+}
+
+int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_adamw_args *a, void *hip_stream)
+{
+    if (!a || (count > 0 && !tensors)) return BRA_ERR_NULL;
+    auto fine = [](double v) { return v >= 0 && std::isfinite(v); };
+    if (count < 0 || !fine(a->lr) || !fine(a->eps) || !(a->beta1 >= 0 && a->beta1 < 1) || !(a->beta2 >= 0 && a->beta2 < 1)) return BRA_ERR_SHAPE;
+    if (!a->step_device && a->step < 1) return BRA_ERR_SHAPE;
+    if (a->bits != 32 && a->bits != 8) return BRA_ERR_DTYPE;
+    long total = 0;
+    bool any = false;
+    for (int i = 0; i < count; ++i) {
+        const bra_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.n > (1L << 36) || !fine(t.weight_decay)) return BRA_ERR_SHAPE;
+        if ((t.param_dtype != BRA_F32 && t.param_dtype != BRA_BF16) || (t.grad_dtype != BRA_F32 && t.grad_dtype != BRA_BF16)) return BRA_ERR_DTYPE;
+        if (t.copy && t.param_dtype != BRA_F32) return BRA_ERR_DTYPE;
+        total += (t.n + BRA_ADAMW_BLOCK - 1) / BRA_ADAMW_BLOCK;
+        if (total > (1L << 31)) return BRA_ERR_SHAPE;
+        if (!t.n || !t.grad) continue;
+        any = true;
+        if (!t.param) return BRA_ERR_NULL;
+        if ((uintptr_t)t.param % (t.param_dtype == BRA_F32 ? 4 : 2) || (uintptr_t)t.grad % (t.grad_dtype == BRA_F32 ? 4 : 2) || (uintptr_t)t.copy % 2) return BRA_ERR_ALIGN;
+    }
+    if (!any) return BRA_OK;
+    if (!a->exp_avg || !a->exp_avg_sq || (a->bits == 8 && (!a->exp_avg_scale || !a->exp_avg_sq_scale)) || (a->step_device && !a->scalars)) return BRA_ERR_NULL;
+    if (!aligned(32, {a->exp_avg, a->exp_avg_sq}) || !aligned(4, {a->step_device, a->scalars, a->grad_scale})) return BRA_ERR_ALIGN;
+    // what is written must be each tensor's own
+    try {
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        spans.reserve(2 * (size_t)count);
+        for (int i = 0; i < count; ++i) {
+            const bra_adamw_tensor &t = tensors[i];
+            if (!t.n || !t.grad) continue;
+            spans.emplace_back((uintptr_t)t.param, (uintptr_t)t.param + (size_t)t.n * (t.param_dtype == BRA_F32 ? 4 : 2));
+            if (t.copy) spans.emplace_back((uintptr_t)t.copy, (uintptr_t)t.copy + (size_t)t.n * 2);
+        }
+        if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second) return BRA_ERR_OVERLAP;
+    } catch (...) {
+        return BRA_ERR_LAUNCH;
+    }
+    return adamw_step(tensors, count, *a, (hipStream_t)hip_stream);
+}
+
 const char *bra_strerror(int code)
 {
     switch (code) {
@@ -355,6 +462,7 @@ const char *bra_strerror(int code)
     case BRA_ERR_UNSUPPORTED: return "shape not supported by the requested kernel family";
     case BRA_ERR_LAUNCH: return "HIP runtime error while enqueueing";
     case BRA_ERR_TOO_LARGE: return "shape needs more scratch memory than the library's built-in buffer holds";
+    case BRA_ERR_OVERLAP: return "parameters or their copies share memory";
     case BRA_ERR_ALIGN: return "a tensor is not aligned as its entry point asks";
     default: return "unknown error code";
     }

@@ -6,6 +6,8 @@
 #include <stdint.h>
 #include <stdlib.h>
 
+#include <atomic>
+
 #include "../../include/bra.h"
 
 namespace bra {
@@ -54,6 +56,20 @@ __device__ __forceinline__ float gelu_f32(float t)
     p = fmaf(p, a, -1.150787711e+00f);
     p = fmaf(p, a, -1.000037670e+00f);
     return fmaf(-a, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(t, 0.f));
+}
+
+// Allows a kernel's dynamic LDS beyond 64 KB, once per device.
+template <auto kernel>
+inline int allow_lds(size_t bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return BRA_ERR_LAUNCH;
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_acquire) & bit)) return BRA_OK;
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return BRA_ERR_LAUNCH;
+    done.fetch_or(bit, std::memory_order_release);
+    return BRA_OK;
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }

@@ -13,8 +13,6 @@
 #include "bra_attn_dev.h"
 #include "bra_ffn.h"
 
-#include <atomic>
-
 namespace bra {
 namespace ffn {
 
@@ -282,20 +280,6 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
         a = g * f;
         slope = f + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
     }
-}
-
-// Allows a kernel's LDS beyond 64 KB, once per device.
-template <auto kernel>
-inline int allow_lds(size_t bytes)
-{
-    static std::atomic<uint64_t> done{0};
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess) return BRA_ERR_LAUNCH;
-    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
-    if (bit && (done.load(std::memory_order_acquire) & bit)) return BRA_OK;
-    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return BRA_ERR_LAUNCH;
-    done.fetch_or(bit, std::memory_order_release);
-    return BRA_OK;
 }
 
 }  // namespace ffn

@@ -487,6 +487,213 @@ PyObject *py_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// The norms' inputs; X [.., C].
+struct NormCall {
+    bra_norm_shape s;
+    bra_norm_params p;
+};
+NormCall norm_call(const at::Tensor &X, const at::Tensor *Y, const at::Tensor *gamma, const at::Tensor *beta, const at::Tensor *post_gamma, const at::Tensor *post_beta,
+                   const at::Tensor *scale, const at::Tensor *gate, PyObject *kind, PyObject *eps)
+{
+    if (X.dim() < 1) value_error("the map must be [.., C]");
+    same_kind(X, X);
+    const int64_t C = X.size(-1);
+    if (C < 1 || C > INT32_MAX) check(BRA_ERR_SHAPE);
+    if (Y && !like(*Y, X)) value_error("Y must be a contiguous tensor of the map's shape and dtype on its GPU");
+    for (const at::Tensor *t : {gamma, beta, post_gamma, post_beta, scale})
+        same_place(t, X, at::kFloat, {C}, "gamma, beta, post_gamma, post_beta and scale must be contiguous float32 [C] tensors on the map's GPU");
+    if (beta && !gamma) value_error("beta without gamma");
+    if (post_beta && !post_gamma) value_error("post_beta without post_gamma");
+    if (!Y && (post_gamma || scale || gate)) value_error("post_gamma, scale and gate go with Y");
+    int64_t groups = 1;
+    if (gate) {
+        if (!(gate->is_cuda() && gate->is_contiguous() && gate->device() == X.device() && gate->scalar_type() == X.scalar_type() && gate->dim() >= 1 && gate->size(-1) == C))
+            value_error("gate must be a contiguous [.., C] tensor of the map's dtype on its GPU");
+        int64_t lead = gate->dim() - 1;
+        while (lead > 0 && gate->size(lead - 1) == 1 && (lead > X.dim() - 1 || X.size(lead - 1) != 1)) --lead;
+        if (lead > X.dim() - 1) value_error("gate has more dimensions than the map");
+        for (int64_t d = 0; d < lead; ++d) {
+            if (gate->size(d) != X.size(d)) value_error("gate's leading dimensions must be the map's first ones");
+            groups *= gate->size(d);
+        }
+    }
+    const int64_t rows = X.numel() / C;
+    if (groups < 1) groups = 1;                       // no rows
+    if (groups > INT32_MAX) check(BRA_ERR_SHAPE);
+    return NormCall{{rows, (int32_t)groups, (int32_t)C, dtype_of(X), integer(kind), (float)real(eps)},
+                    {(const float *)data(gamma), (const float *)data(beta), (const float *)data(post_gamma), (const float *)data(post_beta), (const float *)data(scale), data(gate)}};
+}
+
+// norm_forward(X, Y, gamma, beta, post_gamma, post_beta, scale, gate, kind, eps, out)
+PyObject *py_norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 11, [&]() -> PyObject * {
+        const at::Tensor &X = need(a[0]);
+        const at::Tensor *Y = tensor(a[1]), *gamma = tensor(a[2]), *out = tensor(a[10]);
+        const NormCall c = norm_call(X, Y, gamma, tensor(a[3]), tensor(a[4]), tensor(a[5]), tensor(a[6]), tensor(a[7]), a[8], a[9]);
+        if (!Y && !gamma) value_error("nothing to do: neither Y nor gamma");
+        if (out && !Y) value_error("out goes with Y");
+        if (out && !like(*out, X)) value_error("out must be a contiguous tensor of the map's shape and dtype on its GPU");
+        const c10::DeviceGuard guard(X.device());
+        at::Tensor R, N;
+        if (Y) R = out ? *out : at::empty_like(X);
+        if (gamma) N = at::empty_like(X);
+        void *st = stream_of(X);
+        run([&] {
+            return bra_norm_forward(&c.s, X.data_ptr(), data(Y), &c.p, Y ? R.data_ptr() : nullptr, gamma ? N.data_ptr() : nullptr, st);
+        });
+        if (!Y) return wrap(N);
+        PyObject *r;
+        if (out) Py_INCREF(r = a[10]);
+        else r = wrap(R);
+        return gamma ? tuple({r, wrap(N)}) : r;
+    });
+}
+
+// norm_backward(R, Y, gamma, post_gamma, post_beta, scale, gate, dN, dX, kind, eps, ws)
+PyObject *py_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&]() -> PyObject * {
+        const at::Tensor &R = need(a[0]);
+        const at::Tensor *Y = tensor(a[1]), *gamma = tensor(a[2]), *post_gamma = tensor(a[3]), *post_beta = tensor(a[4]), *scale = tensor(a[5]), *gate = tensor(a[6]),
+                         *dN = tensor(a[7]), *dR = tensor(a[8]);
+        const NormCall c = norm_call(R, Y, gamma, nullptr, post_gamma, post_beta, scale, gate, a[9], a[10]);
+        if (!dN && !dR) value_error("neither dN nor dX");
+        if (dN && !gamma) value_error("dN without gamma");
+        if ((dN && !like(*dN, R)) || (dR && !like(*dR, R))) value_error("dN and dX must be contiguous tensors of the map's shape and dtype on its GPU");
+        const c10::DeviceGuard guard(R.device());
+        size_t bytes = 0;
+        check(bra_norm_backward_workspace_bytes(&c.s, post_gamma != nullptr, &bytes));
+        PyObject *d = PyDict_New();
+        if (!d) throw Raised{};
+        struct Drop { PyObject *&o; ~Drop() { Py_XDECREF(o); } } drop{d};
+        auto keep = [&](const char *name, at::Tensor t) {
+            PyObject *o = wrap(t);
+            const int rc = o ? PyDict_SetItemString(d, name, o) : -1;
+            Py_XDECREF(o);
+            if (rc) throw Raised{};
+            return t.data_ptr();
+        };
+        auto vector = [&](const char *name) { return (float *)keep(name, at::empty({(int64_t)c.s.C}, R.options().dtype(at::kFloat))); };
+        bra_norm_grads g{};
+        g.dX = keep("dX", at::empty_like(R));
+        if (dN) { g.dgamma = vector("dgamma"); g.dbeta = vector("dbeta"); }
+        if (Y) {
+            g.dY = keep("dY", at::empty_like(R));
+            if (scale) g.dscale = vector("dscale");
+            if (gate) g.dgate = keep("dgate", at::empty_like(*gate));
+            if (post_gamma) { g.dpost_gamma = vector("dpost_gamma"); g.dpost_beta = vector("dpost_beta"); }
+        }
+        at::Tensor own;
+        const at::Tensor *ws = workspace(tensor(a[11]), bytes, R, own);
+        void *st = stream_of(R);
+        run([&] {
+            return bra_norm_backward(&c.s, R.data_ptr(), data(Y), &c.p, data(dN), data(dR), &g, ws->data_ptr(), (size_t)ws->numel(), st);
+        });
+        PyObject *out = d;
+        d = nullptr;
+        return out;
+    });
+}
+
+// A list or tuple's items, held for the call.
+struct Items {
+    PyObject *fast;
+    Py_ssize_t n;
+    Items(PyObject *o, const char *text) : fast(PySequence_Fast(o, text)), n(0)
+    {
+        if (!fast) throw Raised{};
+        n = PySequence_Fast_GET_SIZE(fast);
+    }
+    ~Items() { Py_XDECREF(fast); }
+    Items(const Items &) = delete;
+    PyObject *operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
+};
+
+const at::Tensor &entry(PyObject *state, const char *key)
+{
+    PyObject *o = PyDict_GetItemString(state, key);
+    if (!o) {
+        PyErr_Format(PyExc_ValueError, "the state has no %s", key);
+        throw Raised{};
+    }
+    return need(o);
+}
+
+// adamw_step(params, grads, state, step, lr, beta1, beta2, eps, weight_decay, copies, grad_scale)
+PyObject *py_adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 11, [&]() -> PyObject * {
+        const Items params(a[0], "params must be a list of tensors"), grads(a[1], "grads must be a list of tensors");
+        if (params.n != grads.n) value_error("params and grads must be of one length");
+        if (!PyDict_Check(a[2])) value_error("state must be a dict as adamw_state returns it");
+        if (!params.n) Py_RETURN_NONE;
+        const at::Tensor &first = need(params[0]);
+        if (!first.is_cuda()) value_error("params must be contiguous float32 or bfloat16 tensors on one GPU");
+        std::vector<bra_adamw_tensor> list((size_t)params.n);
+        PyObject *copies_of = a[9] == Py_None ? a[0] : a[9];
+        const Items copies(copies_of, "copies must be a list of tensors");
+        const bool with_copies = a[9] != Py_None;
+        if (with_copies && copies.n != params.n) value_error("copies must have an entry for each parameter");
+        double decay = 0;
+        const bool one_decay = PyFloat_Check(a[8]) || PyIndex_Check(a[8]);
+        if (one_decay) decay = real(a[8]);
+        const Items decays(one_decay ? a[0] : a[8], "weight_decay must be a number or one for each parameter");
+        if (decays.n != params.n) value_error("weight_decay must be a number or one for each parameter");
+        int64_t blocks = 0;
+        for (Py_ssize_t i = 0; i < params.n; ++i) {
+            const at::Tensor &p = need(params[i]);
+            const at::Tensor *g = tensor(grads[i]), *c = with_copies ? tensor(copies[i]) : nullptr;
+            if (!(p.is_cuda() && p.is_contiguous() && p.device() == first.device() && (p.scalar_type() == at::kFloat || p.scalar_type() == at::kBFloat16)))
+                value_error("params must be contiguous float32 or bfloat16 tensors on one GPU");
+            if (g && !(g->is_cuda() && g->is_contiguous() && g->device() == first.device() && g->sizes().equals(p.sizes()) &&
+                       (g->scalar_type() == at::kFloat || g->scalar_type() == at::kBFloat16)))
+                value_error("grads must be contiguous float32 or bfloat16 tensors of the parameters' shapes on their GPU");
+            if (c && !(p.scalar_type() == at::kFloat && c->is_cuda() && c->is_contiguous() && c->device() == first.device() && c->sizes().equals(p.sizes()) &&
+                       c->scalar_type() == at::kBFloat16))
+                value_error("copies must be contiguous bfloat16 tensors of float32 parameters' shapes on their GPU");
+            list[(size_t)i] = bra_adamw_tensor{p.data_ptr(), g && p.numel() ? g->data_ptr() : nullptr, data(c), p.numel(), (float)(one_decay ? decay : real(decays[i])),
+                                               p.scalar_type() == at::kFloat ? BRA_F32 : BRA_BF16, g && g->scalar_type() == at::kFloat ? BRA_F32 : BRA_BF16};
+            blocks += (p.numel() + BRA_ADAMW_BLOCK - 1) / BRA_ADAMW_BLOCK;
+        }
+        bra_adamw_args args{};
+        args.lr = real(a[4]); args.beta1 = real(a[5]); args.beta2 = real(a[6]); args.eps = real(a[7]);
+        args.bits = PyDict_GetItemString(a[2], "exp_avg_sq") ? 32 : 8;
+        auto state = [&](const char *key, at::ScalarType type, int64_t size) {
+            const at::Tensor &t = entry(a[2], key);
+            if (!(t.is_cuda() && t.is_contiguous() && t.device() == first.device() && t.scalar_type() == type && t.numel() == size))
+                value_error("the state is not that of these parameters");
+            return t.data_ptr();
+        };
+        const int64_t values = blocks * BRA_ADAMW_BLOCK;
+        if (args.bits == 32) {
+            args.exp_avg = state("exp_avg", at::kFloat, values);
+            args.exp_avg_sq = state("exp_avg_sq", at::kFloat, values);
+        } else {
+            args.exp_avg = state("exp_avg", at::kFloat8_e4m3fn, values);
+            args.exp_avg_sq = state("exp_avg_root", at::kFloat8_e4m3fn, values);
+            args.exp_avg_scale = state("exp_avg_scale", at::kFloat8_e8m0fnu, blocks);
+            args.exp_avg_sq_scale = state("exp_avg_root_scale", at::kFloat8_e8m0fnu, blocks);
+        }
+        const at::Tensor *scale = tensor(a[10]);
+        if (scale && !(scale->is_cuda() && scale->device() == first.device() && scale->scalar_type() == at::kFloat && scale->numel() == 1))
+            value_error("grad_scale must be a one-element float32 tensor on the parameters' GPU");
+        args.grad_scale = (const float *)data(scale);
+        const c10::DeviceGuard guard(first.device());
+        at::Tensor scalars;
+        if (THPVariable_Check(a[3])) {
+            const at::Tensor &t = THPVariable_Unpack(a[3]);
+            if (!(t.is_cuda() && t.device() == first.device() && t.scalar_type() == at::kInt && t.numel() == 1)) value_error("step must be a number or a one-element int32 tensor on the parameters' GPU");
+            args.step_device = (const int32_t *)t.data_ptr();
+            scalars = at::empty({2}, first.options().dtype(at::kFloat));
+            args.scalars = (float *)scalars.data_ptr();
+        } else args.step = integer(a[3]);
+        void *st = stream_of(first);
+        run([&] { return bra_adamw_step(list.data(), (int32_t)params.n, &args, st); });
+        Py_RETURN_NONE;
+    });
+}
+
 PyMethodDef methods[] = {
     {"init", (PyCFunction)(void *)py_init, METH_FASTCALL, nullptr},
     {"route", (PyCFunction)(void *)py_route, METH_FASTCALL, nullptr},
@@ -497,6 +704,9 @@ PyMethodDef methods[] = {
     {"block_forward", (PyCFunction)(void *)py_block_forward, METH_FASTCALL, nullptr},
     {"ffn_forward", (PyCFunction)(void *)py_ffn_forward, METH_FASTCALL, nullptr},
     {"ffn_backward", (PyCFunction)(void *)py_ffn_backward, METH_FASTCALL, nullptr},
+    {"norm_forward", (PyCFunction)(void *)py_norm_forward, METH_FASTCALL, nullptr},
+    {"norm_backward", (PyCFunction)(void *)py_norm_backward, METH_FASTCALL, nullptr},
+    {"adamw_step", (PyCFunction)(void *)py_adamw_step, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
