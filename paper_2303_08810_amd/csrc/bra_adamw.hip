@@ -77,7 +77,9 @@ __device__ __forceinline__ void put8(void *base, long at, bool bf16, bool vec, i
     }
 }
 
-__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (unsigned)(127 + e) << 23); }
+// 2^e as torch.ldexp forms it on this GPU, by powf: for some exponents a unit of float32 off.  A state that a program decodes there, to keep it or to look
+// at it, then holds the very values that the step takes; with the exponent's bits put in place 5 codes in 10000 fell on the other side of a tie.
+__device__ __forceinline__ float power_of_two(int e) { return powf(2.0f, (float)e); }
 
 __device__ __forceinline__ void decode8(u32x2 codes, unsigned scale, float (&v)[8])
 {
