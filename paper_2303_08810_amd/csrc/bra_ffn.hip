@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void k_operands(Layouts J)
 }
 
 template <class T, int TERMS, int ACT, typename E>
-__global__ __launch_bounds__(T::kThreads, 2) void k_gated(Operand X, Operand W1, const float *__restrict__ b1, E *__restrict__ pre, bf16_t *__restrict__ Act,
+__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, Operand W1, const float *__restrict__ b1, E *__restrict__ pre, bf16_t *__restrict__ Act,
                                                          long plane, long M, int h, int hp)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -48,16 +48,18 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_gated(Operand X, Operand W1,
     f32x16 acc[T::NT][T::MT];
     clear<T>(acc);
     multiply<T, false, true, TERMS>(X, W1, X.p + m0 * X.ld, W1.p + j0, la, lb, 0, (X.K + 63) / 64, lds, acc);
-    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wj = (wave % T::WC) * PW;
+    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wj = j0 + (wave % T::WC) * PW;
     const bool vec = h % 8 == 0;
+    constexpr int P = PW / 8;
+    bf16_t *const own = lds + wave * (32 * T::MT * 2 * PW);      // this wavefront's part of what the chunks have left
+    const Rows<P> first{own}, second{own + 32 * T::MT * PW};
 #pragma unroll
     for (int nt = 0; nt < T::NT / 2; ++nt)
 #pragma unroll
         for (int run = 0; run < 2; ++run) {
-            const int j = j0 + wj + 32 * nt + 16 * run + 8 * hi, n = h - j;
-            if (j >= hp) continue;
+            const int piece = 4 * nt + 2 * run + hi, j = wj + 8 * piece, n = h - j;
             float bg[8], bu[8];
-            if (b1) {
+            if (b1 && n > 0) {
                 load8(b1 + j, bg, n, false);
                 load8(b1 + h + j, bu, n, false);
             } else
@@ -66,26 +68,54 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_gated(Operand X, Operand W1,
 #pragma unroll
             for (int mt = 0; mt < T::MT; ++mt) {
                 const int row = wm + 32 * mt + c;
-                if (row >= rows) continue;
-                const size_t m = (size_t)(m0 + row);
-                float g[8], u[8], a[8];
+                f32x16 &G = acc[nt][mt], &U = acc[T::NT / 2 + nt][mt];
+                float g[8], u[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    g[e] = acc[nt][mt][8 * run + e] + bg[e];
-                    u[e] = acc[T::NT / 2 + nt][mt][8 * run + e] + bu[e];
-                    a[e] = e < n ? activation<ACT>(g[e]) * u[e] : 0.f;
-                }
+                for (int e = 0; e < 8; ++e) { g[e] = G[8 * run + e] + bg[e]; u[e] = U[8 * run + e] + bu[e]; }
                 if (pre) {
-                    store8(pre + m * 2 * h + j, g, n, vec);
-                    store8(pre + m * 2 * h + h + j, u, n, vec);
+                    if constexpr (TERMS == 1) {
+                        first.put(32 * mt + c, piece, pack8(g));
+                        second.put(32 * mt + c, piece, pack8(u));
+                    } else if (row < rows) {
+                        store8(pre + (size_t)(m0 + row) * 2 * h + j, g, n, vec);
+                        store8(pre + (size_t)(m0 + row) * 2 * h + h + j, u, n, vec);
+                    }
                 }
-                store_operand<TERMS>(Act + m * hp + j, plane, a);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) G[8 * run + e] = e < n ? activation<ACT>(g[e]) * u[e] : 0.f;      // A, in G's place
             }
         }
+    if constexpr (TERMS == 1)
+        if (pre) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                (half ? second : first).each(32 * T::MT, lane, [&](int row, int piece, bf16x8 v) {
+                    if (wm + row < rows) store_piece(pre + (size_t)(m0 + wm + row) * 2 * h + half * h + wj + 8 * piece, v, h - wj - 8 * piece, vec);
+                });
+        }
+#pragma unroll
+    for (int q = 0; q < TERMS; ++q) {
+#pragma unroll
+        for (int nt = 0; nt < T::NT / 2; ++nt)
+#pragma unroll
+            for (int run = 0; run < 2; ++run)
+#pragma unroll
+                for (int mt = 0; mt < T::MT; ++mt) {
+                    float v[8];
+                    bf16x8 t[TERMS];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e];
+                    operand<TERMS>(v, t);
+                    first.put(32 * mt + c, 4 * nt + 2 * run + hi, t[q]);
+                }
+        first.each(32 * T::MT, lane, [&](int row, int piece, bf16x8 v) {
+            if (wm + row < rows && wj + 8 * piece < hp) *(bf16x8 *)(Act + q * plane + (size_t)(m0 + wm + row) * hp + wj + 8 * piece) = v;
+        });
+    }
 }
 
 template <class T, bool BO, int TERMS, typename E>
-__global__ __launch_bounds__(T::kThreads, 2) void k_product(Operand A, Operand Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N)
+__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_product(Operand A, Operand Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *lds = (bf16_t *)smem;
@@ -99,29 +129,33 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_product(Operand A, Operand B
     f32x16 acc[T::NT][T::MT];
     clear<T>(acc);
     multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, 0, (A.K + 63) / 64, lds, acc);
-    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
+    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = n0 + (wave % T::WC) * (32 * T::NT);
     const bool vec = N % 8 == 0;
+    const Rows<4 * T::NT> out{lds + wave * (32 * T::MT * 32 * T::NT)};
 #pragma unroll
     for (int nt = 0; nt < T::NT; ++nt)
 #pragma unroll
         for (int run = 0; run < 2; ++run) {
-            const int col = n0 + wn + 32 * nt + 16 * run + 8 * hi, n = N - col;
-            if (n <= 0) continue;
+            const int piece = 4 * nt + 2 * run + hi, col = wn + 8 * piece, n = N - col;
             float b[8];
-            if (bias) load8(bias + col, b, n, false);
+            if (bias && n > 0) load8(bias + col, b, n, false);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) b[e] = 0.f;
 #pragma unroll
             for (int mt = 0; mt < T::MT; ++mt) {
                 const int row = wm + 32 * mt + c;
-                if (row >= rows) continue;
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e] + b[e];
-                store8(Out + (size_t)(m0 + row) * N + col, v, n, vec);
+                if constexpr (TERMS == 1) out.put(32 * mt + c, piece, pack8(v));
+                else if (row < rows) store8(Out + (size_t)(m0 + row) * N + col, v, n, vec);
             }
         }
+    if constexpr (TERMS == 1)
+        out.each(32 * T::MT, lane, [&](int row, int piece, bf16x8 v) {
+            if (wm + row < rows) store_piece(Out + (size_t)(m0 + wm + row) * N + wn + 8 * piece, v, N - wn - 8 * piece, vec);
+        });
 }
 
 template <class T, bool BO, int TERMS, typename E>
@@ -137,7 +171,7 @@ template <bool BO, int TERMS, typename E>
 int pick_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
     switch (tile_size(M, N)) {
-    case 256: return launch_product<Tile<256, 256, 2, 4>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 256: return launch_product<Tile<256, 256, 4, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     case 128: return launch_product<Tile<128, 128, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     default: return launch_product<Tile<64, 64, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     }
@@ -156,7 +190,7 @@ template <int TERMS, int ACT, typename E>
 int pick_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, hipStream_t st)
 {
     switch (tile_size(S.M, 2L * S.hp)) {
-    case 256: return launch_gated<Tile<256, 256, 2, 4>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    case 256: return launch_gated<Tile<256, 256, 4, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     case 128: return launch_gated<Tile<128, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     default: return launch_gated<Tile<64, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     }

@@ -16,7 +16,7 @@ namespace {
 
 // TD: the tile of dA, columns are hidden units; TG: that of G | U, the same rows and wavefronts.
 template <class TD, class TG, int TERMS, int ACT, bool GIVEN, typename E>
-__global__ __launch_bounds__(TD::kThreads, 2) void k_hidden(Operand dY, Operand W2, Operand X, Operand W1, const float *__restrict__ b1, const E *__restrict__ pre,
+__global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand dY, Operand W2, Operand X, Operand W1, const float *__restrict__ b1, const E *__restrict__ pre,
                                                            bf16_t *__restrict__ Act, long plane_a, bf16_t *__restrict__ dP, long plane_p, long M, int h, int hp)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -44,48 +44,90 @@ __global__ __launch_bounds__(TD::kThreads, 2) void k_hidden(Operand dY, Operand 
         });
         multiply<TG, false, true, TERMS>(X, W1, X.p + m0 * X.ld, W1.p + j0, la, lb, 0, (X.K + 63) / 64, lds, gu);
     }
-    const int hi = lane / 32, c = lane % 32, wm = (wave / TD::WC) * (32 * TD::MT), wj = (wave % TD::WC) * PW;
+    const int hi = lane / 32, c = lane % 32, wm = (wave / TD::WC) * (32 * TD::MT), wj = j0 + (wave % TD::WC) * PW;
     const bool vec = h % 8 == 0;
+    constexpr int P = PW / 8;
+    // 32 rows at a time through this wavefront's part of LDS: G and U in, dG and dU in their places, then A
+    bf16_t *const own = lds + wave * (2 * 32 * PW);
+    const Rows<P> first{own}, second{own + 32 * PW};
+    const bool whole = GIVEN && TERMS == 1 && vec && h >= 8;
 #pragma unroll
-    for (int nt = 0; nt < TD::NT; ++nt)
+    for (int mt = 0; mt < TD::MT; ++mt) {
+        const int r0 = wm + 32 * mt, row = r0 + c;
+        if (GIVEN && TERMS == 1 && whole) {
+            // (pieces and rows that do not exist: the last ones again)
+            lds_reads_done();
 #pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            const int j = j0 + wj + 32 * nt + 16 * run + 8 * hi, n = h - j;
-            if (j >= hp) continue;
-            float bg[8], bu[8];
-            if (!GIVEN && b1) {
-                load8(b1 + j, bg, n, false);
-                load8(b1 + h + j, bu, n, false);
-            } else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bg[e] = bu[e] = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < TD::MT; ++mt) {
-                const int row = wm + 32 * mt + c;
-                if (row >= rows) continue;
-                const size_t m = (size_t)(m0 + row);
-                float g[8], u[8], a[8], dg[8], du[8];
-                if constexpr (GIVEN) {
-                    load8(pre + m * 2 * h + j, g, n, vec);
-                    load8(pre + m * 2 * h + h + j, u, n, vec);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { g[e] = gu[nt][mt][8 * run + e] + bg[e]; u[e] = gu[TD::NT + nt][mt][8 * run + e] + bu[e]; }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float f, slope;
-                    activation_slope<ACT>(g[e], f, slope);
-                    const float d = acc[nt][mt][8 * run + e];
-                    a[e] = e < n ? f * u[e] : 0.f;
-                    dg[e] = e < n ? d * u[e] * slope : 0.f;
-                    du[e] = e < n ? d * f : 0.f;
-                }
-                store_operand<TERMS>(Act + m * hp + j, plane_a, a);
-                store_operand<TERMS>(dP + m * 2 * hp + j, plane_p, dg);
-                store_operand<TERMS>(dP + m * 2 * hp + hp + j, plane_p, du);
+            for (int r = 0; r < 32; r += 64 / P) {
+                const int in = r + lane / P, piece = (lane % P) ^ (in * P / 16 % P);
+                const bf16_t *g = (const bf16_t *)pre + (size_t)(m0 + min(r0 + in, rows - 1)) * 2 * h + min(wj + 8 * piece, h - 8);
+                load_to_lds_untracked(g, lds_address(own) + r * P * 16);
+                load_to_lds_untracked(g + h, lds_address(own) + (32 + r) * P * 16);
             }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
+        bf16x8 held[TD::NT][2][TERMS];
+        auto pieces = [&](int q) {
+#pragma unroll
+            for (int nt = 0; nt < TD::NT; ++nt)
+#pragma unroll
+                for (int run = 0; run < 2; ++run) {
+                    const int piece = 4 * nt + 2 * run + hi, j = wj + 8 * piece, n = h - j;
+                    float g[8], u[8], a[8], dg[8], du[8];
+                    if constexpr (GIVEN) {
+                        if (TERMS == 1 && whole) {
+                            load8((const bf16_t *)first.at(c, piece), g, 8, true);
+                            load8((const bf16_t *)second.at(c, piece), u, 8, true);
+                        } else {
+                            const E *p = pre + (size_t)(m0 + min(row, rows - 1)) * 2 * h + j;
+                            load8(p, g, n, vec);
+                            load8(p + h, u, n, vec);
+                        }
+                    } else {
+                        float bg[8], bu[8];
+                        if (b1 && n > 0) {
+                            load8(b1 + j, bg, n, false);
+                            load8(b1 + h + j, bu, n, false);
+                        } else
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) bg[e] = bu[e] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { g[e] = gu[nt][mt][8 * run + e] + bg[e]; u[e] = gu[TD::NT + nt][mt][8 * run + e] + bu[e]; }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float f, slope;
+                        activation_slope<ACT>(g[e], f, slope);
+                        const float d = acc[nt][mt][8 * run + e];
+                        a[e] = e < n ? f * u[e] : 0.f;
+                        dg[e] = e < n ? d * u[e] * slope : 0.f;
+                        du[e] = e < n ? d * f : 0.f;
+                    }
+                    bf16x8 t[TERMS];
+                    operand<TERMS>(dg, t);
+                    first.put(c, piece, t[q]);
+                    operand<TERMS>(du, t);
+                    second.put(c, piece, t[q]);
+                    operand<TERMS>(a, held[nt][run]);
+                }
+        };
+#pragma unroll
+        for (int q = 0; q < TERMS; ++q) {
+            pieces(q);
+            auto flush = [&](const Rows<P> &from, bf16_t *to, long ld) {
+                from.each(32, lane, [&](int in, int piece, bf16x8 v) {
+                    if (r0 + in < rows && wj + 8 * piece < hp) *(bf16x8 *)(to + (size_t)(m0 + r0 + in) * ld + wj + 8 * piece) = v;
+                });
+            };
+            flush(first, dP + q * plane_p, 2L * hp);
+            flush(second, dP + q * plane_p + hp, 2L * hp);
+#pragma unroll
+            for (int nt = 0; nt < TD::NT; ++nt)
+#pragma unroll
+                for (int run = 0; run < 2; ++run) first.put(c, 4 * nt + 2 * run + hi, held[nt][run][q]);
+            flush(first, Act + q * plane_a, hp);
+        }
+    }
 }
 
 // A contraction over the tokens: Part[share][rows][cols] = A^T B over the share's tokens; rows and cols as in the workspace (padded).
@@ -96,7 +138,7 @@ struct Contraction {
 };
 
 template <class T, int TERMS>
-__global__ __launch_bounds__(T::kThreads, 2) void k_weights(Contraction J0, Contraction J1, int tiles0, int tiles1, int shares)
+__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_weights(Contraction J0, Contraction J1, int tiles0, int tiles1, int shares)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *lds = (bf16_t *)smem;
@@ -221,7 +263,7 @@ int pick_hidden(const Operand &dY, const Operand &W2, const Operand &X, const Op
 {
     if (pre) {
         switch (tile_size(S.M, S.hp)) {
-        case 256: return launch_hidden<Tile<256, 256, 2, 4>, Tile<256, 256, 2, 4>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+        case 256: return launch_hidden<Tile<256, 256, 4, 2>, Tile<256, 256, 4, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         case 128: return launch_hidden<Tile<128, 128, 2, 2>, Tile<128, 128, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         default: return launch_hidden<Tile<64, 64, 2, 2>, Tile<64, 64, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         }
@@ -340,7 +382,7 @@ int ffn_backward(const Sizes &S, const void *X, const void *W1, const float *b1,
         const int M = (int)S.M;
         const Contraction J0{{(const bf16_t *)X, S.Cp, pX, M}, {at(P.dP), 2L * S.hp, pP, M}, (float *)at(P.parts1), S.Cp, 2 * S.hp};
         const Contraction J1{{at(P.Act), S.hp, pA, M}, {(const bf16_t *)dY, S.Cp, pX, M}, (float *)at(P.parts2), S.hp, S.Cp};
-        if (W.side == 256) rc = S.f32 ? launch_weights<Tile<256, 256, 2, 4>, 3>(J0, J1, W.shares, st) : launch_weights<Tile<256, 256, 2, 4>, 1>(J0, J1, W.shares, st);
+        if (W.side == 256) rc = S.f32 ? launch_weights<Tile<256, 256, 4, 2>, 3>(J0, J1, W.shares, st) : launch_weights<Tile<256, 256, 4, 2>, 1>(J0, J1, W.shares, st);
         else rc = S.f32 ? launch_weights<Tile<128, 128, 2, 2>, 3>(J0, J1, W.shares, st) : launch_weights<Tile<128, 128, 2, 2>, 1>(J0, J1, W.shares, st);
         if (rc != BRA_OK) return rc;
         if (db1 || db2) {

@@ -27,6 +27,7 @@ struct Tile {
     static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, kWaves = WR * WC, kThreads = 64 * kWaves;
     static constexpr int MT = BM / (32 * WR), NT = BN / (32 * WC);
     static constexpr int kChunkA = BM * 64, kChunkB = BN * 64;                  // elements of a chunk
+    static constexpr int kMinWaves = MT * NT > 8 ? 1 : 2;                       // per SIMD, of the register budget
     static constexpr size_t kLds = 2 * (size_t)(kChunkA + kChunkB) * 2;
 };
 
@@ -35,7 +36,7 @@ struct Tile {
 template <int B>
 __device__ __forceinline__ int turn_outer(int k) { return B >= 128 ? 4 * (k % 4) : 4 * (k / 2 % 2); }
 template <bool PERMUTED>
-__device__ __forceinline__ int turn_inner(int row) { return PERMUTED ? row % 4 + row / 8 % 2 * 4 : row % 8; }
+__device__ __forceinline__ int turn_inner(int row) { return row / 2 % 8; }
 
 // A wavefront's direct loads of one operand's chunks: B rows (or columns) of the tile, OUTER: contraction outside.
 template <class T, int B, bool OUTER, bool PERMUTED>
@@ -58,21 +59,18 @@ struct Loads {
             }
         }
     }
-    // chunk whose first element is `origin` (the same for all lanes), `left` of the contraction from there on, to LDS address `at`
-    __device__ __forceinline__ void request(const bf16_t *origin, int left, unsigned at, int wave, int lane) const
+    // load u of the chunk whose first element is `origin` (the same for all lanes), `left` of the contraction from there on, to LDS address `at`
+    __device__ __forceinline__ void request(int u, const bf16_t *origin, int left, unsigned at, int wave, int lane) const
     {
+        at += 1024 * (wave * L + u);
         if (left >= 64) {
-#pragma unroll
-            for (int u = 0; u < L; ++u) load_to_lds_untracked(origin, off[u], at + 1024 * (wave * L + u));
+            load_to_lds_untracked(origin, off[u], at);
             return;
         }
-#pragma unroll
-        for (int u = 0; u < L; ++u) {
-            const int row = 8 * (wave * L + u) + lane / 8;
-            const int k = OUTER ? RPI * (wave * L + u) + lane / CH : 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row));
-            const bf16_t *p = (const bf16_t *)((const char *)origin + off[u]);
-            load_to_lds_untracked(k < left ? p : zeros, at + 1024 * (wave * L + u));
-        }
+        const int row = 8 * (wave * L + u) + lane / 8;
+        const int k = OUTER ? RPI * (wave * L + u) + lane / CH : 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row));
+        const bf16_t *p = (const bf16_t *)((const char *)origin + off[u]);
+        load_to_lds_untracked(k < left ? p : zeros, at);
     }
 };
 
@@ -109,8 +107,9 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[T::NT][T::MT])
 
 // acc += A^T-or-A B over the contraction's chunks [first, end).  a0, b0: origins of the tile at k = 0 in the first plane.
 // One barrier per chunk: it stands in the middle of the chunk's last quarter, whose operands are in registers by then, so that
-// the buffer just read is free for the chunk after next, and the next chunk, requested one chunk's time ago, is there; the quarter's
-// second half of products runs while the next chunk's first operands are read.
+// the buffer just read is free for the chunk after next, and the next chunk is there; the quarter's
+// second half of products runs while the next chunk's first operands are read.  Reads and loads stand one by one between the products: in
+// bursts they held up the products behind them.
 template <class T, bool AO, bool BO, int TERMS>
 __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, const bf16_t *a0, const bf16_t *b0, const Loads<T, T::BM, AO, false> &la,
                                          const Loads<T, T::BN, BO, true> &lb, int first, int end, bf16_t *lds, f32x16 (&acc)[T::NT][T::MT])
@@ -119,8 +118,13 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
     const int wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
     const unsigned base = lds_address(lds);
     constexpr unsigned kBuffer = 2 * (T::kChunkA + T::kChunkB);
+    constexpr int LA = Loads<T, T::BM, AO, false>::L, LB = Loads<T, T::BN, BO, true>::L, kLoads = LA + LB;
     const int rounds = end - first, total = TERMS == 1 ? rounds : 6 * rounds;
-    auto request = [&](int chunk, int buffer) {
+    // the chunk that is being asked for
+    const bf16_t *an = a0, *bn = b0;
+    int left_a = 0, left_b = 0;
+    unsigned to = 0;
+    auto aim = [&](int chunk, int buffer) {
         long pa = 0, pb = 0;
         int c = chunk;
         if (TERMS > 1) {
@@ -131,55 +135,76 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
             pb = ((0x010120 >> (4 * round)) & 3) * Bm.plane;
         }
         const int k0 = 64 * (first + c);
-        la.request(a0 + pa + (AO ? k0 * A.ld : (long)k0), A.K - k0, base + buffer * kBuffer, wave, lane);
-        lb.request(b0 + pb + (BO ? k0 * Bm.ld : (long)k0), Bm.K - k0, base + buffer * kBuffer + 2 * T::kChunkA, wave, lane);
+        an = a0 + pa + (AO ? k0 * A.ld : (long)k0);
+        bn = b0 + pb + (BO ? k0 * Bm.ld : (long)k0);
+        left_a = A.K - k0;
+        left_b = Bm.K - k0;
+        to = base + buffer * kBuffer;
+    };
+    auto ask = [&](int u) {
+        if (u < LA) la.request(u, an, left_a, to, wave, lane);
+        else if (u < kLoads) lb.request(u - LA, bn, left_b, to + 2 * T::kChunkA, wave, lane);
     };
     bf16x8 xf[2][T::MT], wf[2][T::NT];
-    auto read = [&](int buffer, int ks, int to) {
+    constexpr int kReads = T::NT + T::MT;
+    // operand r of a step: buffer, quarter, and the registers it goes to
+    auto read = [&](int r, int buffer, int ks, int reg) {
         const bf16_t *As = lds + buffer * (T::kChunkA + T::kChunkB), *Bs = As + T::kChunkA;
-#pragma unroll
-        for (int nt = 0; nt < T::NT; ++nt) wf[to][nt] = fragment<T::BN, BO, true>(Bs, wn + 32 * nt, ks, lane);
-#pragma unroll
-        for (int mt = 0; mt < T::MT; ++mt) xf[to][mt] = fragment<T::BM, AO, false>(As, wm + 32 * mt, ks, lane);
+        if (r < T::NT) wf[reg][r] = fragment<T::BN, BO, true>(Bs, wn + 32 * r, ks, lane);
+        else xf[reg][r - T::NT] = fragment<T::BM, AO, false>(As, wm + 32 * (r - T::NT), ks, lane);
     };
-    auto products = [&](int from, int mt0, int mt1) {
+    // The products of the row tiles [mt0, mt1) with what is in registers `reg`; between them the reads of a step and the loads [u0, u1), as
+    // evenly as they go.
+    auto step = [&](int reg, int mt0, int mt1, bool reading, int buffer, int ks, int u0, int u1, bool asking) {
+        const int n = (mt1 - mt0) * T::NT, side = (reading ? kReads : 0) + u1 - u0, reads = reading ? kReads : 0;
+        int d = 0, s = 0;
 #pragma unroll
         for (int mt = mt0; mt < mt1; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < T::NT; ++nt) acc[nt][mt] = mfma32(wf[from][nt], xf[from][mt], acc[nt][mt]);
+            for (int nt = 0; nt < T::NT; ++nt) {
+                acc[nt][mt] = mfma32(wf[reg][nt], xf[reg][mt], acc[nt][mt]);
+                __builtin_amdgcn_sched_barrier(0);
+                ++d;
+#pragma unroll
+                for (; s * n < side * d; ++s) {
+                    if (s < reads) read(s, buffer, ks, reg ^ 1);
+                    else if (asking) ask(u0 + s - reads);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
-    constexpr int kHalf = (T::MT + 1) / 2;
-    constexpr int kLoads = Loads<T, T::BM, AO, false>::L + Loads<T, T::BN, BO, true>::L;
+    constexpr int kHalf = (T::MT + 1) / 2, kFirst = T::MT > 1 ? kLoads / 4 : 0;
     __builtin_amdgcn_s_barrier();                  // the buffers are free
-    request(0, 0);
+    aim(0, 0);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) ask(u);
     if (total > 1) {
-        request(1, 1);
+        aim(1, 1);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) ask(u);
         asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
     } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read(0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < kReads; ++r) read(r, 0, 0, 0);
+    bool asking = false;
     for (int i = 0; i < total; ++i) {
         const int buffer = i & 1;
+        step(0, 0, T::MT, true, buffer, 1, kFirst, kLoads, asking);
+        step(1, 0, T::MT, true, buffer, 2, 0, 0, false);
+        step(0, 0, T::MT, true, buffer, 3, 0, 0, false);
+        step(1, 0, kHalf, false, 0, 0, 0, 0, false);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        asking = i + 2 < total;
+        if (asking) aim(i + 2, buffer);
+        // (behind the last chunk the reads find what is there, which nobody uses)
+        if (T::MT > 1) step(1, kHalf, T::MT, true, buffer ^ 1, 0, 0, kFirst, asking);
+        else
 #pragma unroll
-        for (int ks = 0; ks < 3; ++ks) {
-            read(buffer, ks + 1, (ks + 1) & 1);
-            __builtin_amdgcn_sched_barrier(0);
-            products(ks & 1, 0, T::MT);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        products(1, 0, kHalf);
-        __builtin_amdgcn_sched_barrier(0);
-        if (i + 1 < total) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (i + 2 < total) request(i + 2, buffer);
-            read(buffer ^ 1, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        products(1, kHalf, T::MT);
-        __builtin_amdgcn_sched_barrier(0);
+            for (int r = 0; r < kReads; ++r) read(r, buffer ^ 1, 0, 0);
     }
     // the wait between the last products and the first use of their results, spelled out: where a branch lies between them the
     // compiler has left it short
@@ -197,6 +222,39 @@ __device__ __forceinline__ void tile_of(int block, int mtiles, int ntiles, int &
     const int group = 4 * ntiles, g = i / group, m0 = 4 * g, ms = min(4, mtiles - m0), r = i - g * group;
     m = m0 + r % ms;
     n = r / ms;
+}
+
+// Rows x 8 P bf16 of one wavefront, on their way between the products' layout (a lane has 8 columns of a row) and rows as they
+// lie in memory, where a whole row of the wavefront's goes in one piece: stored from the products' layout, lines were written in pieces of 32
+// bytes, and G | U of 32768 x 5632 took 160 us where its bytes take 75.
+template <int P>
+struct Rows {
+    bf16_t *base;
+    __device__ __forceinline__ bf16_t *at(int row, int piece) const { return base + (row * P + (piece ^ (row * P / 16 % P))) * 8; }
+    __device__ __forceinline__ void put(int row, int piece, bf16x8 v) const { *(bf16x8 *)at(row, piece) = v; }
+    // to(row, piece, value) for every piece of `rows` rows
+    template <class F>
+    __device__ __forceinline__ void each(int rows, int lane, F to) const
+    {
+#pragma unroll
+        for (int r = 0; r < rows; r += 64 / P) {
+            const int row = r + lane / P, piece = lane % P;
+            to(row, piece, *(const bf16x8 *)at(row, piece));
+        }
+    }
+};
+
+// A piece of a row to memory: `n` of its 8 values exist, `vec`: rows are whole pieces.
+__device__ __forceinline__ void store_piece(bf16_t *p, bf16x8 v, int n, bool vec)
+{
+    if (vec && n >= 8) {
+        *(bf16x8 *)p = v;
+        return;
+    }
+    const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = (bf16_t)(u[e / 2] >> (16 * (e % 2)));
 }
 
 // 8 consecutive values; `n` of them exist, `vec`: in whole 16-byte pieces.
@@ -246,16 +304,18 @@ __device__ __forceinline__ void load8(const float *p, float (&v)[8], int n, bool
 
 // 8 values of an operand that a later product reads: one bf16 rounding, or three terms.
 template <int TERMS>
+__device__ __forceinline__ void operand(const float (&v)[8], bf16x8 (&t)[TERMS])
+{
+    if constexpr (TERMS == 1) t[0] = pack8(v);
+    else split3(v, t);
+}
+template <int TERMS>
 __device__ __forceinline__ void store_operand(bf16_t *p, long plane, const float (&v)[8])
 {
-    if (TERMS == 1) {
-        *(bf16x8 *)p = pack8(v);
-        return;
-    }
-    bf16x8 t[3];
-    split3(v, t);
+    bf16x8 t[TERMS];
+    operand<TERMS>(v, t);
 #pragma unroll
-    for (int q = 0; q < 3; ++q) *(bf16x8 *)(p + q * plane) = t[q];
+    for (int q = 0; q < TERMS; ++q) *(bf16x8 *)(p + q * plane) = t[q];
 }
 
 // The activations' distribution functions: act(g) = g F(g), act'(g) = F(g) + g F'(g).
