@@ -217,8 +217,8 @@ int bra_backward(const bra_shape *shape, const void *X, const void *Wqkv, const 
  * Any sizes; rows that are no multiple of 8 elements, and float32, take one more pass over the operands.  bf16: A is
  * rounded to bf16 between the products, the rest is float32.  float32: products of three bf16 terms per operand
  * (relative error of a product 2^-23); a value that is not finite, or above 3.3e38, makes NaN of what depends on it.
- * Alignment: where C and hidden are multiples of 8 (4 for float32 outputs) all of X, W1, W2, Y, pre, dY, dX and the weight
- * gradients must lie on 16 bytes, else on their element's size; BRA_ERR_ALIGN otherwise.
+ * Alignment: a matrix whose row blocks (C elements; hidden elements for W1, dW1 and pre) are multiples of 8 elements must lie on 16
+ * bytes, the others on their element's size; BRA_ERR_ALIGN otherwise.
  * Errors: NULL; SHAPE (M < 0, C or hidden < 1 or above 2^20, M above 2^30); DTYPE (dtype or act); WORKSPACE; ALIGN; LAUNCH. */
 enum { BRA_SILU = 0, BRA_GELU = 1 };                /* bra_ffn_shape.act */
 typedef struct bra_ffn_shape {

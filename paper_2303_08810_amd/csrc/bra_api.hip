@@ -101,11 +101,8 @@ static bool aligned(size_t bytes, std::initializer_list<const void *> pointers)
     return true;
 }
 
-// Alignment of the block's matrices: whole 16-byte pieces where the rows are, else elements.
-static size_t ffn_alignment(const ffn::Sizes &S)
-{
-    return S.C % 8 == 0 && S.h % 8 == 0 ? 16 : S.f32 ? 4 : 2;
-}
+// Alignment of the block's matrices, rows of C or of hidden elements of `element` bytes: whole 16-byte pieces where the rows are.
+static size_t row_alignment(int columns, size_t element) { return columns % 8 == 0 ? 16 : element; }
 
 static int make_norm_sizes(const bra_norm_shape *s, bool post, NormSizes &S)
 {
@@ -333,7 +330,8 @@ int bra_ffn_forward(const bra_ffn_shape *shape, const void *X, const void *W1, c
     if (rc != BRA_OK) return rc;
     if (S.M == 0) return BRA_OK;
     if (!X || !W1 || !W2 || !Y) return BRA_ERR_NULL;
-    if (!aligned(ffn_alignment(S), {X, W1, W2, Y, pre}) || !aligned(4, {b1, b2})) return BRA_ERR_ALIGN;
+    const size_t e = S.f32 ? 4 : 2;
+    if (!aligned(row_alignment(S.C, e), {X, W2, Y}) || !aligned(row_alignment(S.h, e), {W1, pre}) || !aligned(4, {b1, b2})) return BRA_ERR_ALIGN;
     if (!ws_ok(ws, ws_bytes, ffn_workspace_bytes(S))) return BRA_ERR_WORKSPACE;
     return ffn_forward(S, X, W1, b1, W2, b2, Y, pre, ws, (hipStream_t)hip_stream);
 }
@@ -356,8 +354,9 @@ int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, 
     if (rc != BRA_OK) return rc;
     if (grad_dtype != BRA_F32 && grad_dtype != BRA_BF16) return BRA_ERR_DTYPE;
     if (!dW1 || !dW2 || (S.M > 0 && (!X || !W1 || !W2 || !dY || !dX))) return BRA_ERR_NULL;
-    if (!aligned(ffn_alignment(S), {X, W1, W2, pre, dY, dX}) || !aligned(4, {b1})) return BRA_ERR_ALIGN;
-    if (!aligned(ffn_alignment(S) == 16 ? 16 : grad_dtype == BRA_F32 ? 4 : 2, {dW1, dW2, db1, db2})) return BRA_ERR_ALIGN;
+    const size_t e = S.f32 ? 4 : 2, ge = grad_dtype == BRA_F32 ? 4 : 2;
+    if (!aligned(row_alignment(S.C, e), {X, W2, dY, dX}) || !aligned(row_alignment(S.h, e), {W1, pre}) || !aligned(4, {b1})) return BRA_ERR_ALIGN;
+    if (!aligned(row_alignment(S.h, ge), {dW1}) || !aligned(row_alignment(S.C, ge), {dW2}) || !aligned(ge, {db1, db2})) return BRA_ERR_ALIGN;
     if (!ws_ok(ws, ws_bytes, ffn_backward_workspace_bytes(S))) return BRA_ERR_WORKSPACE;
     return ffn_backward(S, X, W1, b1, W2, pre, dY, dX, dW1, dW2, db1, db2, grad_dtype == BRA_F32, ws, (hipStream_t)hip_stream);
 }

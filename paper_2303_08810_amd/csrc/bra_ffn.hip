@@ -118,44 +118,7 @@ template <class T, bool BO, int TERMS, typename E>
 __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_product(Operand A, Operand Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    bf16_t *lds = (bf16_t *)smem;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    int mt0, nt0;
-    tile_of(blockIdx.x, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
-    const long m0 = (long)mt0 * T::BM;
-    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), last = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
-    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
-    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, last); });
-    f32x16 acc[T::NT][T::MT];
-    clear<T>(acc);
-    multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, 0, (A.K + 63) / 64, lds, acc);
-    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = n0 + (wave % T::WC) * (32 * T::NT);
-    const bool vec = N % 8 == 0;
-    const Rows<4 * T::NT> out{lds + wave * (32 * T::MT * 32 * T::NT)};
-#pragma unroll
-    for (int nt = 0; nt < T::NT; ++nt)
-#pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            const int piece = 4 * nt + 2 * run + hi, col = wn + 8 * piece, n = N - col;
-            float b[8];
-            if (bias && n > 0) load8(bias + col, b, n, false);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b[e] = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < T::MT; ++mt) {
-                const int row = wm + 32 * mt + c;
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e] + b[e];
-                if constexpr (TERMS == 1) out.put(32 * mt + c, piece, pack8(v));
-                else if (row < rows) store8(Out + (size_t)(m0 + row) * N + col, v, n, vec);
-            }
-        }
-    if constexpr (TERMS == 1)
-        out.each(32 * T::MT, lane, [&](int row, int piece, bf16x8 v) {
-            if (wm + row < rows) store_piece(Out + (size_t)(m0 + wm + row) * N + wn + 8 * piece, v, N - wn - 8 * piece, vec);
-        });
+    product_tile<T, BO, TERMS, E>(A, Bm, bias, Out, M, N, blockIdx.x, (bf16_t *)smem);
 }
 
 template <class T, bool BO, int TERMS, typename E>
@@ -171,9 +134,9 @@ template <bool BO, int TERMS, typename E>
 int pick_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
     switch (tile_size(M, N)) {
-    case 256: return launch_product<Tile<256, 256, 4, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
-    case 128: return launch_product<Tile<128, 128, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
-    default: return launch_product<Tile<64, 64, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 256: return launch_product<Tile<256, 256, 4, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 128: return launch_product<Tile<128, 128, 2, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    default: return launch_product<Tile<64, 64, 2, 2, 4>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     }
 }
 
@@ -190,9 +153,9 @@ template <int TERMS, int ACT, typename E>
 int pick_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, hipStream_t st)
 {
     switch (tile_size(S.M, 2L * S.hp)) {
-    case 256: return launch_gated<Tile<256, 256, 4, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
-    case 128: return launch_gated<Tile<128, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
-    default: return launch_gated<Tile<64, 128, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    case 256: return launch_gated<Tile<256, 256, 4, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    case 128: return launch_gated<Tile<128, 128, 2, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+    default: return launch_gated<Tile<64, 128, 2, 2, 3>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     }
 }
 

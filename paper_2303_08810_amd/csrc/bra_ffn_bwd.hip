@@ -2,12 +2,13 @@
 //
 //   k_hidden      dA = dY W2^T and, from it and G | U, dG | dU and A in bf16 (float32: three terms).  G | U are read, or formed
 //                 again in the same tile by a second product, so that they are not rounded and not stored
-//   k_product     dX = [dG | dU] W1^T
-//   k_weights     dW1 = X^T [dG | dU] and dW2 = A^T dY, contractions over all tokens in shares, in one launch
-//   k_columns     sums over the tokens for the biases' gradients
-//   k_shares      the shares' sums, in order, in the type that is asked for
+//   k_gradients   dX = [dG | dU] W1^T in tiles, dW1 = X^T [dG | dU] and dW2 = A^T dY in parts of the contraction over all tokens, and the
+//                 columns' sums for the biases: one launch, none of them waits for another
+//   k_sums        the parts' sums, in order, in the type that is asked for
 #include "bra_ffn.h"
 #include "bra_ffn_dev.h"
+
+#include <algorithm>
 
 namespace bra {
 namespace ffn {
@@ -130,70 +131,95 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
     }
 }
 
-// A contraction over the tokens: Part[share][rows][cols] = A^T B over the share's tokens; rows and cols as in the workspace (padded).
+// Contractions over the tokens, dW = A^T B, rows x cols as they lie in the workspace (padded).  The tiles of both stand in one row, each with
+// `chunks` chunks.  The first `main` tiles come in `shares` equal shares, as many as there are workgroups at once (or whole, some to each
+// workgroup); those of one share next to each other on an XCD read the same tokens at the same time.  The chunks of the tiles that are left go
+// to all workgroups in equal parts, so that all end together.  One share per tile more than fits took a second round for 8 of 132 tiles;
+// all tiles in equal parts, wherever those begin, shared nothing in the L2 (dW and dX of 16384 x 1024 x 2816: 478 us).
+// Sums go to slots: a share to its own, a part of what is left to (tile + workgroup) behind them, which no two have the same.
 struct Contraction {
     Operand A, B;
-    float *part;
     int rows, cols;
 };
+struct Weights {
+    Contraction job[2];
+    float *part;            // slots of BM x BN sums in the order of the wavefronts' registers
+    int tiles0, tiles, chunks, main, shares, per, workgroups;
+};
+template <class T>
+constexpr int kSlot = T::BM * T::BN;
 
-template <class T, int TERMS>
-__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_weights(Contraction J0, Contraction J1, int tiles0, int tiles1, int shares)
+// Tile i of the row: its job and where it lies.
+template <class T>
+__device__ __forceinline__ void weight_tile(const Weights &W, int i, int &job, int &r0, int &c0)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    bf16_t *lds = (bf16_t *)smem;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    const int share = blockIdx.x / (tiles0 + tiles1), i = blockIdx.x % (tiles0 + tiles1);
-    const Contraction &J = i < tiles0 ? J0 : J1;
-    int mt0, nt0;
-    tile_of(i < tiles0 ? i : i - tiles0, (J.rows + T::BM - 1) / T::BM, (J.cols + T::BN - 1) / T::BN, mt0, nt0);
-    const int r0 = mt0 * T::BM, c0 = nt0 * T::BN;
-    const Loads<T, T::BM, true, false> la(wave, lane, J.A.ld, [&](int row) { return (long)min(row, J.rows - 8 - r0); });
-    const Loads<T, T::BN, true, true> lb(wave, lane, J.B.ld, [&](int col) { return (long)min(col, J.cols - 8 - c0); });
-    const int chunks = (J.A.K + 63) / 64, first = (int)((long)chunks * share / shares), end = (int)((long)chunks * (share + 1) / shares);
-    f32x16 acc[T::NT][T::MT];
-    clear<T>(acc);
-    if (end > first) multiply<T, true, true, TERMS>(J.A, J.B, J.A.p + r0, J.B.p + c0, la, lb, first, end, lds, acc);
-    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
-    float *part = J.part + (size_t)share * J.rows * J.cols;
-#pragma unroll
-    for (int nt = 0; nt < T::NT; ++nt)
-#pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            const int col = c0 + wn + 32 * nt + 16 * run + 8 * hi;
-            if (col >= J.cols) continue;
-#pragma unroll
-            for (int mt = 0; mt < T::MT; ++mt) {
-                const int row = r0 + wm + 32 * mt + c;
-                if (row >= J.rows) continue;
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e];
-                store8(part + (size_t)row * J.cols + col, v, 8, true);
-            }
-        }
+    job = i >= W.tiles0;
+    const Contraction &J = W.job[job];
+    const int t = i - (job ? W.tiles0 : 0), mtiles = (J.rows + T::BM - 1) / T::BM, ntiles = (J.cols + T::BN - 1) / T::BN;
+    const int g = t / (4 * ntiles), ms = min(4, mtiles - 4 * g), r = t - g * 4 * ntiles;
+    r0 = (4 * g + r % ms) * T::BM;
+    c0 = r / ms * T::BN;
 }
 
-// Part[share][col] = sum over the share's rows of the columns of two maps (each the sum of its planes), 8 columns per thread, 32 rows
-// of threads per workgroup.
+template <class T, int TERMS>
+__device__ __forceinline__ void weights_part(const Weights &W, int workgroup, bf16_t *lds)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    long at = (long)workgroup * W.per;
+    const long end = min(at + W.per, (long)(W.tiles - W.main) * W.chunks);
+    for (int i = workgroup;;) {
+        int tile, first, last, slot;
+        if (i < W.main * W.shares) {
+            const int share = i / W.main;
+            tile = i % W.main;
+            first = (int)((long)W.chunks * share / W.shares);
+            last = (int)((long)W.chunks * (share + 1) / W.shares);
+            slot = i;
+            i += W.workgroups;
+        } else if (at < end) {
+            const int t = (int)(at / W.chunks);
+            tile = W.main + t;
+            first = (int)(at % W.chunks);
+            last = (int)min((long)W.chunks, first + end - at);
+            slot = W.main * W.shares + t + workgroup;
+            at += last - first;
+        } else return;
+        int job, r0, c0;
+        weight_tile<T>(W, tile, job, r0, c0);
+        const Operand A = W.job[job].A, B = W.job[job].B;
+        const int rows = W.job[job].rows, cols = W.job[job].cols;
+        const Loads<T, T::BM, true, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 8 - r0); });
+        const Loads<T, T::BN, true, true> lb(wave, lane, B.ld, [&](int col) { return (long)min(col, cols - 8 - c0); });
+        f32x16 acc[T::NT][T::MT];
+        clear<T>(acc);
+        multiply<T, true, true, TERMS>(A, B, A.p + r0, B.p + c0, la, lb, first, last, lds, acc);
+        f32x4 *part = (f32x4 *)(W.part + (size_t)slot * kSlot<T>) + wave * (T::NT * T::MT * 256) + lane;
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) part[((nt * T::MT + mt) * 4 + q) * 64] = f32x4{acc[nt][mt][4 * q], acc[nt][mt][4 * q + 1], acc[nt][mt][4 * q + 2], acc[nt][mt][4 * q + 3]};
+    }
+}
+
+// Part[share][col] = sum over the share's rows of a map's columns (the sum of its planes), 8 columns per thread, 64 per workgroup.
 struct Columns {
     const bf16_t *map;
     long ld, plane;
     float *part;
-    int cols;
+    int cols, groups;
 };
 template <int TERMS>
-__global__ __launch_bounds__(256) void k_columns(Columns J0, Columns J1, int groups0, long M, int shares)
+__device__ __forceinline__ void columns_part(const Columns &J, int group, int share, int shares, long M, float *sums)
 {
-    __shared__ float sums[32][64 + 4];
-    const Columns J = (int)blockIdx.x < groups0 ? J0 : J1;
-    const int group = (int)blockIdx.x < groups0 ? blockIdx.x : blockIdx.x - groups0, share = blockIdx.y;
-    const int piece = threadIdx.x % 8, slot = threadIdx.x / 8, col = 64 * group + 8 * piece;
+    constexpr int kPitch = 64 + 4;
+    const int piece = threadIdx.x % 8, slot = threadIdx.x / 8, slots = blockDim.x / 8, col = 64 * group + 8 * piece;
     float acc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
     if (col < J.cols)
-        for (long m = M * share / shares + slot; m < M * (share + 1) / shares; m += 32)
+        for (long m = M * share / shares + slot; m < M * (share + 1) / shares; m += slots)
 #pragma unroll
             for (int q = TERMS - 1; q >= 0; --q) {
                 float v[8];
@@ -202,48 +228,109 @@ __global__ __launch_bounds__(256) void k_columns(Columns J0, Columns J1, int gro
                 for (int e = 0; e < 8; ++e) acc[e] += v[e];
             }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[slot][8 * piece + e] = acc[e];
+    for (int e = 0; e < 8; ++e) sums[slot * kPitch + 8 * piece + e] = acc[e];
     __syncthreads();
     if (threadIdx.x < 64 && 64 * group + (int)threadIdx.x < J.cols) {
         float s = 0.f;
-        for (int r = 0; r < 32; ++r) s += sums[r][threadIdx.x];
+        for (int r = 0; r < slots; ++r) s += sums[r * kPitch + threadIdx.x];
         J.part[(size_t)share * J.cols + 64 * group + threadIdx.x] = s;
     }
 }
 
-// out[row][block * cols + col] = sum over the shares of part[share][row][block * cols_p + col], 8 columns per thread.
-struct Shares {
-    const float *part;
-    void *out;
-    long size;          // of a share
-    int blocks, cols, cols_p, shares;
+// Everything that follows from dG | dU and A, in one launch: the weights' parts, dX = [dG | dU] W1^T in tiles, the columns' sums.
+struct Gradients {
+    Weights W;
+    Operand dP, W1;
+    void *dX;
+    long M;
+    int C, product_tiles;
+    Columns columns[2];
+    int shares;
 };
-struct SharesList {
-    Shares job[4];
-    long end[4];
-    int count;
+template <class T, int TERMS, typename E>
+__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradients G)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *lds = (bf16_t *)smem;
+    int block = blockIdx.x;
+    if (block < G.W.workgroups) {
+        // workgroups of an XCD have neighbouring parts
+        const int xcd = block % 8, per = G.W.workgroups / 8, rest = G.W.workgroups % 8;
+        weights_part<T, TERMS>(G.W, xcd * per + min(xcd, rest) + block / 8, lds);
+        return;
+    }
+    block -= G.W.workgroups;
+    if (block < G.product_tiles) {
+        product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
+        return;
+    }
+    block -= G.product_tiles;
+    const int j = block >= G.columns[0].groups * G.shares;
+    if (j) block -= G.columns[0].groups * G.shares;
+    columns_part<TERMS>(G.columns[j], block / G.shares, block % G.shares, G.shares, G.M, (float *)smem);
+}
+
+// The parts' sums, in order: a thread has 8 columns of a row of a tile, in the place where its wavefront had them; behind the tiles the columns.
+struct SumsArgs {
+    Weights W;
+    void *dW[2];
+    int rows[2], blocks[2], cols[2], cols_p[2];         // as they are returned; column blocks of cols_p columns in the workspace
+    void *db[2];
+    const float *columns[2];
+    int shares, tile_blocks;
 };
+template <class T, typename E>
+__global__ __launch_bounds__(256) void k_sums(SumsArgs S)
+{
+    if ((int)blockIdx.x < S.tile_blocks) {
+        constexpr int kPer = kSlot<T> / 8 / 256;        // workgroups per tile
+        const int tile = blockIdx.x / kPer, i = blockIdx.x % kPer * 256 + threadIdx.x, lane = i % 64, run = i / 64 % 2, frag = i / 128;
+        const int mt = frag % T::MT, nt = frag / T::MT % T::NT, wave = frag / (T::MT * T::NT);
+        int job, r0, c0;
+        weight_tile<T>(S.W, tile, job, r0, c0);
+        const int row = r0 + (wave / T::WC) * (32 * T::MT) + 32 * mt + lane % 32, col = c0 + (wave % T::WC) * (32 * T::NT) + 32 * nt + 16 * run + 8 * (lane / 32);
+        if (row >= S.rows[job] || col >= S.W.job[job].cols) return;
+        const int t = tile - S.W.main;          // of those that are left
+        int first = tile, apart = S.W.main, count = S.W.shares;
+        if (t >= 0) {
+            const int w0 = (int)((long)t * S.W.chunks / S.W.per), w1 = (int)(((long)(t + 1) * S.W.chunks - 1) / S.W.per);
+            first = S.W.main * S.W.shares + t + w0;
+            apart = 1;
+            count = w1 - w0 + 1;
+        }
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < count; ++k) {
+            const f32x4 *p = (const f32x4 *)(S.W.part + (size_t)(first + k * apart) * kSlot<T>) + (frag * 4 + 2 * run) * 64 + lane;
+            const f32x4 a = p[0], b = p[64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { acc[e] += a[e]; acc[4 + e] += b[e]; }
+        }
+        const int block = col / S.cols_p[job], in = col % S.cols_p[job], n = S.cols[job] - in;
+        store8((E *)S.dW[job] + ((size_t)row * S.blocks[job] + block) * S.cols[job] + in, acc, n, S.cols[job] % 8 == 0);
+        return;
+    }
+    int i = ((int)blockIdx.x - S.tile_blocks) * 256 + threadIdx.x;
+    for (int j = 0; j < 2; ++j) {
+        const int count = S.db[j] ? S.blocks[j] * S.cols[j] : 0;
+        if (i < count) {
+            const int at = i / S.cols[j] * S.cols_p[j] + i % S.cols[j];
+            float s = 0.f;
+            for (int p = 0; p < S.shares; ++p) s += S.columns[j][(size_t)p * S.blocks[j] * S.cols_p[j] + at];
+            store_from_f32((E *)S.db[j] + i, s);
+            return;
+        }
+        i -= count;
+    }
+}
+
 template <typename E>
-__global__ __launch_bounds__(256) void k_shares(SharesList L)
+__global__ __launch_bounds__(256) void k_zero(E *p, long n)
 {
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    int j = 0;
-    while (j < L.count && i >= L.end[j]) ++j;
-    if (j == L.count) return;
-    const Shares S = L.job[j];
-    const long p = i - (j ? L.end[j - 1] : 0);
-    const int per = S.cols_p / 8, piece = (int)(p % per);
-    const long line = p / per;
-    float acc[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    for (int s = 0; s < S.shares; ++s) {
-        float v[8];
-        load8(S.part + s * S.size + line * S.cols_p + 8 * piece, v, 8, true);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += v[e];
-    }
-    store8((E *)S.out + line * S.cols + 8 * piece, acc, S.cols - 8 * piece, S.cols % 8 == 0);
+    if (i < n) store_from_f32(p + i, 0.f);
 }
 
 template <class TD, class TG, int TERMS, int ACT, bool GIVEN, typename E>
@@ -263,55 +350,75 @@ int pick_hidden(const Operand &dY, const Operand &W2, const Operand &X, const Op
 {
     if (pre) {
         switch (tile_size(S.M, S.hp)) {
-        case 256: return launch_hidden<Tile<256, 256, 4, 2>, Tile<256, 256, 4, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
-        case 128: return launch_hidden<Tile<128, 128, 2, 2>, Tile<128, 128, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
-        default: return launch_hidden<Tile<64, 64, 2, 2>, Tile<64, 64, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+        case 256: return launch_hidden<Tile<256, 256, 4, 2, 2>, Tile<256, 256, 4, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+        case 128: return launch_hidden<Tile<128, 128, 2, 2, 2>, Tile<128, 128, 2, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+        default: return launch_hidden<Tile<64, 64, 2, 2, 4>, Tile<64, 64, 2, 2, 4>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         }
     }
     if (tile_size(S.M, S.hp) >= 128)
-        return launch_hidden<Tile<128, 128, 2, 4>, Tile<128, 256, 2, 4>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
-    return launch_hidden<Tile<64, 64, 2, 2>, Tile<64, 128, 2, 2>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+        return launch_hidden<Tile<128, 128, 2, 4, 2>, Tile<128, 256, 2, 4, 2>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
+    return launch_hidden<Tile<64, 64, 2, 2, 4>, Tile<64, 128, 2, 2, 3>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
 }
-
-template <class T, int TERMS>
-int launch_weights(const Contraction &J0, const Contraction &J1, int shares, hipStream_t st)
-{
-    if (allow_lds<k_weights<T, TERMS>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
-    auto tiles = [](const Contraction &J) { return ((J.rows + T::BM - 1) / T::BM) * ((J.cols + T::BN - 1) / T::BN); };
-    const int t0 = tiles(J0), t1 = tiles(J1);
-    k_weights<T, TERMS><<<(unsigned)((t0 + t1) * shares), T::kThreads, T::kLds, st>>>(J0, J1, t0, t1, shares);
-    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
-}
-
-// Tiles of the weights' gradients and the shares of the tokens: workgroups for every compute unit, in rounds that are
-// nearly full, each with at least four chunks of 64 tokens.
-struct WeightsPlan {
-    int side, shares;
-    WeightsPlan(const Sizes &S)
-    {
-        const int chunks = (int)((S.M + 63) / 64);
-        auto tiles = [&](int side) {
-            auto n = [&](int v) { return (v + side - 1) / side; };
-            return (long)n(S.Cp) * n(2 * S.hp) + (long)n(S.hp) * n(S.Cp);
-        };
-        side = tiles(256) * std::min(8, std::max(1, chunks / 8)) >= 192 ? 256 : 128;
-        const int resident = side == 256 ? 256 : 512;        // workgroups that run at once
-        const long t = tiles(side);
-        const int most = (int)std::max(1L, std::min<long>({(long)std::max(1, chunks / 4), 64L, 4 * resident / t + 1}));
-        double best = 0;
-        shares = 1;
-        for (int s = 1; s <= most; ++s) {
-            const long w = t * s;
-            const double use = (double)w / (double)((w + resident - 1) / resident * resident) * (1 - 0.01 * s);
-            if (use > best) { best = use; shares = s; }
-        }
-    }
-};
 
 constexpr int kColumnShares = 32;
 
+template <class T, int TERMS, typename E>
+int launch_gradients(Gradients G, bool columns, hipStream_t st)
+{
+    constexpr size_t bytes = std::max<size_t>(T::kLds, T::kThreads / 8 * 68 * 4);
+    if (allow_lds<k_gradients<T, TERMS, E>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
+    G.product_tiles = (int)(((G.M + T::BM - 1) / T::BM) * ((G.C + T::BN - 1) / T::BN));
+    const int groups = columns ? G.columns[0].groups + G.columns[1].groups : 0;
+    k_gradients<T, TERMS, E><<<(unsigned)(G.W.workgroups + G.product_tiles + groups * G.shares), T::kThreads, bytes, st>>>(G);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+template <class T>
+int launch_sums(SumsArgs S, bool grads_f32, hipStream_t st)
+{
+    S.tile_blocks = S.W.tiles * (kSlot<T> / 8 / 256);
+    const int columns = (S.db[0] ? S.blocks[0] * S.cols[0] : 0) + (S.db[1] ? S.cols[1] : 0);
+    const unsigned blocks = (unsigned)(S.tile_blocks + (columns + 255) / 256);
+    if (grads_f32) k_sums<T, float><<<blocks, 256, 0, st>>>(S);
+    else k_sums<T, bf16_t><<<blocks, 256, 0, st>>>(S);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+// Side of the tiles of k_gradients, and how the weights' tiles are shared out (see Weights).
+struct WeightsPlan {
+    int side, tiles0, tiles, chunks, main, shares, per, workgroups;
+    WeightsPlan(const Sizes &S)
+    {
+        chunks = (int)((S.M + 63) / 64);
+        auto tiles_of = [&](int side, int rows, int cols) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); };
+        auto work = [&](int side) {         // of both, in chunks of a tile
+            const long t = tiles_of(side, S.Cp, 2 * S.hp) + tiles_of(side, S.hp, S.Cp), p = ((S.M + side - 1) / side) * (long)((S.C + side - 1) / side);
+            return t * chunks + p * ((2 * S.hp + 63) / 64);
+        };
+        side = work(256) >= 256 * 24 ? 256 : work(128) >= 512 * 4 ? 128 : 64;
+        tiles0 = tiles_of(side, S.Cp, 2 * S.hp);
+        tiles = tiles0 + tiles_of(side, S.hp, S.Cp);
+        const int at_once = side == 256 ? 256 : 512, least = S.f32 ? 1 : 2;     // chunks of a share (of float32 a chunk is six)
+        per = 0;
+        if (tiles >= at_once) {
+            shares = 1;
+            main = tiles / at_once * at_once;
+        } else {
+            shares = std::min((at_once + tiles - 1) / tiles, std::max(1, chunks / least));
+            main = std::min(tiles, at_once / shares);
+        }
+        workgroups = std::min(at_once, main * shares);
+        if (main < tiles) {
+            workgroups = at_once;
+            // (more than 16 parts of a tile took k_sums longer than they saved here: 53 us against 28, with 64)
+            per = std::max({(int)(((long)(tiles - main) * chunks + at_once - 1) / at_once), least, (chunks + 15) / 16});
+        }
+    }
+    int slots() const { return main * shares + (main < tiles ? tiles - main + workgroups : 0); }
+};
+
 struct BackwardPlan {
-    size_t X, W1, W2, dY, Act, dP, parts1, parts2, cols1, cols2, total;
+    size_t X, W1, W2, dY, Act, dP, parts, cols1, cols2, total;
     BackwardPlan(const Sizes &S, const WeightsPlan &P)
     {
         size_t at = 0;
@@ -327,8 +434,7 @@ struct BackwardPlan {
         dY = S.copies() ? take(M * S.Cp * e) : 0;
         Act = take(M * S.hp * e);
         dP = take(M * 2 * S.hp * e);
-        parts1 = take((size_t)P.shares * S.Cp * 2 * S.hp * 4);
-        parts2 = take((size_t)P.shares * S.hp * S.Cp * 4);
+        parts = take((size_t)P.slots() * P.side * P.side * 4);
         cols1 = take((size_t)kColumnShares * 2 * S.hp * 4);
         cols2 = take((size_t)kColumnShares * S.Cp * 4);
         total = at;
@@ -339,6 +445,10 @@ struct BackwardPlan {
 }  // namespace ffn
 
 using namespace ffn;
+
+typedef Tile<256, 256, 4, 2, 2> T256;
+typedef Tile<128, 128, 2, 2, 2> T128;
+typedef Tile<64, 64, 2, 2, 4> T64;
 
 size_t ffn_backward_workspace_bytes(const Sizes &S) { return BackwardPlan(S, WeightsPlan(S)).total; }
 
@@ -373,43 +483,49 @@ int ffn_backward(const Sizes &S, const void *X, const void *W1, const float *b1,
             if (rc != BRA_OK) return rc;
         }
         const Operand odP{at(P.dP), 2L * S.hp, pP, 2 * S.hp};
-        Operand iW1 = oW1;
-        iW1.K = 2 * S.hp;
-        rc = product(odP, iW1, false, S.M, S.C, dX, nullptr, S.f32, K_FFN_PRODUCT, st);
-        if (rc != BRA_OK) return rc;
-        // over the tokens
-        ProfScope prof(st, K_FFN_WEIGHT_GRADS);
+        Gradients G{};
         const int M = (int)S.M;
-        const Contraction J0{{(const bf16_t *)X, S.Cp, pX, M}, {at(P.dP), 2L * S.hp, pP, M}, (float *)at(P.parts1), S.Cp, 2 * S.hp};
-        const Contraction J1{{at(P.Act), S.hp, pA, M}, {(const bf16_t *)dY, S.Cp, pX, M}, (float *)at(P.parts2), S.hp, S.Cp};
-        if (W.side == 256) rc = S.f32 ? launch_weights<Tile<256, 256, 4, 2>, 3>(J0, J1, W.shares, st) : launch_weights<Tile<256, 256, 4, 2>, 1>(J0, J1, W.shares, st);
-        else rc = S.f32 ? launch_weights<Tile<128, 128, 2, 2>, 3>(J0, J1, W.shares, st) : launch_weights<Tile<128, 128, 2, 2>, 1>(J0, J1, W.shares, st);
-        if (rc != BRA_OK) return rc;
-        if (db1 || db2) {
-            const Columns C0{at(P.dP), 2L * S.hp, pP, (float *)at(P.cols1), 2 * S.hp}, C1{(const bf16_t *)dY, S.Cp, pX, (float *)at(P.cols2), S.Cp};
-            const int g0 = db1 ? (2 * S.hp + 63) / 64 : 0, g1 = db2 ? (S.Cp + 63) / 64 : 0;
-            const dim3 grid(g0 + g1, kColumnShares);
-            if (S.f32) k_columns<3><<<grid, 256, 0, st>>>(C0, C1, g0, S.M, kColumnShares);
-            else k_columns<1><<<grid, 256, 0, st>>>(C0, C1, g0, S.M, kColumnShares);
-            if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+        G.W.job[0] = Contraction{{(const bf16_t *)X, S.Cp, pX, M}, {at(P.dP), 2L * S.hp, pP, M}, S.Cp, 2 * S.hp};
+        G.W.job[1] = Contraction{{at(P.Act), S.hp, pA, M}, {(const bf16_t *)dY, S.Cp, pX, M}, S.hp, S.Cp};
+        G.W.part = (float *)at(P.parts);
+        G.W.tiles0 = W.tiles0; G.W.tiles = W.tiles; G.W.chunks = W.chunks; G.W.main = W.main; G.W.shares = W.shares; G.W.per = W.per; G.W.workgroups = W.workgroups;
+        G.dP = odP;
+        G.W1 = oW1;
+        G.W1.K = 2 * S.hp;
+        G.dX = dX; G.M = S.M; G.C = S.C; G.shares = kColumnShares;
+        G.columns[0] = Columns{at(P.dP), 2L * S.hp, pP, (float *)at(P.cols1), 2 * S.hp, db1 ? (2 * S.hp + 63) / 64 : 0};
+        G.columns[1] = Columns{(const bf16_t *)dY, S.Cp, pX, (float *)at(P.cols2), S.Cp, db2 ? (S.Cp + 63) / 64 : 0};
+        {
+            ProfScope prof(st, K_FFN_WEIGHT_GRADS);
+            const bool columns = db1 || db2;
+            if (S.f32) rc = W.side == 256 ? launch_gradients<T256, 3, float>(G, columns, st) : W.side == 128 ? launch_gradients<T128, 3, float>(G, columns, st)
+                                                                                                 : launch_gradients<T64, 3, float>(G, columns, st);
+            else rc = W.side == 256 ? launch_gradients<T256, 1, bf16_t>(G, columns, st) : W.side == 128 ? launch_gradients<T128, 1, bf16_t>(G, columns, st)
+                                                                                                : launch_gradients<T64, 1, bf16_t>(G, columns, st);
+            if (rc != BRA_OK) return rc;
         }
+        ProfScope prof(st, K_FFN_SUMS);
+        SumsArgs A{};
+        A.W = G.W;
+        A.dW[0] = dW1; A.dW[1] = dW2; A.db[0] = db1; A.db[1] = db2;
+        A.rows[0] = S.C; A.rows[1] = S.h;
+        A.blocks[0] = 2; A.blocks[1] = 1;
+        A.cols[0] = S.h; A.cols[1] = S.C;
+        A.cols_p[0] = S.hp; A.cols_p[1] = S.Cp;
+        A.columns[0] = (const float *)at(P.cols1); A.columns[1] = (const float *)at(P.cols2);
+        A.shares = kColumnShares;
+        return W.side == 256 ? launch_sums<T256>(A, grads_f32, st) : W.side == 128 ? launch_sums<T128>(A, grads_f32, st) : launch_sums<T64>(A, grads_f32, st);
     }
     ProfScope prof(st, K_FFN_SUMS);
-    SharesList L{};
-    auto add = [&](const float *part, void *out, int rows, int rows_p, int blocks, int cols, int cols_p, int shares) {
-        if (!out) return;
-        const long before = L.count ? L.end[L.count - 1] : 0;
-        L.job[L.count] = Shares{part, out, (long)rows_p * blocks * cols_p, blocks, cols, cols_p, S.M > 0 ? shares : 0};
-        L.end[L.count++] = before + (long)rows * blocks * (cols_p / 8);
-    };
-    add((const float *)at(P.parts1), dW1, S.C, S.Cp, 2, S.h, S.hp, W.shares);
-    add((const float *)at(P.parts2), dW2, S.h, S.hp, 1, S.C, S.Cp, W.shares);
-    add((const float *)at(P.cols1), db1, 1, 1, 2, S.h, S.hp, kColumnShares);
-    add((const float *)at(P.cols2), db2, 1, 1, 1, S.C, S.Cp, kColumnShares);
-    const unsigned blocks = (unsigned)((L.end[L.count - 1] + 255) / 256);
-    if (grads_f32) k_shares<float><<<blocks, 256, 0, st>>>(L);
-    else k_shares<bf16_t><<<blocks, 256, 0, st>>>(L);
-    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+    const struct { void *p; long n; } all[4] = {{dW1, (long)S.C * 2 * S.h}, {dW2, (long)S.h * S.C}, {db1, 2L * S.h}, {db2, S.C}};
+    for (const auto &z : all) {
+        if (!z.p) continue;
+        const unsigned blocks = (unsigned)((z.n + 255) / 256);
+        if (grads_f32) k_zero<float><<<blocks, 256, 0, st>>>((float *)z.p, z.n);
+        else k_zero<bf16_t><<<blocks, 256, 0, st>>>((bf16_t *)z.p, z.n);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
 }
 
 }  // namespace bra

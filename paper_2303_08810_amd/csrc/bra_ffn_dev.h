@@ -1,7 +1,7 @@
 // Building blocks of the gated feed-forward block's products (internal).
 //
-// A tile of BM rows m x BN columns n of a product, the contraction in chunks of 64 that direct loads bring into one of two
-// buffers in LDS while the other is multiplied.  Either operand may lie with the contraction axis inside (rows of k) or
+// A tile of BM rows m x BN columns n of a product, the contraction in chunks of 64 that direct loads bring into a ring of
+// buffers in LDS while one of them is multiplied.  Either operand may lie with the contraction axis inside (rows of k) or
 // outside (rows of m or n): the second kind is read by the transposing LDS read, so that no product of the forward or the
 // backward pass needs a transposed copy.  The product is formed transposed (rows n, columns m of the 32x32x16 instruction), the two
 // middle bits of n exchanged, so that a lane ends up with 8 consecutive columns of one row.
@@ -21,14 +21,14 @@ using namespace mfma;
 // What chunks read beyond the contraction's end.
 alignas(16) static __device__ bf16_t zeros[8];
 
-// BM x BN outputs by WR x WC wavefronts, MT x NT 32 x 32 tiles each.
-template <int BM_, int BN_, int WR_, int WC_>
+// BM x BN outputs by WR x WC wavefronts, MT x NT 32 x 32 tiles each, NB buffers.
+template <int BM_, int BN_, int WR_, int WC_, int NB_>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, kWaves = WR * WC, kThreads = 64 * kWaves;
+    static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, NB = NB_, kWaves = WR * WC, kThreads = 64 * kWaves;
     static constexpr int MT = BM / (32 * WR), NT = BN / (32 * WC);
     static constexpr int kChunkA = BM * 64, kChunkB = BN * 64;                  // elements of a chunk
     static constexpr int kMinWaves = MT * NT > 8 ? 1 : 2;                       // per SIMD, of the register budget
-    static constexpr size_t kLds = 2 * (size_t)(kChunkA + kChunkB) * 2;
+    static constexpr size_t kLds = NB * (size_t)(kChunkA + kChunkB) * 2;
 };
 
 // Swizzle of the 16-byte pieces of a row: by rows of k where the contraction is outside (the four rows that a transposing
@@ -175,36 +175,37 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
     };
     constexpr int kHalf = (T::MT + 1) / 2, kFirst = T::MT > 1 ? kLoads / 4 : 0;
     __builtin_amdgcn_s_barrier();                  // the buffers are free
-    aim(0, 0);
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) ask(u);
-    if (total > 1) {
-        aim(1, 1);
+    for (int i = 0; i < min(T::NB, total); ++i) {
+        aim(i, i);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) ask(u);
-        asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
-    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    if (total >= T::NB) asm volatile("s_waitcnt vmcnt(%0)" : : "n"((T::NB - 1) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int r = 0; r < kReads; ++r) read(r, 0, 0, 0);
     bool asking = false;
-    for (int i = 0; i < total; ++i) {
-        const int buffer = i & 1;
+    for (int i = 0, buffer = 0; i < total; ++i) {
+        const int next = buffer + 1 == T::NB ? 0 : buffer + 1;
         step(0, 0, T::MT, true, buffer, 1, kFirst, kLoads, asking);
         step(1, 0, T::MT, true, buffer, 2, 0, 0, false);
         step(0, 0, T::MT, true, buffer, 3, 0, 0, false);
         step(1, 0, kHalf, false, 0, 0, 0, 0, false);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // the next chunk is there; those behind it may be on their way, while as many are
+        if (T::NB > 2 && i + T::NB <= total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((T::NB - 2) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        asking = i + 2 < total;
-        if (asking) aim(i + 2, buffer);
+        asking = i + T::NB < total;
+        if (asking) aim(i + T::NB, buffer);
         // (behind the last chunk the reads find what is there, which nobody uses)
-        if (T::MT > 1) step(1, kHalf, T::MT, true, buffer ^ 1, 0, 0, kFirst, asking);
+        if (T::MT > 1) step(1, kHalf, T::MT, true, next, 0, 0, kFirst, asking);
         else
 #pragma unroll
-            for (int r = 0; r < kReads; ++r) read(r, buffer ^ 1, 0, 0);
+            for (int r = 0; r < kReads; ++r) read(r, next, 0, 0);
+        buffer = next;
     }
     // the wait between the last products and the first use of their results, spelled out: where a branch lies between them the
     // compiler has left it short
@@ -340,6 +341,49 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
         a = g * f;
         slope = f + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
     }
+}
+
+// Tile `block` of Out [M, N] = A B + bias, A's contraction inside, B's outside (BO) or inside.
+template <class T, bool BO, int TERMS, typename E>
+__device__ __forceinline__ void product_tile(const Operand &A, const Operand &Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N, int block, bf16_t *lds)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    int mt0, nt0;
+    tile_of(block, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
+    const long m0 = (long)mt0 * T::BM;
+    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), last = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
+    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, last); });
+    f32x16 acc[T::NT][T::MT];
+    clear<T>(acc);
+    multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, 0, (A.K + 63) / 64, lds, acc);
+    const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = n0 + (wave % T::WC) * (32 * T::NT);
+    const bool vec = N % 8 == 0;
+    const Rows<4 * T::NT> out{lds + wave * (32 * T::MT * 32 * T::NT)};
+#pragma unroll
+    for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
+            const int piece = 4 * nt + 2 * run + hi, col = wn + 8 * piece, n = N - col;
+            float b[8];
+            if (bias && n > 0) load8(bias + col, b, n, false);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[e] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < T::MT; ++mt) {
+                const int row = wm + 32 * mt + c;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = acc[nt][mt][8 * run + e] + b[e];
+                if constexpr (TERMS == 1) out.put(32 * mt + c, piece, pack8(v));
+                else if (row < rows) store8(Out + (size_t)(m0 + row) * N + col, v, n, vec);
+            }
+        }
+    if constexpr (TERMS == 1)
+        out.each(32 * T::MT, lane, [&](int row, int piece, bf16x8 v) {
+            if (wm + row < rows) store_piece(Out + (size_t)(m0 + wm + row) * N + wn + 8 * piece, v, N - wn - 8 * piece, vec);
+        });
 }
 
 }  // namespace ffn
