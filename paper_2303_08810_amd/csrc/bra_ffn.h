@@ -25,11 +25,21 @@ struct Operand {
 // Out [M, N] = A B + bias: A's contraction inside, B's outside (`outer`) or inside.  Out in bf16, or float32 where the operands have three terms.
 int product(const Operand &A, const Operand &Bm, bool outer, long M, int N, void *Out, const float *bias, bool f32, int kernel_id, hipStream_t st);
 
-// Side of the tiles (256, 128 or 64) for a product of M x N outputs.
-inline int tile_size(long M, long N)
+// Sides of the tiles (256, 128 or 64), by the number of tiles there would be: large ones multiply faster (one workgroup per compute unit,
+// 1.2 PFLOP/s in long loops, against 0.9 and 0.5), small ones fill the chip.  Measured (us with 256 / 128 / 64):
+//   k_gated    4096 x 512 x 1368 (176 large tiles) 22.8 / 25.0 / 27.7, 12544 x 128 x 256 (98; 392 of 128) 12.9 / 9.8 / 11.9,
+//              1024 x 768 x 2048 (256 of 128) 26.1 / 17.8 / 15.2
+//   k_product  12544 x 768 x 2048 (147) 48.8 / 65.2 / 70.9, 12544 x 512 x 1368 (98; 392) 38.7 / 29.8 / 42.5, 4096 x 768 x 2048 (192 of 128) 45.8 / 30.9 / 27.3
+//   k_hidden   given G | U, bound by its reads and stores: 12544 x 768 (392) 99 / 103 / 119, 12544 x 512 (294) 75.9 / 64.4 / 63.5,
+//              4096 x 256 (128 of 128) 29.1 / 16.2 / 10.4;  otherwise 12544 x 128 (196 of 128) - / 15.2 / 17.1, 4096 x 256 (128) - / 16.8 / 13.4
+inline long tiles(long M, long N, long side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
+inline int gated_side(const Sizes &S) { return tiles(S.M, 2L * S.hp, 256) >= 160 ? 256 : tiles(S.M, 2L * S.hp, 128) >= 300 ? 128 : 64; }
+inline int product_side(long M, long N) { return tiles(M, N, 256) >= 140 ? 256 : tiles(M, N, 128) >= 195 ? 128 : 64; }
+inline int hidden_side(const Sizes &S, bool given)
 {
-    auto tiles = [&](long side) { return ((M + side - 1) / side) * ((N + side - 1) / side); };
-    return tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+    const long t = tiles(S.M, S.hp, 128);
+    if (!given) return t >= 170 ? 128 : 64;
+    return S.C >= 512 && tiles(S.M, S.hp, 256) >= 350 ? 256 : t >= 300 ? 128 : 64;
 }
 
 // A matrix of `blocks` column blocks of `cols` columns laid out anew: each block padded with zeros to `cols_p` columns, float32 as three

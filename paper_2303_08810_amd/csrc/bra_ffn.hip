@@ -133,7 +133,7 @@ int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out
 template <bool BO, int TERMS, typename E>
 int pick_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
-    switch (tile_size(M, N)) {
+    switch (product_side(M, N)) {
     case 256: return launch_product<Tile<256, 256, 4, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     case 128: return launch_product<Tile<128, 128, 2, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
     default: return launch_product<Tile<64, 64, 2, 2, 4>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
@@ -152,7 +152,7 @@ int launch_gated(const Operand &X, const Operand &W1, const float *b1, void *pre
 template <int TERMS, int ACT, typename E>
 int pick_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, hipStream_t st)
 {
-    switch (tile_size(S.M, 2L * S.hp)) {
+    switch (gated_side(S)) {
     case 256: return launch_gated<Tile<256, 256, 4, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     case 128: return launch_gated<Tile<128, 128, 2, 2, 2>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
     default: return launch_gated<Tile<64, 128, 2, 2, 3>, TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);

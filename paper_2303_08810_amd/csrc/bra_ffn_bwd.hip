@@ -349,13 +349,13 @@ int pick_hidden(const Operand &dY, const Operand &W2, const Operand &X, const Op
                 const Sizes &S, hipStream_t st)
 {
     if (pre) {
-        switch (tile_size(S.M, S.hp)) {
+        switch (hidden_side(S, true)) {
         case 256: return launch_hidden<Tile<256, 256, 4, 2, 2>, Tile<256, 256, 4, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         case 128: return launch_hidden<Tile<128, 128, 2, 2, 2>, Tile<128, 128, 2, 2, 2>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         default: return launch_hidden<Tile<64, 64, 2, 2, 4>, Tile<64, 64, 2, 2, 4>, TERMS, ACT, true, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
         }
     }
-    if (tile_size(S.M, S.hp) >= 128)
+    if (hidden_side(S, false) == 128)
         return launch_hidden<Tile<128, 128, 2, 4, 2>, Tile<128, 256, 2, 4, 2>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
     return launch_hidden<Tile<64, 64, 2, 2, 4>, Tile<64, 128, 2, 2, 3>, TERMS, ACT, false, E>(dY, W2, X, W1, b1, pre, Act, pa, dP, pp, S, st);
 }
@@ -390,14 +390,12 @@ struct WeightsPlan {
     WeightsPlan(const Sizes &S)
     {
         chunks = (int)((S.M + 63) / 64);
-        auto tiles_of = [&](int side, int rows, int cols) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); };
-        auto work = [&](int side) {         // of both, in chunks of a tile
-            const long t = tiles_of(side, S.Cp, 2 * S.hp) + tiles_of(side, S.hp, S.Cp), p = ((S.M + side - 1) / side) * (long)((S.C + side - 1) / side);
-            return t * chunks + p * ((2 * S.hp + 63) / 64);
-        };
-        side = work(256) >= 256 * 24 ? 256 : work(128) >= 512 * 4 ? 128 : 64;
-        tiles0 = tiles_of(side, S.Cp, 2 * S.hp);
-        tiles = tiles0 + tiles_of(side, S.hp, S.Cp);
+        // By the operations and, because dX's tiles have the long contraction, their number (us with 256 / 128 / 64): 12544 x 768 x 2048 (147 large
+        // tiles) 212 / 265 / 353, 12544 x 512 x 1368 (98; 392) 141 / 133 / 172, 1024 x 768 x 2048 (48 of 128) 109 / 70 / 45, 32768 x 128 x 256 (13 GFLOP) 69 / 47 / 32
+        const double flops = 12.0 * (double)S.M * S.Cp * S.hp;
+        side = flops >= 2e11 && ffn::tiles(S.M, S.C, 256) >= 140 ? 256 : flops >= 1.5e10 && ffn::tiles(S.M, S.C, 128) >= 190 ? 128 : 64;
+        tiles0 = (int)ffn::tiles(S.Cp, 2 * S.hp, side);
+        tiles = tiles0 + (int)ffn::tiles(S.hp, S.Cp, side);
         const int at_once = side == 256 ? 256 : 512, least = S.f32 ? 1 : 2;     // chunks of a share (of float32 a chunk is six)
         per = 0;
         if (tiles >= at_once) {

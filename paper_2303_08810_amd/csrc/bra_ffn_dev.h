@@ -145,8 +145,66 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
         if (u < LA) la.request(u, an, left_a, to, wave, lane);
         else if (u < kLoads) lb.request(u - LA, bn, left_b, to + 2 * T::kChunkA, wave, lane);
     };
-    bf16x8 xf[2][T::MT], wf[2][T::NT];
     constexpr int kReads = T::NT + T::MT;
+    if constexpr (T::MT * T::NT <= 2) {
+        // Few products per chunk: a whole chunk's operands are in registers before its first product, read while the chunk before is multiplied.
+        // Quarter by quarter, each waiting for LDS, a chunk of a 64 x 64 tile took 0.45 us.
+        bf16x8 x[2][4][T::MT], w[2][4][T::NT];
+        auto read = [&](int buffer, int reg) {
+            const bf16_t *As = lds + buffer * (T::kChunkA + T::kChunkB), *Bs = As + T::kChunkA;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+                for (int nt = 0; nt < T::NT; ++nt) w[reg][ks][nt] = fragment<T::BN, BO, true>(Bs, wn + 32 * nt, ks, lane);
+#pragma unroll
+                for (int mt = 0; mt < T::MT; ++mt) x[reg][ks][mt] = fragment<T::BM, AO, false>(As, wm + 32 * mt, ks, lane);
+            }
+        };
+        __builtin_amdgcn_s_barrier();              // the buffers are free
+        for (int i = 0; i < min(T::NB, total); ++i) {
+            aim(i, i);
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) ask(u);
+        }
+        if (total >= T::NB) asm volatile("s_waitcnt vmcnt(%0)" : : "n"((T::NB - 1) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(0, 0);
+        int buffer = 0;
+        auto turn = [&](int i, int reg) {
+            const int next = buffer + 1 == T::NB ? 0 : buffer + 1;
+            // the next chunk is there, and this one is in registers everywhere
+            if (i + T::NB <= total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((T::NB - 2) * kLoads) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            read(next, reg ^ 1);                   // (behind the last chunk: what is there, which nobody uses)
+            if (i + T::NB < total) {
+                aim(i + T::NB, buffer);
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) ask(u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+                    for (int nt = 0; nt < T::NT; ++nt) acc[nt][mt] = mfma32(w[reg][ks][nt], x[reg][ks][mt], acc[nt][mt]);
+            __builtin_amdgcn_sched_barrier(0);
+            buffer = next;
+        };
+        for (int i = 0; i < total; i += 2) {
+            turn(i, 0);
+            if (i + 1 < total) turn(i + 1, 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        return;
+    }
+    bf16x8 xf[2][T::MT], wf[2][T::NT];
     // operand r of a step: buffer, quarter, and the registers it goes to
     auto read = [&](int r, int buffer, int ks, int reg) {
         const bf16_t *As = lds + buffer * (T::kChunkA + T::kChunkB), *Bs = As + T::kChunkA;
