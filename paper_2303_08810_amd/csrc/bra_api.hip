@@ -384,6 +384,8 @@ int bra_norm_backward_workspace_bytes(const bra_norm_shape *shape, int32_t post,
     const int rc = make_norm_sizes(shape, post != 0, S);
     if (rc != BRA_OK) return rc;
     *out_bytes = norm_backward_workspace_bytes(S);
+    S.vec = false;          // pointers that are not aligned share the rows out differently
+    *out_bytes = std::max(*out_bytes, norm_backward_workspace_bytes(S));
     return BRA_OK;
 }
 

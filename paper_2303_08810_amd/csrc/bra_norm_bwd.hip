@@ -17,7 +17,9 @@ using namespace norm;
 namespace {
 
 constexpr int kSums = 5;            // dgamma, dbeta, and where groups are finished in this kernel dscale, dpost_gamma, dpost_beta
-constexpr int kTarget = 768;        // workgroups
+// Wavefronts per SIMD, with `values` channels per thread: three where the registers allow it, or nearly (33 spilled at most;
+// 32768 x 768 115 -> 97 us), two where they do not (6475 x 192 in float32 19 us, with three and their spills 24).
+constexpr int waves(int values, bool f32, bool finish) { return values == 16 || (values == 12 && (f32 || finish)) ? 2 : 3; }
 
 // Lines of LDS in which teams meet.
 __host__ __device__ constexpr int meeting_lines(int teams) { return teams > 1 ? teams : 0; }
@@ -31,27 +33,25 @@ struct BackArgs {
     unsigned per_group;
     int C, tpr, parts;
     float eps;
+    bool vec;                       // rows are whole 16-byte pieces
     int whole;                      // FINISH: a workgroup has a whole group at a time, otherwise each of its teams has one
 };
 
 // How rows are shared out.
 struct Split {
-    int tpr, nch, threads, teams, parts;
+    Team T;
+    int parts;
     bool finish, whole;
     long units;
     unsigned blocks;
-    Split(const NormSizes &S)
+    Split(const NormSizes &S) : T(S.C, S.vec)
     {
-        const int one = team_size(S.C, 1);
-        nch = one <= 64 ? 1 : 2;
-        tpr = one / nch;
-        threads = std::max(kThreads, tpr);
-        teams = threads / tpr;
+        const int teams = T.teams(), kTarget = 256 * waves(T.V * T.nch, S.f32, false);        // workgroups that run at once
         // A group of fewer rows than half of a workgroup's teams: each team takes whole groups.  Otherwise a workgroup takes a group, or, where
         // groups are few, a part of one
         const bool by_team = S.per_group <= teams / 2;
         parts = 1;
-        if (!by_team) parts = (int)std::max(1L, std::min<long>((kTarget + S.groups - 1) / S.groups, (S.per_group + 4 * teams - 1) / (4 * teams)));
+        if (!by_team) parts = (int)std::max(1L, std::min<long>((kTarget + S.groups - 1) / S.groups, (S.per_group + 2 * teams - 1) / (2 * teams)));
         finish = parts == 1;
         whole = !by_team;
         units = (long)S.groups * parts;
@@ -60,18 +60,19 @@ struct Split {
     int sums() const { return finish ? kSums : 2; }
 };
 
-template <typename E, bool LAYER, bool POST, int NCH, bool VEC, bool FINISH>
-__global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
+template <typename E, bool LAYER, bool POST, int V, int NCH, bool FULL, bool FINISH>
+__global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) void k_norm_backward(BackArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) float smem[];
-    const int C = A.C, tpr = A.tpr, team = threadIdx.x / tpr, teams = blockDim.x / tpr, t = threadIdx.x % tpr, width = 8 * NCH * tpr;
+    const int C = A.C, tpr = A.tpr, team = threadIdx.x / tpr, teams = blockDim.x / tpr, t = threadIdx.x % tpr, width = V * NCH * tpr;
+    const bool vec = A.vec;
     float *meet = smem;                                     // [teams][width]
-    float *vectors = meet + meeting_lines(teams) * width;                  // gamma, scale, post_gamma, post_beta: [4][width]
+    float *vectors = meet + meeting_lines(teams) * width;   // gamma, scale, post_gamma, post_beta: [4][width]
     float *lds = vectors + 4 * width;                       // of team_sums
     const float c_inv = 1.0f / (float)C;
     int n[NCH];
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) n[k] = VEC ? (8 * (t + k * tpr) < C ? 8 : 0) : C - 8 * (t + k * tpr);
+    for (int k = 0; k < NCH; ++k) n[k] = C - V * (t + k * tpr);
     for (int c = threadIdx.x; c < width; c += blockDim.x) {
         const bool in = c < C;
         vectors[c] = in && A.I.gamma ? A.I.gamma[c] : 0.f;
@@ -80,147 +81,157 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
         vectors[3 * width + c] = in && POST && A.I.post_beta ? A.I.post_beta[c] : 0.f;
     }
     __syncthreads();
-    auto vector = [&](int which, int k, float (&v)[8]) {
-        const f32x4 *p = (const f32x4 *)(vectors + which * width + 8 * (t + k * tpr));
-        const f32x4 a = p[0], b = p[1];
+    int own = V * t;
+    auto vector = [&](int which, int k, float (&v)[V]) {
+        const f32x4 *p = (const f32x4 *)(vectors + which * width + own + V * k * tpr);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+        for (int q = 0; q < V / 4; ++q) {
+            const f32x4 a = p[q];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = a[e];
+        }
     };
+    auto gate_of = [&](long group, int k) { return load<FULL, E, V>((const E *)A.I.gate + (size_t)group * C + V * (t + k * tpr), n[k], vec); };
 
-    float sums[FINISH ? kSums : 2][NCH][8], Q[NCH][8], S[POST ? NCH : 1][8];
+    float sums[FINISH ? kSums : 2][NCH][V], Q[NCH][V], S[POST ? NCH : 1][V];
 #pragma unroll
     for (int s = 0; s < (FINISH ? kSums : 2); ++s)
 #pragma unroll
         for (int k = 0; k < NCH; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[s][k][e] = 0.f;
+            for (int e = 0; e < V; ++e) sums[s][k][e] = 0.f;
     auto clear = [&]() {
 #pragma unroll
         for (int k = 0; k < NCH; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { Q[k][e] = 0.f; if (POST) S[k][e] = 0.f; }
+            for (int e = 0; e < V; ++e) { Q[k][e] = 0.f; if (POST) S[k][e] = 0.f; }
     };
 
-    // one row per team; teams without one (`mine` unset) go along with the last row and add nothing
-    auto row = [&](long r, long group, bool mine) {
-        const size_t at = (size_t)r * C + 8 * t;
-        float x[NCH][8], y[NCH][8];
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+    // one row per team; the next one is on its way while one is worked on
+    Raw<E, V> rx[NCH], ry[NCH], rn[NCH], rd[NCH];
+    auto fetch = [&](long r) {
+        const size_t at = (size_t)r * C + V * t;
 #pragma unroll
         for (int k = 0; k < NCH; ++k) {
-            load8<VEC>((const E *)A.I.X + at + 8 * k * tpr, n[k], x[k]);
-            if (A.I.Y) load8<VEC>((const E *)A.I.Y + at + 8 * k * tpr, n[k], y[k]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[k][e] = 0.f;
+            rx[k] = load<FULL, E, V>((const E *)A.I.X + at + V * k * tpr, n[k], vec);
+            if (A.I.Y) ry[k] = load<FULL, E, V>((const E *)A.I.Y + at + V * k * tpr, n[k], vec);
+            if (A.dN) rn[k] = load<FULL, E, V>((const E *)A.dN + at + V * k * tpr, n[k], vec);
+            if (A.dR) rd[k] = load<FULL, E, V>((const E *)A.dR + at + V * k * tpr, n[k], vec);
         }
-        float dn[NCH][8], d[NCH][8];
+    };
+    // row r, which has been fetched; then row `next` (-1: none).  Teams without a row (`mine` unset) go along with another's and add nothing
+    auto row = [&](long r, long next, long group, bool mine) {
+        // the vectors stay in LDS: kept in registers over the rows, they cost a wavefront per SIMD
+        asm volatile("" : "+v"(own));
+        const size_t at = (size_t)r * C + V * t;
+        float x[NCH][V], y[NCH][V], dn[NCH][V], d[NCH][V];
+        Raw<E, V> gate[NCH];
 #pragma unroll
         for (int k = 0; k < NCH; ++k) {
-            if (A.dN) load8<VEC>((const E *)A.dN + at + 8 * k * tpr, n[k], dn[k]);
-            else
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dn[k][e] = 0.f;
-            if (A.dR) load8<VEC>((const E *)A.dR + at + 8 * k * tpr, n[k], d[k]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[k][e] = 0.f;
+            for (int e = 0; e < V; ++e) {
+                x[k][e] = value(rx[k], e);
+                y[k][e] = A.I.Y ? value(ry[k], e) : 0.f;
+                dn[k][e] = A.dN ? value(rn[k], e) : 0.f;
+                d[k][e] = A.dR ? value(rd[k], e) : 0.f;
+            }
+            if (A.I.gate) gate[k] = gate_of(group, k);
         }
+        if (next >= 0) fetch(next);
         if (LAYER) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { m[0] += x[k][e]; if (POST) m[1] += y[k][e]; }
+                for (int e = 0; e < V; ++e) { m[0] += x[k][e]; if (POST) m[1] += y[k][e]; }
             team_sums(m, tpr, lds);
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[k][e] = e < n[k] ? x[k][e] - m[0] * c_inv : 0.f;
-                    if (POST) y[k][e] = e < n[k] ? y[k][e] - m[1] * c_inv : 0.f;
+                for (int e = 0; e < V; ++e) {
+                    x[k][e] = FULL || e < n[k] ? x[k][e] - m[0] * c_inv : 0.f;
+                    if (POST) y[k][e] = FULL || e < n[k] ? y[k][e] - m[1] * c_inv : 0.f;
                 }
         }
         float v[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NCH; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { v[0] = fmaf(x[k][e], x[k][e], v[0]); if (POST) v[1] = fmaf(y[k][e], y[k][e], v[1]); }
+            for (int e = 0; e < V; ++e) { v[0] = fmaf(x[k][e], x[k][e], v[0]); if (POST) v[1] = fmaf(y[k][e], y[k][e], v[1]); }
         team_sums(v, tpr, lds);
         const float inv = 1.0f / sqrtf(fmaf(v[0], c_inv, A.eps)), yinv = POST ? 1.0f / sqrtf(fmaf(v[1], c_inv, A.eps)) : 1.f;
         if (A.dN) {
+            float p[2] = {0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < NCH; ++k) {
-                float gamma[8];
+                float gamma[V];
                 vector(0, k, gamma);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < V; ++e) {
                     x[k][e] *= inv;
-                    if (mine) {
-                        sums[0][k][e] = fmaf(dn[k][e], x[k][e], sums[0][k][e]);
-                        sums[1][k][e] += dn[k][e];
-                    }
+                    const float w = mine ? dn[k][e] : 0.f;
+                    sums[0][k][e] = fmaf(w, x[k][e], sums[0][k][e]);
+                    sums[1][k][e] += w;
                     dn[k][e] *= gamma[e];
-                    s[0] += dn[k][e];
-                    s[1] = fmaf(dn[k][e], x[k][e], s[1]);
+                    p[0] += dn[k][e];
+                    p[1] = fmaf(dn[k][e], x[k][e], p[1]);
                 }
             }
-            float p[2] = {s[0], s[1]};
             team_sums(p, tpr, lds);
+            const float m1 = LAYER ? p[0] * c_inv : 0.f, m2 = p[1] * c_inv;
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float g = fmaf(-x[k][e], p[1] * c_inv, LAYER ? dn[k][e] - p[0] * c_inv : dn[k][e]);
-                    d[k][e] = e < n[k] ? fmaf(g, inv, d[k][e]) : 0.f;
+                for (int e = 0; e < V; ++e) {
+                    const float g = fmaf(-x[k][e], m2, dn[k][e] - m1);
+                    d[k][e] = FULL || e < n[k] ? fmaf(g, inv, d[k][e]) : 0.f;
                 }
         }
         if (mine)
 #pragma unroll
-            for (int k = 0; k < NCH; ++k) store8<VEC>((E *)A.dX + at + 8 * k * tpr, n[k], d[k]);
+            for (int k = 0; k < NCH; ++k) store<FULL>((E *)A.dX + at + V * k * tpr, d[k], n[k], vec);
         if (!A.I.Y) return;
+        float p[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NCH; ++k) {
-            float scale[8], gate[8], pg[8];
+            float scale[V], pg[V];
             vector(1, k, scale);
-            if (A.I.gate) load8<VEC>((const E *)A.I.gate + (size_t)group * C + 8 * (t + k * tpr), n[k], gate);
             if (POST) vector(2, k, pg);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < V; ++e) {
                 if (POST) y[k][e] *= yinv;
-                if (mine) {
-                    Q[k][e] = fmaf(d[k][e], y[k][e], Q[k][e]);
-                    if (POST) S[k][e] += d[k][e];
-                }
-                d[k][e] *= A.I.gate ? scale[e] * gate[e] : scale[e];
+                const float w = mine ? d[k][e] : 0.f;
+                Q[k][e] = fmaf(w, y[k][e], Q[k][e]);
+                if (POST) S[k][e] += w;
+                d[k][e] *= A.I.gate ? scale[e] * value(gate[k], e) : scale[e];
                 if (POST) {
                     d[k][e] *= pg[e];
-                    s[2] += d[k][e];
-                    s[3] = fmaf(d[k][e], y[k][e], s[3]);
+                    p[0] += d[k][e];
+                    p[1] = fmaf(d[k][e], y[k][e], p[1]);
                 }
             }
         }
         if constexpr (POST) {
-            float p[2] = {s[2], s[3]};
             team_sums(p, tpr, lds);
+            const float m1 = LAYER ? p[0] * c_inv : 0.f, m2 = p[1] * c_inv;
 #pragma unroll
             for (int k = 0; k < NCH; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[k][e] = yinv * fmaf(-y[k][e], p[1] * c_inv, LAYER ? d[k][e] - p[0] * c_inv : d[k][e]);
+                for (int e = 0; e < V; ++e) d[k][e] = yinv * fmaf(-y[k][e], m2, d[k][e] - m1);
         }
         if (mine)
 #pragma unroll
-            for (int k = 0; k < NCH; ++k) store8<VEC>((E *)A.dY + at + 8 * k * tpr, n[k], d[k]);
+            for (int k = 0; k < NCH; ++k) store<FULL>((E *)A.dY + at + V * k * tpr, d[k], n[k], vec);
     };
 
     // the sum over the teams of what each of their threads holds, for every thread; the whole workgroup calls it
-    auto over_teams = [&](float (&v)[NCH][8]) {
+    auto over_teams = [&](float (&v)[NCH][V]) {
         if (teams == 1) return;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < NCH; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; e += 4) *(f32x4 *)(meet + team * width + 8 * (t + k * tpr) + e) = f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
+            for (int e = 0; e < V; e += 4) *(f32x4 *)(meet + team * width + V * (t + k * tpr) + e) = f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
         __syncthreads();
         for (int c = threadIdx.x; c < width; c += blockDim.x) {
             float s = 0.f;
@@ -231,8 +242,8 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
 #pragma unroll
         for (int k = 0; k < NCH; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const f32x4 s = *(const f32x4 *)(meet + 8 * (t + k * tpr) + e);
+            for (int e = 0; e < V; e += 4) {
+                const f32x4 s = *(const f32x4 *)(meet + V * (t + k * tpr) + e);
                 v[k][e] = s[0]; v[k][e + 1] = s[1]; v[k][e + 2] = s[2]; v[k][e + 3] = s[3];
             }
     };
@@ -240,25 +251,26 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
     auto finish = [&](long group) {
 #pragma unroll
         for (int k = 0; k < NCH; ++k) {
-            float scale[8], gate[8], pg[8], pb[8], T[8];
+            float scale[V], pg[V], pb[V], T[V];
             vector(1, k, scale);
             vector(2, k, pg);
             vector(3, k, pb);
-            if (A.I.gate) load8<VEC>((const E *)A.I.gate + (size_t)group * C + 8 * (t + k * tpr), n[k], gate);
+            Raw<E, V> gate;
+            if (A.I.gate) gate = gate_of(group, k);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!A.I.gate) gate[e] = 1.f;
+            for (int e = 0; e < V; ++e) {
+                const float g = A.I.gate ? value(gate, e) : 1.f;
                 T[e] = POST ? fmaf(pg[e], Q[k][e], pb[e] * S[POST ? k : 0][e]) : Q[k][e];
                 if constexpr (FINISH) {
-                    sums[2][k][e] = fmaf(gate[e], T[e], sums[2][k][e]);
+                    sums[2][k][e] = fmaf(g, T[e], sums[2][k][e]);
                     if (POST) {
-                        sums[3][k][e] = fmaf(scale[e] * gate[e], Q[k][e], sums[3][k][e]);
-                        sums[4][k][e] = fmaf(scale[e] * gate[e], S[k][e], sums[4][k][e]);
+                        sums[3][k][e] = fmaf(scale[e] * g, Q[k][e], sums[3][k][e]);
+                        sums[4][k][e] = fmaf(scale[e] * g, S[POST ? k : 0][e], sums[4][k][e]);
                     }
                 }
                 T[e] *= scale[e];
             }
-            if (A.dgate) store8<VEC>((E *)A.dgate + (size_t)group * C + 8 * (t + k * tpr), n[k], T);
+            if (A.dgate) store<FULL>((E *)A.dgate + (size_t)group * C + V * (t + k * tpr), T, n[k], vec);
         }
     };
 
@@ -267,17 +279,16 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
             const bool mine = g0 + team < A.groups;
             const long g = mine ? g0 + team : A.groups - 1;
             clear();
-            for (unsigned i = 0; i < A.per_group; ++i) row(g * A.per_group + i, g, mine);
+            fetch(g * A.per_group);
+            for (unsigned i = 0; i < A.per_group; ++i) row(g * A.per_group + i, i + 1 < A.per_group ? g * A.per_group + i + 1 : -1, g, mine);
             if (mine && A.I.Y) finish(g);
         }
     } else {
         for (long u = blockIdx.x; u < A.groups * A.parts; u += gridDim.x) {
-            const long g = u / A.parts, part = u % A.parts, begin = A.per_group * part / A.parts, end = A.per_group * (part + 1) / A.parts;
+            const long g = u / A.parts, part = u % A.parts, begin = A.per_group * part / A.parts, end = A.per_group * (part + 1) / A.parts, base = g * A.per_group;
             clear();
-            for (long i = begin; i < end; i += teams) {
-                const bool mine = i + team < end;
-                row(g * A.per_group + (mine ? i + team : end - 1), g, mine);
-            }
+            fetch(base + min(begin + team, end - 1));
+            for (long i = begin; i < end; i += teams) row(base + min(i + team, end - 1), i + teams < end ? base + min(i + teams + team, end - 1) : -1, g, i + team < end);
             if (!A.I.Y) continue;
             over_teams(Q);
             if constexpr (POST) over_teams(S);
@@ -286,9 +297,9 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
             else
 #pragma unroll
                 for (int k = 0; k < NCH; ++k) {
-                    float *to = A.units + (size_t)u * 2 * C + 8 * (t + k * tpr);
-                    store8<VEC>(to, n[k], Q[k]);
-                    if constexpr (POST) store8<VEC>(to + C, n[k], S[k]);
+                    float *to = A.units + (size_t)u * 2 * C + V * (t + k * tpr);
+                    store<FULL>(to, Q[k], n[k], vec);
+                    if constexpr (POST) store<FULL>(to + C, S[k], n[k], vec);
                 }
         }
     }
@@ -298,7 +309,7 @@ __global__ __launch_bounds__(kMaxTeam, 2) void k_norm_backward(BackArgs A)
         over_teams(sums[s]);
         if (team == 0)
 #pragma unroll
-            for (int k = 0; k < NCH; ++k) store8<VEC>(A.part + ((size_t)blockIdx.x * (FINISH ? kSums : 2) + s) * C + 8 * (t + k * tpr), n[k], sums[s][k]);
+            for (int k = 0; k < NCH; ++k) store<FULL>(A.part + ((size_t)blockIdx.x * (FINISH ? kSums : 2) + s) * C + V * (t + k * tpr), sums[s][k], n[k], vec);
     }
 }
 
@@ -313,18 +324,21 @@ struct SumArgs {
     bool post;
 };
 
-// Columns in workgroups of 16, 64 threads to a column; behind them, where groups came in parts, their gates' gradients.
+// Columns in workgroups of 16, 64 threads to a column: dgamma, dbeta, and what the groups give (one workgroup each: blockIdx.y); behind
+// them, where groups came in parts, their gates' gradients.
 template <typename E>
 __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
 {
     __shared__ float meet[64][17];
+    const int y = blockIdx.y;
     if ((int)blockIdx.x >= A.column_blocks) {
-        const long i = (long)(blockIdx.x - A.column_blocks) * 1024 + threadIdx.x;
+        const long i = ((long)(blockIdx.x - A.column_blocks) * gridDim.y + y) * 1024 + threadIdx.x;
         if (i >= A.groups * A.C) return;
         const long g = i / A.C;
         const int c = (int)(i % A.C);
         float q = 0.f, s = 0.f;
-        for (int p = 0; p < A.parts && A.blocks; ++p) {
+#pragma unroll 4
+        for (int p = 0; p < (A.blocks ? A.parts : 0); ++p) {
             const float *u = A.units + (size_t)(g * A.parts + p) * 2 * A.C + c;
             q += u[0];
             if (A.post) s += u[A.C];
@@ -344,28 +358,29 @@ __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
         }
         return meet[0][x];
     };
-#pragma unroll
-    for (int s = 0; s < kSums; ++s) {
-        if (s >= A.sums || !A.out[s]) continue;
+    for (int s = y; s < A.sums; s += 3) {
+        if (!A.out[s]) continue;
         float v = 0.f;
         if (in)
+#pragma unroll 4
             for (int b = slot; b < A.blocks; b += 64) v += A.part[((size_t)b * A.sums + s) * A.C + c];
         v = total(v);
         if (in && slot == 0) A.out[s][c] = v;
     }
-    if (A.parts == 1 || !A.out[2]) return;
+    if (y != 2 || A.parts == 1 || !(A.out[2] || A.out[3])) return;
     float q = 0.f, s = 0.f;
     if (in)
-        for (long u = slot; u < A.groups * A.parts; u += 64) {
-            const float gate = A.gate ? load_f32((const E *)A.gate + (u / A.parts) * A.C + c) : 1.f;
-            q = fmaf(gate, A.units[u * 2 * A.C + c], q);
-            if (A.post) s = fmaf(gate, A.units[(u * 2 + 1) * A.C + c], s);
+#pragma unroll 4
+        for (int u = slot; u < (int)A.groups * A.parts; u += 64) {
+            const float gate = A.gate ? load_f32((const E *)A.gate + (size_t)((unsigned)u / (unsigned)A.parts) * A.C + c) : 1.f;
+            q = fmaf(gate, A.units[(size_t)u * 2 * A.C + c], q);
+            if (A.post) s = fmaf(gate, A.units[((size_t)u * 2 + 1) * A.C + c], s);
         }
     q = total(q);
     if (A.post) s = total(s);
     if (!in || slot != 0) return;
     const float scale = A.scale ? A.scale[c] : 1.f;
-    A.out[2][c] = A.post ? fmaf(A.post_gamma[c], q, (A.post_beta ? A.post_beta[c] : 0.f) * s) : q;
+    if (A.out[2]) A.out[2][c] = A.post ? fmaf(A.post_gamma[c], q, (A.post_beta ? A.post_beta[c] : 0.f) * s) : q;
     if (A.out[3]) A.out[3][c] = scale * q;
     if (A.out[4]) A.out[4][c] = scale * s;
 }
@@ -373,23 +388,24 @@ __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
 size_t part_floats(const NormSizes &S, const Split &P) { return align256((size_t)P.blocks * P.sums() * S.C * 4) / 4; }
 size_t unit_floats(const NormSizes &S, const Split &P) { return P.finish ? 0 : (size_t)P.units * 2 * S.C; }
 
-template <typename E, bool LAYER, bool POST, int NCH, bool VEC>
+template <typename E, bool LAYER, bool POST, int V, int NCH, bool FULL>
 int launch(const BackArgs &A, const Split &P, hipStream_t st)
 {
-    const int width = 8 * P.nch * P.tpr;
-    const size_t bytes = ((size_t)(meeting_lines(P.teams) + 4) * width + 2 * (P.threads / 64)) * 4;
-    if ((P.finish ? allow_lds<k_norm_backward<E, LAYER, POST, NCH, VEC, true>>(kMaxLds) : allow_lds<k_norm_backward<E, LAYER, POST, NCH, VEC, false>>(kMaxLds)) != BRA_OK)
+    const int width = V * NCH * P.T.tpr, threads = P.T.threads();
+    const size_t bytes = ((size_t)(meeting_lines(P.T.teams()) + 4) * width + 2 * (threads / 64)) * 4;
+    if ((P.finish ? allow_lds<k_norm_backward<E, LAYER, POST, V, NCH, FULL, true>>(kMaxLds) : allow_lds<k_norm_backward<E, LAYER, POST, V, NCH, FULL, false>>(kMaxLds)) != BRA_OK)
         return BRA_ERR_LAUNCH;
-    if (P.finish) k_norm_backward<E, LAYER, POST, NCH, VEC, true><<<P.blocks, P.threads, bytes, st>>>(A);
-    else k_norm_backward<E, LAYER, POST, NCH, VEC, false><<<P.blocks, P.threads, bytes, st>>>(A);
+    if (P.finish) k_norm_backward<E, LAYER, POST, V, NCH, FULL, true><<<P.blocks, threads, bytes, st>>>(A);
+    else k_norm_backward<E, LAYER, POST, V, NCH, FULL, false><<<P.blocks, threads, bytes, st>>>(A);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
 template <typename E, bool LAYER, bool POST>
-int pick(const NormSizes &S, const BackArgs &A, const Split &P, hipStream_t st)
+int pick(const BackArgs &A, const Split &P, hipStream_t st)
 {
-    if (P.nch == 1) return S.vec ? launch<E, LAYER, POST, 1, true>(A, P, st) : launch<E, LAYER, POST, 1, false>(A, P, st);
-    return S.vec ? launch<E, LAYER, POST, 2, true>(A, P, st) : launch<E, LAYER, POST, 2, false>(A, P, st);
+    if (P.T.nch == 3) return launch<E, LAYER, POST, 4, 3, true>(A, P, st);
+    if (P.T.nch == 1) return P.T.full ? launch<E, LAYER, POST, 8, 1, true>(A, P, st) : launch<E, LAYER, POST, 8, 1, false>(A, P, st);
+    return P.T.full ? launch<E, LAYER, POST, 8, 2, true>(A, P, st) : launch<E, LAYER, POST, 8, 2, false>(A, P, st);
 }
 
 }  // namespace
@@ -416,34 +432,34 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
         const Split P(S);
         F.part = (const float *)ws; F.units = (const float *)ws + part_floats(S, P);
         F.blocks = (int)P.blocks; F.sums = P.sums(); F.parts = P.parts; F.groups = S.groups;
-        const BackArgs A{I, dN, dR, G.dX, G.dY, P.finish ? G.dgate : nullptr, (float *)ws, (float *)ws + part_floats(S, P), S.rows, S.groups, (unsigned)S.per_group, S.C, P.tpr,
-                         P.parts, S.eps, P.whole};
+        const BackArgs A{I, dN, dR, G.dX, G.dY, P.finish ? G.dgate : nullptr, (float *)ws, (float *)ws + part_floats(S, P), S.rows, S.groups, (unsigned)S.per_group, S.C, P.T.tpr,
+                         P.parts, S.eps, S.vec, P.whole};
         {
             ProfScope prof(st, K_NORM_BACKWARD);
             int rc;
             if (S.f32) {
-                if (S.layer) rc = S.post ? pick<float, true, true>(S, A, P, st) : pick<float, true, false>(S, A, P, st);
-                else rc = S.post ? pick<float, false, true>(S, A, P, st) : pick<float, false, false>(S, A, P, st);
+                if (S.layer) rc = S.post ? pick<float, true, true>(A, P, st) : pick<float, true, false>(A, P, st);
+                else rc = S.post ? pick<float, false, true>(A, P, st) : pick<float, false, false>(A, P, st);
             } else {
-                if (S.layer) rc = S.post ? pick<bf16_t, true, true>(S, A, P, st) : pick<bf16_t, true, false>(S, A, P, st);
-                else rc = S.post ? pick<bf16_t, false, true>(S, A, P, st) : pick<bf16_t, false, false>(S, A, P, st);
+                if (S.layer) rc = S.post ? pick<bf16_t, true, true>(A, P, st) : pick<bf16_t, true, false>(A, P, st);
+                else rc = S.post ? pick<bf16_t, false, true>(A, P, st) : pick<bf16_t, false, false>(A, P, st);
             }
             if (rc != BRA_OK) return rc;
         }
         if (!P.finish && I.Y && G.dgate) {
             F.dgate = G.dgate;
-            gate_blocks = (unsigned)(((long)S.groups * S.C + 1023) / 1024);
+            gate_blocks = (unsigned)(((long)S.groups * S.C + 3071) / 3072);
         }
     } else if (G.dgate) {
         F.dgate = G.dgate; F.groups = S.groups;
-        gate_blocks = (unsigned)(((long)S.groups * S.C + 1023) / 1024);
+        gate_blocks = (unsigned)(((long)S.groups * S.C + 3071) / 3072);
     }
     bool any = gate_blocks > 0;
     for (int s = 0; s < kSums; ++s) any = any || outs[s];
     if (!any) return BRA_OK;
     ProfScope prof(st, K_NORM_SUMS);
-    if (S.f32) k_norm_sums<float><<<F.column_blocks + gate_blocks, 1024, 0, st>>>(F);
-    else k_norm_sums<bf16_t><<<F.column_blocks + gate_blocks, 1024, 0, st>>>(F);
+    if (S.f32) k_norm_sums<float><<<dim3(F.column_blocks + gate_blocks, 3), 1024, 0, st>>>(F);
+    else k_norm_sums<bf16_t><<<dim3(F.column_blocks + gate_blocks, 3), 1024, 0, st>>>(F);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
