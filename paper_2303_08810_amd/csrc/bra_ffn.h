@@ -42,6 +42,10 @@ inline int hidden_side(const Sizes &S, bool given)
     return S.C >= 512 && tiles(S.M, S.hp, 256) >= 350 ? 256 : t >= 300 ? 128 : 64;
 }
 
+// Whether the forward goes to k_few: up to 128 rows it is the faster one at every width (us, k_few / tiles: 1 x 768 x 2048 8.8 / 21.2,
+// 128 x 768 x 2048 15.2 / 21.9, 128 x 1024 x 4096 29 / 34).
+inline bool few_rows(const Sizes &S) { return !S.f32 && S.M <= 128; }
+
 // A matrix of `blocks` column blocks of `cols` columns laid out anew: each block padded with zeros to `cols_p` columns, float32 as three
 // planes of terms.
 struct Layout {

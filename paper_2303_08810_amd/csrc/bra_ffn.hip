@@ -121,6 +121,121 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_product(Operand A
     product_tile<T, BO, TERMS, E>(A, Bm, bias, Out, M, N, blockIdx.x, (bf16_t *)smem);
 }
 
+// Few rows: 32 x 32 outputs per workgroup, the contraction's chunks shared out to its kFewWaves wavefronts, each with a ring of its own and no
+// barrier before the sums meet in LDS.  Few columns per workgroup spread the weights over the chip; the direct loads of all wavefronts
+// are on their way at once.  Of X only ROWS rows are read (the rest of the tile is whatever LDS holds: a row's results depend on no
+// other).  ACT < 0: Out = X W + b; otherwise the 32 columns are those of G and U of 16 hidden units, 16 registers apart in a lane, and Out = act(G) U.
+constexpr int kFewWaves = 8, kFewRing = 2;
+typedef Tile<32, 32, 1, 1, kFewRing> TFew;
+template <int ACT, int ROWS>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(Operand X, Operand W, const float *__restrict__ bias, bf16_t *__restrict__ pre, bf16_t *__restrict__ Out, int M, int N, int Np)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr bool GATED = ACT >= 0;
+    constexpr int LA = ROWS / 8, LB = Loads<TFew, 32, true, true>::L, kLoads = LA + LB, kChunk = TFew::kChunkA + TFew::kChunkB;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    // an XCD has neighbouring columns: they lie in the same lines
+    const int xcd = blockIdx.x % 8, per = gridDim.x / 8, rest = gridDim.x % 8, tile = xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int c0 = tile * (GATED ? 16 : 32), m0 = blockIdx.y * 32, rows = min(M - m0, 32), last = Np - 8 - c0;
+    const Loads<TFew, 32, false, false> la(0, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<TFew, 32, true, true> lb(0, lane, W.ld, [&](int col) { return (long)(GATED ? min(col % 16, last) + (col >= 16 ? Np : 0) : min(col, last)); });
+    bf16_t *const ring = (bf16_t *)smem + wave * (kFewRing * kChunk);
+    const unsigned at = lds_address(ring);
+    const bf16_t *const a0 = X.p + m0 * X.ld, *const b0 = W.p + c0;
+    const int chunks = (X.K + 63) / 64, mine = (chunks - wave + kFewWaves - 1) / kFewWaves;
+    auto ask = [&](int i) {
+        const int k0 = 64 * (wave + i * kFewWaves);
+        const unsigned to = at + (i % kFewRing) * (kChunk * 2);
+#pragma unroll
+        for (int u = 0; u < LA; ++u) la.request(u, a0 + k0, X.K - k0, to, 0, lane);
+#pragma unroll
+        for (int u = 0; u < LB; ++u) lb.request(u, b0 + k0 * W.ld, W.K - k0, to + 2 * TFew::kChunkA, 0, lane);
+    };
+    f32x16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    for (int i = 0; i < min(mine, kFewRing); ++i) ask(i);
+    for (int i = 0; i < mine; ++i) {
+        if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kFewRing - 1) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const bf16_t *As = ring + (i % kFewRing) * kChunk, *Bs = As + TFew::kChunkA;
+        bf16x8 x[4], w[4];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            w[ks] = fragment<32, true, true>(Bs, 0, ks, lane);
+            x[ks] = fragment<32, false, false>(As, 0, ks, lane);
+        }
+        lds_reads_done();
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + kFewRing < mine) ask(i + kFewRing);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) acc = mfma32(w[ks], x[ks], acc);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
+    // the wavefronts' sums, [wave][quarter of the registers][lane][4]; then a wavefront has a quarter (GATED: one of G's and the same of U's)
+    __syncthreads();
+    f32x4 *const sums = (f32x4 *)smem;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sums[(wave * 4 + q) * 64 + lane] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    if (wave >= (GATED ? 2 : 4)) return;
+    auto total = [&](int q) {
+        f32x4 s = sums[q * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) s += sums[(w * 4 + q) * 64 + lane];
+        return s;
+    };
+    const int row = lane % 32, col = c0 + 16 * (wave / 2) + 8 * (lane / 32) + 4 * (wave % 2);
+    // (N columns exist; an operand of a later product has its columns up to Np written, with zeros)
+    f32x4 g = total(wave);
+    if (row >= rows || col >= (GATED ? Np : N)) return;
+    const size_t m = (size_t)(m0 + row);
+    const int n = N - col;
+    auto put = [&](bf16_t *p, f32x4 v) {
+        if (N % 8 == 0) {
+            *(u32x2 *)p = pack4(v);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) p[e] = f32_to_bf16(v[e]);
+    };
+    if (bias)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] += e < n ? bias[col + e] : 0.f;
+    if constexpr (GATED) {
+        f32x4 u = total(wave + 2);
+        if (bias)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] += e < n ? bias[N + col + e] : 0.f;
+        if (pre) {
+            put(pre + m * 2 * N + col, g);
+            put(pre + m * 2 * N + N + col, u);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] = e < n ? activation<GATED ? ACT : 0>(g[e]) * u[e] : 0.f;
+        *(u32x2 *)(Out + m * Np + col) = pack4(g);
+    } else put(Out + m * N + col, g);
+}
+
+template <int ACT>
+int few(const Operand &X, const Operand &W, const float *bias, void *pre, bf16_t *Out, int M, int N, int Np, hipStream_t st)
+{
+    constexpr size_t bytes = kFewWaves * kFewRing * (size_t)(TFew::kChunkA + TFew::kChunkB) * 2;
+    const dim3 grid((Np + (ACT >= 0 ? 15 : 31)) / (ACT >= 0 ? 16 : 32), (M + 31) / 32);
+    if (M <= 8) {
+        if (allow_lds<k_few<ACT, 8>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
+        k_few<ACT, 8><<<grid, 64 * kFewWaves, bytes, st>>>(X, W, bias, (bf16_t *)pre, Out, M, N, Np);
+    } else {
+        if (allow_lds<k_few<ACT, 32>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
+        k_few<ACT, 32><<<grid, 64 * kFewWaves, bytes, st>>>(X, W, bias, (bf16_t *)pre, Out, M, N, Np);
+    }
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
 template <class T, bool BO, int TERMS, typename E>
 int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
@@ -226,6 +341,12 @@ int ffn_forward(const Sizes &S, const void *X, const void *W1, const float *b1, 
     const Operand oX{(const bf16_t *)X, S.Cp, pX, S.Cp}, oW1{(const bf16_t *)W1, 2L * S.hp, pW1, S.C}, oW2{(const bf16_t *)W2, S.Cp, pW2, S.h},
         oA{at(P.Act), S.hp, pA, S.hp};
     int rc;
+    if (few_rows(S)) {
+        ProfScope prof(st, K_FFN_FEW);
+        rc = S.act == BRA_SILU ? few<BRA_SILU>(oX, oW1, b1, pre, at(P.Act), (int)S.M, S.h, S.hp, st) : few<BRA_GELU>(oX, oW1, b1, pre, at(P.Act), (int)S.M, S.h, S.hp, st);
+        if (rc != BRA_OK) return rc;
+        return few<-1>(oA, oW2, b2, nullptr, (bf16_t *)Y, (int)S.M, S.C, S.Cp, st);
+    }
     {
         ProfScope prof(st, K_FFN_GATED);
         if (S.f32) rc = S.act == BRA_SILU ? pick_gated<3, BRA_SILU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, st)

@@ -34,7 +34,7 @@ struct Tile {
 // Swizzle of the 16-byte pieces of a row: by rows of k where the contraction is outside (the four rows that a transposing
 // read touches lie in different quarters of the banks), else differently for the 8 rows that 8 lanes next to each other read.
 template <int B>
-__device__ __forceinline__ int turn_outer(int k) { return B >= 128 ? 4 * (k % 4) : 4 * (k / 2 % 2); }
+__device__ __forceinline__ int turn_outer(int k) { return B >= 128 ? 4 * (k % 4) : B == 64 ? 4 * (k / 2 % 2) : 0; }
 template <bool PERMUTED>
 __device__ __forceinline__ int turn_inner(int row) { return row / 2 % 8; }
 

@@ -111,15 +111,16 @@ __device__ __forceinline__ float add_32(float x)
 template <int K>
 __device__ __forceinline__ void team_sums(float (&v)[K], int tpr, float *lds)
 {
+    auto add = [&](auto f) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (tpr > 1) v[k] = dpp_fadd<0xB1>(v[k]);       // lane ^ 1
-        if (tpr > 2) v[k] = dpp_fadd<0x4E>(v[k]);       // lane ^ 2
-        if (tpr > 4) v[k] = dpp_fadd<0x141>(v[k]);      // mirrored halves of 8: the other 4
-        if (tpr > 8) v[k] = dpp_fadd<0x140>(v[k]);      // mirrored rows of 16: the other 8
-        if (tpr > 16) v[k] = add_16(v[k]);
-        if (tpr > 32) v[k] = add_32(v[k]);
-    }
+        for (int k = 0; k < K; ++k) v[k] = f(v[k]);
+    };
+    if (tpr > 1) add([](float x) { return dpp_fadd<0xB1>(x); });        // lane ^ 1
+    if (tpr > 2) add([](float x) { return dpp_fadd<0x4E>(x); });        // lane ^ 2
+    if (tpr > 4) add([](float x) { return dpp_fadd<0x141>(x); });       // mirrored halves of 8: the other 4
+    if (tpr > 8) add([](float x) { return dpp_fadd<0x140>(x); });       // mirrored rows of 16: the other 8
+    if (tpr > 16) add(add_16);
+    if (tpr > 32) add(add_32);
     if (tpr <= 64) return;
     const int wave = threadIdx.x / 64, waves = tpr / 64, first = wave / waves * waves;
     __syncthreads();                                    // the last sums have been read
