@@ -77,13 +77,13 @@ __device__ __forceinline__ void put8(void *base, long at, bool bf16, bool vec, i
     }
 }
 
-// 2^e as torch.ldexp forms it on this GPU, by powf: for some exponents a unit of float32 off.  A state that a program decodes there, to keep it or to look
-// at it, then holds the very values that the step takes; with the exponent's bits put in place 5 codes in 10000 fell on the other side of a tie.
-__device__ __forceinline__ float power_of_two(int e) { return powf(2.0f, (float)e); }
+// Powers of two from 2^-127 on as torch.ldexp forms them on this GPU, by powf: for some exponents a unit of float32 off.  A state that a program
+// decodes there, to keep it or to look at it, then holds the very values that the step takes; with the exponent's bits put in place 5 codes in
+// 10000 fell on the other side of a tie.  A workgroup forms them once, a thread one of them, while its loads are on their way.
+constexpr int kPowers = 256;
 
-__device__ __forceinline__ void decode8(u32x2 codes, unsigned scale, float (&v)[8])
+__device__ __forceinline__ void decode8(u32x2 codes, float by, float (&v)[8])
 {
-    const float by = power_of_two((int)scale - 127);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], true);
@@ -93,7 +93,7 @@ __device__ __forceinline__ void decode8(u32x2 codes, unsigned scale, float (&v)[
 
 // The codes of this thread's 8 values and the scale of the 32 that 4 threads hold.
 template <bool ROOT>
-__device__ __forceinline__ u32x2 encode8(const float (&v)[8], unsigned &scale)
+__device__ __forceinline__ u32x2 encode8(const float (&v)[8], const float *powers, unsigned &scale)
 {
     float most = 0.f;
 #pragma unroll
@@ -101,9 +101,9 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], unsigned &scale)
     most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, most), 0xB1, 0xf, 0xf, true)));
     most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, most), 0x4E, 0xf, 0xf, true)));
     const unsigned bits = __builtin_bit_cast(unsigned, most);
-    const int e2 = max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -126);
+    const int e2 = max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -126);       // at most 120
     scale = (unsigned)(e2 + 127);
-    const float by = power_of_two(-e2);
+    const float by = powers[127 - e2];
     float q[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -131,20 +131,36 @@ __global__ __launch_bounds__(256) void k_adamw(Table T, AdamwSteps A, void *__re
         else hi = mid - 1;
     }
     const Entry &E = T.e[lo];
+    __shared__ float powers[BITS == 8 ? kPowers : 1];
     const long i = (long)(blockIdx.x - E.first) * kChunk + 8 * threadIdx.x;
-    if (i >= (E.n + kBlock - 1) / kBlock * kBlock) return;      // whole blocks: 4 threads leave or stay together
-    const int n = (int)min(E.n - i, 8L);                        // may be negative in the last block
+    const bool live = i < (E.n + kBlock - 1) / kBlock * kBlock;     // whole blocks: 4 threads go on or stay behind together
+    const int n = (int)max(0L, min(E.n - i, 8L));
     const bool pb = E.kinds & 1, gb = E.kinds & 2, vec = E.kinds & 4;
     float p[8], g[8], m[8], v[8];
     const long at = (long)E.place * kBlock + i;
-    get8(E.param, i, pb, vec, n, p);
-    get8(E.grad, i, gb, vec, n, g);
-    if (BITS == 32) {
-        get8(moments, at, false, true, 8, m);
-        get8(squares, at, false, true, 8, v);
-    } else {
-        decode8(*(const u32x2 *)((const unsigned char *)moments + at), scales[at / kBlock], m);
-        decode8(*(const u32x2 *)((const unsigned char *)squares + at), root_scales[at / kBlock], v);
+    u32x2 mc = {0u, 0u}, vc = {0u, 0u};
+    unsigned ms = 0, vs = 0;
+    if (live) {
+        get8(E.param, i, pb, vec, n, p);
+        get8(E.grad, i, gb, vec, n, g);
+        if (BITS == 32) {
+            get8(moments, at, false, true, 8, m);
+            get8(squares, at, false, true, 8, v);
+        } else {
+            mc = *(const u32x2 *)((const unsigned char *)moments + at);
+            vc = *(const u32x2 *)((const unsigned char *)squares + at);
+            ms = scales[at / kBlock];
+            vs = root_scales[at / kBlock];
+        }
+    }
+    if constexpr (BITS == 8) {
+        powers[threadIdx.x] = powf(2.0f, (float)((int)threadIdx.x - 127));
+        __syncthreads();
+    }
+    if (!live) return;
+    if (BITS == 8) {
+        decode8(mc, powers[ms], m);
+        decode8(vc, powers[vs], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = v[e] * v[e];
     }
@@ -169,9 +185,9 @@ __global__ __launch_bounds__(256) void k_adamw(Table T, AdamwSteps A, void *__re
         put8(squares, at, false, true, 8, v);
     } else {
         unsigned s;
-        *(u32x2 *)((unsigned char *)moments + at) = encode8<false>(m, s);
+        *(u32x2 *)((unsigned char *)moments + at) = encode8<false>(m, powers, s);
         if (threadIdx.x % 4 == 0) scales[at / kBlock] = (unsigned char)s;
-        *(u32x2 *)((unsigned char *)squares + at) = encode8<true>(root, s);
+        *(u32x2 *)((unsigned char *)squares + at) = encode8<true>(root, powers, s);
         if (threadIdx.x % 4 == 0) root_scales[at / kBlock] = (unsigned char)s;
     }
 }

@@ -236,6 +236,114 @@ int few(const Operand &X, const Operand &W, const float *bias, void *pre, bf16_t
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
+// Few rows in float32, the weights read once and as they lie (no terms, no copies): 8 rows x 32 columns per workgroup, a lane has 4 columns and every
+// 64th group of 4 of the contraction; the rows wait in LDS, kFewK of the contraction at a time.  Bound by the weights' bytes.  Columns as in k_few.
+constexpr int kFewK = 2048, kFewRows = 8;
+template <int ACT>
+__global__ __launch_bounds__(512, 2) void k_few_f32(const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, float *__restrict__ pre,
+                                                   float *__restrict__ Out, int M, int K, int N)
+{
+    constexpr bool GATED = ACT >= 0;
+    constexpr int cols = GATED ? 16 : 32;
+    typedef f32x4 f32x4u __attribute__((aligned(4)));
+    __shared__ __attribute__((aligned(16))) float xs[kFewRows][kFewK];
+    __shared__ float sums[8][8][kFewRows * 4];
+    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, piece = lane % 8, group = wave * 8 + lane / 8;
+    const int xcd = blockIdx.x % 8, per = gridDim.x / 8, rest = gridDim.x % 8, tile = xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int c0 = tile * (GATED ? 16 : 32), m0 = blockIdx.y * kFewRows, rows = min(M - m0, kFewRows);
+    const int ld = GATED ? 2 * N : N, unit = c0 + (GATED ? 4 * (piece % 4) : 4 * piece), n = N - unit;      // columns from `unit` on
+    const float *const w = W + unit + (GATED && piece >= 4 ? N : 0);
+    float acc[kFewRows][4];
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
+    for (int k0 = 0; k0 < K; k0 += kFewK) {
+        const int kn = min(kFewK, K - k0);
+        if (k0) __syncthreads();
+        if (wave < rows)
+            for (int k = lane; k < (kn + 3) / 4 * 4; k += 64) xs[wave][k] = k < kn ? X[(size_t)(m0 + wave) * K + k0 + k] : 0.f;
+        __syncthreads();
+        auto add = [&](int k, const f32x4 (&v)[4]) {
+#pragma unroll
+            for (int m = 0; m < kFewRows; ++m) {
+                if (m >= rows) continue;
+                const f32x4 x = *(const f32x4 *)&xs[m][k];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[m][e] = fmaf(x[j], v[j][e], acc[m][e]);
+            }
+        };
+        int k = 4 * group;
+        if (c0 + cols <= N) {
+            // four groups' loads on their way at a time, without a question in between
+            const float *p = w + (size_t)(k0 + k) * ld;
+            const size_t row = ld, step = 256 * row;
+            for (; k + 3 * 256 + 4 <= kn; k += 4 * 256, p += 4 * step) {
+                f32x4 v[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[i][j] = *(const f32x4u *)(p + i * step + j * row);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) add(k + 256 * i, v[i]);
+            }
+        }
+        for (; k < kn; k += 256) {
+            f32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float *p = w + (size_t)(k0 + min(k + j, kn - 1)) * ld;
+                if (n >= 4) v[j] = *(const f32x4u *)p;
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j][e] = e < n ? p[e] : 0.f;
+                if (k + j >= kn) v[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            add(k, v);
+        }
+    }
+    // over the groups of a wavefront, then over the wavefronts
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m) {
+        if (m >= rows) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s = cross_row_sum(dpp_fadd<0x128>(acc[m][e]));      // lanes 8 apart, then rows of 16
+            if (lane < 8) sums[wave][lane][4 * m + e] = s;
+        }
+    }
+    __syncthreads();
+    auto total = [&](int p, int i) {
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += sums[q][p][i];
+        return s;
+    };
+    const int m = tid / cols, col = tid % cols;
+    if (m >= rows || c0 + col >= N) return;
+    float g = total(col / 4, 4 * m + col % 4) + (bias ? bias[c0 + col] : 0.f);
+    const size_t row = (size_t)(m0 + m);
+    if constexpr (GATED) {
+        const float u = total(4 + col / 4, 4 * m + col % 4) + (bias ? bias[N + c0 + col] : 0.f);
+        if (pre) {
+            pre[row * 2 * N + c0 + col] = g;
+            pre[row * 2 * N + N + c0 + col] = u;
+        }
+        g = activation<GATED ? ACT : 0>(g) * u;
+    }
+    Out[row * N + c0 + col] = g;
+}
+
+template <int ACT>
+int few_f32(const void *X, const void *W, const float *bias, void *pre, void *Out, int M, int K, int N, hipStream_t st)
+{
+    const dim3 grid((N + (ACT >= 0 ? 15 : 31)) / (ACT >= 0 ? 16 : 32), (M + kFewRows - 1) / kFewRows);
+    k_few_f32<ACT><<<grid, 512, 0, st>>>((const float *)X, (const float *)W, bias, (float *)pre, (float *)Out, M, K, N);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
 template <class T, bool BO, int TERMS, typename E>
 int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
@@ -329,6 +437,12 @@ int ffn_forward(const Sizes &S, const void *X, const void *W1, const float *b1, 
     const ForwardPlan P(S);
     auto at = [&](size_t offset) { return (bf16_t *)((char *)ws + offset); };
     const long pX = S.M * S.Cp, pW1 = (long)S.C * 2 * S.hp, pW2 = (long)S.h * S.Cp, pA = S.M * S.hp;
+    if (few_rows_f32(S)) {
+        ProfScope prof(st, K_FFN_FEW);
+        float *A = (float *)at(P.Act);
+        const int rc = S.act == BRA_SILU ? few_f32<BRA_SILU>(X, W1, b1, pre, A, (int)S.M, S.C, S.h, st) : few_f32<BRA_GELU>(X, W1, b1, pre, A, (int)S.M, S.C, S.h, st);
+        return rc != BRA_OK ? rc : few_f32<-1>(A, W2, b2, nullptr, Y, (int)S.M, S.h, S.C, st);
+    }
     if (S.copies()) {
         Layouts J{};
         add_layout(J, X, at(P.X), S.M, 1, S.C, S.Cp, pX);

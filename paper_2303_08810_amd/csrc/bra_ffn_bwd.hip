@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256) void k_sums(SumsArgs S)
         float acc[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < count; ++k) {
             const f32x4 *p = (const f32x4 *)(S.W.part + (size_t)(first + k * apart) * kSlot<T>) + (frag * 4 + 2 * run) * 64 + lane;
             const f32x4 a = p[0], b = p[64];
@@ -318,6 +318,7 @@ __global__ __launch_bounds__(256) void k_sums(SumsArgs S)
         if (i < count) {
             const int at = i / S.cols[j] * S.cols_p[j] + i % S.cols[j];
             float s = 0.f;
+#pragma unroll 8
             for (int p = 0; p < S.shares; ++p) s += S.columns[j][(size_t)p * S.blocks[j] * S.cols_p[j] + at];
             store_from_f32((E *)S.db[j] + i, s);
             return;
