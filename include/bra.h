@@ -309,7 +309,7 @@ int bra_norm_backward(const bra_norm_shape *shape, const void *R, const void *Y_
  * with a step that counts on); `scalars` is then device scratch for 2 floats.  grad_scale: NULL or one float32 on the device, for a
  * loss scale or clipping.  No workspace otherwise; 72 tensors go into a launch.
  * Alignment: exp_avg, exp_avg_sq 32 bytes, the others their elements' size (16 bytes are faster).
- * Errors: NULL; SHAPE (count < 0, n < 0 or above 2^36, step < 1, betas outside [0, 1), lr, eps or weight_decay negative or not finite); DTYPE
+ * Errors: NULL; SHAPE (count < 0, n < 0 or above 2^34, step < 1, betas outside [0, 1), lr, eps or weight_decay negative or not finite); DTYPE
  * (dtypes; bits; a copy of a bf16 parameter); OVERLAP (parameters or copies that share memory); ALIGN; LAUNCH. */
 #define BRA_ADAMW_BLOCK 32
 typedef struct bra_adamw_tensor {

@@ -231,7 +231,7 @@ int adamw_step(const bra_adamw_tensor *tensors, int count, const bra_adamw_args 
         place += (unsigned long)((t.n + kBlock - 1) / kBlock);
         if (!t.n || !t.grad) continue;
         const unsigned long chunks = (unsigned long)((t.n + kChunk - 1) / kChunk);
-        if (T.count == kPerLaunch || blocks + chunks > 0x7fffffffu) {
+        if (T.count == kPerLaunch || blocks + chunks > 0xffffffu) {        // (2^32 threads and more cannot be launched)
             const int rc = launch();
             if (rc != BRA_OK) return rc;
         }

@@ -419,7 +419,7 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
     bool any = false;
     for (int i = 0; i < count; ++i) {
         const bra_adamw_tensor &t = tensors[i];
-        if (t.n < 0 || t.n > (1L << 36) || !fine(t.weight_decay)) return BRA_ERR_SHAPE;
+        if (t.n < 0 || t.n > (1L << 34) || !fine(t.weight_decay)) return BRA_ERR_SHAPE;
         if ((t.param_dtype != BRA_F32 && t.param_dtype != BRA_BF16) || (t.grad_dtype != BRA_F32 && t.grad_dtype != BRA_BF16)) return BRA_ERR_DTYPE;
         if (t.copy && t.param_dtype != BRA_F32) return BRA_ERR_DTYPE;
         total += (t.n + BRA_ADAMW_BLOCK - 1) / BRA_ADAMW_BLOCK;
