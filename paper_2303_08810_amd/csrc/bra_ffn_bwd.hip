@@ -67,7 +67,9 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
-        bf16x8 held[TD::NT][2][TERMS];
+        // A waits in registers, and with it all terms of dG and dU where they fit: otherwise they are formed again for each term
+        constexpr bool kHold = TERMS > 1 && TD::NT <= 2;
+        bf16x8 held[TD::NT][2][TERMS], held_g[kHold ? TD::NT : 1][2][TERMS], held_u[kHold ? TD::NT : 1][2][TERMS];
         auto pieces = [&](int q) {
 #pragma unroll
             for (int nt = 0; nt < TD::NT; ++nt)
@@ -98,23 +100,36 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float f, slope;
-                        activation_slope<ACT>(g[e], f, slope);
+                        activation_slope<ACT, TERMS != 1>(g[e], f, slope);
                         const float d = acc[nt][mt][8 * run + e];
                         a[e] = e < n ? f * u[e] : 0.f;
                         dg[e] = e < n ? d * u[e] * slope : 0.f;
                         du[e] = e < n ? d * f : 0.f;
                     }
-                    bf16x8 t[TERMS];
-                    operand<TERMS>(dg, t);
-                    first.put(c, piece, t[q]);
-                    operand<TERMS>(du, t);
-                    second.put(c, piece, t[q]);
                     operand<TERMS>(a, held[nt][run]);
+                    if constexpr (kHold) {
+                        operand<TERMS>(dg, held_g[nt][run]);
+                        operand<TERMS>(du, held_u[nt][run]);
+                    } else {
+                        bf16x8 t[TERMS];
+                        operand<TERMS>(dg, t);
+                        first.put(c, piece, t[q]);
+                        operand<TERMS>(du, t);
+                        second.put(c, piece, t[q]);
+                    }
                 }
         };
 #pragma unroll
         for (int q = 0; q < TERMS; ++q) {
-            pieces(q);
+            if (!kHold || q == 0) pieces(q);
+            if constexpr (kHold)
+#pragma unroll
+                for (int nt = 0; nt < TD::NT; ++nt)
+#pragma unroll
+                    for (int run = 0; run < 2; ++run) {
+                        first.put(c, 4 * nt + 2 * run + hi, held_g[nt][run][q]);
+                        second.put(c, 4 * nt + 2 * run + hi, held_u[nt][run][q]);
+                    }
             auto flush = [&](const Rows<P> &from, bf16_t *to, long ld) {
                 from.each(32, lane, [&](int in, int piece, bf16x8 v) {
                     if (r0 + in < rows && wj + 8 * piece < hp) *(bf16x8 *)(to + (size_t)(m0 + r0 + in) * ld + wj + 8 * piece) = v;
@@ -244,6 +259,7 @@ struct Gradients {
     void *dX;
     long M;
     int C, product_tiles;
+    int product_first;      // dX's tiles ahead of the weights' parts: whichever takes a workgroup longer
     Columns columns[2];
     int shares;
 };
@@ -253,6 +269,13 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradien
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *lds = (bf16_t *)smem;
     int block = blockIdx.x;
+    if (G.product_first) {
+        if (block < G.product_tiles) {
+            product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
+            return;
+        }
+        block -= G.product_tiles;
+    }
     if (block < G.W.workgroups) {
         // workgroups of an XCD have neighbouring parts
         const int xcd = block % 8, per = G.W.workgroups / 8, rest = G.W.workgroups % 8;
@@ -260,11 +283,13 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradien
         return;
     }
     block -= G.W.workgroups;
-    if (block < G.product_tiles) {
-        product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
-        return;
+    if (!G.product_first) {
+        if (block < G.product_tiles) {
+            product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
+            return;
+        }
+        block -= G.product_tiles;
     }
-    block -= G.product_tiles;
     const int j = block >= G.columns[0].groups * G.shares;
     if (j) block -= G.columns[0].groups * G.shares;
     columns_part<TERMS>(G.columns[j], block / G.shares, block % G.shares, G.shares, G.M, (float *)smem);
@@ -369,6 +394,7 @@ int launch_gradients(Gradients G, bool columns, hipStream_t st)
     constexpr size_t bytes = std::max<size_t>(T::kLds, T::kThreads / 8 * 68 * 4);
     if (allow_lds<k_gradients<T, TERMS, E>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
     G.product_tiles = (int)(((G.M + T::BM - 1) / T::BM) * ((G.C + T::BN - 1) / T::BN));
+    G.product_first = (G.dP.K + 63) / 64 > G.W.chunks / std::max(1, G.W.shares);
     const int groups = columns ? G.columns[0].groups + G.columns[1].groups : 0;
     k_gradients<T, TERMS, E><<<(unsigned)(G.W.workgroups + G.product_tiles + groups * G.shares), T::kThreads, bytes, st>>>(G);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;

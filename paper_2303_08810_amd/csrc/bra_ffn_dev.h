@@ -387,7 +387,9 @@ __device__ __forceinline__ float activation(float g)
     return ACT == BRA_SILU ? g * sigmoid(g) : gelu_f32(g);
 }
 
-template <int ACT>
+// EXACT: Phi by erf; else log2 Phi(-a) by the polynomial of gelu_f32, within 1.4e-5, a 280th of a bf16 step, for half the instructions (gradients of
+// 12544 x 128 x 256 with GELU are bound by them).
+template <int ACT, bool EXACT>
 __device__ __forceinline__ void activation_slope(float g, float &a, float &slope)
 {
     if (ACT == BRA_SILU) {
@@ -395,7 +397,19 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
         a = g * f;
         slope = f + a * (1.f - f);
     } else {
-        const float f = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+        float f;
+        if (EXACT) f = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+        else {
+            const float x = fminf(fabsf(g), 16.0f);
+            float p = fmaf(-4.732939124e-04f, x, 7.084460463e-03f);
+            p = fmaf(p, x, -5.182716623e-02f);
+            p = fmaf(p, x, -4.599926472e-01f);
+            p = fmaf(p, x, -1.150787711e+00f);
+            p = fmaf(p, x, -1.000037670e+00f);
+            const float q = __builtin_amdgcn_exp2f(p);
+            f = g > 0.f ? 1.f - q : q;
+            f = g != g ? g : f;
+        }
         a = g * f;
         slope = f + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
     }
