@@ -34,6 +34,7 @@ struct BackArgs {
     int C, tpr, parts;
     float eps;
     bool vec;                       // rows are whole 16-byte pieces
+    float *out[kSums];              // where a single workgroup finishes everything: the results
     int whole;                      // FINISH: a workgroup has a whole group at a time, otherwise each of its teams has one
 };
 
@@ -47,9 +48,9 @@ struct Split {
     Split(const NormSizes &S) : T(S.C, S.vec)
     {
         const int teams = T.teams(), kTarget = 256 * waves(T.V * T.nch, S.f32, false);        // workgroups that run at once
-        // A group of fewer rows than half of a workgroup's teams: each team takes whole groups.  Otherwise a workgroup takes a group, or, where
-        // groups are few, a part of one
-        const bool by_team = S.per_group <= teams / 2;
+        // Many groups of fewer rows than half of a workgroup's teams: each team takes whole groups.  Otherwise a workgroup takes a group, or,
+        // where groups are few, a part of one
+        const bool by_team = S.per_group <= teams / 2 && S.groups > kTarget;
         parts = 1;
         if (!by_team) parts = (int)std::max(1L, std::min<long>((kTarget + S.groups - 1) / S.groups, (S.per_group + 2 * teams - 1) / (2 * teams)));
         finish = parts == 1;
@@ -307,7 +308,15 @@ __global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) v
     for (int s = 0; s < (FINISH ? kSums : 2); ++s) {
         if (s < 2 ? !A.dN : !A.I.Y || (s > 2 && !POST)) continue;
         over_teams(sums[s]);
-        if (team == 0)
+        if (team != 0) continue;
+        if (FINISH && gridDim.x == 1) {
+            if (A.out[s])
+#pragma unroll
+                for (int k = 0; k < NCH; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (FULL || e < n[k]) A.out[s][V * (t + k * tpr) + e] = sums[s][k][e];
+        } else
 #pragma unroll
             for (int k = 0; k < NCH; ++k) store<FULL>(A.part + ((size_t)blockIdx.x * (FINISH ? kSums : 2) + s) * C + V * (t + k * tpr), sums[s][k], n[k], vec);
     }
@@ -432,8 +441,9 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
         const Split P(S);
         F.part = (const float *)ws; F.units = (const float *)ws + part_floats(S, P);
         F.blocks = (int)P.blocks; F.sums = P.sums(); F.parts = P.parts; F.groups = S.groups;
-        const BackArgs A{I, dN, dR, G.dX, G.dY, P.finish ? G.dgate : nullptr, (float *)ws, (float *)ws + part_floats(S, P), S.rows, S.groups, (unsigned)S.per_group, S.C, P.T.tpr,
-                         P.parts, S.eps, S.vec, P.whole};
+        BackArgs A{I, dN, dR, G.dX, G.dY, P.finish ? G.dgate : nullptr, (float *)ws, (float *)ws + part_floats(S, P), S.rows, S.groups, (unsigned)S.per_group, S.C, P.T.tpr,
+                         P.parts, S.eps, S.vec, {}, P.whole};
+        for (int s = 0; s < kSums; ++s) A.out[s] = outs[s];
         {
             ProfScope prof(st, K_NORM_BACKWARD);
             int rc;
@@ -444,7 +454,7 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
                 if (S.layer) rc = S.post ? pick<bf16_t, true, true>(A, P, st) : pick<bf16_t, true, false>(A, P, st);
                 else rc = S.post ? pick<bf16_t, false, true>(A, P, st) : pick<bf16_t, false, false>(A, P, st);
             }
-            if (rc != BRA_OK) return rc;
+            if (rc != BRA_OK || (P.finish && P.blocks == 1)) return rc;
         }
         if (!P.finish && I.Y && G.dgate) {
             F.dgate = G.dgate;
