@@ -46,8 +46,9 @@ inline int hidden_side(const Sizes &S, bool given)
 // 128 x 768 x 2048 15.2 / 21.9, 128 x 1024 x 4096 29 / 34).
 inline bool few_rows(const Sizes &S) { return !S.f32 && S.M <= 128; }
 
-// And to k_few_f32 (1 x 768 x 2048 18 / 133, 128 x 768 x 2048 65 / 134, 128 x 1024 x 4096 158 / 235).
-inline bool few_rows_f32(const Sizes &S) { return S.f32 && S.M <= 128; }
+// And to k_few_f32, whose vector instructions take a time that grows with the rows (us, k_few_f32 / tiles: 1 x 768 x 2048 18 / 43, 32 rows 37 / 44, 64 rows 53 / 45;
+// 32 x 1024 x 2816 62 / 57; 128 x 256 x 512 19 / 29, 48 x 512 x 1368 37 / 36).
+inline bool few_rows_f32(const Sizes &S) { return S.f32 && (S.M <= 32 || (S.M <= 128 && (double)S.M * S.C * S.h <= 32e6)); }
 
 // A matrix of `blocks` column blocks of `cols` columns laid out anew: each block padded with zeros to `cols_p` columns, float32 as three
 // planes of terms.

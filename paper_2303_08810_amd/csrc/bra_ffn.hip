@@ -7,6 +7,8 @@
 #include "bra_ffn.h"
 #include "bra_ffn_dev.h"
 
+#include <algorithm>
+
 namespace bra {
 namespace ffn {
 
@@ -344,6 +346,84 @@ int few_f32(const void *X, const void *W, const float *bias, void *pre, void *Ou
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
+// Few tiles and a long contraction: each tile in `shares` shares of it, the sums joined (with all that follows them) by k_join.  GATED: the columns of
+// k_gated's tiles, N of them hidden units (padded); otherwise those of a product.  Tile i of share s in slot (s * tiles + i).
+template <class T, bool GATED, int TERMS>
+__global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_split(Operand A, Operand Bm, float *__restrict__ part, long M, int N, int tiles, int shares)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, share = blockIdx.x / tiles, i = blockIdx.x % tiles;
+    const int chunks = (A.K + 63) / 64, first = (int)((long)chunks * share / shares), last = (int)((long)chunks * (share + 1) / shares);
+    f32x16 acc[T::NT][T::MT];
+    if constexpr (GATED) {
+        constexpr int BJ = T::BN / 2, PW = 16 * T::NT;
+        int mt0, nt0;
+        tile_of(i, (int)((M + T::BM - 1) / T::BM), (N + BJ - 1) / BJ, mt0, nt0);
+        const long m0 = (long)mt0 * T::BM;
+        const int j0 = nt0 * BJ, rows = (int)min((long)T::BM, M - m0), most = N - 8 - j0;
+        const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+        const Loads<T, T::BN, true, true> lb(wave, lane, Bm.ld, [&](int col) {
+            const int w = col / (2 * PW), in = col % (2 * PW);
+            return (long)(min(w * PW + in % PW, most) + (in >= PW ? N : 0));
+        });
+        clear<T>(acc);
+        multiply<T, false, true, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + j0, la, lb, first, last, (bf16_t *)smem, acc);
+    } else product_sums<T, true, TERMS>(A, Bm, M, N, i, first, last, (bf16_t *)smem, acc);
+    store_slot<T>(part + (size_t)blockIdx.x * kSlot<T>, acc, wave, lane);
+}
+
+// N columns exist, Np in the rows that a later product reads.
+template <class T, int ACT, int TERMS, typename E>
+__global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, const float *__restrict__ bias, E *__restrict__ pre, void *__restrict__ Out, long plane, long M, int N, int Np,
+                                             int tiles, int shares)
+{
+    constexpr bool GATED = ACT >= 0;
+    constexpr int BJ = GATED ? T::BN / 2 : T::BN, NT = GATED ? T::NT / 2 : T::NT, kPer = T::BM * BJ / 8 / 256;      // workgroups per tile
+    const int tile = blockIdx.x / kPer, i = blockIdx.x % kPer * 256 + threadIdx.x, lane = i % 64, run = i / 64 % 2, f = i / 128;
+    const int mt = f % T::MT, nt = f / T::MT % NT, wave = f / (T::MT * NT);
+    int mt0, nt0;
+    tile_of(tile, (int)((M + T::BM - 1) / T::BM), ((GATED ? Np : N) + BJ - 1) / BJ, mt0, nt0);
+    const long m = (long)mt0 * T::BM + (wave / T::WC) * (32 * T::MT) + 32 * mt + lane % 32;
+    const int col = nt0 * BJ + (wave % T::WC) * (32 * NT) + 32 * nt + 16 * run + 8 * (lane / 32), n = N - col;
+    if (m >= M || col >= (GATED ? Np : N)) return;
+    float g[8], b[8];
+    sum_slots<T>(part, tile, tiles, shares, (wave * T::NT + nt) * T::MT + mt, run, lane, g);
+    if (bias) {
+        load8(bias + col, b, n, false);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] += b[e];
+    }
+    if constexpr (GATED) {
+        float u[8];
+        sum_slots<T>(part, tile, tiles, shares, (wave * T::NT + NT + nt) * T::MT + mt, run, lane, u);
+        if (bias) {
+            load8(bias + N + col, b, n, false);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] += b[e];
+        }
+        if (pre) {
+            store8(pre + (size_t)m * 2 * N + col, g, n, N % 8 == 0);
+            store8(pre + (size_t)m * 2 * N + N + col, u, n, N % 8 == 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = e < n ? activation<GATED ? ACT : 0>(g[e]) * u[e] : 0.f;
+        store_operand<TERMS>((bf16_t *)Out + (size_t)m * Np + col, plane, g);
+    } else store8((E *)Out + (size_t)m * N + col, g, n, N % 8 == 0);
+}
+
+template <class T, int ACT, int TERMS, typename E>
+int split(const Operand &A, const Operand &Bm, const float *bias, void *pre, void *Out, long plane, long M, int N, int Np, int shares, float *part, hipStream_t st)
+{
+    constexpr bool GATED = ACT >= 0;
+    constexpr int BJ = GATED ? T::BN / 2 : T::BN;
+    if (allow_lds<k_split<T, GATED, TERMS>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
+    const int count = (int)(((M + T::BM - 1) / T::BM) * (((GATED ? Np : N) + BJ - 1) / BJ));
+    k_split<T, GATED, TERMS><<<(unsigned)(count * shares), T::kThreads, T::kLds, st>>>(A, Bm, part, M, GATED ? Np : N, count, shares);
+    if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    k_join<T, ACT, TERMS, E><<<(unsigned)(count * (T::BM * BJ / 8 / 256)), 256, 0, st>>>(part, bias, (E *)pre, Out, plane, M, N, Np, count, shares);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
 template <class T, bool BO, int TERMS, typename E>
 int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
@@ -408,11 +488,28 @@ using namespace ffn;
 
 namespace {
 
+typedef Tile<64, 128, 2, 2, 3> TSplitGated;
+typedef Tile<64, 64, 2, 2, 4> TSplit;
+
+// Shares of the contraction of K for `count` tiles: for two workgroups per compute unit, if that saves more than the joining launch costs.  A chunk takes about
+// 0.25 us where a compute unit has one or two workgroups (six of them in float32).  Forward, us, whole / shared out: float32 129 x 768 x 2048 134 / 58,
+// 129 x 256 x 512 42 / 29, 1024 x 512 x 1368 104 / 77; bf16 129 x 1024 x 2816 27.4 / 22.2, 512 x 768 x 2048 23.5 / 22.4.
+int split_shares(const Sizes &S, long count, int K)
+{
+    const int chunks = (K + 63) / 64, shares = (int)std::min<long>({512 / std::max(1L, count), chunks, 16});
+    return shares > 1 && 0.25 * chunks * (S.f32 ? 6 : 1) * (1 - 1.0 / shares) > 6 ? shares : 1;
+}
+
 // What the forward keeps in the workspace.
 struct ForwardPlan {
-    size_t X, W1, W2, Act, total;
+    size_t X, W1, W2, Act, parts, total;
+    int gated_shares, product_shares;
     ForwardPlan(const Sizes &S)
     {
+        auto tiles = [](long M, int BM, long N, int BN) { return ((M + BM - 1) / BM) * ((N + BN - 1) / BN); };
+        const bool few = few_rows(S) || few_rows_f32(S);
+        gated_shares = few || gated_side(S) != 64 ? 1 : split_shares(S, tiles(S.M, 64, S.hp, 64), S.Cp);
+        product_shares = few || product_side(S.M, S.C) != 64 ? 1 : split_shares(S, tiles(S.M, 64, S.C, 64), S.hp);
         size_t at = 0;
         auto take = [&](size_t elements) {
             const size_t here = at;
@@ -423,9 +520,19 @@ struct ForwardPlan {
         W1 = S.copies() ? take((size_t)S.C * 2 * S.hp) : 0;
         W2 = S.copies() ? take((size_t)S.h * S.Cp) : 0;
         Act = take((size_t)S.M * S.hp);
+        auto slots = [](long count, int shares, size_t floats) { return shares > 1 ? (size_t)count * shares * floats * 4 : 0; };
+        parts = at;
+        at += std::max(slots(tiles(S.M, 64, S.hp, 64), gated_shares, kSlot<TSplitGated>), slots(tiles(S.M, 64, S.C, 64), product_shares, kSlot<TSplit>));
         total = at;
     }
 };
+
+template <int TERMS, int ACT, typename E>
+int gated(const Operand &X, const Operand &W1, const float *b1, void *pre, bf16_t *Act, long plane, const Sizes &S, const ForwardPlan &P, void *parts, hipStream_t st)
+{
+    if (P.gated_shares > 1) return split<TSplitGated, ACT, TERMS, E>(X, W1, b1, pre, Act, plane, S.M, S.h, S.hp, P.gated_shares, (float *)parts, st);
+    return pick_gated<TERMS, ACT, E>(X, W1, b1, pre, Act, plane, S, st);
+}
 
 }  // namespace
 
@@ -463,12 +570,18 @@ int ffn_forward(const Sizes &S, const void *X, const void *W1, const float *b1, 
     }
     {
         ProfScope prof(st, K_FFN_GATED);
-        if (S.f32) rc = S.act == BRA_SILU ? pick_gated<3, BRA_SILU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, st)
-                                          : pick_gated<3, BRA_GELU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, st);
-        else rc = S.act == BRA_SILU ? pick_gated<1, BRA_SILU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, st)
-                                    : pick_gated<1, BRA_GELU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, st);
+        if (S.f32) rc = S.act == BRA_SILU ? gated<3, BRA_SILU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, P, at(P.parts), st)
+                                          : gated<3, BRA_GELU, float>(oX, oW1, b1, pre, at(P.Act), pA, S, P, at(P.parts), st);
+        else rc = S.act == BRA_SILU ? gated<1, BRA_SILU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, P, at(P.parts), st)
+                                    : gated<1, BRA_GELU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, P, at(P.parts), st);
     }
     if (rc != BRA_OK) return rc;
+    if (P.product_shares > 1) {
+        ProfScope prof(st, K_FFN_PRODUCT);
+        float *part = (float *)at(P.parts);
+        return S.f32 ? split<TSplit, -1, 3, float>(oA, oW2, b2, nullptr, Y, 0, S.M, S.C, S.Cp, P.product_shares, part, st)
+                     : split<TSplit, -1, 1, bf16_t>(oA, oW2, b2, nullptr, Y, 0, S.M, S.C, S.Cp, P.product_shares, part, st);
+    }
     return product(oA, oW2, true, S.M, S.C, Y, b2, S.f32, K_FFN_PRODUCT, st);
 }
 

@@ -161,9 +161,6 @@ struct Weights {
     float *part;            // slots of BM x BN sums in the order of the wavefronts' registers
     int tiles0, tiles, chunks, main, shares, per, workgroups;
 };
-template <class T>
-constexpr int kSlot = T::BM * T::BN;
-
 // Tile i of the row: its job and where it lies.
 template <class T>
 __device__ __forceinline__ void weight_tile(const Weights &W, int i, int &job, int &r0, int &c0)
@@ -208,13 +205,7 @@ __device__ __forceinline__ void weights_part(const Weights &W, int workgroup, bf
         f32x16 acc[T::NT][T::MT];
         clear<T>(acc);
         multiply<T, true, true, TERMS>(A, B, A.p + r0, B.p + c0, la, lb, first, last, lds, acc);
-        f32x4 *part = (f32x4 *)(W.part + (size_t)slot * kSlot<T>) + wave * (T::NT * T::MT * 256) + lane;
-#pragma unroll
-        for (int nt = 0; nt < T::NT; ++nt)
-#pragma unroll
-            for (int mt = 0; mt < T::MT; ++mt)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) part[((nt * T::MT + mt) * 4 + q) * 64] = f32x4{acc[nt][mt][4 * q], acc[nt][mt][4 * q + 1], acc[nt][mt][4 * q + 2], acc[nt][mt][4 * q + 3]};
+        store_slot<T>(W.part + (size_t)slot * kSlot<T>, acc, wave, lane);
     }
 }
 
@@ -252,13 +243,15 @@ __device__ __forceinline__ void columns_part(const Columns &J, int group, int sh
     }
 }
 
-// Everything that follows from dG | dU and A, in one launch: the weights' parts, dX = [dG | dU] W1^T in tiles, the columns' sums.
+// Everything that follows from dG | dU and A, in one launch: the weights' parts, dX = [dG | dU] W1^T in tiles (or, few of them, shares of
+// their long contraction, to slots that k_sums joins), the columns' sums.
 struct Gradients {
     Weights W;
     Operand dP, W1;
     void *dX;
     long M;
-    int C, product_tiles;
+    int C, product_tiles, product_shares;
+    float *product_part;    // share s of tile i in slot (s * product_tiles + i)
     int product_first;      // dX's tiles ahead of the weights' parts: whichever takes a workgroup longer
     Columns columns[2];
     int shares;
@@ -269,12 +262,21 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradien
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *lds = (bf16_t *)smem;
     int block = blockIdx.x;
-    if (G.product_first) {
-        if (block < G.product_tiles) {
+    const int products = G.product_tiles * G.product_shares;
+    auto product = [&] {
+        if (G.product_shares == 1) {
             product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
             return;
         }
-        block -= G.product_tiles;
+        const int chunks = (G.dP.K + 63) / 64, share = block / G.product_tiles;
+        f32x16 acc[T::NT][T::MT];
+        product_sums<T, false, TERMS>(G.dP, G.W1, G.M, G.C, block % G.product_tiles, (int)((long)chunks * share / G.product_shares),
+                                      (int)((long)chunks * (share + 1) / G.product_shares), lds, acc);
+        store_slot<T>(G.product_part + (size_t)block * kSlot<T>, acc, threadIdx.x / 64, threadIdx.x % 64);
+    };
+    if (G.product_first) {
+        if (block < products) return product();
+        block -= products;
     }
     if (block < G.W.workgroups) {
         // workgroups of an XCD have neighbouring parts
@@ -284,11 +286,8 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradien
     }
     block -= G.W.workgroups;
     if (!G.product_first) {
-        if (block < G.product_tiles) {
-            product_tile<T, false, TERMS, E>(G.dP, G.W1, nullptr, (E *)G.dX, G.M, G.C, block, lds);
-            return;
-        }
-        block -= G.product_tiles;
+        if (block < products) return product();
+        block -= products;
     }
     const int j = block >= G.columns[0].groups * G.shares;
     if (j) block -= G.columns[0].groups * G.shares;
@@ -303,6 +302,12 @@ struct SumsArgs {
     void *db[2];
     const float *columns[2];
     int shares, tile_blocks;
+    // dX [M, C], if its tiles came in shares; `product_blocks` workgroups behind the weights'
+    const float *product_part;
+    void *dX;
+    long M;
+    int C, product_tiles, product_shares, product_blocks;
+    bool f32;
 };
 template <class T, typename E>
 __global__ __launch_bounds__(256) void k_sums(SumsArgs S)
@@ -324,20 +329,28 @@ __global__ __launch_bounds__(256) void k_sums(SumsArgs S)
             count = w1 - w0 + 1;
         }
         float acc[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll 8
-        for (int k = 0; k < count; ++k) {
-            const f32x4 *p = (const f32x4 *)(S.W.part + (size_t)(first + k * apart) * kSlot<T>) + (frag * 4 + 2 * run) * 64 + lane;
-            const f32x4 a = p[0], b = p[64];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { acc[e] += a[e]; acc[4 + e] += b[e]; }
-        }
+        sum_slots<T>(S.W.part, first, apart, count, frag, run, lane, acc);
         const int block = col / S.cols_p[job], in = col % S.cols_p[job], n = S.cols[job] - in;
         store8((E *)S.dW[job] + ((size_t)row * S.blocks[job] + block) * S.cols[job] + in, acc, n, S.cols[job] % 8 == 0);
         return;
     }
     int i = ((int)blockIdx.x - S.tile_blocks) * 256 + threadIdx.x;
+    if ((int)blockIdx.x < S.tile_blocks + S.product_blocks) {
+        constexpr int kEach = kSlot<T> / 8;
+        const int tile = i / kEach, in = i % kEach, lane = in % 64, run = in / 64 % 2, frag = in / 128;
+        const int mt = frag % T::MT, nt = frag / T::MT % T::NT, wave = frag / (T::MT * T::NT);
+        int mt0, nt0;
+        tile_of(tile, (int)((S.M + T::BM - 1) / T::BM), (S.C + T::BN - 1) / T::BN, mt0, nt0);
+        const long row = (long)mt0 * T::BM + (wave / T::WC) * (32 * T::MT) + 32 * mt + lane % 32;
+        const int col = nt0 * T::BN + (wave % T::WC) * (32 * T::NT) + 32 * nt + 16 * run + 8 * (lane / 32);
+        if (row >= S.M || col >= S.C) return;
+        float acc[8];
+        sum_slots<T>(S.product_part, tile, S.product_tiles, S.product_shares, frag, run, lane, acc);
+        if (S.f32) store8((float *)S.dX + (size_t)row * S.C + col, acc, S.C - col, S.C % 8 == 0);
+        else store8((bf16_t *)S.dX + (size_t)row * S.C + col, acc, S.C - col, S.C % 8 == 0);
+        return;
+    }
+    i -= S.product_blocks * 256;
     for (int j = 0; j < 2; ++j) {
         const int count = S.db[j] ? S.blocks[j] * S.cols[j] : 0;
         if (i < count) {
@@ -394,9 +407,9 @@ int launch_gradients(Gradients G, bool columns, hipStream_t st)
     constexpr size_t bytes = std::max<size_t>(T::kLds, T::kThreads / 8 * 68 * 4);
     if (allow_lds<k_gradients<T, TERMS, E>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
     G.product_tiles = (int)(((G.M + T::BM - 1) / T::BM) * ((G.C + T::BN - 1) / T::BN));
-    G.product_first = (G.dP.K + 63) / 64 > G.W.chunks / std::max(1, G.W.shares);
+    G.product_first = (G.dP.K + 63) / 64 / G.product_shares > G.W.chunks / std::max(1, G.W.shares);
     const int groups = columns ? G.columns[0].groups + G.columns[1].groups : 0;
-    k_gradients<T, TERMS, E><<<(unsigned)(G.W.workgroups + G.product_tiles + groups * G.shares), T::kThreads, bytes, st>>>(G);
+    k_gradients<T, TERMS, E><<<(unsigned)(G.W.workgroups + G.product_tiles * G.product_shares + groups * G.shares), T::kThreads, bytes, st>>>(G);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
@@ -404,8 +417,10 @@ template <class T>
 int launch_sums(SumsArgs S, bool grads_f32, hipStream_t st)
 {
     S.tile_blocks = S.W.tiles * (kSlot<T> / 8 / 256);
+    S.product_tiles = (int)(((S.M + T::BM - 1) / T::BM) * ((S.C + T::BN - 1) / T::BN));
+    S.product_blocks = S.product_shares > 1 ? S.product_tiles * (kSlot<T> / 8 / 256) : 0;
     const int columns = (S.db[0] ? S.blocks[0] * S.cols[0] : 0) + (S.db[1] ? S.cols[1] : 0);
-    const unsigned blocks = (unsigned)(S.tile_blocks + (columns + 255) / 256);
+    const unsigned blocks = (unsigned)(S.tile_blocks + S.product_blocks + (columns + 255) / 256);
     if (grads_f32) k_sums<T, float><<<blocks, 256, 0, st>>>(S);
     else k_sums<T, bf16_t><<<blocks, 256, 0, st>>>(S);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
@@ -413,7 +428,7 @@ int launch_sums(SumsArgs S, bool grads_f32, hipStream_t st)
 
 // Side of the tiles of k_gradients, and how the weights' tiles are shared out (see Weights).
 struct WeightsPlan {
-    int side, tiles0, tiles, chunks, main, shares, per, workgroups;
+    int side, tiles0, tiles, chunks, main, shares, per, workgroups, product_shares;
     WeightsPlan(const Sizes &S)
     {
         chunks = (int)((S.M + 63) / 64);
@@ -432,6 +447,10 @@ struct WeightsPlan {
             shares = std::min((at_once + tiles - 1) / tiles, std::max(1, chunks / least));
             main = std::min(tiles, at_once / shares);
         }
+        // dX's few tiles of a long contraction are shared out (us with one share / these: 129 x 768 x 2048 244 / 149 in float32, 46 / 42 in bf16, whose chunks are
+        // soon done: shares of 4 at least, and not more than one per compute unit; with 2 and two 1024 x 256 x 512 took 27.1 for 25.4)
+        const int products = (int)ffn::tiles(S.M, S.C, side), long_chunks = (2 * S.hp + 63) / 64;
+        product_shares = side != 64 || products == 0 ? 1 : std::max(1, std::min({(S.f32 ? 512 : 256) / products, long_chunks / (S.f32 ? 1 : 4), 16}));
         workgroups = std::min(at_once, main * shares);
         if (main < tiles) {
             workgroups = at_once;
@@ -443,7 +462,7 @@ struct WeightsPlan {
 };
 
 struct BackwardPlan {
-    size_t X, W1, W2, dY, Act, dP, parts, cols1, cols2, total;
+    size_t X, W1, W2, dY, Act, dP, parts, products, cols1, cols2, total;
     BackwardPlan(const Sizes &S, const WeightsPlan &P)
     {
         size_t at = 0;
@@ -460,6 +479,7 @@ struct BackwardPlan {
         Act = take(M * S.hp * e);
         dP = take(M * 2 * S.hp * e);
         parts = take((size_t)P.slots() * P.side * P.side * 4);
+        products = P.product_shares > 1 ? take((size_t)ffn::tiles(S.M, S.C, P.side) * P.product_shares * P.side * P.side * 4) : 0;
         cols1 = take((size_t)kColumnShares * 2 * S.hp * 4);
         cols2 = take((size_t)kColumnShares * S.Cp * 4);
         total = at;
@@ -517,6 +537,8 @@ int ffn_backward(const Sizes &S, const void *X, const void *W1, const float *b1,
         G.dP = odP;
         G.W1 = oW1;
         G.W1.K = 2 * S.hp;
+        G.product_shares = W.product_shares;
+        G.product_part = (float *)at(P.products);
         G.dX = dX; G.M = S.M; G.C = S.C; G.shares = kColumnShares;
         G.columns[0] = Columns{at(P.dP), 2L * S.hp, pP, (float *)at(P.cols1), 2 * S.hp, db1 ? (2 * S.hp + 63) / 64 : 0};
         G.columns[1] = Columns{(const bf16_t *)dY, S.Cp, pX, (float *)at(P.cols2), S.Cp, db2 ? (S.Cp + 63) / 64 : 0};
@@ -539,6 +561,8 @@ int ffn_backward(const Sizes &S, const void *X, const void *W1, const float *b1,
         A.cols_p[0] = S.hp; A.cols_p[1] = S.Cp;
         A.columns[0] = (const float *)at(P.cols1); A.columns[1] = (const float *)at(P.cols2);
         A.shares = kColumnShares;
+        A.product_part = G.product_part;
+        A.dX = dX; A.M = S.M; A.C = S.C; A.product_shares = W.product_shares; A.f32 = S.f32;
         return W.side == 256 ? launch_sums<T256>(A, grads_f32, st) : W.side == 128 ? launch_sums<T128>(A, grads_f32, st) : launch_sums<T64>(A, grads_f32, st);
     }
     ProfScope prof(st, K_FFN_SUMS);

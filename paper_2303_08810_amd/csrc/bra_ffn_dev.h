@@ -316,6 +316,35 @@ __device__ __forceinline__ void store_piece(bf16_t *p, bf16x8 v, int n, bool vec
         if (e < n) p[e] = (bf16_t)(u[e / 2] >> (16 * (e % 2)));
 }
 
+// A wavefront's sums to a slot of BM x BN floats, in the order of its registers.
+template <class T>
+constexpr int kSlot = T::BM * T::BN;
+template <class T>
+__device__ __forceinline__ void store_slot(float *slot, const f32x16 (&acc)[T::NT][T::MT], int wave, int lane)
+{
+    f32x4 *part = (f32x4 *)slot + wave * (T::NT * T::MT * 256) + lane;
+#pragma unroll
+    for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) part[((nt * T::MT + mt) * 4 + q) * 64] = f32x4{acc[nt][mt][4 * q], acc[nt][mt][4 * q + 1], acc[nt][mt][4 * q + 2], acc[nt][mt][4 * q + 3]};
+}
+// The sum over `count` slots, `apart` from each other, of the 8 columns that lane `lane` has of 32 x 32 tile `frag` (of the workgroup's: wave, nt, mt), run `run`.
+template <class T>
+__device__ __forceinline__ void sum_slots(const float *part, size_t first, size_t apart, int count, int frag, int run, int lane, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) {
+        const f32x4 *p = (const f32x4 *)(part + (first + k * apart) * kSlot<T>) + (frag * 4 + 2 * run) * 64 + lane;
+        const f32x4 a = p[0], b = p[64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] += a[e]; v[4 + e] += b[e]; }
+    }
+}
+
 // 8 consecutive values; `n` of them exist, `vec`: in whole 16-byte pieces.
 __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8], int n, bool vec)
 {
@@ -415,7 +444,22 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
     }
 }
 
-// Tile `block` of Out [M, N] = A B + bias, A's contraction inside, B's outside (BO) or inside.
+// The sums of tile `block` of A B [M, N] over chunks [first, last) of the contraction: A's inside, B's outside (BO) or inside.
+template <class T, bool BO, int TERMS>
+__device__ __forceinline__ void product_sums(const Operand &A, const Operand &Bm, long M, int N, int block, int first, int last, bf16_t *lds, f32x16 (&acc)[T::NT][T::MT])
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    int mt0, nt0;
+    tile_of(block, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
+    const long m0 = (long)mt0 * T::BM;
+    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), most = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
+    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, most); });
+    clear<T>(acc);
+    multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, first, last, lds, acc);
+}
+
+// Tile `block` of Out = A B + bias.
 template <class T, bool BO, int TERMS, typename E>
 __device__ __forceinline__ void product_tile(const Operand &A, const Operand &Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N, int block, bf16_t *lds)
 {
@@ -423,12 +467,9 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &Bm
     int mt0, nt0;
     tile_of(block, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
     const long m0 = (long)mt0 * T::BM;
-    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), last = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
-    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
-    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, last); });
+    const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0);
     f32x16 acc[T::NT][T::MT];
-    clear<T>(acc);
-    multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, 0, (A.K + 63) / 64, lds, acc);
+    product_sums<T, BO, TERMS>(A, Bm, M, N, block, 0, (A.K + 63) / 64, lds, acc);
     const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = n0 + (wave % T::WC) * (32 * T::NT);
     const bool vec = N % 8 == 0;
     const Rows<4 * T::NT> out{lds + wave * (32 * T::MT * 32 * T::NT)};

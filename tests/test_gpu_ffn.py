@@ -53,3 +53,26 @@ def test_large_tiles(M, C, h):
     check_forward(Y, X, W1, W2, b1, b2, "silu", pre)
     for given in (None, pre):
         check_backward(bra.bra_ffn_backward(X, W1, W2, dY, b1=b1, pre=given, bias_grads=True), X, W1, W2, dY, b1, "silu", given)
+
+
+# Few rows of wide channels: contractions that are shared out and joined, in the forward, in dX and in the weights' gradients.
+SHARED = [(33, 768, 2048), (40, 1001, 3900), (65, 1024, 2816), (129, 771, 2051), (257, 1024, 4096), (700, 331, 1401)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,C,h", SHARED)
+def test_shared_contractions(M, C, h, dtype):
+    act = ("silu", "gelu")[M % 2]
+    X, W1, W2, dY, b1, b2 = make(M, C, h, dtype, C % 2 == 1, seed=M + C + h)
+    print(f"ffn shared {M} x {C} x {h} {dtype} {act}", flush=True)
+    shape = bra.make_ffn_shape(M, C, h, dtype, act)
+    ws = torch.full((bra.ffn_workspace_bytes(shape),), 0xFF, dtype=torch.uint8, device="cuda")
+    Y, pre = bra.bra_ffn_forward(X, W1, W2, b1=b1, b2=b2, act=act, want_pre=True, ws=ws)
+    assert torch.equal(Y, bra.bra_ffn_forward(X, W1, W2, b1=b1, b2=b2, act=act))
+    check_forward(Y, X, W1, W2, b1, b2, act, pre)
+    for given in (None, pre):
+        ws = torch.full((bra.ffn_workspace_bytes(shape, backward=True),), 0xFF, dtype=torch.uint8, device="cuda")
+        grads = bra.bra_ffn_backward(X, W1, W2, dY, b1=b1, pre=given, act=act, bias_grads=True, ws=ws)
+        check_backward(grads, X, W1, W2, dY, b1, act, given)
+        again = bra.bra_ffn_backward(X, W1, W2, dY, b1=b1, pre=given, act=act, bias_grads=True)
+        assert all(torch.equal(a, b) for a, b in zip(grads, again))
