@@ -458,11 +458,11 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
         }
         if (!P.finish && I.Y && G.dgate) {
             F.dgate = G.dgate;
-            gate_blocks = (unsigned)(((long)S.groups * S.C + 3071) / 3072);
+            gate_blocks = (unsigned)(((long)S.groups * S.C + 3 * 1024 - 1) / (3 * 1024));
         }
     } else if (G.dgate) {
         F.dgate = G.dgate; F.groups = S.groups;
-        gate_blocks = (unsigned)(((long)S.groups * S.C + 3071) / 3072);
+        gate_blocks = (unsigned)(((long)S.groups * S.C + 3 * 1024 - 1) / (3 * 1024));
     }
     bool any = gate_blocks > 0;
     for (int s = 0; s < kSums; ++s) any = any || outs[s];
