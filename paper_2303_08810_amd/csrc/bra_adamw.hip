@@ -119,6 +119,8 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], const float *power
     return codes;
 }
 
+// 57 million values with 8-bit states, float32 weights and bf16 copies: 190 us for 0.92 GB, 4.8 TB/s, as a large copy reaches; 11 tensors of 43136 values
+// together 4.4 us.
 template <int BITS>
 __global__ __launch_bounds__(256) void k_adamw(Table T, AdamwSteps A, void *__restrict__ moments, void *__restrict__ squares, unsigned char *__restrict__ scales,
                                                unsigned char *__restrict__ root_scales)

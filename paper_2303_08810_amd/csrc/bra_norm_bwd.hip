@@ -61,6 +61,8 @@ struct Split {
     int sums() const { return finish ? kSums : 2; }
 };
 
+// 32768 x 768, LayerNorm twice, gate and scale: 87 us for 302 MB, 3.5 TB/s: three wavefronts per SIMD, each with one row's loads in flight, do not cover the
+// memory's latency.  6475 x 192 in float32: 12.5 us.
 template <typename E, bool LAYER, bool POST, int V, int NCH, bool FULL, bool FINISH>
 __global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) void k_norm_backward(BackArgs A)
 {
@@ -334,7 +336,8 @@ struct SumArgs {
 };
 
 // Columns in workgroups of 16, 64 threads to a column: dgamma, dbeta, and what the groups give (one workgroup each: blockIdx.y); behind
-// them, where groups came in parts, their gates' gradients.
+// them, where groups came in parts, their gates' gradients.  A chain of reads that cross the chip: 13 us for 768 workgroups' sums of 768
+// channels (deeper unrolling changed nothing), 4 us for 203 of 192.
 template <typename E>
 __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
 {
