@@ -219,7 +219,7 @@ int bra_backward(const bra_shape *shape, const void *X, const void *Wqkv, const 
  * (relative error of a product 2^-23); a value that is not finite, or above 3.3e38, makes NaN of what depends on it.
  * Alignment: a matrix whose row blocks (C elements; hidden elements for W1, dW1 and pre) are multiples of 8 elements must lie on 16
  * bytes, the others on their element's size; BRA_ERR_ALIGN otherwise.
- * Errors: NULL; SHAPE (M < 0, C or hidden < 1 or above 2^20, M above 2^30); DTYPE (dtype or act); WORKSPACE; ALIGN; LAUNCH. */
+ * Errors: NULL; SHAPE (M < 0, C or hidden < 1 or above 2^20, M above 2^30, in the backward pass 2^30 too); DTYPE (dtype or act); WORKSPACE; ALIGN; LAUNCH. */
 enum { BRA_SILU = 0, BRA_GELU = 1 };                /* bra_ffn_shape.act */
 typedef struct bra_ffn_shape {
     int64_t M;                /* tokens */
@@ -254,7 +254,7 @@ int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, 
  * R goes on as the residual stream, N into the next block.  X, Y, R, N [rows, C] and gate [groups, C] have shape->dtype, the vectors are
  * float32 [C].  Any of them may be absent (NULL): scale and gate (factors 1), beta and post_beta (0); Y (then R is X: pass R = NULL,
  * only N is written); gamma (then N is not formed: pass N = NULL).  Statistics and sums are float32, N is that of the float32 sum,
- * not of the rounded R.  R may be X or Y.  groups divides rows.  Rows of zeros give N = beta.
+ * not of the rounded R.  R may be X or Y.  groups divides rows.  Rows of zeros give N = beta where eps > 0.
  * Any C up to 8192; rows that are no multiple of 16 bytes are read by elements.  Alignment: elements.
  * Errors: NULL; SHAPE (rows < 0 or above 2^30, C < 1, groups < 1 or not a divisor of rows, eps < 0); DTYPE (dtype or kind);
  * UNSUPPORTED (C > 8192); ALIGN; LAUNCH. */

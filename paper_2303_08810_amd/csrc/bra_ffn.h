@@ -50,6 +50,9 @@ inline bool few_rows(const Sizes &S) { return !S.f32 && S.M <= 128; }
 // 32 x 1024 x 2816 62 / 57; 128 x 256 x 512 19 / 29, 48 x 512 x 1368 37 / 36).
 inline bool few_rows_f32(const Sizes &S) { return S.f32 && (S.M <= 32 || (S.M <= 128 && (double)S.M * S.C * S.h <= 32e6)); }
 
+// Workgroups of 256 in a launch: 2^32 threads and more cannot be launched.
+constexpr long kMaxBlocks = 1L << 23;
+
 // A matrix of `blocks` column blocks of `cols` columns laid out anew: each block padded with zeros to `cols_p` columns, float32 as three
 // planes of terms.
 struct Layout {

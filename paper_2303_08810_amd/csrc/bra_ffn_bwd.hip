@@ -372,8 +372,7 @@ __global__ __launch_bounds__(256) void k_sums(SumsArgs S)
 template <typename E>
 __global__ __launch_bounds__(256) void k_zero(E *p, long n)
 {
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) store_from_f32(p + i, 0.f);
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += 256L * gridDim.x) store_from_f32(p + i, 0.f);
 }
 
 template <class TD, class TG, int TERMS, int ACT, bool GIVEN, typename E>
@@ -573,7 +572,7 @@ int ffn_backward(const Sizes &S, const void *X, const void *W1, const float *b1,
     const struct { void *p; long n; } all[4] = {{dW1, (long)S.C * 2 * S.h}, {dW2, (long)S.h * S.C}, {db1, 2L * S.h}, {db2, S.C}};
     for (const auto &z : all) {
         if (!z.p) continue;
-        const unsigned blocks = (unsigned)((z.n + 255) / 256);
+        const unsigned blocks = (unsigned)std::min((z.n + 255) / 256, kMaxBlocks);
         if (grads_f32) k_zero<float><<<blocks, 256, 0, st>>>((float *)z.p, z.n);
         else k_zero<bf16_t><<<blocks, 256, 0, st>>>((bf16_t *)z.p, z.n);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;

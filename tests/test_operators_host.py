@@ -185,3 +185,10 @@ def test_adamw_state_layout():
         "exp_avg": (160, torch.float8_e4m3fn), "exp_avg_scale": (5, torch.float8_e8m0fnu), "exp_avg_root": (160, torch.float8_e4m3fn),
         "exp_avg_root_scale": (5, torch.float8_e8m0fnu)}
     assert not any(v.view(torch.uint8).any() for v in s.values())
+
+
+def test_ffn_most_tokens():
+    shape = bra.BraFfnShape(1 << 30, 8, 8, bra.BRA_BF16, 0)
+    assert ffn(shape, True) == -2                           # 2^32 threads cannot be launched
+    assert ffn(bra.BraFfnShape((1 << 30) - 1, 8, 8, bra.BRA_BF16, 0), True, ws=None) == -5
+    assert ffn(shape, False, ws=None) == -5
