@@ -55,7 +55,7 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, 
     clear<T>(acc);
     multiply<T, false, true, TERMS>(X, W1, X.p + m0 * X.ld, W1.p + j0, la, lb, 0, (X.K + 63) / 64, lds, acc);
     const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wj = j0 + (wave % T::WC) * PW;
-    const bool vec = h % 8 == 0;
+    const bool vec = h % 8 == 0, vec_b = vec && (uintptr_t)b1 % 16 == 0;
     constexpr int P = PW / 8;
     bf16_t *const own = lds + wave * (32 * T::MT * 2 * PW);      // this wavefront's part of what the chunks have left
     const Rows<P> first{own}, second{own + 32 * T::MT * PW};
@@ -66,8 +66,8 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, 
             const int piece = 4 * nt + 2 * run + hi, j = wj + 8 * piece, n = h - j;
             float bg[8], bu[8];
             if (b1 && n > 0) {
-                load8(b1 + j, bg, n, false);
-                load8(b1 + h + j, bu, n, false);
+                load8(b1 + j, bg, n, vec_b);
+                load8(b1 + h + j, bu, n, vec_b);
             } else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) bg[e] = bu[e] = 0.f;
@@ -391,10 +391,11 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, co
     const long m = (long)mt0 * T::BM + (wave / T::WC) * (32 * T::MT) + 32 * mt + lane % 32;
     const int col = nt0 * BJ + (wave % T::WC) * (32 * NT) + 32 * nt + 16 * run + 8 * (lane / 32), n = N - col;
     if (m >= M || col >= (GATED ? Np : N)) return;
+    const bool vec_b = N % 8 == 0 && (uintptr_t)bias % 16 == 0;
     float g[8], b[8];
     sum_slots<T>(part, tile, tiles, shares, (wave * T::NT + nt) * T::MT + mt, run, lane, g);
     if (bias) {
-        load8(bias + col, b, n, false);
+        load8(bias + col, b, n, vec_b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) g[e] += b[e];
     }
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, co
         float u[8];
         sum_slots<T>(part, tile, tiles, shares, (wave * T::NT + NT + nt) * T::MT + mt, run, lane, u);
         if (bias) {
-            load8(bias + N + col, b, n, false);
+            load8(bias + N + col, b, n, vec_b);
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] += b[e];
         }

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
         multiply<TG, false, true, TERMS>(X, W1, X.p + m0 * X.ld, W1.p + j0, la, lb, 0, (X.K + 63) / 64, lds, gu);
     }
     const int hi = lane / 32, c = lane % 32, wm = (wave / TD::WC) * (32 * TD::MT), wj = j0 + (wave % TD::WC) * PW;
-    const bool vec = h % 8 == 0;
+    const bool vec = h % 8 == 0, vec_b = vec && (uintptr_t)b1 % 16 == 0;
     constexpr int P = PW / 8;
     // 32 rows at a time through this wavefront's part of LDS: G and U in, dG and dU in their places, then A
     bf16_t *const own = lds + wave * (2 * 32 * PW);
@@ -91,8 +91,8 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
                     } else {
                         float bg[8], bu[8];
                         if (b1 && n > 0) {
-                            load8(b1 + j, bg, n, false);
-                            load8(b1 + h + j, bu, n, false);
+                            load8(b1 + j, bg, n, vec_b);
+                            load8(b1 + h + j, bu, n, vec_b);
                         } else
 #pragma unroll
                             for (int e = 0; e < 8; ++e) bg[e] = bu[e] = 0.f;

@@ -471,7 +471,7 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &Bm
     f32x16 acc[T::NT][T::MT];
     product_sums<T, BO, TERMS>(A, Bm, M, N, block, 0, (A.K + 63) / 64, lds, acc);
     const int hi = lane / 32, c = lane % 32, wm = (wave / T::WC) * (32 * T::MT), wn = n0 + (wave % T::WC) * (32 * T::NT);
-    const bool vec = N % 8 == 0;
+    const bool vec = N % 8 == 0, vec_b = (uintptr_t)bias % 16 == 0;
     const Rows<4 * T::NT> out{lds + wave * (32 * T::MT * 32 * T::NT)};
 #pragma unroll
     for (int nt = 0; nt < T::NT; ++nt)
@@ -479,7 +479,7 @@ __device__ __forceinline__ void product_tile(const Operand &A, const Operand &Bm
         for (int run = 0; run < 2; ++run) {
             const int piece = 4 * nt + 2 * run + hi, col = wn + 8 * piece, n = N - col;
             float b[8];
-            if (bias && n > 0) load8(bias + col, b, n, false);
+            if (bias && n > 0) load8(bias + col, b, n, vec_b);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) b[e] = 0.f;
