@@ -32,8 +32,8 @@ __global__ __launch_bounds__(256) void k_operands(Layouts J)
     }
 }
 
-// Bound by the matrix cores and, with G | U stored, by the epilogue that they wait for: 32768 x 1024 x 2816 430 to 444 us, 0.87 PFLOP/s, matrix
-// cores busy in 49 % of the cycles at a clock that their power brings down to 1.8 GHz.  12544 x 256 x 512, one round of 196 workgroups: 18 us.
+// Bound by the matrix cores and, with G | U stored, by the epilogue that they wait for: 32768 x 1024 x 2816 430 to 447 us, 0.87 PFLOP/s, matrix
+// cores busy in 49 % of the cycles at a clock that their power brings down to 1.8 GHz.  12544 x 256 x 512, one round of 196 workgroups: 17 us.
 template <class T, int TERMS, int ACT, typename E>
 __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, Operand W1, const float *__restrict__ b1, E *__restrict__ pre, bf16_t *__restrict__ Act,
                                                          long plane, long M, int h, int hp)
