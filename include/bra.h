@@ -219,6 +219,8 @@ int bra_backward(const bra_shape *shape, const void *X, const void *Wqkv, const 
  * (relative error of a product 2^-23); a value that is not finite, or above 3.3e38, makes NaN of what depends on it.
  * Alignment: a matrix whose row blocks (C elements; hidden elements for W1, dW1 and pre) are multiples of 8 elements must lie on 16
  * bytes, the others on their element's size; BRA_ERR_ALIGN otherwise.
+ * Workspace: that of the call's own shape; fewer tokens can need more (shares of long contractions), so ask for each M, or take the
+ * largest.  BRA_ERR_WORKSPACE otherwise.
  * Errors: NULL; SHAPE (M < 0, C or hidden < 1 or above 2^20, M above 2^30, in the backward pass 2^30 too); DTYPE (dtype or act); WORKSPACE; ALIGN; LAUNCH. */
 enum { BRA_SILU = 0, BRA_GELU = 1 };                /* bra_ffn_shape.act */
 typedef struct bra_ffn_shape {

@@ -273,6 +273,7 @@ def make_ffn_shape(M, C, hidden, dtype, act="silu") -> BraFfnShape:
 
 
 def ffn_workspace_bytes(shape: BraFfnShape, backward: bool = False) -> int:
+    """Workspace of a call of this shape.  Fewer tokens can need more: ask for each number of tokens, or take the largest."""
     out = ctypes.c_size_t(0)
     query = lib().bra_ffn_backward_workspace_bytes if backward else lib().bra_ffn_workspace_bytes
     _check(query(ctypes.byref(shape), ctypes.byref(out)))

@@ -192,3 +192,11 @@ def test_ffn_most_tokens():
     assert ffn(shape, True) == -2                           # 2^32 threads cannot be launched
     assert ffn(bra.BraFfnShape((1 << 30) - 1, 8, 8, bra.BRA_BF16, 0), True, ws=None) == -5
     assert ffn(shape, False, ws=None) == -5
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_ffn_workspace_is_that_of_the_shape(backward):
+    """A byte less than what a shape asks for is refused, whatever more tokens would ask for."""
+    for M in (1, 130, 442, 519, 2045, 2052):
+        n = bra.ffn_workspace_bytes(bra.make_ffn_shape(M, 768, 2048, torch.bfloat16), backward)
+        assert ffn(bra.BraFfnShape(M, 768, 2048, bra.BRA_BF16, 0), backward, ws_bytes=n - 1) == -5
