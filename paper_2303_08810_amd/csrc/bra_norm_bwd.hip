@@ -379,7 +379,7 @@ __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
         v = total(v);
         if (in && slot == 0) A.out[s][c] = v;
     }
-    if (y != 2 || A.parts == 1 || !(A.out[2] || A.out[3])) return;
+    if (y != 2 || A.parts == 1 || !(A.out[2] || A.out[3] || A.out[4])) return;
     float q = 0.f, s = 0.f;
     if (in)
 #pragma unroll 4
