@@ -216,7 +216,8 @@ int bra_backward(const bra_shape *shape, const void *X, const void *Wqkv, const 
  * backward pass can be given.  M = 0 is allowed and does nothing.
  * Any sizes; rows that are no multiple of 8 elements, and float32, take one more pass over the operands.  bf16: A is
  * rounded to bf16 between the products, the rest is float32.  float32: products of three bf16 terms per operand
- * (relative error of a product 2^-23); a value that is not finite, or above 3.3e38, makes NaN of what depends on it.
+ * (relative error of a product 2^-23), GELU within (2 g^2 + 36) 2^-24 of its value, SiLU within (2 |g| + 8) 2^-24; a value that is not
+ * finite, or above 3.3e38, makes NaN of what depends on it.
  * Alignment: a matrix whose row blocks (C elements; hidden elements for W1, dW1 and pre) are multiples of 8 elements must lie on 16
  * bytes, the others on their element's size; BRA_ERR_ALIGN otherwise.
  * Workspace: that of the call's own shape; fewer tokens can need more (shares of long contractions), so ask for each M, or take the

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, 
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) G[8 * run + e] = e < n ? activation<ACT>(g[e]) * u[e] : 0.f;      // A, in G's place
+                for (int e = 0; e < 8; ++e) G[8 * run + e] = e < n ? activation<ACT, TERMS != 1>(g[e]) * u[e] : 0.f;      // A, in G's place
             }
         }
     if constexpr (TERMS == 1)
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(Operand X, Operand W,
             put(pre + m * 2 * N + N + col, u);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) g[e] = e < n ? activation<GATED ? ACT : 0>(g[e]) * u[e] : 0.f;
+        for (int e = 0; e < 4; ++e) g[e] = e < n ? activation<GATED ? ACT : 0, false>(g[e]) * u[e] : 0.f;
         *(u32x2 *)(Out + m * Np + col) = pack4(g);
     } else put(Out + m * N + col, g);
 }
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(512, 2) void k_few_f32(const float *__restrict__ X,
             pre[row * 2 * N + c0 + col] = g;
             pre[row * 2 * N + N + c0 + col] = u;
         }
-        g = activation<GATED ? ACT : 0>(g) * u;
+        g = activation<GATED ? ACT : 0, true>(g) * u;
     }
     Out[row * N + c0 + col] = g;
 }
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, co
             store8(pre + (size_t)m * 2 * N + N + col, u, n, N % 8 == 0);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = e < n ? activation<GATED ? ACT : 0>(g[e]) * u[e] : 0.f;
+        for (int e = 0; e < 8; ++e) g[e] = e < n ? activation<GATED ? ACT : 0, TERMS != 1>(g[e]) * u[e] : 0.f;
         store_operand<TERMS>((bf16_t *)Out + (size_t)m * Np + col, plane, g);
     } else store8((E *)Out + (size_t)m * N + col, g, n, N % 8 == 0);
 }

@@ -410,13 +410,35 @@ __device__ __forceinline__ void store_operand(bf16_t *p, long plane, const float
 //   silu: F = 1 / (1 + e^-g), F' = F (1 - F);  gelu: F = Phi, F' = e^(-g^2 / 2) / sqrt(2 pi).
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)); }
 
-template <int ACT>
+// Phi for float32 results: Phi(-a) = e^(-a^2 / 2) t P(t), t = 1 / (1 + 0.35 a), a = |g|.  P, of degree 8, is the least maximum relative error of the
+// rest on a <= 14.5 (by linear programming), 1.2 units of 2^-24 with its coefficients rounded; with the arithmetic's the value is within 2 g^2 + 36 units.
+// 0.5 + 0.5 erf has lost the digits of Phi(g) below 0 (10 % of it at -5), the polynomial of gelu_f32 is within 7e-7 of 1, not of the value (2.6e-5 of it
+// close to 0, 0.3 % at -4), and the library's erfc has branches that keep the epilogues' loops from being unrolled.
+__device__ __forceinline__ float phi(float g)
+{
+    const float a = fabsf(g), t = __builtin_amdgcn_rcpf(fmaf(0.35f, a, 1.f));
+    float p = fmaf(-2.915759198e-02f, t, 1.440297663e-01f);
+    p = fmaf(p, t, -2.558371425e-01f);
+    p = fmaf(p, t, 1.593181789e-01f);
+    p = fmaf(p, t, -2.321167663e-02f);
+    p = fmaf(p, t, 1.055523455e-01f);
+    p = fmaf(p, t, 1.198213026e-01f);
+    p = fmaf(p, t, 1.398635209e-01f);
+    p = fmaf(p, t, 1.396213025e-01f);
+    const float q = p * t * __builtin_amdgcn_exp2f(-0.72134752044448170f * (a * a));
+    return g > 0.f ? 1.f - q : q;
+}
+// (-infinity gives 0)
+__device__ __forceinline__ float gelu_exact(float g, float f) { return fmaxf(g, -16.f) * f; }
+
+// EXACT: for float32 results.
+template <int ACT, bool EXACT>
 __device__ __forceinline__ float activation(float g)
 {
-    return ACT == BRA_SILU ? g * sigmoid(g) : gelu_f32(g);
+    return ACT == BRA_SILU ? g * sigmoid(g) : EXACT ? gelu_exact(g, phi(g)) : gelu_f32(g);
 }
 
-// EXACT: Phi by erf; else log2 Phi(-a) by the polynomial of gelu_f32, within 1.4e-5, a 280th of a bf16 step, for half the instructions (gradients of
+// EXACT as above; else log2 Phi(-a) by the polynomial of gelu_f32, within 1.4e-5, a 280th of a bf16 step, for half the instructions (gradients of
 // 12544 x 128 x 256 with GELU are bound by them).
 template <int ACT, bool EXACT>
 __device__ __forceinline__ void activation_slope(float g, float &a, float &slope)
@@ -427,7 +449,7 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
         slope = f + a * (1.f - f);
     } else {
         float f;
-        if (EXACT) f = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+        if (EXACT) f = phi(g);
         else {
             const float x = fminf(fabsf(g), 16.0f);
             float p = fmaf(-4.732939124e-04f, x, 7.084460463e-03f);
@@ -439,7 +461,7 @@ __device__ __forceinline__ void activation_slope(float g, float &a, float &slope
             f = g > 0.f ? 1.f - q : q;
             f = g != g ? g : f;
         }
-        a = g * f;
+        a = EXACT ? gelu_exact(g, f) : g * f;
         slope = f + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
     }
 }
