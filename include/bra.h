@@ -304,10 +304,10 @@ int bra_norm_backward(const bra_norm_shape *shape, const void *R, const void *Y_
  * The states of all tensors lie in flat buffers: tensor i takes ceil(n / 32) blocks of 32 values behind those of the tensors before it
  * (zeros to begin with; the rest of a last block stays zero).
  *   bits 32: exp_avg, exp_avg_sq float32.
- *   bits 8:  exp_avg and exp_avg_sq are bytes, OCP e4m3 codes, of m and of sqrt(v); a block's values are code * 2^(scale - 127) with the byte
- *            `scale` of exp_avg_scale, exp_avg_sq_scale [blocks]: the smallest with which the block's largest value is at most 448 (at
- *            least 2^-126).  A root that is not 0 is kept as the smallest code at least.  The power is powf's on the GPU, within a
- *            unit of float32, as torch.ldexp has it there.
+ *   bits 8:  exp_avg and exp_avg_sq are bytes, OCP e4m3 codes, of m and of sqrt(v); a block's values are code * 2^(scale - 127), exact, with the
+ *            byte `scale` of exp_avg_scale, exp_avg_sq_scale [blocks]: the smallest with which the block's largest value is at most 448
+ *            (at least 2^-126).  A root that is not 0 is kept as the smallest code at least.  Codes are nearest; a value half way
+ *            between two goes to one of them (by the power as powf has it on the GPU, within a unit of float32).
  * t: `step` (from 1 on), or, where step_device is not NULL, the int32 there when the kernel runs (so that a captured graph can be replayed
  * with a step that counts on); `scalars` is then device scratch for 2 floats.  grad_scale: NULL or one float32 on the device, for a
  * loss scale or clipping.  No workspace otherwise; 72 tensors go into a launch.

@@ -77,13 +77,17 @@ __device__ __forceinline__ void put8(void *base, long at, bool bf16, bool vec, i
     }
 }
 
-// Powers of two from 2^-127 on as torch.ldexp forms them on this GPU, by powf: for some exponents a unit of float32 off.  A state that a program
-// decodes there, to keep it or to look at it, then holds the very values that the step takes; with the exponent's bits put in place 5 codes in
-// 10000 fell on the other side of a tie.  A workgroup forms them once, a thread one of them, while its loads are on their way.
+// What a state holds is code * 2^(scale - 127), exact, as the scale's own conversion to float32 has it: here, on the CPU, and with any math library.
+__device__ __forceinline__ float power_of_two(unsigned scale) { return __builtin_bit_cast(float, scale ? scale << 23 : 0x400000u); }
+
+// Codes are formed with powers of two as torch.ldexp has them on this GPU, by powf, which is a unit of float32 low for 41 of 254 exponents (2^16 to 2^20 among
+// them): a value half way between two codes goes to the lower one there, not to the even one, 5 codes in 10000.  A state that a program forms
+// with torch.ldexp then has the step's codes.  A workgroup forms the powers once, a thread one of them, while its loads are on their way.
 constexpr int kPowers = 256;
 
-__device__ __forceinline__ void decode8(u32x2 codes, float by, float (&v)[8])
+__device__ __forceinline__ void decode8(u32x2 codes, unsigned scale, float (&v)[8])
 {
+    const float by = power_of_two(scale);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], true);
@@ -161,8 +165,8 @@ __global__ __launch_bounds__(256) void k_adamw(Table T, AdamwSteps A, void *__re
     }
     if (!live) return;
     if (BITS == 8) {
-        decode8(mc, powers[ms], m);
-        decode8(vc, powers[vs], v);
+        decode8(mc, ms, m);
+        decode8(vc, vs, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = v[e] * v[e];
     }
