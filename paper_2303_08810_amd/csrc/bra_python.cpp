@@ -510,7 +510,7 @@ NormCall norm_call(const at::Tensor &X, const at::Tensor *Y, const at::Tensor *g
         if (!(gate->is_cuda() && gate->is_contiguous() && gate->device() == X.device() && gate->scalar_type() == X.scalar_type() && gate->dim() >= 1 && gate->size(-1) == C))
             value_error("gate must be a contiguous [.., C] tensor of the map's dtype on its GPU");
         int64_t lead = gate->dim() - 1;
-        while (lead > 0 && gate->size(lead - 1) == 1 && (lead > X.dim() - 1 || X.size(lead - 1) != 1)) --lead;
+        while (lead > 0 && gate->size(lead - 1) == 1) --lead;       // (of the map's size or standing for it: the groups are the same)
         if (lead > X.dim() - 1) value_error("gate has more dimensions than the map");
         for (int64_t d = 0; d < lead; ++d) {
             if (gate->size(d) != X.size(d)) value_error("gate's leading dimensions must be the map's first ones");
