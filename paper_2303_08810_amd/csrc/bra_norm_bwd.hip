@@ -122,7 +122,9 @@ __global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) v
             if (A.dR) rd[k] = load<FULL, E, V>((const E *)A.dR + at + V * k * tpr, n[k], vec);
         }
     };
-    // row r, which has been fetched; then row `next` (-1: none).  Teams without a row (`mine` unset) go along with another's and add nothing
+    // row r, which has been fetched; then row `next` (-1: none).  Teams without a row (`mine` unset) go along with another's and add nothing: both factors
+    // are 0, for where dX or dY lies in R's, dN's or Y's place that row may have been overwritten by its own team, and 0 times what is there now
+    // may be NaN
     auto row = [&](long r, long next, long group, bool mine) {
         // the vectors stay in LDS: kept in registers over the rows, they cost a wavefront per SIMD
         asm volatile("" : "+v"(own));
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) v
                 for (int e = 0; e < V; ++e) {
                     x[k][e] *= inv;
                     const float w = mine ? dn[k][e] : 0.f;
-                    sums[0][k][e] = fmaf(w, x[k][e], sums[0][k][e]);
+                    sums[0][k][e] = fmaf(w, mine ? x[k][e] : 0.f, sums[0][k][e]);
                     sums[1][k][e] += w;
                     dn[k][e] *= gamma[e];
                     p[0] += dn[k][e];
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(kMaxTeam, waves(V * NCH, sizeof(E) == 4, FINISH)) v
             for (int e = 0; e < V; ++e) {
                 if (POST) y[k][e] *= yinv;
                 const float w = mine ? d[k][e] : 0.f;
-                Q[k][e] = fmaf(w, y[k][e], Q[k][e]);
+                Q[k][e] = fmaf(w, mine ? y[k][e] : 0.f, Q[k][e]);
                 if (POST) S[k][e] += w;
                 d[k][e] *= A.I.gate ? scale[e] * value(gate[k], e) : scale[e];
                 if (POST) {
