@@ -352,7 +352,7 @@ int bra_ffn_backward(const bra_ffn_shape *shape, const void *X, const void *W1, 
     ffn::Sizes S;
     const int rc = make_ffn_sizes(shape, S);
     if (rc != BRA_OK) return rc;
-    if (S.M == 1L << 30) return BRA_ERR_SHAPE;          // k_hidden: 2^32 threads
+    if (S.M == 1L << 30) return BRA_ERR_SHAPE;          // (as the header has it)
     if (grad_dtype != BRA_F32 && grad_dtype != BRA_BF16) return BRA_ERR_DTYPE;
     if (!dW1 || !dW2 || (S.M > 0 && (!X || !W1 || !W2 || !dY || !dX))) return BRA_ERR_NULL;
     const size_t e = S.f32 ? 4 : 2, ge = grad_dtype == BRA_F32 ? 4 : 2;

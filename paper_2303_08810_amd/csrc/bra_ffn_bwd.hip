@@ -20,14 +20,15 @@ namespace {
 // of the cycles.  Forming G | U again 12544 x 128 x 256 takes 17 us: one round of 196 workgroups, half of it the slope's arithmetic.
 template <class TD, class TG, int TERMS, int ACT, bool GIVEN, typename E>
 __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand dY, Operand W2, Operand X, Operand W1, const float *__restrict__ b1, const E *__restrict__ pre,
-                                                           bf16_t *__restrict__ Act, long plane_a, bf16_t *__restrict__ dP, long plane_p, long M, int h, int hp)
+                                                           bf16_t *__restrict__ Act, long plane_a, bf16_t *__restrict__ dP, long plane_p, long M, int h, int hp,
+                                                           int first_tile)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *lds = (bf16_t *)smem;
     constexpr int BJ = TD::BN, PW = 32 * TD::NT;         // hidden units of a tile, of a wavefront
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     int mt0, nt0;
-    tile_of(blockIdx.x, (int)((M + TD::BM - 1) / TD::BM), (hp + BJ - 1) / BJ, mt0, nt0);
+    tile_of(first_tile + blockIdx.x, (int)((M + TD::BM - 1) / TD::BM), (hp + BJ - 1) / BJ, mt0, nt0);
     const long m0 = (long)mt0 * TD::BM;
     const int j0 = nt0 * BJ, last = hp - 8 - j0, rows = (int)min((long)TD::BM, M - m0);
     f32x16 acc[TD::NT][TD::MT];
@@ -382,8 +383,14 @@ int launch_hidden(const Operand &dY, const Operand &W2, const Operand &X, const 
     constexpr size_t bytes = GIVEN || TD::kLds > TG::kLds ? TD::kLds : TG::kLds;
     if (allow_lds<k_hidden<TD, TG, TERMS, ACT, GIVEN, E>>(bytes) != BRA_OK) return BRA_ERR_LAUNCH;
     const long tiles = ((S.M + TD::BM - 1) / TD::BM) * ((S.hp + TD::BN - 1) / TD::BN);
-    k_hidden<TD, TG, TERMS, ACT, GIVEN, E><<<(unsigned)tiles, TD::kThreads, bytes, st>>>(dY, W2, X, W1, b1, (const E *)pre, Act, plane_a, dP, plane_p, S.M, S.h, S.hp);
-    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+    // (one launch but for close to 2^30 tokens, whose tiles make 2^32 threads)
+    constexpr long kMost = kMaxBlocks * 256 / TD::kThreads;
+    for (long first = 0; first < tiles; first += kMost) {
+        k_hidden<TD, TG, TERMS, ACT, GIVEN, E>
+            <<<(unsigned)std::min(tiles - first, kMost), TD::kThreads, bytes, st>>>(dY, W2, X, W1, b1, (const E *)pre, Act, plane_a, dP, plane_p, S.M, S.h, S.hp, (int)first);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
 }
 
 template <int TERMS, int ACT, typename E>
