@@ -283,7 +283,8 @@ int bra_norm_forward(const bra_norm_shape *shape, const void *X, const void *Y_o
 /* Gradients of it.  R: the sum that the forward returned (X where there was no Y), Y_opt: its Y; dN_opt, dR_opt: what came
  * back to N and to R (at least one of them).  dX [rows, C] is the gradient of X, and with it that of R.
  * Where Y_opt is given dY [rows, C] is required; dscale [C], dgate [groups, C] (in shape->dtype) and, with the post norm, dpost_gamma and
- * dpost_beta [C] may be NULL, as may dgamma and dbeta [C].  What is asked for is OVERWRITTEN, the vectors in float32, summed over all rows;
+ * dpost_beta [C] may be NULL, as may dgamma and dbeta [C].  What is asked for is OVERWRITTEN, the vectors in float32, summed over all rows (dscale and
+ * dgate of factors that are absent are those of ones);
  * dgamma and dbeta are left as they were where dN_opt is NULL.  dX may be dR, dN or R; dY may be Y.  No atomic adds: a repeat gives
  * the same bits.  Errors as above, and WORKSPACE. */
 typedef struct bra_norm_grads {         /* a HOST struct of DEVICE pointers */

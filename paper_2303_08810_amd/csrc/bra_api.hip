@@ -405,7 +405,7 @@ int bra_norm_backward(const bra_norm_shape *shape, const void *R, const void *Y,
     const size_t need = norm_backward_workspace_bytes(S);
     if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
     const NormIn I{R, Y, Y ? p->gate : nullptr, p->gamma, p->beta, p->post_gamma, p->post_beta, p->scale};
-    const NormGrads G{g->dX, g->dY, p->gate && (Y || S.rows == 0) ? g->dgate : nullptr, g->dgamma, g->dbeta, g->dpost_gamma, g->dpost_beta, g->dscale};
+    const NormGrads G{g->dX, g->dY, Y || S.rows == 0 ? g->dgate : nullptr, g->dgamma, g->dbeta, g->dpost_gamma, g->dpost_beta, g->dscale};
     return norm_backward(S, I, dN, dR, G, ws, (hipStream_t)hip_stream);
 }
 
