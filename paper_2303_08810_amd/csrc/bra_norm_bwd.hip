@@ -346,18 +346,21 @@ __global__ __launch_bounds__(1024) void k_norm_sums(SumArgs A)
     __shared__ float meet[64][17];
     const int y = blockIdx.y;
     if ((int)blockIdx.x >= A.column_blocks) {
-        const long i = ((long)(blockIdx.x - A.column_blocks) * gridDim.y + y) * 1024 + threadIdx.x;
-        if (i >= A.groups * A.C) return;
-        const long g = i / A.C;
-        const int c = (int)(i % A.C);
-        float q = 0.f, s = 0.f;
+        const long count = A.groups * A.C, step = (long)(gridDim.x - A.column_blocks) * gridDim.y * 1024;
+        for (long i = ((long)(blockIdx.x - A.column_blocks) * gridDim.y + y) * 1024 + threadIdx.x; i < count; i += step) {
+            const long g = i / A.C;
+            const int c = (int)(i % A.C);
+            float q = 0.f, s = 0.f;
 #pragma unroll 4
-        for (int p = 0; p < (A.blocks ? A.parts : 0); ++p) {
-            const float *u = A.units + (size_t)(g * A.parts + p) * 2 * A.C + c;
-            q += u[0];
-            if (A.post) s += u[A.C];
+            for (int p = 0; p < (A.blocks ? A.parts : 0); ++p) {
+                const float *u = A.units + (size_t)(g * A.parts + p) * 2 * A.C + c;
+                q += u[0];
+                if (A.post) s += u[A.C];
+            }
+            // (0 without rows, whatever scale is)
+            const float t = A.post ? fmaf(A.post_gamma[c], q, (A.post_beta ? A.post_beta[c] : 0.f) * s) : q;
+            store_from_f32((E *)A.dgate + i, A.blocks ? (A.scale ? A.scale[c] : 1.f) * t : 0.f);
         }
-        store_from_f32((E *)A.dgate + i, (A.scale ? A.scale[c] : 1.f) * (A.post ? fmaf(A.post_gamma[c], q, (A.post_beta ? A.post_beta[c] : 0.f) * s) : q));
         return;
     }
     const int x = threadIdx.x % 16, slot = threadIdx.x / 16, c = blockIdx.x * 16 + x;
@@ -441,6 +444,8 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
     F.gate = I.gate; F.scale = I.scale; F.post_gamma = I.post_gamma; F.post_beta = I.post_beta;
     for (int s = 0; s < kSums; ++s) F.out[s] = outs[s];
     F.C = S.C; F.sums = kSums; F.parts = 1; F.column_blocks = (S.C + 15) / 16; F.post = S.post && !none;
+    // (more than these only where there are no rows: 2^32 threads cannot be launched)
+    auto gates = [&] { return (unsigned)std::min(((long)S.groups * S.C + 3 * 1024 - 1) / (3 * 1024), 1L << 16); };
     unsigned gate_blocks = 0;
     if (S.rows > 0) {
         const Split P(S);
@@ -463,11 +468,11 @@ int norm_backward(const NormSizes &S, const NormIn &I, const void *dN, const voi
         }
         if (!P.finish && I.Y && G.dgate) {
             F.dgate = G.dgate;
-            gate_blocks = (unsigned)(((long)S.groups * S.C + 3 * 1024 - 1) / (3 * 1024));
+            gate_blocks = gates();
         }
     } else if (G.dgate) {
         F.dgate = G.dgate; F.groups = S.groups;
-        gate_blocks = (unsigned)(((long)S.groups * S.C + 3 * 1024 - 1) / (3 * 1024));
+        gate_blocks = gates();
     }
     bool any = gate_blocks > 0;
     for (int s = 0; s < kSums; ++s) any = any || outs[s];
