@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void k_adamw(Table T, AdamwSteps A, void *__re
     if (A.grad_scale) {
         const float s = *A.grad_scale;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = g[e] * s;
+        for (int e = 0; e < 8; ++e) g[e] = e < n ? g[e] * s : 0.f;       // (what lies behind a tensor's end stays 0 whatever s is)
     }
     float root[8];
 #pragma unroll
