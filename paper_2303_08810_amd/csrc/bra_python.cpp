@@ -53,15 +53,17 @@ const at::Tensor &need(PyObject *o)
 }
 
 // ints and what converts to one without loss (numpy integers, anything with __index__); no floats, no strings
-int integer(PyObject *o)
+long long_integer(PyObject *o)
 {
     PyObject *i = PyNumber_Index(o);
     if (!i) throw Raised{};
     const long v = PyLong_AsLong(i);
     Py_DECREF(i);
     if (v == -1 && PyErr_Occurred()) throw Raised{};
-    return (int)v;
+    return v;
 }
+
+int integer(PyObject *o) { return (int)long_integer(o); }
 
 // what float() takes
 double real(PyObject *o)
@@ -692,7 +694,7 @@ PyObject *py_adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n)
             args.step_device = (const int32_t *)t.data_ptr();
             scalars = at::empty({2}, first.options().dtype(at::kFloat));
             args.scalars = (float *)scalars.data_ptr();
-        } else args.step = integer(a[3]);
+        } else args.step = long_integer(a[3]);
         void *st = stream_of(first);
         run([&] { return bra_adamw_step(list.data(), (int32_t)params.n, &args, st); });
         Py_RETURN_NONE;
