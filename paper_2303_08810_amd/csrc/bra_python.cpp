@@ -576,12 +576,9 @@ PyObject *py_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (rc) throw Raised{};
             return t.data_ptr();
         };
-        // the vectors in one allocation
-        const int vectors = (dN ? 2 : 0) + (Y && scale ? 1 : 0) + (Y && post_gamma ? 2 : 0);
-        at::Tensor all;
-        if (vectors) all = at::empty({vectors, (int64_t)c.s.C}, R.options().dtype(at::kFloat));
-        int used = 0;
-        auto vector = [&](const char *name) { return (float *)keep(name, all.select(0, used++)); };
+        // each vector has memory and a version of its own
+        const auto options = R.options().dtype(at::kFloat);
+        auto vector = [&](const char *name) { return (float *)keep(name, at::empty({(int64_t)c.s.C}, options)); };
         bra_norm_grads g{};
         g.dX = keep("dX", at::empty_like(R));
         if (dN) { g.dgamma = vector("dgamma"); g.dbeta = vector("dbeta"); }
