@@ -22,9 +22,6 @@ struct Operand {
     int K;              // beyond it reads as zero
 };
 
-// Out [M, N] = A B + bias: A's contraction inside, B's outside (`outer`) or inside.  Out in bf16, or float32 where the operands have three terms.
-int product(const Operand &A, const Operand &Bm, bool outer, long M, int N, void *Out, const float *bias, bool f32, int kernel_id, hipStream_t st);
-
 // Sides of the tiles (256, 128 or 64), by the number of tiles there would be: large ones multiply faster (one workgroup per compute unit,
 // 1.2 PFLOP/s in long loops, against 0.9 and 0.5), small ones fill the chip.  Measured (us with 256 / 128 / 64):
 //   k_gated    4096 x 512 x 1368 (176 large tiles) 22.8 / 25.0 / 27.7, 12544 x 128 x 256 (98; 392 of 128) 12.9 / 9.8 / 11.9,

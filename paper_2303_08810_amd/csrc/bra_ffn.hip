@@ -46,8 +46,8 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, 
     tile_of(blockIdx.x, (int)((M + T::BM - 1) / T::BM), (hp + BJ - 1) / BJ, mt0, nt0);
     const long m0 = (long)mt0 * T::BM;
     const int j0 = nt0 * BJ, last = hp - 8 - j0, rows = (int)min((long)T::BM, M - m0);
-    const Loads<T, T::BM, false, false> la(wave, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
-    const Loads<T, T::BN, true, true> lb(wave, lane, W1.ld, [&](int col) {
+    const Loads<T, T::BM, false> la(wave, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, true> lb(wave, lane, W1.ld, [&](int col) {
         const int w = col / (2 * PW), in = col % (2 * PW);
         return (long)(min(w * PW + in % PW, last) + (in >= PW ? hp : 0));
     });
@@ -121,11 +121,11 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gated(Operand X, 
 }
 
 // 32768 x 2816 x 1024: 195 us, 0.97 PFLOP/s, matrix cores busy in 52 % of the cycles (the library's product of these sizes 145).
-template <class T, bool BO, int TERMS, typename E>
+template <class T, int TERMS, typename E>
 __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_product(Operand A, Operand Bm, const float *__restrict__ bias, E *__restrict__ Out, long M, int N)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    product_tile<T, BO, TERMS, E>(A, Bm, bias, Out, M, N, blockIdx.x, (bf16_t *)smem);
+    product_tile<T, true, TERMS, E>(A, Bm, bias, Out, M, N, blockIdx.x, (bf16_t *)smem);
 }
 
 // Few rows: 32 x 32 outputs per workgroup, the contraction's chunks shared out to its kFewWaves wavefronts, each with a ring of its own and no
@@ -139,13 +139,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_few(Operand X, Operand W,
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr bool GATED = ACT >= 0;
-    constexpr int LA = ROWS / 8, LB = Loads<TFew, 32, true, true>::L, kLoads = LA + LB, kChunk = TFew::kChunkA + TFew::kChunkB;
+    constexpr int LA = ROWS / 8, LB = Loads<TFew, 32, true>::L, kLoads = LA + LB, kChunk = TFew::kChunkA + TFew::kChunkB;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     // an XCD has neighbouring columns: they lie in the same lines
     const int xcd = blockIdx.x % 8, per = gridDim.x / 8, rest = gridDim.x % 8, tile = xcd * per + min(xcd, rest) + blockIdx.x / 8;
     const int c0 = tile * (GATED ? 16 : 32), m0 = blockIdx.y * 32, rows = min(M - m0, 32), last = Np - 8 - c0;
-    const Loads<TFew, 32, false, false> la(0, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
-    const Loads<TFew, 32, true, true> lb(0, lane, W.ld, [&](int col) { return (long)(GATED ? min(col % 16, last) + (col >= 16 ? Np : 0) : min(col, last)); });
+    const Loads<TFew, 32, false> la(0, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<TFew, 32, true> lb(0, lane, W.ld, [&](int col) { return (long)(GATED ? min(col % 16, last) + (col >= 16 ? Np : 0) : min(col, last)); });
     bf16_t *const ring = (bf16_t *)smem + wave * (kFewRing * kChunk);
     const unsigned at = lds_address(ring);
     const bf16_t *const a0 = X.p + m0 * X.ld, *const b0 = W.p + c0;
@@ -366,8 +366,8 @@ __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_split(Operand A, 
         tile_of(i, (int)((M + T::BM - 1) / T::BM), (N + BJ - 1) / BJ, mt0, nt0);
         const long m0 = (long)mt0 * T::BM;
         const int j0 = nt0 * BJ, rows = (int)min((long)T::BM, M - m0), most = N - 8 - j0;
-        const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
-        const Loads<T, T::BN, true, true> lb(wave, lane, Bm.ld, [&](int col) {
+        const Loads<T, T::BM, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+        const Loads<T, T::BN, true> lb(wave, lane, Bm.ld, [&](int col) {
             const int w = col / (2 * PW), in = col % (2 * PW);
             return (long)(min(w * PW + in % PW, most) + (in >= PW ? N : 0));
         });
@@ -430,22 +430,23 @@ int split(const Operand &A, const Operand &Bm, const float *bias, void *pre, voi
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
-template <class T, bool BO, int TERMS, typename E>
+template <class T, int TERMS, typename E>
 int launch_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
-    if (allow_lds<k_product<T, BO, TERMS, E>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
+    if (allow_lds<k_product<T, TERMS, E>>(T::kLds) != BRA_OK) return BRA_ERR_LAUNCH;
     const long tiles = ((M + T::BM - 1) / T::BM) * ((N + T::BN - 1) / T::BN);
-    k_product<T, BO, TERMS, E><<<(unsigned)tiles, T::kThreads, T::kLds, st>>>(A, Bm, bias, (E *)Out, M, N);
+    k_product<T, TERMS, E><<<(unsigned)tiles, T::kThreads, T::kLds, st>>>(A, Bm, bias, (E *)Out, M, N);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
-template <bool BO, int TERMS, typename E>
-int pick_product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
+// Out [M, N] = A B + bias: A's contraction inside, B's outside.
+template <int TERMS, typename E>
+int product(const Operand &A, const Operand &Bm, long M, int N, void *Out, const float *bias, hipStream_t st)
 {
     switch (product_side(M, N)) {
-    case 256: return launch_product<Tile<256, 256, 4, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
-    case 128: return launch_product<Tile<128, 128, 2, 2, 2>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
-    default: return launch_product<Tile<64, 64, 2, 2, 4>, BO, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 256: return launch_product<Tile<256, 256, 4, 2, 2>, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    case 128: return launch_product<Tile<128, 128, 2, 2, 2>, TERMS, E>(A, Bm, M, N, Out, bias, st);
+    default: return launch_product<Tile<64, 64, 2, 2, 4>, TERMS, E>(A, Bm, M, N, Out, bias, st);
     }
 }
 
@@ -469,13 +470,6 @@ int pick_gated(const Operand &X, const Operand &W1, const float *b1, void *pre, 
 }
 
 }  // namespace
-
-int product(const Operand &A, const Operand &Bm, bool outer, long M, int N, void *Out, const float *bias, bool f32, int kernel_id, hipStream_t st)
-{
-    ProfScope prof(st, kernel_id);
-    if (f32) return outer ? pick_product<true, 3, float>(A, Bm, M, N, Out, bias, st) : pick_product<false, 3, float>(A, Bm, M, N, Out, bias, st);
-    return outer ? pick_product<true, 1, bf16_t>(A, Bm, M, N, Out, bias, st) : pick_product<false, 1, bf16_t>(A, Bm, M, N, Out, bias, st);
-}
 
 int lay_out(const Layouts &J, bool f32, hipStream_t st)
 {
@@ -582,13 +576,13 @@ int ffn_forward(const Sizes &S, const void *X, const void *W1, const float *b1, 
                                     : gated<1, BRA_GELU, bf16_t>(oX, oW1, b1, pre, at(P.Act), pA, S, P, at(P.parts), st);
     }
     if (rc != BRA_OK) return rc;
+    ProfScope prof(st, K_FFN_PRODUCT);
     if (P.product_shares > 1) {
-        ProfScope prof(st, K_FFN_PRODUCT);
         float *part = (float *)at(P.parts);
         return S.f32 ? split<TSplit, -1, 3, float>(oA, oW2, b2, nullptr, Y, 0, S.M, S.C, S.Cp, P.product_shares, part, st)
                      : split<TSplit, -1, 1, bf16_t>(oA, oW2, b2, nullptr, Y, 0, S.M, S.C, S.Cp, P.product_shares, part, st);
     }
-    return product(oA, oW2, true, S.M, S.C, Y, b2, S.f32, K_FFN_PRODUCT, st);
+    return S.f32 ? product<3, float>(oA, oW2, S.M, S.C, Y, b2, st) : product<1, bf16_t>(oA, oW2, S.M, S.C, Y, b2, st);
 }
 
 }  // namespace bra

@@ -34,15 +34,15 @@ __global__ __launch_bounds__(TD::kThreads, TD::kMinWaves) void k_hidden(Operand 
     f32x16 acc[TD::NT][TD::MT];
     clear<TD>(acc);
     {
-        const Loads<TD, TD::BM, false, false> la(wave, lane, dY.ld, [&](int row) { return (long)min(row, rows - 1); });
-        const Loads<TD, TD::BN, false, true> lb(wave, lane, W2.ld, [&](int i) { return (long)min(i, h - 1 - j0); });
+        const Loads<TD, TD::BM, false> la(wave, lane, dY.ld, [&](int row) { return (long)min(row, rows - 1); });
+        const Loads<TD, TD::BN, false> lb(wave, lane, W2.ld, [&](int i) { return (long)min(i, h - 1 - j0); });
         multiply<TD, false, false, TERMS>(dY, W2, dY.p + m0 * dY.ld, W2.p + j0 * W2.ld, la, lb, 0, (dY.K + 63) / 64, lds, acc);
     }
     f32x16 gu[GIVEN ? 1 : TG::NT][TG::MT];
     if constexpr (!GIVEN) {
         clear<TG>(gu);
-        const Loads<TG, TG::BM, false, false> la(wave, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
-        const Loads<TG, TG::BN, true, true> lb(wave, lane, W1.ld, [&](int col) {
+        const Loads<TG, TG::BM, false> la(wave, lane, X.ld, [&](int row) { return (long)min(row, rows - 1); });
+        const Loads<TG, TG::BN, true> lb(wave, lane, W1.ld, [&](int col) {
             const int w = col / (2 * PW), in = col % (2 * PW);
             return (long)(min(w * PW + in % PW, last) + (in >= PW ? hp : 0));
         });
@@ -203,8 +203,8 @@ __device__ __forceinline__ void weights_part(const Weights &W, int workgroup, bf
         weight_tile<T>(W, tile, job, r0, c0);
         const Operand A = W.job[job].A, B = W.job[job].B;
         const int rows = W.job[job].rows, cols = W.job[job].cols;
-        const Loads<T, T::BM, true, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 8 - r0); });
-        const Loads<T, T::BN, true, true> lb(wave, lane, B.ld, [&](int col) { return (long)min(col, cols - 8 - c0); });
+        const Loads<T, T::BM, true> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 8 - r0); });
+        const Loads<T, T::BN, true> lb(wave, lane, B.ld, [&](int col) { return (long)min(col, cols - 8 - c0); });
         f32x16 acc[T::NT][T::MT];
         clear<T>(acc);
         multiply<T, true, true, TERMS>(A, B, A.p + r0, B.p + c0, la, lb, first, last, lds, acc);

@@ -35,11 +35,10 @@ struct Tile {
 // read touches lie in different quarters of the banks), else differently for the 8 rows that 8 lanes next to each other read.
 template <int B>
 __device__ __forceinline__ int turn_outer(int k) { return B >= 128 ? 4 * (k % 4) : B == 64 ? 4 * (k / 2 % 2) : 0; }
-template <bool PERMUTED>
 __device__ __forceinline__ int turn_inner(int row) { return row / 2 % 8; }
 
 // A wavefront's direct loads of one operand's chunks: B rows (or columns) of the tile, OUTER: contraction outside.
-template <class T, int B, bool OUTER, bool PERMUTED>
+template <class T, int B, bool OUTER>
 struct Loads {
     static constexpr int L = B / 8 / T::kWaves, CH = B / 8, RPI = 64 / CH;
     static_assert(L * 8 * T::kWaves == B, "a chunk is a whole number of loads per wavefront");
@@ -55,7 +54,7 @@ struct Loads {
                 off[u] = 2u * (unsigned)(k * ld + at(8 * ((lane % CH) ^ turn_outer<B>(k))));
             } else {
                 const int row = 8 * (wave * L + u) + lane / 8;
-                off[u] = 2u * (unsigned)(at(row) * ld + 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row)));
+                off[u] = 2u * (unsigned)(at(row) * ld + 8 * ((lane % 8) ^ turn_inner(row)));
             }
         }
     }
@@ -68,7 +67,7 @@ struct Loads {
             return;
         }
         const int row = 8 * (wave * L + u) + lane / 8;
-        const int k = OUTER ? RPI * (wave * L + u) + lane / CH : 8 * ((lane % 8) ^ turn_inner<PERMUTED>(row));
+        const int k = OUTER ? RPI * (wave * L + u) + lane / CH : 8 * ((lane % 8) ^ turn_inner(row));
         const bf16_t *p = (const bf16_t *)((const char *)origin + off[u]);
         load_to_lds_untracked(k < left ? p : zeros, at);
     }
@@ -81,7 +80,7 @@ __device__ __forceinline__ bf16x8 fragment(const bf16_t *S, int first, int ks, i
     const int h = lane / 32, c = lane % 32;
     if (!OUTER) {
         const int row = first + (PERMUTED ? (c & 0x13) + ((c & 4) << 1) + ((c & 8) >> 1) : c);
-        return *(const bf16x8 *)(S + row * 64 + 8 * ((2 * ks + h) ^ turn_inner<PERMUTED>(row)));
+        return *(const bf16x8 *)(S + row * 64 + 8 * ((2 * ks + h) ^ turn_inner(row)));
     }
     // lane s of a 16-lane group q gives the address of 4 columns of row k
     const int s = lane % 16, q = lane / 16, col4 = PERMUTED ? (s % 2) * 2 + s % 4 / 2 : s % 4;
@@ -111,14 +110,14 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[T::NT][T::MT])
 // second half of products runs while the next chunk's first operands are read.  Reads and loads stand one by one between the products: in
 // bursts they held up the products behind them.
 template <class T, bool AO, bool BO, int TERMS>
-__device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, const bf16_t *a0, const bf16_t *b0, const Loads<T, T::BM, AO, false> &la,
-                                         const Loads<T, T::BN, BO, true> &lb, int first, int end, bf16_t *lds, f32x16 (&acc)[T::NT][T::MT])
+__device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, const bf16_t *a0, const bf16_t *b0, const Loads<T, T::BM, AO> &la,
+                                         const Loads<T, T::BN, BO> &lb, int first, int end, bf16_t *lds, f32x16 (&acc)[T::NT][T::MT])
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const int wm = (wave / T::WC) * (32 * T::MT), wn = (wave % T::WC) * (32 * T::NT);
     const unsigned base = lds_address(lds);
     constexpr unsigned kBuffer = 2 * (T::kChunkA + T::kChunkB);
-    constexpr int LA = Loads<T, T::BM, AO, false>::L, LB = Loads<T, T::BN, BO, true>::L, kLoads = LA + LB;
+    constexpr int LA = Loads<T, T::BM, AO>::L, LB = Loads<T, T::BN, BO>::L, kLoads = LA + LB;
     const int rounds = end - first, total = TERMS == 1 ? rounds : 6 * rounds;
     // the chunk that is being asked for
     const bf16_t *an = a0, *bn = b0;
@@ -231,7 +230,8 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
-    constexpr int kHalf = (T::MT + 1) / 2, kFirst = T::MT > 1 ? kLoads / 4 : 0;
+    static_assert(T::MT * T::NT <= 2 || (T::MT > 1 && T::NB == 2), "the products of a step's second half cover the next chunk's first reads");
+    constexpr int kHalf = T::MT / 2, kFirst = kLoads / 4;
     __builtin_amdgcn_s_barrier();                  // the buffers are free
     for (int i = 0; i < min(T::NB, total); ++i) {
         aim(i, i);
@@ -251,18 +251,14 @@ __device__ __forceinline__ void multiply(const Operand &A, const Operand &Bm, co
         step(1, 0, T::MT, true, buffer, 2, 0, 0, false);
         step(0, 0, T::MT, true, buffer, 3, 0, 0, false);
         step(1, 0, kHalf, false, 0, 0, 0, 0, false);
-        // the next chunk is there; those behind it may be on their way, while as many are
-        if (T::NB > 2 && i + T::NB <= total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((T::NB - 2) * kLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // the next chunk is there
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         asking = i + T::NB < total;
         if (asking) aim(i + T::NB, buffer);
         // (behind the last chunk the reads find what is there, which nobody uses)
-        if (T::MT > 1) step(1, kHalf, T::MT, true, next, 0, 0, kFirst, asking);
-        else
-#pragma unroll
-            for (int r = 0; r < kReads; ++r) read(r, next, 0, 0);
+        step(1, kHalf, T::MT, true, next, 0, 0, kFirst, asking);
         buffer = next;
     }
     // the wait between the last products and the first use of their results, spelled out: where a branch lies between them the
@@ -475,8 +471,8 @@ __device__ __forceinline__ void product_sums(const Operand &A, const Operand &Bm
     tile_of(block, (int)((M + T::BM - 1) / T::BM), (N + T::BN - 1) / T::BN, mt0, nt0);
     const long m0 = (long)mt0 * T::BM;
     const int n0 = nt0 * T::BN, rows = (int)min((long)T::BM, M - m0), most = BO ? (N + 7) / 8 * 8 - 8 - n0 : N - 1 - n0;
-    const Loads<T, T::BM, false, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
-    const Loads<T, T::BN, BO, true> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, most); });
+    const Loads<T, T::BM, false> la(wave, lane, A.ld, [&](int row) { return (long)min(row, rows - 1); });
+    const Loads<T, T::BN, BO> lb(wave, lane, Bm.ld, [&](int i) { return (long)min(i, most); });
     clear<T>(acc);
     multiply<T, false, BO, TERMS>(A, Bm, A.p + m0 * A.ld, Bm.p + n0 * (BO ? 1 : Bm.ld), la, lb, first, last, lds, acc);
 }
