@@ -27,6 +27,8 @@ struct Operand {
 //   k_gated    4096 x 512 x 1368 (176 large tiles) 22.8 / 25.0 / 27.7, 12544 x 128 x 256 (98; 392 of 128) 12.9 / 9.8 / 11.9,
 //              1024 x 768 x 2048 (256 of 128) 26.1 / 17.8 / 15.2
 //   k_product  12544 x 768 x 2048 (147) 48.8 / 65.2 / 70.9, 12544 x 512 x 1368 (98; 392) 38.7 / 29.8 / 42.5, 4096 x 768 x 2048 (192 of 128) 45.8 / 30.9 / 27.3
+//              12544 x 256 (196 of 128; 784 of 64 are more than three to a compute unit, a second round) with a contraction of 512 - / 10.4 / 12.1, 2048 - / 30.5 / 32.0,
+//              12288 x 256 (192; 768) 512 - / 10.2 / 10.8, 1024 - / 17.1 / 16.8, 2048 - / 30.1 / 28.1
 //   k_hidden   given G | U, bound by its reads and stores: 12544 x 768 (392) 99 / 103 / 119, 12544 x 512 (294) 75.9 / 64.4 / 63.5,
 //              4096 x 256 (128 of 128) 29.1 / 16.2 / 10.4;  otherwise 12544 x 128 (196 of 128) - / 15.2 / 17.1, 4096 x 256 (128) - / 16.8 / 13.4
 inline long tiles(long M, long N, long side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
