@@ -259,7 +259,7 @@ struct Gradients {
     Columns columns[2];
     int shares;
 };
-// Bound by the matrix cores: 16384 x 1024 x 2816 447 us for 472 GFLOP, 1.06 PFLOP/s, busy in 61 % of the cycles.
+// Bound by the matrix cores: 16384 x 1024 x 2816 447 to 462 us for 472 GFLOP, 1.02 to 1.06 PFLOP/s, busy in 61 % of the cycles.
 template <class T, int TERMS, typename E>
 __global__ __launch_bounds__(T::kThreads, T::kMinWaves) void k_gradients(Gradients G)
 {
