@@ -71,7 +71,7 @@ enum {
     BRA_ERR_LAUNCH = -7,      /* the HIP runtime reported an error at enqueue time */
     BRA_ERR_TOO_LARGE = -8,   /* bra_forward_static: the shape needs more than BRA_STATIC_SCRATCH_BYTES */
     BRA_ERR_OVERLAP = -10,    /* bra_adamw_step: parameters that share memory */
-    BRA_ERR_ALIGN = -9        /* bra_ffn_*, bra_norm_*, bra_adamw_step: a pointer is not aligned as its entry point asks */
+    BRA_ERR_ALIGN = -9        /* bra_ffn_*, bra_norm_*, bra_adamw_step, bra_attention_*, bra_qk_norm_*: a pointer (or stride) is not aligned as its entry point asks */
 };
 
 typedef struct bra_shape {
@@ -335,6 +335,86 @@ typedef struct bra_adamw_args {
 } bra_adamw_args;
 
 int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_adamw_args *args, void *hip_stream);
+
+/* Attention between whole sequences, beside the routed one above: every query of a sequence sees all of its keys (as in the last stage and in
+ * plain transformers), or those up to its own place.  With query i, key j of sequence b, head a of the queries and its key head a / (heads / kv_heads):
+ *     S[i,j] = scale Q_a[i] . K[j],   key j is visible to query i where j < nk, i < nq and, if `causal`, j <= i + nk - nq
+ *     P = exp(S - max S) on the visible keys,  O_a[i] = sum_j P[i,j] V[j] / sum_j P[i,j],  lse_a[i] = log sum_j exp S[i,j]
+ * nq, nk: Nq and Nk, or q_lens[b] and k_lens[b] (int32 [B] on the device, read when the kernel runs and clamped to 0 .. Nq and 0 .. Nk) where given.
+ * A query with no visible key (or none of finite score) has O = 0 and lse = -infinity; so do the queries from nq on.  Keys and values from nk
+ * on, queries and what comes back from nq on are not read; what is read beyond a causal mask's edge must be finite.
+ * A tensor [B, N, heads, d] is given by a bra_rows: its element (b, n, h, c) lies at data + b batch + n token + h head + c, in elements, so that
+ * parts of one buffer, or a cache with the heads outside, are taken as they lie.  Pointers, and strides in bytes, are multiples of 16 (the stride
+ * of a dimension of one entry is not looked at); inputs may have strides of 0.  What is written overlaps neither itself nor an input.
+ * d: a multiple of 8 up to 128 (heads that are no multiple of 32 wide take the time of the next one).  bf16 tensors: bf16 matrix instructions, P
+ * rounded to bf16 before its product with V, everything else float32.  float32 tensors: the float32 matrix instruction.
+ * scale <= 0 selects 1 / sqrt(d).  No atomic adds: a repeat gives the same bits.  Nothing else than `ws` is needed; its size depends on the shape and
+ * may be 0.
+ * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite, negative
+ * strides, B heads or Nq heads above 2^30); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; LAUNCH. */
+typedef struct bra_attention_shape {
+    int32_t B, Nq, Nk;        /* sequences; queries and keys of each, at most */
+    int32_t heads, kv_heads;  /* heads of the queries, of keys and values */
+    int32_t d;
+    int32_t dtype;            /* BRA_F32 or BRA_BF16 */
+    int32_t causal;
+    float scale;
+} bra_attention_shape;
+typedef struct bra_rows {
+    void *data;               /* read only where an input */
+    int64_t batch, token, head;
+} bra_rows;
+
+int bra_attention_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes);
+int bra_attention_forward(const bra_attention_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_rows *V,
+                          const int32_t *q_lens_opt, const int32_t *k_lens_opt, const bra_rows *O, float *lse_opt, void *ws,
+                          size_t ws_bytes, void *hip_stream);
+
+/* Gradients of it; O and lse [B, heads, Nq] as the forward returned them, dO = dLoss/dO.  The probabilities are formed again from them:
+ *     P = exp(S - lse),  delta_i = dO[i] . O[i],  dS = P (dO V^T - delta),
+ *     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO, dK and dV summed over the heads that share a key head.
+ * dQ, dK, dV have the inputs' dtype, and are OVERWRITTEN, with zeros from nq (nk) on.  bf16: P and dS are rounded to bf16 before the products.
+ * Errors as above. */
+int bra_attention_backward_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes);
+int bra_attention_backward(const bra_attention_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_rows *V,
+                           const bra_rows *O, const float *lse, const bra_rows *dO, const int32_t *q_lens_opt,
+                           const int32_t *k_lens_opt, const bra_rows *dQ, const bra_rows *dK, const bra_rows *dV, void *ws,
+                           size_t ws_bytes, void *hip_stream);
+
+/* What goes before it: norms of queries and keys for each head, and the rotation of their channels by position, in one pass over both.
+ *     u = x / sqrt(mean of squares + eps) * gamma         over a head's d channels, for each token and head; u = x where the gammas are NULL
+ *     (a, b) -> (a cos - b sin, b cos + a sin)            for each pair p of the first `turned` channels: (p, p + turned / 2)
+ *                                                         (BRA_PAIRS_HALVES) or (2 p, 2 p + 1) (BRA_PAIRS_NEIGHBOURS); the others stay
+ * with cos, sin [table_rows, turned / 2] float32 at row positions[b N + n] (int32, clamped to the table), or n where positions is NULL.
+ * Q [B, N, heads, d] and K [B, N, kv_heads, d] as bra_rows (see above); K NULL with kv_heads = 0: queries alone.  q_gamma and k_gamma [d] float32, both or
+ * neither.  The outputs have the inputs' dtype, rounded once; Qout may be Q, Kout may be K.
+ * Errors: NULL; SHAPE (B, N < 0, heads < 1, kv_heads < 0, B N (heads + kv_heads) above 2^30, turned odd or outside 0 .. d, table_rows < 1, or < N without
+ * positions, where turned > 0, eps < 0, negative strides); DTYPE (dtype or pairs); UNSUPPORTED (d no multiple of 8 or above 128); ALIGN; LAUNCH. */
+enum { BRA_PAIRS_HALVES = 0, BRA_PAIRS_NEIGHBOURS = 1 };    /* bra_qk_norm_shape.pairs */
+typedef struct bra_qk_norm_shape {
+    int32_t B, N, heads, kv_heads, d;
+    int32_t turned;           /* channels of a head that are rotated */
+    int32_t table_rows;
+    int32_t pairs;
+    int32_t dtype;            /* BRA_F32 or BRA_BF16 */
+    float eps;
+} bra_qk_norm_shape;
+typedef struct bra_qk_norm_params {     /* a HOST struct of DEVICE pointers */
+    const float *q_gamma, *k_gamma;
+    const float *cos, *sin;
+    const int32_t *positions;
+} bra_qk_norm_params;
+
+int bra_qk_norm_forward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K_opt,
+                        const bra_qk_norm_params *params, const bra_rows *Qout, const bra_rows *Kout_opt, void *hip_stream);
+
+/* Gradients of it.  Q, K: its inputs (not read without gammas); gQ, gK: what came back to its outputs.  dQ, dK have the inputs' dtype; dq_gamma and
+ * dk_gamma [d] float32 or NULL, summed over tokens and heads, OVERWRITTEN.  dQ may be gQ or Q, dK may be gK or K.  No atomic adds: a repeat gives the
+ * same bits.  Errors as above, and WORKSPACE. */
+int bra_qk_norm_backward_workspace_bytes(const bra_qk_norm_shape *shape, size_t *out_bytes);
+int bra_qk_norm_backward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K_opt, const bra_qk_norm_params *params,
+                         const bra_rows *gQ, const bra_rows *gK_opt, const bra_rows *dQ, const bra_rows *dK_opt, float *dq_gamma_opt,
+                         float *dk_gamma_opt, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Optional per-launch timing, for benchmarks (Sec. "Limitation": the paper locates
  * BRA's cost in kernel launches and memory transactions, so the benchmark reports

@@ -21,7 +21,9 @@ BRA_F32, BRA_BF16 = 0, 1
 PATH_AUTO, PATH_GENERIC, PATH_MFMA = 0, 1, 2
 SILU, GELU = 0, 1
 LAYERNORM, RMSNORM = 0, 1
+PAIRS_HALVES, PAIRS_NEIGHBOURS = 0, 1
 _KINDS = {"layer": LAYERNORM, "rms": RMSNORM}
+_PAIRS = {"halves": PAIRS_HALVES, "neighbours": PAIRS_NEIGHBOURS}
 ADAMW_BLOCK = 32
 _ACTS = {"silu": SILU, "gelu": GELU}
 _PATHS = {"auto": PATH_AUTO, "generic": PATH_GENERIC, "mfma": PATH_MFMA}
@@ -32,7 +34,8 @@ EXPORTS = ("bra_workspace_bytes", "bra_route", "bra_forward", "bra_forward_stati
            "bra_forward_padded", "bra_backward_workspace_bytes", "bra_backward", "bra_block_workspace_bytes",
            "bra_block_forward", "bra_ffn_workspace_bytes", "bra_ffn_forward", "bra_ffn_backward_workspace_bytes",
            "bra_ffn_backward", "bra_norm_forward", "bra_norm_backward_workspace_bytes", "bra_norm_backward",
-           "bra_adamw_step", "bra_strerror", "bra_version",
+           "bra_adamw_step", "bra_attention_workspace_bytes", "bra_attention_forward", "bra_attention_backward_workspace_bytes",
+           "bra_attention_backward", "bra_qk_norm_forward", "bra_qk_norm_backward_workspace_bytes", "bra_qk_norm_backward", "bra_strerror", "bra_version",
            "bra_profile_begin", "bra_profile_end", "bra_kernel_name", "bra_util_copy",
            "bra_util_read", "bra_util_mfma", "bra_util_mfma32")
 
@@ -78,6 +81,26 @@ class BraAdamwArgs(ctypes.Structure):
                 [("step", ctypes.c_int64), ("step_device", ctypes.c_void_p), ("scalars", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p),
                  ("bits", ctypes.c_int32)] +
                 [(name, ctypes.c_void_p) for name in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")])
+
+
+class BraAttentionShape(ctypes.Structure):
+    """bra_attention_shape."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "Nq", "Nk", "heads", "kv_heads", "d", "dtype", "causal")] + [("scale", ctypes.c_float)]
+
+
+class BraRows(ctypes.Structure):
+    """bra_rows: a device pointer and strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p)] + [(name, ctypes.c_int64) for name in ("batch", "token", "head")]
+
+
+class BraQkNormShape(ctypes.Structure):
+    """bra_qk_norm_shape."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "N", "heads", "kv_heads", "d", "turned", "table_rows", "pairs", "dtype")] + [("eps", ctypes.c_float)]
+
+
+class BraQkNormParams(ctypes.Structure):
+    """bra_qk_norm_params: device pointers."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("q_gamma", "k_gamma", "cos", "sin", "positions")]
 
 
 class BraBlockParams(ctypes.Structure):
@@ -143,6 +166,21 @@ def lib() -> ctypes.CDLL:
                                         ctypes.POINTER(BraNormGrads), vp, sz, vp]
         L.bra_adamw_step.restype = ctypes.c_int
         L.bra_adamw_step.argtypes = [ctypes.POINTER(BraAdamwTensor), ctypes.c_int32, ctypes.POINTER(BraAdamwArgs), vp]
+        rows = ctypes.POINTER(BraRows)
+        L.bra_attention_workspace_bytes.restype = ctypes.c_int
+        L.bra_attention_workspace_bytes.argtypes = [ctypes.POINTER(BraAttentionShape), ctypes.POINTER(sz)]
+        L.bra_attention_forward.restype = ctypes.c_int
+        L.bra_attention_forward.argtypes = [ctypes.POINTER(BraAttentionShape)] + [rows] * 3 + [vp, vp, rows, vp, vp, sz, vp]
+        L.bra_attention_backward_workspace_bytes.restype = ctypes.c_int
+        L.bra_attention_backward_workspace_bytes.argtypes = [ctypes.POINTER(BraAttentionShape), ctypes.POINTER(sz)]
+        L.bra_attention_backward.restype = ctypes.c_int
+        L.bra_attention_backward.argtypes = [ctypes.POINTER(BraAttentionShape)] + [rows] * 4 + [vp, rows, vp, vp] + [rows] * 3 + [vp, sz, vp]
+        L.bra_qk_norm_forward.restype = ctypes.c_int
+        L.bra_qk_norm_forward.argtypes = [ctypes.POINTER(BraQkNormShape), rows, rows, ctypes.POINTER(BraQkNormParams), rows, rows, vp]
+        L.bra_qk_norm_backward_workspace_bytes.restype = ctypes.c_int
+        L.bra_qk_norm_backward_workspace_bytes.argtypes = [ctypes.POINTER(BraQkNormShape), ctypes.POINTER(sz)]
+        L.bra_qk_norm_backward.restype = ctypes.c_int
+        L.bra_qk_norm_backward.argtypes = [ctypes.POINTER(BraQkNormShape), rows, rows, ctypes.POINTER(BraQkNormParams)] + [rows] * 4 + [vp, vp, vp, sz, vp]
         L.bra_strerror.restype = ctypes.c_char_p
         L.bra_strerror.argtypes = [ctypes.c_int]
         L.bra_version.restype = ctypes.c_int
@@ -333,6 +371,62 @@ def bra_adamw_step(params, grads, state, *, step, lr=1e-3, beta1=0.9, beta2=0.99
     graphs).  weight_decay: a number, or one for each parameter.  copies: bf16 tensors (or None) that receive the float32 parameters'
     new values.  grad_scale: None or a one-element float32 tensor on the GPU that the gradients are multiplied by (see include/bra.h)."""
     (_native_module or _load_native()).adamw_step(params, grads, state, step, lr, beta1, beta2, eps, weight_decay, copies, grad_scale)
+
+
+def make_attention_shape(B, Nq, Nk, heads, kv_heads, d, dtype, causal=False, scale=None) -> BraAttentionShape:
+    dt = {torch.float32: BRA_F32, torch.bfloat16: BRA_BF16}.get(dtype, dtype)
+    return BraAttentionShape(B, Nq, Nk, heads, kv_heads, d, int(dt), int(bool(causal)), float(scale) if scale else 0.0)
+
+
+def attention_workspace_bytes(shape: BraAttentionShape, backward: bool = False) -> int:
+    """Workspace of a call of this shape; 0 where it needs none."""
+    out = ctypes.c_size_t(0)
+    query = lib().bra_attention_backward_workspace_bytes if backward else lib().bra_attention_workspace_bytes
+    _check(query(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def bra_attention_forward(Q, K, V, *, causal=False, q_lens=None, k_lens=None, scale=None, want_lse=False, ws=None, out=None):
+    """Attention between whole sequences: O [B, Nq, heads, d] = softmax(scale Q K^T) V with Q [B, Nq, heads, d], K and V [B, Nk, kv_heads, d];
+    heads / kv_heads query heads share a key head.  Any strides that keep channels next to each other and rows on 16 bytes (parts of one buffer, a cache
+    with the heads outside).  causal: the last query of a sequence sees all of its keys, the one before one key less, and so on.  q_lens, k_lens: int32 [B] on
+    the GPU, valid queries and keys of each sequence; O is zero behind them and where a query sees no key.  want_lse: also the logarithms of the sums of
+    exponentials [B, heads, Nq] (float32), for the backward pass (see include/bra.h)."""
+    return (_native_module or _load_native()).attention_forward(Q, K, V, causal, q_lens, k_lens, scale, want_lse, ws, out)
+
+
+def bra_attention_backward(Q, K, V, O, lse, dO, *, causal=False, q_lens=None, k_lens=None, scale=None, ws=None, out=None):
+    """Gradients (dQ, dK, dV) of bra_attention_forward from its O and lse; the other arguments as it had them.  out: three tensors that receive them, for
+    instance the parts of one buffer."""
+    return (_native_module or _load_native()).attention_backward(Q, K, V, O, lse, dO, causal, q_lens, k_lens, scale, ws, out)
+
+
+def rotary_table(H, W=None, channels=64, base=10000.0, device=None):
+    """(cos, sin) [positions, channels / 2] float32 for bra_qk_norm_forward, angles formed in 64 bits: position n turns pair p by n base^(-2 p / channels).
+    With W for a map of H x W tokens: the first half of the pairs by a token's row, the second by its column, each as a table of channels / 2."""
+    if channels < 0 or channels % (2 if W is None else 4):
+        raise ValueError("channels must be a multiple of 2, of 4 for a map")
+    at = lambda n, c: torch.arange(n, dtype=torch.float64, device=device)[:, None] * base ** (-torch.arange(0, c, 2, dtype=torch.float64, device=device) / max(c, 1))
+    if W is None:
+        angle = at(H, channels)
+    else:
+        rows, columns = at(H, channels // 2), at(W, channels // 2)
+        angle = torch.cat([rows[:, None].expand(-1, W, -1), columns[None].expand(H, -1, -1)], -1).reshape(H * W, channels // 2)
+    return angle.cos().float(), angle.sin().float()
+
+
+def bra_qk_norm_forward(Q, K=None, q_gamma=None, k_gamma=None, *, cos=None, sin=None, positions=None, pairs="halves", eps=1e-6, out=None):
+    """Norms of queries and keys for each head (x / rms(x) * gamma; none without gammas) and the rotation of their channels by position, in one pass.
+    Q [B, N, heads, d], K [B, N, kv_heads, d] or None, as in bra_attention_forward; gammas float32 [d]; cos, sin float32 [positions, rotated channels / 2] (see
+    rotary_table; none: no rotation); positions int32 [B, N] (None: a token's place in its sequence).  pairs: "halves" (p, p + rotated / 2) or "neighbours"
+    (2 p, 2 p + 1).  Returns (Q', K') (K' None without K).  out: two tensors that receive them; may be Q and K (see include/bra.h)."""
+    return (_native_module or _load_native()).qk_norm_forward(Q, K, q_gamma, k_gamma, cos, sin, positions, _PAIRS[pairs], eps, out)
+
+
+def bra_qk_norm_backward(Q, K, dQ, dK, q_gamma=None, k_gamma=None, *, cos=None, sin=None, positions=None, pairs="halves", eps=1e-6, ws=None, out=None):
+    """Gradients of bra_qk_norm_forward: (dQ, dK), with gammas also dq_gamma and dk_gamma (float32).  Q, K: its inputs; dQ, dK: what came back to its
+    outputs.  out: two tensors that receive the first two; may be dQ and dK, or Q and K."""
+    return (_native_module or _load_native()).qk_norm_backward(Q, K, dQ, dK, q_gamma, k_gamma, cos, sin, positions, _PAIRS[pairs], eps, ws, out)
 
 
 def profile_begin(max_records: int) -> None:

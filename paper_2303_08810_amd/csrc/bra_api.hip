@@ -3,6 +3,8 @@
 #include "bra_adamw.h"
 #include "bra_ffn.h"
 #include "bra_norm.h"
+#include "bra_attention.h"
+#include "bra_qk_norm.h"
 
 #include <math.h>
 
@@ -120,6 +122,62 @@ static int make_norm_sizes(const bra_norm_shape *s, bool post, NormSizes &S)
 static bool ws_ok(const void *ws, size_t have, size_t need)
 {
     return ws && ((uintptr_t)ws % 256 == 0) && have >= need;
+}
+
+// Attention's sizes; what depends on the tensors comes later.
+static int make_attention_sizes(const bra_attention_shape *s, att::Sizes &S)
+{
+    if (!s) return BRA_ERR_NULL;
+    constexpr int kMost = 1 << 28;
+    if (s->B < 0 || s->Nq < 0 || s->Nk < 0 || s->B > kMost || s->Nq > kMost || s->Nk > kMost || s->kv_heads < 1 || s->heads < s->kv_heads || s->heads % s->kv_heads || s->heads > 65536 ||
+        s->d < 1 || !std::isfinite(s->scale))
+        return BRA_ERR_SHAPE;
+    if ((long)s->B * s->heads > (1L << 30) || (long)s->Nq * s->heads > (1L << 30)) return BRA_ERR_SHAPE;
+    if (s->dtype != BRA_F32 && s->dtype != BRA_BF16) return BRA_ERR_DTYPE;
+    if (s->d % 8 || s->d > 128) return BRA_ERR_UNSUPPORTED;
+    S = att::Sizes{s->B, s->Nq, s->Nk, s->heads, s->kv_heads, s->d, s->dtype == BRA_F32, s->causal != 0, s->scale > 0.f ? s->scale : 1.0f / sqrtf((float)s->d), nullptr, nullptr};
+    return BRA_OK;
+}
+
+// A [B, N, heads, d] tensor's place, strides in bytes; a tensor without elements may have no memory.
+static int make_rows(const bra_rows *r, long B, long N, long heads, size_t element, att::Rows &R)
+{
+    R = att::Rows{};
+    if (B == 0 || N == 0 || heads == 0) return BRA_OK;
+    if (!r || !r->data) return BRA_ERR_NULL;
+    const long e = (long)element;
+    R = att::Rows{(char *)r->data, B > 1 ? r->batch * e : 0, N > 1 ? r->token * e : 0, heads > 1 ? r->head * e : 0};
+    if ((B > 1 && r->batch < 0) || (N > 1 && r->token < 0) || (heads > 1 && r->head < 0)) return BRA_ERR_SHAPE;
+    if ((uintptr_t)R.p % 16 || R.batch % 16 || R.token % 16 || R.head % 16) return BRA_ERR_ALIGN;
+    return BRA_OK;
+}
+
+static int make_qk_norm_sizes(const bra_qk_norm_shape *s, QkNormSizes &S)
+{
+    if (!s) return BRA_ERR_NULL;
+    if (s->B < 0 || s->N < 0 || s->heads < 1 || s->kv_heads < 0 || s->d < 1 || s->turned < 0 || s->turned > s->d || s->turned % 2 || !(s->eps >= 0.f)) return BRA_ERR_SHAPE;
+    const long most = 1L << 30, tokens = (long)s->B * s->N, heads = (long)s->heads + s->kv_heads;
+    if (tokens > most || heads > most || tokens * heads > most) return BRA_ERR_SHAPE;
+    if (s->dtype != BRA_F32 && s->dtype != BRA_BF16) return BRA_ERR_DTYPE;
+    if (s->pairs != BRA_PAIRS_HALVES && s->pairs != BRA_PAIRS_NEIGHBOURS) return BRA_ERR_DTYPE;
+    if (s->d % 8 || s->d > 128) return BRA_ERR_UNSUPPORTED;
+    S = QkNormSizes{tokens, s->N, s->heads, s->kv_heads, s->d, s->turned, s->table_rows, s->dtype == BRA_F32, s->pairs == BRA_PAIRS_HALVES, s->eps};
+    return BRA_OK;
+}
+
+// The vectors of norms and rotation.
+static int qk_norm_in(const bra_qk_norm_shape *s, const QkNormSizes &S, const bra_qk_norm_params *p, QkNormIn &I)
+{
+    if (!p) return BRA_ERR_NULL;
+    if ((S.turned && (!p->cos || !p->sin)) || (p->k_gamma && !p->q_gamma) || (S.kv_heads && p->q_gamma && !p->k_gamma)) return BRA_ERR_NULL;
+    if (S.turned && (s->table_rows < 1 || (!p->positions && s->table_rows < s->N))) return BRA_ERR_SHAPE;
+    if (!aligned(4, {p->q_gamma, p->k_gamma, p->cos, p->sin, p->positions})) return BRA_ERR_ALIGN;
+    I.q_gamma = p->q_gamma;
+    I.k_gamma = p->k_gamma;
+    I.cos = p->cos;
+    I.sin = p->sin;
+    I.positions = p->positions;
+    return BRA_OK;
 }
 
 }  // namespace bra
@@ -450,6 +508,114 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
         return BRA_ERR_LAUNCH;
     }
     return adamw_step(tensors, count, *a, (hipStream_t)hip_stream);
+}
+
+int bra_attention_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    att::Sizes S;
+    const int rc = make_attention_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = attention_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_attention_forward(const bra_attention_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_rows *V, const int32_t *q_lens, const int32_t *k_lens, const bra_rows *O,
+                          float *lse, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    att::Sizes S;
+    int rc = make_attention_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    const size_t e = S.f32 ? 4 : 2;
+    att::Rows q, k, v, o;
+    if ((rc = make_rows(Q, S.B, S.Nq, S.H, e, q)) || (rc = make_rows(K, S.B, S.Nk, S.Hk, e, k)) || (rc = make_rows(V, S.B, S.Nk, S.Hk, e, v)) ||
+        (rc = make_rows(O, S.B, S.Nq, S.H, e, o)))
+        return rc;
+    if (!aligned(4, {q_lens, k_lens, lse})) return BRA_ERR_ALIGN;
+    if (S.B == 0 || S.Nq == 0) return BRA_OK;
+    const size_t need = attention_workspace_bytes(S);
+    if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    S.q_lens = q_lens;
+    S.k_lens = k_lens;
+    return attention_forward(S, q, k, v, o, lse, ws, (hipStream_t)hip_stream);
+}
+
+int bra_attention_backward_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    att::Sizes S;
+    const int rc = make_attention_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = attention_backward_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_attention_backward(const bra_attention_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_rows *V, const bra_rows *O, const float *lse, const bra_rows *dO,
+                           const int32_t *q_lens, const int32_t *k_lens, const bra_rows *dQ, const bra_rows *dK, const bra_rows *dV, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    att::Sizes S;
+    int rc = make_attention_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    const size_t e = S.f32 ? 4 : 2;
+    att::Rows q, k, v, o, go, dq, dk, dv;
+    if ((rc = make_rows(Q, S.B, S.Nq, S.H, e, q)) || (rc = make_rows(K, S.B, S.Nk, S.Hk, e, k)) || (rc = make_rows(V, S.B, S.Nk, S.Hk, e, v)) ||
+        (rc = make_rows(O, S.B, S.Nq, S.H, e, o)) || (rc = make_rows(dO, S.B, S.Nq, S.H, e, go)) || (rc = make_rows(dQ, S.B, S.Nq, S.H, e, dq)) ||
+        (rc = make_rows(dK, S.B, S.Nk, S.Hk, e, dk)) || (rc = make_rows(dV, S.B, S.Nk, S.Hk, e, dv)))
+        return rc;
+    if (S.B > 0 && S.Nq > 0 && !lse) return BRA_ERR_NULL;
+    if (!aligned(4, {q_lens, k_lens, lse})) return BRA_ERR_ALIGN;
+    if (S.B == 0 || (S.Nq == 0 && S.Nk == 0)) return BRA_OK;
+    const size_t need = attention_backward_workspace_bytes(S);
+    if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    S.q_lens = q_lens;
+    S.k_lens = k_lens;
+    return attention_backward(S, q, k, v, o, lse, go, dq, dk, dv, ws, (hipStream_t)hip_stream);
+}
+
+int bra_qk_norm_forward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_qk_norm_params *params, const bra_rows *Qout, const bra_rows *Kout,
+                        void *hip_stream)
+{
+    QkNormSizes S;
+    int rc = make_qk_norm_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    QkNormIn I{};
+    if ((rc = qk_norm_in(shape, S, params, I)) != BRA_OK) return rc;
+    const size_t e = S.f32 ? 4 : 2;
+    att::Rows q, k;
+    if ((rc = make_rows(Q, shape->B, S.N, S.heads, e, I.Q)) || (rc = make_rows(K, shape->B, S.N, S.kv_heads, e, I.K)) || (rc = make_rows(Qout, shape->B, S.N, S.heads, e, q)) ||
+        (rc = make_rows(Kout, shape->B, S.N, S.kv_heads, e, k)))
+        return rc;
+    return qk_norm_forward(S, I, q, k, (hipStream_t)hip_stream);
+}
+
+int bra_qk_norm_backward_workspace_bytes(const bra_qk_norm_shape *shape, size_t *out_bytes)
+{
+    if (!out_bytes) return BRA_ERR_NULL;
+    QkNormSizes S;
+    const int rc = make_qk_norm_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    *out_bytes = qk_norm_backward_workspace_bytes(S);
+    return BRA_OK;
+}
+
+int bra_qk_norm_backward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_qk_norm_params *params, const bra_rows *gQ, const bra_rows *gK,
+                         const bra_rows *dQ, const bra_rows *dK, float *dq_gamma, float *dk_gamma, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    QkNormSizes S;
+    int rc = make_qk_norm_sizes(shape, S);
+    if (rc != BRA_OK) return rc;
+    QkNormIn I{};
+    if ((rc = qk_norm_in(shape, S, params, I)) != BRA_OK) return rc;
+    const size_t e = S.f32 ? 4 : 2;
+    att::Rows gq, gk, dq, dk;
+    if ((I.q_gamma && ((rc = make_rows(Q, shape->B, S.N, S.heads, e, I.Q)) || (rc = make_rows(K, shape->B, S.N, S.kv_heads, e, I.K)))) ||
+        (rc = make_rows(gQ, shape->B, S.N, S.heads, e, gq)) || (rc = make_rows(gK, shape->B, S.N, S.kv_heads, e, gk)) ||
+        (rc = make_rows(dQ, shape->B, S.N, S.heads, e, dq)) || (rc = make_rows(dK, shape->B, S.N, S.kv_heads, e, dk)))
+        return rc;
+    if (!aligned(4, {dq_gamma, dk_gamma})) return BRA_ERR_ALIGN;
+    const size_t need = qk_norm_backward_workspace_bytes(S);
+    if (I.q_gamma && need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    return qk_norm_backward(S, I, gq, gk, dq, dk, dq_gamma, dk_gamma, ws, (hipStream_t)hip_stream);
 }
 
 const char *bra_strerror(int code)

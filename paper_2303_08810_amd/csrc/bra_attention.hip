@@ -1,0 +1,297 @@
+// Attention between whole sequences, forward:
+//     S = scale Q K^T, P = exp(S - max) masked, O = P V / sum P, lse = max + log sum P
+// in one pass over keys and values with the running maximum and sum of each query.  A wavefront has 32 rows (queries of the heads that share
+// a key head) in its lanes; tiles of keys and values come to LDS by direct loads while the tile before is worked on.  Few rows: the
+// wavefronts of a workgroup have the same rows and share the keys out.  Where workgroups are few, the keys are shared out to several, whose sums
+// k_attention_join puts together.
+#include "bra_attention_dev.h"
+
+#include <algorithm>
+
+namespace bra {
+namespace att {
+namespace {
+
+// KT keys a tile.
+template <class E, int D, int KT, int WAVES, bool FEW>
+struct Forward {
+    typedef Geometry<E, D> G;
+    static constexpr int kThreads = 64 * WAVES, kLoaders = FEW ? 64 : kThreads, kRows = FEW ? 32 : 32 * WAVES;
+    static constexpr int kTile = KT * G::kPitch, kBuffer = 2 * kTile, kKeyTile = KT;
+    static constexpr int kRings = 2 * kBuffer * (FEW ? WAVES : 1);
+    static constexpr int kJoin = FEW ? WAVES * 32 * (D + 2) * 4 : 0;
+    static constexpr int kLds = kRings > kJoin ? kRings : kJoin;
+    typedef Stage<G, KT, kLoaders> Loads;
+};
+
+// O (or its share before the division) and the statistics of one row.
+template <class E, class G>
+__device__ __forceinline__ void finish(const Call &A, int b, int hk, int split, int row, int h, const f32x16 (&acc)[G::NT], float m, float l)
+{
+    const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
+    if (A.splits > 1) {
+        const long at = ((long)(b * A.Hk + hk) * A.splits + split) * A.rows + row;
+        store_columns<float, G>((char *)(A.part + at * G::D), acc, 1.f, G::D, h);
+        if (h == 0) {
+            A.part_ml[2 * at] = m;
+            A.part_ml[2 * at + 1] = l;
+        }
+        return;
+    }
+    store_columns<E, G>(A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, acc, l == 0.f ? 0.f : 1.f / l, A.d, h);
+    if (A.lse && h == 0) A.lse[((long)b * A.Hk * A.G + head) * A.Nq + query] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <class E, int D, int KT, int WAVES, bool FEW>
+__global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D > 96) ? 1 : 2) void k_attention(Call A)
+{
+    typedef Forward<E, D, KT, WAVES, FEW> F;
+    typedef typename F::G G;
+    extern __shared__ char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
+    const long block = swizzled(A.first + blockIdx.x, A.blocks);
+    const int tile = A.tiles - 1 - (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);     // those of a causal mask's long rows first
+    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
+    const Sequence seq(A, b);
+    const int pieces = A.d * (int)sizeof(E) / 16;
+
+    const int first_row = tile * F::kRows, row = first_row + (FEW ? 0 : 32 * wave) + c;
+    const bool valid = row < A.rows;
+    const int query = row_query(A, min(row, A.rows - 1)), limit = valid ? seq.limit(query) : 0;
+    const int least = columns_min(limit), most = columns_max(limit);
+    // keys that any row of the workgroup sees
+    int end = 0;
+    if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
+    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, last = min(all, (split + 1) * share);
+
+    typename G::Piece x[G::kSteps];
+    {
+        const int head = hk * A.G + min(row, A.rows - 1) - query * A.G;
+        load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
+    }
+    const char *keys = A.K.p + b * A.K.batch + hk * A.K.head, *values = A.V.p + b * A.V.batch + hk * A.V.head;
+    char *ring = lds + (FEW ? wave * 2 * F::kBuffer : 0);
+    const unsigned ring_at = lds_address(ring);
+    const int thread = FEW ? lane : threadIdx.x;
+    auto request = [&](int t, int buffer) {
+        const int k0 = t * KT;
+        const char *k = keys + k0 * A.K.token, *v = values + k0 * A.V.token;
+        F::Loads::request([&](int r) { return k + r * A.K.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer, thread);
+        F::Loads::request([&](int r) { return v + r * A.V.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + F::kTile, thread);
+    };
+
+    f32x16 acc[G::NT];
+    clear(acc);
+    Running run;
+    constexpr int kStep = FEW ? WAVES : 1;
+    int t = split * share + (FEW ? wave : 0), buffer = 0;
+    if (t < last) request(t, 0);
+    for (; t < last; t += kStep, buffer ^= 1) {
+        if constexpr (FEW) {
+            lds_reads_done();
+            if (t + kStep < last) {
+                request(t + kStep, buffer ^ 1);
+                asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * F::Loads::L) : "memory");
+            } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + 1 < last) request(t + 1, buffer ^ 1);
+        }
+        const int k0 = t * KT;
+        if (k0 >= most) continue;
+        const char *kt = ring + buffer * F::kBuffer, *vt = kt + F::kTile;
+        f32x16 s[KT / 32];
+        clear(s);
+#pragma unroll
+        for (int i = 0; i < KT / 32; ++i) multiply_rows<G>(s[i], kt, 32 * i, x, lane);
+        if (k0 + KT > least) {
+#pragma unroll
+            for (int i = 0; i < KT / 32; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[i][r] = k0 + 32 * i + result_row(r, h) < limit ? s[i][r] : -INFINITY;
+        }
+        run.weights(s, A.c, acc);
+#pragma unroll
+        for (int i = 0; i < KT / 32; ++i) multiply_columns<G>(acc, vt, 32 * i, s[i], lane);
+    }
+
+    float l = pair_sum(run.l), m = run.m;
+    if constexpr (FEW) {
+        // the wavefronts' shares: [wave][column][D] sums, then [wave][column] m and l
+        float *sums = (float *)lds, *ml = sums + WAVES * 32 * D;
+        __syncthreads();
+        store_columns<float, G>((char *)(sums + (wave * 32 + c) * D), acc, 1.f, D, h);
+        if (h == 0) {
+            ml[2 * (32 * wave + c)] = m;
+            ml[2 * (32 * wave + c) + 1] = l;
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[2 * (32 * w + c)]);
+        clear(acc);
+        l = 0.f;
+        m = top;
+        for (int w = 0; w < WAVES; ++w) {
+            const float mw = ml[2 * (32 * w + c)], factor = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
+            l = fmaf(factor, ml[2 * (32 * w + c) + 1], l);
+            const float *from = sums + (w * 32 + c) * D;
+#pragma unroll
+            for (int n = 0; n < G::NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[n][e] = fmaf(factor, from[32 * n + 16 * (e / 8) + 8 * h + e % 8], acc[n][e]);
+        }
+    }
+    if (valid) finish<E, G>(A, b, hk, split, row, h, acc, m, l);
+}
+
+// The splits' sums put together: a thread has 8 channels of a row.
+template <class E, int D>
+__global__ __launch_bounds__(256) void k_attention_join(Call A)
+{
+    constexpr int CH = D / 8;
+    const long i = (A.first + blockIdx.x) * 256 + threadIdx.x, rows = A.blocks * A.rows;       // here blocks: sequences x key heads
+    if (i >= rows * CH) return;
+    const long r = i / CH;
+    const int ch = 8 * (int)(i % CH), row = (int)(r % A.rows), hb = (int)(r / A.rows), b = hb / A.Hk, hk = hb % A.Hk;
+    const long at = (long)hb * A.splits * A.rows + row;
+    float top = -INFINITY;
+    for (int s = 0; s < A.splits; ++s) top = fmaxf(top, A.part_ml[2 * (at + (long)s * A.rows)]);
+    float o[8] = {}, l = 0.f;
+    for (int s = 0; s < A.splits; ++s) {
+        const long p = at + (long)s * A.rows;
+        const float m = A.part_ml[2 * p], factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l = fmaf(factor, A.part_ml[2 * p + 1], l);
+        const f32x4 v0 = *(const f32x4 *)(A.part + p * D + ch), v1 = *(const f32x4 *)(A.part + p * D + ch + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] = fmaf(factor, v0[e], o[e]);
+            o[4 + e] = fmaf(factor, v1[e], o[4 + e]);
+        }
+    }
+    const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= inv;
+    if (ch < A.d) store8<E>(A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head + ch * sizeof(E), o);
+    if (A.lse && ch == 0) A.lse[((long)b * A.Hk * A.G + head) * A.Nq + query] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+bool few(const Sizes &S) { return S.rows() <= 32; }
+int key_tile(const Sizes &S) { return few(S) || S.f32 ? 32 : 64; }
+int waves(const Sizes &S) { return few(S) && S.f32 && S.width() > 64 ? 2 : 4; }
+long row_tiles(const Sizes &S)
+{
+    const int rows = few(S) ? 32 : 32 * waves(S);
+    return (S.rows() + rows - 1) / rows;
+}
+int splits_of(const Sizes &S)
+{
+    const long blocks = row_tiles(S) * S.B * S.Hk, tiles = (S.Nk + key_tile(S) - 1) / key_tile(S);
+    if (blocks == 0) return 1;
+    const long want = few(S) ? 2048 : 512, least = few(S) ? 2 * waves(S) : 4;
+    return (int)std::max(1L, std::min({want / blocks, tiles / least, 64L}));
+}
+
+template <class E, int D, int KT, int WAVES, bool FEW>
+int launch(Call A, hipStream_t st)
+{
+    typedef Forward<E, D, KT, WAVES, FEW> F;
+    const int rc = allow_lds<k_attention<E, D, KT, WAVES, FEW>>(F::kLds);
+    if (rc != BRA_OK) return rc;
+    for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION);
+        k_attention<E, D, KT, WAVES, FEW><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
+}
+
+template <class E, int D>
+int join(Call A, long heads, hipStream_t st)
+{
+    A.blocks = heads;
+    const long blocks = (heads * A.rows * (D / 8) + 255) / 256;
+    for (A.first = 0; A.first < blocks; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION_JOIN);
+        k_attention_join<E, D><<<(unsigned)std::min(kMaxBlocks, blocks - A.first), 256, 0, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
+}
+
+template <class E, int D>
+int run(const Sizes &S, const Call &A, hipStream_t st)
+{
+    constexpr bool f32 = sizeof(E) == 4;
+    int rc;
+    if (few(S)) rc = launch<E, D, 32, (f32 && D > 64 ? 2 : 4), true>(A, st);
+    else rc = launch<E, D, (f32 ? 32 : 64), 4, false>(A, st);
+    if (rc == BRA_OK && A.splits > 1) rc = join<E, D>(A, (long)S.B * S.Hk, st);
+    return rc;
+}
+
+template <class E>
+int run(const Sizes &S, const Call &A, hipStream_t st)
+{
+    switch (S.width()) {
+    case 32: return run<E, 32>(S, A, st);
+    case 64: return run<E, 64>(S, A, st);
+    case 96: return run<E, 96>(S, A, st);
+    default: return run<E, 128>(S, A, st);
+    }
+}
+
+}  // namespace
+
+Call make_call(const Sizes &S)
+{
+    Call A{};
+    A.q_lens = S.q_lens;
+    A.k_lens = S.k_lens;
+    A.Nq = S.Nq;
+    A.Nk = S.Nk;
+    A.G = S.group();
+    A.Hk = S.Hk;
+    A.d = S.d;
+    A.magic = A.G > 1 ? (unsigned)((1ull << 32) / A.G + 1) : 0;
+    A.rows = (int)S.rows();
+    A.causal = S.causal;
+    A.scale = S.scale;
+    A.c = S.scale * kLog2e;
+    A.splits = 1;
+    return A;
+}
+
+}  // namespace att
+
+using namespace att;
+
+size_t attention_workspace_bytes(const Sizes &S)
+{
+    const long splits = splits_of(S), rows = S.rows() * S.B * S.Hk;
+    return splits > 1 ? align256(sizeof(float) * splits * rows * S.width()) + align256(2 * sizeof(float) * splits * rows) : 0;
+}
+
+int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, float *lse, void *ws, hipStream_t st)
+{
+    Call A = make_call(S);
+    A.Q = Q;
+    A.K = K;
+    A.V = V;
+    A.O = O;
+    A.lse = lse;
+    A.tiles = (int)row_tiles(S);
+    A.splits = splits_of(S);
+    A.blocks = (long)A.tiles * A.splits * S.B * S.Hk;
+    if (A.splits > 1) {
+        A.part = (float *)ws;
+        A.part_ml = (float *)((char *)ws + align256(sizeof(float) * A.splits * S.rows() * S.B * S.Hk * S.width()));
+    }
+    return S.f32 ? run<float>(S, A, st) : run<bf16_t>(S, A, st);
+}
+
+}  // namespace bra

@@ -5,6 +5,7 @@
 // Functions here take every argument by position; the Python functions of the package give them their names and
 // defaults.  No kernel lives here and nothing is computed.
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -698,6 +699,272 @@ PyObject *py_adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// A [B, N, heads, d] tensor of X's dtype and GPU as it lies in memory: channels next to each other, rows on 16 bytes.
+bra_rows rows_of(const at::Tensor &t, const at::Tensor &X, at::IntArrayRef sizes, const char *text)
+{
+    const int64_t piece = 16 / (int64_t)X.element_size();
+    bool fine = t.is_cuda() && t.device() == X.device() && t.scalar_type() == X.scalar_type() && t.sizes().equals(sizes);
+    bra_rows r{};
+    if (fine && t.numel()) {
+        int64_t stride[3];
+        for (int d = 0; d < 3; ++d) {
+            stride[d] = t.size(d) > 1 ? t.stride(d) : 0;
+            fine = fine && stride[d] % piece == 0;
+        }
+        fine = fine && (t.size(3) == 1 || t.stride(3) == 1) && (uintptr_t)t.data_ptr() % 16 == 0;
+        r = bra_rows{t.data_ptr(), stride[0], stride[1], stride[2]};
+    }
+    if (!fine) value_error(text);
+    return r;
+}
+
+// What is written: no two elements in one place, and not where something that is read or written lies (as far as views of one buffer tell).
+void own_memory(const at::Tensor &t, std::initializer_list<const at::Tensor *> others)
+{
+    if (!t.numel()) return;
+    if (at::has_internal_overlap(t) == at::MemOverlap::Yes) value_error("an output overlaps itself");
+    for (const at::Tensor *o : others) {
+        if (!o || !o->numel()) continue;
+        const auto status = at::get_overlap_status(t, *o);
+        if (t.data_ptr() == o->data_ptr() || status == at::MemOverlapStatus::Full || status == at::MemOverlapStatus::Partial) value_error("an output shares memory with another tensor of the call");
+    }
+}
+
+// Attention's operands: Q [B, Nq, heads, d], K and V [B, Nk, kv_heads, d].
+struct AttentionCall {
+    bra_attention_shape s;
+    bra_rows Q, K, V;
+    const int32_t *q_lens, *k_lens;
+};
+AttentionCall attention_call(const at::Tensor &Q, const at::Tensor &K, const at::Tensor &V, PyObject *causal, PyObject *q_lens, PyObject *k_lens, PyObject *scale)
+{
+    if (Q.dim() != 4 || K.dim() != 4) value_error("Q must be [B, Nq, heads, d], K and V [B, Nk, kv_heads, d]");
+    const int dtype = dtype_of(Q);
+    for (int d = 0; d < 4; ++d)
+        if (Q.size(d) > INT32_MAX || K.size(d) > INT32_MAX) check(BRA_ERR_SHAPE);
+    if (K.size(0) != Q.size(0) || K.size(3) != Q.size(3)) value_error("Q must be [B, Nq, heads, d], K and V [B, Nk, kv_heads, d]");
+    AttentionCall c{};
+    const int truth = PyObject_IsTrue(causal);
+    if (truth < 0) throw Raised{};
+    c.s = bra_attention_shape{(int32_t)Q.size(0), (int32_t)Q.size(1), (int32_t)K.size(1), (int32_t)Q.size(2), (int32_t)K.size(2), (int32_t)Q.size(3), dtype, truth, scale_of(scale)};
+    size_t bytes;
+    check(bra_attention_workspace_bytes(&c.s, &bytes));       // the shape before the strides
+    const char *text = "Q, K and V must be on one GPU, of one dtype, [B, N, heads, d] with channels next to each other and every row on 16 bytes";
+    c.Q = rows_of(Q, Q, Q.sizes(), text);
+    c.K = rows_of(K, Q, K.sizes(), text);
+    c.V = rows_of(V, Q, K.sizes(), text);
+    const at::Tensor *q = tensor(q_lens), *k = tensor(k_lens);
+    same_place(q, Q, at::kInt, {Q.size(0)}, "q_lens and k_lens must be contiguous int32 [B] tensors on the queries' GPU");
+    same_place(k, Q, at::kInt, {Q.size(0)}, "q_lens and k_lens must be contiguous int32 [B] tensors on the queries' GPU");
+    c.q_lens = (const int32_t *)data(q);
+    c.k_lens = (const int32_t *)data(k);
+    return c;
+}
+
+// Scratch of `bytes`, none where it is 0.
+const at::Tensor *workspace_if(const at::Tensor *ws, size_t bytes, const at::Tensor &X, at::Tensor &own)
+{
+    if (!ws && !bytes) return nullptr;
+    return workspace(ws, bytes, X, own);
+}
+
+// attention_forward(Q, K, V, causal, q_lens, k_lens, scale, want_lse, ws, out)
+PyObject *py_attention_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&]() -> PyObject * {
+        const at::Tensor &Q = need(a[0]), &K = need(a[1]), &V = need(a[2]);
+        const AttentionCall c = attention_call(Q, K, V, a[3], a[4], a[5], a[6]);
+        const at::Tensor *out = tensor(a[9]);
+        const c10::DeviceGuard guard(Q.device());
+        at::Tensor own, lse, O = out ? *out : at::empty(Q.sizes(), Q.options());
+        const bra_rows o = rows_of(O, Q, Q.sizes(), "out must be a tensor of Q's shape and dtype on its GPU, channels next to each other and every row on 16 bytes");
+        if (out) own_memory(*out, {&Q, &K, &V});
+        const bool want_lse = PyObject_IsTrue(a[7]);
+        if (want_lse) lse = at::empty({Q.size(0), Q.size(2), Q.size(1)}, Q.options().dtype(at::kFloat));
+        size_t bytes = 0;
+        check(bra_attention_workspace_bytes(&c.s, &bytes));
+        const at::Tensor *ws = workspace_if(tensor(a[8]), bytes, Q, own);
+        void *st = stream_of(Q);
+        run([&] {
+            return bra_attention_forward(&c.s, &c.Q, &c.K, &c.V, c.q_lens, c.k_lens, &o, want_lse ? (float *)lse.data_ptr() : nullptr, data(ws), ws ? (size_t)ws->numel() : 0, st);
+        });
+        PyObject *r;
+        if (out) Py_INCREF(r = a[9]);
+        else r = wrap(O);
+        return want_lse ? tuple({r, wrap(lse)}) : r;
+    });
+}
+
+// attention_backward(Q, K, V, O, lse, dO, causal, q_lens, k_lens, scale, ws, out)
+PyObject *py_attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&]() -> PyObject * {
+        const at::Tensor &Q = need(a[0]), &K = need(a[1]), &V = need(a[2]), &O = need(a[3]), &lse = need(a[4]), &dO = need(a[5]);
+        const AttentionCall c = attention_call(Q, K, V, a[6], a[7], a[8], a[9]);
+        const char *text = "O and dO must be tensors of Q's shape and dtype on its GPU, channels next to each other and every row on 16 bytes";
+        const bra_rows o = rows_of(O, Q, Q.sizes(), text), go = rows_of(dO, Q, Q.sizes(), text);
+        same_place(&lse, Q, at::kFloat, {Q.size(0), Q.size(2), Q.size(1)}, "lse must be what bra_attention_forward returned: contiguous float32 [B, heads, Nq] on the queries' GPU");
+        const c10::DeviceGuard guard(Q.device());
+        at::Tensor own, grads[3];
+        bra_rows d[3];
+        PyObject *objects[3] = {};
+        const bool given = a[11] != Py_None;
+        if (given) {
+            const Items outs(a[11], "out must be three tensors");
+            if (outs.n != 3) value_error("out must be three tensors");
+            for (int i = 0; i < 3; ++i) grads[i] = need(outs[i]);
+        }
+        for (int i = 0; i < 3; ++i) {
+            const at::Tensor &like_of = i ? K : Q;
+            if (!given) grads[i] = at::empty(like_of.sizes(), Q.options());
+            d[i] = rows_of(grads[i], Q, like_of.sizes(), "out must be tensors of Q's, K's and V's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes");
+        }
+        if (given)
+            for (int i = 0; i < 3; ++i) own_memory(grads[i], {&Q, &K, &V, &O, &dO, &grads[(i + 1) % 3], &grads[(i + 2) % 3]});
+        size_t bytes = 0;
+        check(bra_attention_backward_workspace_bytes(&c.s, &bytes));
+        const at::Tensor *ws = workspace(tensor(a[10]), bytes, Q, own);
+        void *st = stream_of(Q);
+        run([&] {
+            return bra_attention_backward(&c.s, &c.Q, &c.K, &c.V, &o, (const float *)lse.data_ptr(), &go, c.q_lens, c.k_lens, &d[0], &d[1], &d[2], ws->data_ptr(), (size_t)ws->numel(), st);
+        });
+        for (int i = 0; i < 3; ++i) objects[i] = wrap(grads[i]);        // (the caller's own object where it gave one)
+        return tuple({objects[0], objects[1], objects[2]});
+    });
+}
+
+// The operands of the norms and the rotation of queries and keys: Q [B, N, heads, d], K [B, N, kv_heads, d] or None.
+struct QkNormCall {
+    bra_qk_norm_shape s;
+    bra_qk_norm_params p;
+    bra_rows Q, K;
+};
+const char *const kQkRows = "Q and K must be on one GPU, of one dtype, [B, N, heads, d] with channels next to each other and every row on 16 bytes";
+QkNormCall qk_norm_call(const at::Tensor &Q, const at::Tensor *K, PyObject *q_gamma, PyObject *k_gamma, PyObject *cos, PyObject *sin, PyObject *positions, PyObject *pairs, PyObject *eps)
+{
+    if (Q.dim() != 4 || (K && K->dim() != 4)) value_error("Q must be [B, N, heads, d], K [B, N, kv_heads, d]");
+    const int dtype = dtype_of(Q);
+    for (int d = 0; d < 4; ++d)
+        if (Q.size(d) > INT32_MAX || (K && K->size(d) > INT32_MAX)) check(BRA_ERR_SHAPE);
+    if (K && (K->size(0) != Q.size(0) || K->size(1) != Q.size(1) || K->size(3) != Q.size(3) || K->size(2) < 1)) value_error("Q must be [B, N, heads, d], K [B, N, kv_heads, d]");
+    const at::Tensor *qg = tensor(q_gamma), *kg = tensor(k_gamma), *co = tensor(cos), *si = tensor(sin), *at_ = tensor(positions);
+    const int64_t B = Q.size(0), N = Q.size(1), d = Q.size(3);
+    same_place(qg, Q, at::kFloat, {d}, "q_gamma and k_gamma must be contiguous float32 [d] tensors on the queries' GPU");
+    same_place(kg, Q, at::kFloat, {d}, "q_gamma and k_gamma must be contiguous float32 [d] tensors on the queries' GPU");
+    if (K ? !qg != !kg : kg != nullptr) value_error("q_gamma and k_gamma go together, and k_gamma with K");
+    if (!co != !si) value_error("cos and sin go together");
+    if (at_ && !co) value_error("positions without cos and sin");
+    QkNormCall c{};
+    if (co) {
+        if (co->dim() != 2 || co->size(0) > INT32_MAX || 2 * co->size(1) > d) value_error("cos and sin must be contiguous float32 [positions, rotated channels / 2] tensors on the queries' GPU");
+        for (const at::Tensor *t : {co, si})
+            same_place(t, Q, at::kFloat, {co->size(0), co->size(1)}, "cos and sin must be contiguous float32 [positions, rotated channels / 2] tensors on the queries' GPU");
+    }
+    same_place(at_, Q, at::kInt, {B, N}, "positions must be a contiguous int32 [B, N] tensor on the queries' GPU");
+    c.s = bra_qk_norm_shape{(int32_t)B, (int32_t)N, (int32_t)Q.size(2), K ? (int32_t)K->size(2) : 0, (int32_t)d, co ? (int32_t)(2 * co->size(1)) : 0, co ? (int32_t)co->size(0) : 0,
+                            integer(pairs), dtype, (float)real(eps)};
+    size_t bytes;
+    check(bra_qk_norm_backward_workspace_bytes(&c.s, &bytes));        // the shape before the strides
+    c.p = bra_qk_norm_params{(const float *)data(qg), (const float *)data(kg), (const float *)data(co), (const float *)data(si), (const int32_t *)data(at_)};
+    c.Q = rows_of(Q, Q, Q.sizes(), kQkRows);
+    if (K) c.K = rows_of(*K, Q, K->sizes(), kQkRows);
+    return c;
+}
+
+// The results' places: the caller's (out, a pair; its second entry is not looked at without K) or new tensors.
+struct Pair {
+    at::Tensor Q, K;
+    bra_rows q{}, k{};
+    bool given = false;
+    Pair(PyObject *out, const at::Tensor &likeQ, const at::Tensor *likeK)
+    {
+        if (out == Py_None) {
+            Q = at::empty(likeQ.sizes(), likeQ.options());
+            if (likeK) K = at::empty(likeK->sizes(), likeQ.options());
+        } else {
+            const Items outs(out, "out must be two tensors");
+            if (outs.n != 2) value_error("out must be two tensors");
+            Q = need(outs[0]);
+            if (likeK) K = need(outs[1]);
+            given = true;
+        }
+        const char *text = "out must be tensors of Q's and K's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes";
+        q = rows_of(Q, likeQ, likeQ.sizes(), text);
+        if (likeK) k = rows_of(K, likeQ, likeK->sizes(), text);
+    }
+    // An output may be an input of its own kind, at the same places.
+    void check_memory(std::initializer_list<const at::Tensor *> ofQ, std::initializer_list<const at::Tensor *> ofK)
+    {
+        auto same = [](const at::Tensor &t, const at::Tensor *o) { return o && o->data_ptr() == t.data_ptr() && o->strides().equals(t.strides()) && o->sizes().equals(t.sizes()); };
+        if (!given) return;
+        for (const at::Tensor *o : ofQ) {
+            if (!same(Q, o)) own_memory(Q, {o});
+            if (K.defined()) own_memory(K, {o});
+        }
+        for (const at::Tensor *o : ofK) {
+            if (K.defined() && !same(K, o)) own_memory(K, {o});
+            own_memory(Q, {o});
+        }
+        own_memory(Q, {});
+        if (K.defined()) own_memory(K, {&Q});
+    }
+    PyObject *take(int i) { return wrap(i ? K : Q); }      // (the caller's own object where it gave one)
+};
+
+PyObject *none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+
+// qk_norm_forward(Q, K, q_gamma, k_gamma, cos, sin, positions, pairs, eps, out)
+PyObject *py_qk_norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&]() -> PyObject * {
+        const at::Tensor &Q = need(a[0]), *K = tensor(a[1]);
+        const QkNormCall c = qk_norm_call(Q, K, a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
+        const c10::DeviceGuard guard(Q.device());
+        Pair out(a[9], Q, K);
+        out.check_memory({&Q}, {K});
+        void *st = stream_of(Q);
+        run([&] { return bra_qk_norm_forward(&c.s, &c.Q, K ? &c.K : nullptr, &c.p, &out.q, K ? &out.k : nullptr, st); });
+        return tuple({out.take(0), K ? out.take(1) : none()});
+    });
+}
+
+// qk_norm_backward(Q, K, dQ, dK, q_gamma, k_gamma, cos, sin, positions, pairs, eps, ws, out)
+PyObject *py_qk_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 13, [&]() -> PyObject * {
+        const at::Tensor &Q = need(a[0]), *K = tensor(a[1]), &gQ = need(a[2]), *gK = tensor(a[3]);
+        const QkNormCall c = qk_norm_call(Q, K, a[4], a[5], a[6], a[7], a[8], a[9], a[10]);
+        if (!K != !gK) value_error("K and dK go together");
+        const bra_rows gq = rows_of(gQ, Q, Q.sizes(), "dQ and dK must be tensors of Q's and K's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes");
+        bra_rows gk{};
+        if (K) gk = rows_of(*gK, Q, K->sizes(), "dQ and dK must be tensors of Q's and K's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes");
+        const c10::DeviceGuard guard(Q.device());
+        Pair out(a[12], Q, K);
+        out.check_memory({&Q, &gQ}, {K, gK});
+        const bool norm = c.p.q_gamma != nullptr;
+        at::Tensor own, dq_gamma, dk_gamma;
+        const at::Tensor *ws = nullptr;
+        if (norm) {
+            dq_gamma = at::empty({(int64_t)c.s.d}, Q.options().dtype(at::kFloat));
+            if (K) dk_gamma = at::empty({(int64_t)c.s.d}, Q.options().dtype(at::kFloat));
+            size_t bytes = 0;
+            check(bra_qk_norm_backward_workspace_bytes(&c.s, &bytes));
+            ws = workspace(tensor(a[11]), bytes, Q, own);
+        }
+        void *st = stream_of(Q);
+        run([&] {
+            return bra_qk_norm_backward(&c.s, &c.Q, K ? &c.K : nullptr, &c.p, &gq, K ? &gk : nullptr, &out.q, K ? &out.k : nullptr, norm ? (float *)dq_gamma.data_ptr() : nullptr,
+                                        norm && K ? (float *)dk_gamma.data_ptr() : nullptr, data(ws), ws ? (size_t)ws->numel() : 0, st);
+        });
+        if (!norm) return tuple({out.take(0), K ? out.take(1) : none()});
+        return tuple({out.take(0), K ? out.take(1) : none(), wrap(dq_gamma), K ? wrap(dk_gamma) : none()});
+    });
+}
+
 PyMethodDef methods[] = {
     {"init", (PyCFunction)(void *)py_init, METH_FASTCALL, nullptr},
     {"route", (PyCFunction)(void *)py_route, METH_FASTCALL, nullptr},
@@ -711,6 +978,10 @@ PyMethodDef methods[] = {
     {"norm_forward", (PyCFunction)(void *)py_norm_forward, METH_FASTCALL, nullptr},
     {"norm_backward", (PyCFunction)(void *)py_norm_backward, METH_FASTCALL, nullptr},
     {"adamw_step", (PyCFunction)(void *)py_adamw_step, METH_FASTCALL, nullptr},
+    {"attention_forward", (PyCFunction)(void *)py_attention_forward, METH_FASTCALL, nullptr},
+    {"attention_backward", (PyCFunction)(void *)py_attention_backward, METH_FASTCALL, nullptr},
+    {"qk_norm_forward", (PyCFunction)(void *)py_qk_norm_forward, METH_FASTCALL, nullptr},
+    {"qk_norm_backward", (PyCFunction)(void *)py_qk_norm_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,383 @@
+// Norms of queries and keys for each head, and the rotation of their channels by position, in one pass over both:
+//     u = x / sqrt(mean of squares + eps) gamma,   (a, b) -> (a cos - b sin, b cos + a sin) for each pair of the first `turned` channels
+// and backwards g = R^T dy, dgamma = sum g x / rms, dx = (g gamma - x / rms mean(g gamma x / rms)) / rms.
+// A team of lanes has a row (a head of a token) in registers, each lane two chunks of V channels that hold whole pairs, and works on RPT heads
+// of a token, which share the angles.  Bound by memory.
+#include "bra_mfma_dev.h"
+#include "bra_qk_norm.h"
+
+#include <algorithm>
+
+namespace bra {
+
+using namespace mfma;
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Work {
+    QkNormIn I;
+    att::Rows gQ, gK, oQ, oK;   // what comes back (backward), what is written
+    unsigned N, groups;         // a token's heads go to `groups` teams
+    int heads, all, d, turned, table_rows, team;
+    float eps, d_inv;
+    bool halves;
+    unsigned items;             // tokens x groups
+    float *sums;                // [workgroups][2][d]
+};
+
+template <class E, int V>
+__device__ __forceinline__ void load(const char *p, float (&x)[V])
+{
+    if constexpr (sizeof(E) == 4) {
+        typedef float vec __attribute__((ext_vector_type(V)));
+        if constexpr (V == 1) x[0] = *(const float *)p;
+        else {
+            const vec v = *(const vec *)p;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = v[e];
+        }
+    } else if constexpr (V == 1) x[0] = bf16_to_f32(*(const bf16_t *)p);
+    else {
+        typedef unsigned vec __attribute__((ext_vector_type(V / 2)));
+        if constexpr (V == 2) {
+            const unsigned v = *(const unsigned *)p;
+            x[0] = bf16_lo(v);
+            x[1] = bf16_hi(v);
+        } else {
+            const vec v = *(const vec *)p;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = e % 2 ? bf16_hi(v[e / 2]) : bf16_lo(v[e / 2]);
+        }
+    }
+}
+
+template <class E, int V>
+__device__ __forceinline__ void store(char *p, const float (&x)[V])
+{
+    if constexpr (V == 1) store_from_f32((E *)p, x[0]);
+    else if constexpr (sizeof(E) == 4) {
+        typedef float vec __attribute__((ext_vector_type(V)));
+        vec v;
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = x[e];
+        *(vec *)p = v;
+    } else if constexpr (V == 2) *(unsigned *)p = pack_bf16(x[0], x[1]);
+    else {
+        typedef unsigned vec __attribute__((ext_vector_type(V / 2)));
+        vec v;
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) v[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+        *(vec *)p = v;
+    }
+}
+
+// Values of a float32 vector whose alignment is that of its elements.
+template <int V>
+__device__ __forceinline__ void load_vector(const float *p, float (&x)[V])
+{
+    if (V % 4 == 0 && (uintptr_t)p % 16 == 0) {
+#pragma unroll
+        for (int e = 0; e < V / 4; ++e) {
+            const f32x4 v = *(const f32x4 *)(p + 4 * e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * e + i] = v[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = p[e];
+}
+
+__device__ __forceinline__ float team_sum(float v, int team)
+{
+    if (team > 1) v = dpp_fadd<0xB1>(v);        // lane ^ 1
+    if (team > 2) v = dpp_fadd<0x4E>(v);        // lane ^ 2
+    if (team > 4) v = dpp_fadd<0x141>(v);       // mirrored halves of 8
+    if (team > 8) v = dpp_fadd<0x140>(v);       // mirrored rows of 16
+    if (team > 16) v += __shfl_xor(v, 16);
+    if (team > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// The pairs of chunks a, b rotated.  halves: pairs are a[i], b[i], else neighbours within them.
+template <int V>
+__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (&cos)[V], const float (&sin)[V], bool halves)
+{
+    if (halves || V == 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float u = a[e], v = b[e];
+            a[e] = u * cos[e] - v * sin[e];
+            b[e] = v * cos[e] + u * sin[e];
+        }
+        return;
+    }
+    if constexpr (V > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float (&x)[V] = e < V / 2 ? a : b;
+            const int i = 2 * (e % (V / 2));
+            const float u = x[i], v = x[i + 1];
+            x[i] = u * cos[e] - v * sin[e];
+            x[i + 1] = v * cos[e] + u * sin[e];
+        }
+    }
+}
+
+template <class E, int V, int RPT, bool BACK>
+__global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
+{
+    const int lane = threadIdx.x % W.team, teams = kThreads / W.team;
+    const bool active = 2 * V * lane < W.d, turned = 2 * V * lane < W.turned;
+    const int unit = active ? lane : 0, ca = turned && W.halves ? V * unit : 2 * V * unit, cb = turned && W.halves ? W.turned / 2 + V * unit : ca + V;
+    const bool norm = W.I.q_gamma != nullptr;
+    float gamma[2][2 * V], sums[2][2 * V];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+            gamma[k][e] = 1.f;
+            sums[k][e] = 0.f;
+        }
+    if (norm) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float *g = k ? W.I.k_gamma : W.I.q_gamma;
+            if (!g) continue;
+            float t[V];
+            load_vector<V>(g + ca, t);
+#pragma unroll
+            for (int e = 0; e < V; ++e) gamma[k][e] = t[e];
+            load_vector<V>(g + cb, t);
+#pragma unroll
+            for (int e = 0; e < V; ++e) gamma[k][V + e] = t[e];
+        }
+    }
+    for (unsigned item = blockIdx.x * (unsigned)teams + threadIdx.x / W.team; item < W.items; item += gridDim.x * (unsigned)teams) {
+        const unsigned token = item / W.groups, group = item - token * W.groups, b = token / W.N, n = token - b * W.N;
+        float xa[RPT][V], xb[RPT][V], ya[BACK ? RPT : 1][V], yb[BACK ? RPT : 1][V], cos[V], sin[V];
+        // rows that do not exist are read in another's place and not written
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int head = min((int)(group + i * W.groups), W.all - 1);
+            const bool q = head < W.heads;
+            const att::Rows &R = q ? W.I.Q : W.I.K;
+            if (!BACK || norm) {
+                const char *p = R.p + b * R.batch + n * R.token + (q ? head : head - W.heads) * R.head;
+                load<E, V>(p + ca * sizeof(E), xa[i]);
+                load<E, V>(p + cb * sizeof(E), xb[i]);
+            }
+            if constexpr (BACK) {
+                const att::Rows &G = q ? W.gQ : W.gK;
+                const char *p = G.p + b * G.batch + n * G.token + (q ? head : head - W.heads) * G.head;
+                load<E, V>(p + ca * sizeof(E), ya[i]);
+                load<E, V>(p + cb * sizeof(E), yb[i]);
+            }
+        }
+        if (turned) {
+            const int at = W.I.positions ? min(max(W.I.positions[token], 0), W.table_rows - 1) : (int)n;
+            const long pair = (long)at * (W.turned / 2) + V * unit;
+            load_vector<V>(W.I.cos + pair, cos);
+            load_vector<V>(W.I.sin + pair, sin);
+            if (BACK) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) sin[e] = -sin[e];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int head = (int)(group + i * W.groups);
+            const bool q = head < W.heads, live = active && head < W.all;
+            float inv = 1.f;
+            if (norm) {
+                float s = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) s = fmaf(xa[i][e], xa[i][e], fmaf(xb[i][e], xb[i][e], s));
+                inv = 1.0f / sqrtf(fmaf(team_sum(active ? s : 0.f, W.team), W.d_inv, W.eps));
+            }
+            float oa[V], ob[V];
+            if constexpr (!BACK) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    oa[e] = norm ? xa[i][e] * inv * (q ? gamma[0][e] : gamma[1][e]) : xa[i][e];
+                    ob[e] = norm ? xb[i][e] * inv * (q ? gamma[0][V + e] : gamma[1][V + e]) : xb[i][e];
+                }
+                if (turned) turn<V>(oa, ob, cos, sin, W.halves);
+            } else {
+                if (turned) turn<V>(ya[i], yb[i], cos, sin, W.halves);
+                float dot = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    oa[e] = ya[i][e];
+                    ob[e] = yb[i][e];
+                    if (!norm) continue;
+                    xa[i][e] *= inv;
+                    xb[i][e] *= inv;
+                    const float sa = live ? oa[e] * xa[i][e] : 0.f, sb = live ? ob[e] * xb[i][e] : 0.f;
+                    sums[0][e] += q ? sa : 0.f;
+                    sums[1][e] += q ? 0.f : sa;
+                    sums[0][V + e] += q ? sb : 0.f;
+                    sums[1][V + e] += q ? 0.f : sb;
+                    oa[e] *= q ? gamma[0][e] : gamma[1][e];
+                    ob[e] *= q ? gamma[0][V + e] : gamma[1][V + e];
+                    dot = fmaf(oa[e], xa[i][e], fmaf(ob[e], xb[i][e], dot));
+                }
+                if (norm) {
+                    const float mean = team_sum(active ? dot : 0.f, W.team) * W.d_inv;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        oa[e] = inv * (oa[e] - xa[i][e] * mean);
+                        ob[e] = inv * (ob[e] - xb[i][e] * mean);
+                    }
+                }
+            }
+            if (live) {
+                const att::Rows &O = q ? W.oQ : W.oK;
+                char *p = O.p + b * O.batch + n * O.token + (q ? head : head - W.heads) * O.head;
+                store<E, V>(p + ca * sizeof(E), oa);
+                store<E, V>(p + cb * sizeof(E), ob);
+            }
+        }
+    }
+    if constexpr (BACK) {
+        if (!norm) return;
+        // the workgroup's sums: teams of a wavefront first, then its four wavefronts
+        __shared__ float lds[kThreads / 64][2][128];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) {
+                float v = sums[k][e];
+                for (int o = W.team; o < 64; o *= 2) v += __shfl_xor(v, o);
+                if (threadIdx.x % 64 < W.team && active) lds[threadIdx.x / 64][k][e < V ? ca + e : cb + e - V] = v;
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * W.d; i += kThreads) {
+            const int k = i / W.d, c = i % W.d;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kThreads / 64; ++w) v += lds[w][k][c];
+            W.sums[(long)blockIdx.x * 2 * W.d + i] = v;
+        }
+    }
+}
+
+// Sums of the workgroups' sums: 16 columns to a workgroup, 16 shares of the rows.
+__global__ __launch_bounds__(256) void k_qk_norm_sums(const float *sums, int rows, int d, float *dq, float *dk)
+{
+    __shared__ float lds[16][17];
+    const int col = threadIdx.x % 16, share = threadIdx.x / 16, c = blockIdx.x * 16 + col;
+    float v = 0.f;
+    if (c < 2 * d)
+        for (int r = share; r < rows; r += 16) v += sums[(long)r * 2 * d + c];
+    lds[share][col] = v;
+    __syncthreads();
+    if (share || c >= 2 * d) return;
+    v = 0.f;
+#pragma unroll
+    for (int s = 0; s < 16; ++s) v += lds[s][col];
+    float *out = c < d ? dq : dk;
+    if (out) out[c < d ? c : c - d] = v;
+}
+
+// Channels of a chunk: whole pairs of the rotated part to a lane, chunks of up to 16 bytes.
+int chunk(const QkNormSizes &S)
+{
+    int V = S.f32 ? 4 : 8;
+    while (S.turned % (2 * V) || S.d % (2 * V)) V /= 2;
+    return V;
+}
+int team_of(const QkNormSizes &S, int V)
+{
+    int t = 1;
+    while (2 * V * t < S.d) t *= 2;
+    return t;
+}
+// Heads of a token to a team.
+int rows_per_team(const QkNormSizes &S) { return S.tokens * (S.heads + S.kv_heads) >= 16384 ? 4 : 1; }
+long workgroups(const QkNormSizes &S, bool back)
+{
+    const int rpt = rows_per_team(S), teams = kThreads / team_of(S, chunk(S));
+    const long items = S.tokens * ((S.heads + S.kv_heads + rpt - 1) / rpt), blocks = (items + teams - 1) / teams;
+    return std::min(blocks, back ? 1024L : 1L << 20);
+}
+
+template <class E, int V, bool BACK>
+int launch(const QkNormSizes &S, const Work &W, int rpt, hipStream_t st)
+{
+    const ProfScope scope(st, BACK ? K_QK_NORM_BACKWARD : K_QK_NORM);
+    const unsigned blocks = (unsigned)workgroups(S, BACK);
+    if (rpt == 4) k_qk_norm<E, V, 4, BACK><<<blocks, kThreads, 0, st>>>(W);
+    else k_qk_norm<E, V, 1, BACK><<<blocks, kThreads, 0, st>>>(W);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+template <class E, bool BACK>
+int pick(const QkNormSizes &S, const Work &W, int rpt, hipStream_t st)
+{
+    switch (chunk(S)) {
+    case 8:
+        if constexpr (sizeof(E) == 2) return launch<E, 8, BACK>(S, W, rpt, st);
+        [[fallthrough]];
+    case 4: return launch<E, 4, BACK>(S, W, rpt, st);
+    case 2: return launch<E, 2, BACK>(S, W, rpt, st);
+    default: return launch<E, 1, BACK>(S, W, rpt, st);
+    }
+}
+
+Work make_work(const QkNormSizes &S, const QkNormIn &I, int rpt)
+{
+    Work W{};
+    W.I = I;
+    W.N = (unsigned)S.N;
+    W.all = S.heads + S.kv_heads;
+    W.groups = (unsigned)((W.all + rpt - 1) / rpt);
+    W.heads = S.heads;
+    W.d = S.d;
+    W.turned = S.turned;
+    W.table_rows = S.table_rows;
+    W.team = team_of(S, chunk(S));
+    W.eps = S.eps;
+    W.d_inv = 1.0f / (float)S.d;
+    W.halves = S.halves;
+    W.items = (unsigned)(S.tokens * W.groups);
+    return W;
+}
+
+}  // namespace
+
+int qk_norm_forward(const QkNormSizes &S, const QkNormIn &I, const att::Rows &Qout, const att::Rows &Kout, hipStream_t st)
+{
+    if (S.tokens == 0) return BRA_OK;
+    const int rpt = rows_per_team(S);
+    Work W = make_work(S, I, rpt);
+    W.oQ = Qout;
+    W.oK = Kout;
+    return S.f32 ? pick<float, false>(S, W, rpt, st) : pick<bf16_t, false>(S, W, rpt, st);
+}
+
+size_t qk_norm_backward_workspace_bytes(const QkNormSizes &S) { return align256(sizeof(float) * 2 * S.d * workgroups(S, true)); }
+
+int qk_norm_backward(const QkNormSizes &S, const QkNormIn &I, const att::Rows &gQ, const att::Rows &gK, const att::Rows &dQ, const att::Rows &dK, float *dq_gamma,
+                     float *dk_gamma, void *ws, hipStream_t st)
+{
+    const int rpt = rows_per_team(S);
+    Work W = make_work(S, I, rpt);
+    W.gQ = gQ;
+    W.gK = gK;
+    W.oQ = dQ;
+    W.oK = dK;
+    W.sums = (float *)ws;
+    if (S.tokens > 0) {
+        const int rc = S.f32 ? pick<float, true>(S, W, rpt, st) : pick<bf16_t, true>(S, W, rpt, st);
+        if (rc != BRA_OK) return rc;
+    }
+    if (!I.q_gamma || (!dq_gamma && !dk_gamma)) return BRA_OK;
+    const ProfScope scope(st, K_QK_NORM_SUMS);
+    k_qk_norm_sums<<<(2 * S.d + 15) / 16, 256, 0, st>>>(W.sums, (int)workgroups(S, true), S.d, dq_gamma, dk_gamma);
+    return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
+}
+
+}  // namespace bra
