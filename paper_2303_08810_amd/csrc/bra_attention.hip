@@ -148,30 +148,49 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     if (valid) finish<E, G>(A, b, hk, split, row, h, acc, m, l);
 }
 
-// The splits' sums put together: a thread has 8 channels of a row.
+// The splits' sums put together.  A thread has 8 channels of a row and every `groups`-th of its splits (one after another they took 26 us for
+// 32 splits of 256 rows, this way 6); the groups meet in LDS.
 template <class E, int D>
-__global__ __launch_bounds__(256) void k_attention_join(Call A)
+__global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 {
     constexpr int CH = D / 8;
-    const long i = (A.first + blockIdx.x) * 256 + threadIdx.x, rows = A.blocks * A.rows;       // here blocks: sequences x key heads
-    if (i >= rows * CH) return;
-    const long r = i / CH;
-    const int ch = 8 * (int)(i % CH), row = (int)(r % A.rows), hb = (int)(r / A.rows), b = hb / A.Hk, hk = hb % A.Hk;
+    __shared__ float lds[256][11];
+    const int per = 256 / (CH * groups), ch = 8 * (threadIdx.x % CH), group = threadIdx.x / CH % groups, slot = threadIdx.x / (CH * groups);
+    const long r = (A.first + blockIdx.x) * per + slot, rows = A.blocks * A.rows;           // here blocks: sequences x key heads
+    const bool valid = slot < per && r < rows;
+    const int row = valid ? (int)(r % A.rows) : 0, hb = valid ? (int)(r / A.rows) : 0, b = hb / A.Hk, hk = hb % A.Hk;
     const long at = (long)hb * A.splits * A.rows + row;
-    float top = -INFINITY;
-    for (int s = 0; s < A.splits; ++s) top = fmaxf(top, A.part_ml[2 * (at + (long)s * A.rows)]);
-    float o[8] = {}, l = 0.f;
-    for (int s = 0; s < A.splits; ++s) {
-        const long p = at + (long)s * A.rows;
-        const float m = A.part_ml[2 * p], factor = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        l = fmaf(factor, A.part_ml[2 * p + 1], l);
-        const f32x4 v0 = *(const f32x4 *)(A.part + p * D + ch), v1 = *(const f32x4 *)(A.part + p * D + ch + 4);
+    float top = -INFINITY, l = 0.f, o[8] = {};
+    auto add = [&](float m, float sum, const float (&v)[8]) {
+        const float next = fmaxf(top, m), old = next == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next), factor = next == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        top = next;
+        l = fmaf(factor, sum, l * old);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = fmaf(factor, v0[e], o[e]);
-            o[4 + e] = fmaf(factor, v1[e], o[4 + e]);
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(factor, v[e], o[e] * old);
+    };
+    if (valid)
+#pragma unroll 4
+        for (int s = group; s < A.splits; s += groups) {
+            const long p = at + (long)s * A.rows;
+            const f32x4 v0 = *(const f32x4 *)(A.part + p * D + ch), v1 = *(const f32x4 *)(A.part + p * D + ch + 4);
+            const f32x2 ml = *(const f32x2 *)(A.part_ml + 2 * p);
+            const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            add(ml[0], ml[1], v);
+        }
+    if (groups > 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lds[threadIdx.x][e] = o[e];
+        lds[threadIdx.x][8] = top;
+        lds[threadIdx.x][9] = l;
+        __syncthreads();
+        if (group) return;
+        for (int g = 1; g < groups; ++g) {
+            const float *from = lds[threadIdx.x + g * CH];
+            const float v[8] = {from[0], from[1], from[2], from[3], from[4], from[5], from[6], from[7]};
+            add(from[8], from[9], v);
         }
     }
+    if (!valid) return;
     const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -213,11 +232,14 @@ int launch(Call A, hipStream_t st)
 template <class E, int D>
 int join(Call A, long heads, hipStream_t st)
 {
+    constexpr int CH = D / 8;
     A.blocks = heads;
-    const long blocks = (heads * A.rows * (D / 8) + 255) / 256;
+    int groups = 1;
+    while (2 * groups * CH <= 256 && 2 * groups <= A.splits) groups *= 2;
+    const long per = 256 / (CH * groups), blocks = (heads * A.rows + per - 1) / per;
     for (A.first = 0; A.first < blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_JOIN);
-        k_attention_join<E, D><<<(unsigned)std::min(kMaxBlocks, blocks - A.first), 256, 0, st>>>(A);
+        k_attention_join<E, D><<<(unsigned)std::min(kMaxBlocks, blocks - A.first), 256, 0, st>>>(A, groups);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;

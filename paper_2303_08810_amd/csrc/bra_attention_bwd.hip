@@ -27,7 +27,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
     const long block = swizzled(A.first + blockIdx.x, A.blocks);
-    const int tile = A.tiles - 1 - (int)(block % A.tiles), hb = (int)(block / A.tiles), b = hb / A.Hk, hk = hb % A.Hk;
+    const int tile = A.tiles - 1 - (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);
+    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     const int least = columns_min(limit), most = columns_max(limit);
     int end = 0;
     if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
-    const int last = (end + KT - 1) / KT;
+    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, from = split * share, last = min(all, from + share);
 
     const unsigned ring_at = lds_address(lds);
     const char *keys = A.K.p + b * A.K.batch + hk * A.K.head, *values = A.V.p + b * A.V.batch + hk * A.V.head;
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         F::Loads::request([&](int r) { return k + r * A.K.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer, threadIdx.x);
         F::Loads::request([&](int r) { return v + r * A.V.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + F::kTile, threadIdx.x);
     };
-    if (last > 0) request(0, 0);
+    if (from < last) request(from, 0);
 
     typename G::Piece x[G::kSteps], g[G::kSteps];
     load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         delta = pair_sum(delta);
         if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
-        if (valid && h == 0) {
+        if (valid && h == 0 && split == 0) {
             A.row_lse[(long)hb * A.rows + row] = lse;
             A.row_delta[(long)hb * A.rows + row] = delta;
         }
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
 
     f32x16 acc[G::NT];
     clear(acc);
-    for (int t = 0, buffer = 0; t < last; ++t, buffer ^= 1) {
+    for (int t = from, buffer = 0; t < last; ++t, buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -95,7 +96,9 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
             multiply_columns<G>(acc, kt, 32 * i, s[0], lane);
         }
     }
-    if (valid) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
+    if (A.splits > 1) {
+        if (valid) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, D, h);
+    } else if (valid) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
 }
 
 template <class E, int D, int RT, int WAVES>
@@ -107,7 +110,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
     const long block = swizzled(A.first + blockIdx.x, A.blocks);
-    const int tile = (int)(block % A.tiles), hb = (int)(block / A.tiles), b = hb / A.Hk, hk = hb % A.Hk;     // those of a causal mask's long columns first
+    const int tile = (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);      // those of a causal mask's long columns first
+    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
@@ -134,7 +138,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
                           threadIdx.x);
         if (wave < 2) load4_to_lds_untracked((wave ? row_delta : row_lse) + min(r0 + lane, A.rows - 1), at + F::kBuffer + 4 * RT * wave);
     };
-    const int from = first_key < seq.nk ? begin_of(first_key) / RT : 0, last = first_key < seq.nk ? (end + RT - 1) / RT : 0;
+    const int front = begin_of(first_key) / RT, all = first_key < seq.nk ? max((end + RT - 1) / RT - front, 0) : 0, share = (all + A.splits - 1) / A.splits;
+    const int from = front + split * share, last = front + min(all, (split + 1) * share);
     f32x16 dk[G::NT], dv[G::NT];
     clear(dk);
     clear(dv);
@@ -178,36 +183,106 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
             multiply_columns<G>(dk, qt, 32 * i, s[1], lane);
         }
     }
-    if (key < A.Nk) {
+    if (key >= A.Nk) return;
+    if (A.splits > 1) {
+        float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
+        store_columns<float, G>((char *)part, dk, A.scale, D, h);
+        store_columns<float, G>((char *)(part + D), dv, 1.f, D, h);
+    } else {
         store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, dk, A.scale, A.d, h);
         store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, dv, 1.f, A.d, h);
     }
+}
+
+// The splits' sums put together, in their order: dQ, [heads][splits][rows][D], or dK and dV, [heads][splits][Nk][2][D].
+template <class E, int D, bool KEYS>
+__global__ __launch_bounds__(256) void k_grads_join(Call A)
+{
+    constexpr int CH = D / 8, W = KEYS ? 2 : 1;
+    const long i = (A.first + blockIdx.x) * 256 + threadIdx.x, each = KEYS ? A.Nk : A.rows, n = A.blocks * each * W;      // here blocks: sequences x key heads
+    const int ch = 8 * (int)(i % CH);
+    const long r = i / CH;
+    if (r >= n || ch >= A.d) return;
+    const int which = (int)(r % W), row = (int)(r / W % each), hb = (int)(r / W / each), b = hb / A.Hk, hk = hb % A.Hk;
+    const float *p = A.part + (((long)hb * A.splits * each + row) * W + which) * D + ch;
+    float v[8] = {};
+#pragma unroll 4
+    for (int s = 0; s < A.splits; ++s, p += each * W * D) {
+        const f32x4 v0 = *(const f32x4 *)p, v1 = *(const f32x4 *)(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] += v0[e];
+            v[4 + e] += v1[e];
+        }
+    }
+    if (KEYS) {
+        const Rows &R = which ? A.dV : A.dK;
+        store8<E>(R.p + b * R.batch + row * R.token + hk * R.head + ch * sizeof(E), v);
+    } else {
+        const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
+        store8<E>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head + ch * sizeof(E), v);
+    }
+}
+
+constexpr int kWaves = 4, kRowTile = 64;
+int key_tile(const Sizes &S) { return S.f32 ? 32 : 64; }
+
+// Shares of the keys (of the rows) that workgroups walk over, where there are few of them, or a causal mask makes them of different lengths.
+int splits_of(const Sizes &S, bool keys)
+{
+    const long mine = keys ? S.Nk : S.rows(), walked = keys ? S.rows() : S.Nk;
+    const long blocks = (mine + 32 * kWaves - 1) / (32 * kWaves) * S.B * S.Hk, tiles = (walked + (keys ? kRowTile : key_tile(S)) - 1) / (keys ? kRowTile : key_tile(S));
+    if (blocks == 0) return 1;
+    const long want = S.causal ? 1024 : 512;
+    return (int)std::max(1L, std::min({want / blocks, tiles / 4, 16L}));
+}
+size_t part_bytes(const Sizes &S)
+{
+    const size_t q = splits_of(S, false), k = splits_of(S, true), row = sizeof(float) * S.width() * S.B * S.Hk;
+    return std::max(q > 1 ? q * S.rows() * row : 0, k > 1 ? k * S.Nk * 2 * row : 0);
+}
+
+template <class E, int D, bool KEYS>
+int join(Call A, long heads, hipStream_t st)
+{
+    A.blocks = heads;
+    const long blocks = (heads * (KEYS ? 2L * A.Nk : (long)A.rows) * (D / 8) + 255) / 256;
+    for (A.first = 0; A.first < blocks; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION_JOIN);
+        k_grads_join<E, D, KEYS><<<(unsigned)std::min(kMaxBlocks, blocks - A.first), 256, 0, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
 }
 
 template <class E, int D>
 int run(const Sizes &S, Call A, hipStream_t st)
 {
     constexpr int KT = sizeof(E) == 4 ? 32 : 64;
-    typedef Backward<E, D, KT, 4> FQ;
-    typedef Backward<E, D, 64, 4> FK;
-    int rc = allow_lds<k_query_grads<E, D, KT, 4>>(FQ::kQueryLds);
-    if (rc == BRA_OK) rc = allow_lds<k_key_grads<E, D, 64, 4>>(FK::kKeyLds);
+    typedef Backward<E, D, KT, kWaves> FQ;
+    typedef Backward<E, D, kRowTile, kWaves> FK;
+    const long heads = (long)S.B * S.Hk;
+    int rc = allow_lds<k_query_grads<E, D, KT, kWaves>>(FQ::kQueryLds);
+    if (rc == BRA_OK) rc = allow_lds<k_key_grads<E, D, kRowTile, kWaves>>(FK::kKeyLds);
     if (rc != BRA_OK) return rc;
     A.tiles = (A.rows + FQ::kRows - 1) / FQ::kRows;
-    A.blocks = (long)A.tiles * S.B * S.Hk;
+    A.splits = splits_of(S, false);
+    A.blocks = A.tiles * A.splits * heads;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_QUERY_GRADS);
-        k_query_grads<E, D, KT, 4><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FQ::kThreads, FQ::kQueryLds, st>>>(A);
+        k_query_grads<E, D, KT, kWaves><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FQ::kThreads, FQ::kQueryLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
+    if (A.splits > 1 && (rc = join<E, D, false>(A, heads, st)) != BRA_OK) return rc;
     A.tiles = (A.Nk + FK::kRows - 1) / FK::kRows;
-    A.blocks = (long)A.tiles * S.B * S.Hk;
+    A.splits = splits_of(S, true);
+    A.blocks = A.tiles * A.splits * heads;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_KEY_GRADS);
-        k_key_grads<E, D, 64, 4><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FK::kThreads, FK::kKeyLds, st>>>(A);
+        k_key_grads<E, D, kRowTile, kWaves><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FK::kThreads, FK::kKeyLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
-    return BRA_OK;
+    return A.splits > 1 ? join<E, D, true>(A, heads, st) : BRA_OK;
 }
 
 template <class E>
@@ -226,7 +301,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
 
 using namespace att;
 
-size_t attention_backward_workspace_bytes(const Sizes &S) { return 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk); }
+size_t attention_backward_workspace_bytes(const Sizes &S) { return 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)); }
 
 int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, const float *lse, const Rows &dO, const Rows &dQ, const Rows &dK,
                        const Rows &dV, void *ws, hipStream_t st)
@@ -243,6 +318,7 @@ int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows 
     A.lse_in = lse;
     A.row_lse = (float *)ws;
     A.row_delta = (float *)((char *)ws + align256(sizeof(float) * S.rows() * S.B * S.Hk));
+    A.part = (float *)((char *)A.row_delta + align256(sizeof(float) * S.rows() * S.B * S.Hk));
     return S.f32 ? run<float>(S, A, st) : run<bf16_t>(S, A, st);
 }
 
