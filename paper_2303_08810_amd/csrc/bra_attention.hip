@@ -49,9 +49,9 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const long block = swizzled(A.first + blockIdx.x, A.blocks);
-    const int tile = A.tiles - 1 - (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);     // those of a causal mask's long rows first
-    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
+    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
@@ -73,36 +73,19 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     char *ring = lds + (FEW ? wave * 2 * F::kBuffer : 0);
     const unsigned ring_at = lds_address(ring);
     const int thread = FEW ? lane : threadIdx.x;
-    auto request = [&](int t, int buffer) {
+    auto request = [&](bool value, int t, int buffer) {
+        const long token = value ? A.V.token : A.K.token;
         const int k0 = t * KT;
-        const char *k = keys + k0 * A.K.token, *v = values + k0 * A.V.token;
-        F::Loads::request([&](int r) { return k + r * A.K.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer, thread);
-        F::Loads::request([&](int r) { return v + r * A.V.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + F::kTile, thread);
+        const char *from = (value ? values : keys) + k0 * token;
+        F::Loads::request([&](int r) { return from + r * token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + (value ? F::kTile : 0), thread);
     };
 
     f32x16 acc[G::NT];
     clear(acc);
     Running run;
-    constexpr int kStep = FEW ? WAVES : 1;
-    int t = split * share + (FEW ? wave : 0), buffer = 0;
-    if (t < last) request(t, 0);
-    for (; t < last; t += kStep, buffer ^= 1) {
-        if constexpr (FEW) {
-            lds_reads_done();
-            if (t + kStep < last) {
-                request(t + kStep, buffer ^ 1);
-                asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * F::Loads::L) : "memory");
-            } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (t + 1 < last) request(t + 1, buffer ^ 1);
-        }
-        const int k0 = t * KT;
-        if (k0 >= most) continue;
-        const char *kt = ring + buffer * F::kBuffer, *vt = kt + F::kTile;
-        f32x16 s[KT / 32];
+    const char *kt = ring, *vt = ring + F::kTile;
+    f32x16 s[KT / 32];
+    auto scores = [&](int k0) {
         clear(s);
 #pragma unroll
         for (int i = 0; i < KT / 32; ++i) multiply_rows<G>(s[i], kt, 32 * i, x, lane);
@@ -112,9 +95,61 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[i][r] = k0 + 32 * i + result_row(r, h) < limit ? s[i][r] : -INFINITY;
         }
-        run.weights(s, A.c, acc);
+    };
+    auto outputs = [&] {
 #pragma unroll
         for (int i = 0; i < KT / 32; ++i) multiply_columns<G>(acc, vt, 32 * i, s[i], lane);
+    };
+    if constexpr (FEW) {
+        // Each wavefront for itself, two tiles ahead: keys (values) are asked for as soon as those two tiles before them have been read.
+        // One tile ahead the loads' latency was in the way: 604 MB of keys and values for one token each 146 us.
+        constexpr int L = F::Loads::L;
+        int t = split * share + wave;
+        for (int n = 0; n < 2; ++n)
+            if (t + n * WAVES < last) {
+                request(false, t + n * WAVES, n);
+                request(true, t + n * WAVES, n);
+            }
+        arrived<G>(x);
+        for (int buffer = 0; t < last; t += WAVES, buffer ^= 1) {
+            const bool one = t + WAVES < last, two = t + 2 * WAVES < last;
+            kt = ring + buffer * F::kBuffer;
+            vt = kt + F::kTile;
+            if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(L) : "memory");
+            scores(t * KT);
+            lds_reads_done();
+            if (two) request(false, t + 2 * WAVES, buffer);
+            run.weights(s, A.c, acc);
+            if (two) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
+            else if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * L) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            outputs();
+            lds_reads_done();
+            if (two) request(true, t + 2 * WAVES, buffer);
+        }
+    } else {
+        int t = split * share;
+        if (t < last) {
+            request(false, t, 0);
+            request(true, t, 0);
+        }
+        arrived<G>(x);
+        for (int buffer = 0; t < last; ++t, buffer ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + 1 < last) {
+                request(false, t + 1, buffer ^ 1);
+                request(true, t + 1, buffer ^ 1);
+            }
+            if (t * KT >= most) continue;
+            kt = lds + buffer * F::kBuffer;
+            vt = kt + F::kTile;
+            scores(t * KT);
+            run.weights(s, A.c, acc);
+            outputs();
+        }
     }
 
     float l = pair_sum(run.l), m = run.m;
@@ -172,6 +207,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 #pragma unroll 4
         for (int s = group; s < A.splits; s += groups) {
             const long p = at + (long)s * A.rows;
+            if (A.part_ml[2 * p] == -INFINITY) continue;
             const f32x4 v0 = *(const f32x4 *)(A.part + p * D + ch), v1 = *(const f32x4 *)(A.part + p * D + ch + 4);
             const f32x2 ml = *(const f32x2 *)(A.part_ml + 2 * p);
             const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
@@ -211,7 +247,7 @@ int splits_of(const Sizes &S)
 {
     const long blocks = row_tiles(S) * S.B * S.Hk, tiles = (S.Nk + key_tile(S) - 1) / key_tile(S);
     if (blocks == 0) return 1;
-    const long want = few(S) ? 2048 : 512, least = few(S) ? 2 * waves(S) : 4;
+    const long want = 512, least = few(S) ? 2 * waves(S) : 4;
     return (int)std::max(1L, std::min({want / blocks, tiles / least, 64L}));
 }
 

@@ -26,9 +26,9 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const long block = swizzled(A.first + blockIdx.x, A.blocks);
-    const int tile = A.tiles - 1 - (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);
-    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
+    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
@@ -70,6 +70,9 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         }
     }
 
+    arrived<G>(x);
+    arrived<G>(g);
+
     f32x16 acc[G::NT];
     clear(acc);
     for (int t = from, buffer = 0; t < last; ++t, buffer ^= 1) {
@@ -109,9 +112,9 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
     static_assert(RT == 64 && WAVES >= 2, "a wavefront each loads a tile's lse and delta");
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const long block = swizzled(A.first + blockIdx.x, A.blocks);
-    const int tile = (int)(block % A.tiles), split = (int)(block / A.tiles % A.splits);      // those of a causal mask's long columns first
-    const int hb = (int)(block / ((long)A.tiles * A.splits)), b = hb / A.Hk, hk = hb % A.Hk;
+    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
@@ -144,6 +147,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
     clear(dk);
     clear(dv);
     if (from < last) request(from, 0);
+    arrived<G>(kx);
+    arrived<G>(vx);
     for (int t = from, buffer = 0; t < last; ++t, buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();

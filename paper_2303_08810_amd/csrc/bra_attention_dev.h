@@ -57,12 +57,25 @@ struct Sequence {
     __device__ __forceinline__ int limit(int q) const { return q >= nq ? 0 : causal ? min(max(q + off + 1, 0), nk) : nk; }
 };
 
-// Workgroup `block` of `blocks`: an XCD takes neighbouring ones, so that the workgroups of a head meet in its L2.
-__device__ __forceinline__ long swizzled(long block, long blocks)
-{
-    const long xcd = block % 8, per = blocks / 8, rest = blocks % 8;
-    return xcd * per + min(xcd, rest) + block / 8;
-}
+// What workgroup `block` works on: `per` workgroups to a head, those of a head on one XCD, where they meet in its L2, heads next to each other on
+// different ones, since those of a batch's long sequences would otherwise come to one.  The workgroups of the last heads, fewer than XCDs, are dealt out evenly.
+struct Place {
+    int head, inner;
+    __device__ __forceinline__ Place(long block, long blocks, long per)
+    {
+        const long whole = blocks / per / 8 * 8 * per;
+        long i;
+        if (block < whole) {
+            const long j = block / 8;
+            i = (j / per * 8 + block % 8) * per + j % per;
+        } else {
+            const long left = blocks - whole, j = block - whole, xcd = j % 8, each = left / 8, rest = left % 8;
+            i = whole + xcd * each + min(xcd, rest) + j / 8;
+        }
+        head = (int)(i / per);
+        inner = (int)(i - head * per);
+    }
+};
 
 // Elements E, heads of up to D channels: rows of P elements in LDS.
 template <class E, int D_>
@@ -109,6 +122,15 @@ __device__ __forceinline__ void load_columns(const char *p, bool valid, int piec
         const int piece = 2 * ks + h;
         x[ks] = *(const typename G::Piece *)(valid && piece < pieces ? p + 16 * piece : (const char *)zeros);
     }
+}
+
+// The operands have arrived.  Without it the compiler, which does not count the direct loads, waits for the registers' loads at their first use in
+// the loop over the tiles, and with them for the tile that is on its way, every time.
+template <class G>
+__device__ __forceinline__ void arrived(typename G::Piece (&x)[G::kSteps])
+{
+#pragma unroll
+    for (int ks = 0; ks < G::kSteps; ++ks) asm volatile("" : "+v"(x[ks]));
 }
 
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }

@@ -2,7 +2,7 @@
 //     u = x / sqrt(mean of squares + eps) gamma,   (a, b) -> (a cos - b sin, b cos + a sin) for each pair of the first `turned` channels
 // and backwards g = R^T dy, dgamma = sum g x / rms, dx = (g gamma - x / rms mean(g gamma x / rms)) / rms.
 // A team of lanes has a row (a head of a token) in registers, each lane two chunks of V channels that hold whole pairs, and works on RPT heads
-// of a token, which share the angles.  Bound by memory.
+// of a token, which share the angles.  A workgroup has queries or keys alone: one gamma and one set of its gradient's sums.  Bound by memory.
 #include "bra_mfma_dev.h"
 #include "bra_qk_norm.h"
 
@@ -16,15 +16,24 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Queries or keys.
+struct Part {
+    att::Rows x, g, o;          // what goes in, what comes back (backward), what is written
+    const float *gamma;         // or NULL: no norm
+    unsigned groups, items;     // a token's heads go to `groups` teams; tokens x groups
+    int heads;
+};
+
 struct Work {
-    QkNormIn I;
-    att::Rows gQ, gK, oQ, oK;   // what comes back (backward), what is written
-    unsigned N, groups;         // a token's heads go to `groups` teams
-    int heads, all, d, turned, table_rows, team;
+    Part part[2];
+    const float *cos, *sin;
+    const int *positions;
+    unsigned N;
+    int d, turned, table_rows, team;
     float eps, d_inv;
     bool halves;
-    unsigned items;             // tokens x groups
-    float *sums;                // [workgroups][2][d]
+    unsigned query_blocks;      // workgroups of the queries, the others are the keys'
+    float *sums;                // [workgroups][d]
 };
 
 template <class E, int V>
@@ -129,58 +138,46 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (
 template <class E, int V, int RPT, bool BACK>
 __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
 {
+    const bool keys = blockIdx.x >= W.query_blocks;
+    const Part &P = W.part[keys];
+    const unsigned block = blockIdx.x - (keys ? W.query_blocks : 0), blocks = keys ? gridDim.x - W.query_blocks : W.query_blocks;
     const int lane = threadIdx.x % W.team, teams = kThreads / W.team;
     const bool active = 2 * V * lane < W.d, turned = 2 * V * lane < W.turned;
     const int unit = active ? lane : 0, ca = turned && W.halves ? V * unit : 2 * V * unit, cb = turned && W.halves ? W.turned / 2 + V * unit : ca + V;
-    const bool norm = W.I.q_gamma != nullptr;
-    float gamma[2][2 * V], sums[2][2 * V];
+    const bool norm = P.gamma != nullptr;
+    float ga[V], gb[V], suma[V], sumb[V];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-            gamma[k][e] = 1.f;
-            sums[k][e] = 0.f;
-        }
-    if (norm) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float *g = k ? W.I.k_gamma : W.I.q_gamma;
-            if (!g) continue;
-            float t[V];
-            load_vector<V>(g + ca, t);
-#pragma unroll
-            for (int e = 0; e < V; ++e) gamma[k][e] = t[e];
-            load_vector<V>(g + cb, t);
-#pragma unroll
-            for (int e = 0; e < V; ++e) gamma[k][V + e] = t[e];
-        }
+    for (int e = 0; e < V; ++e) {
+        ga[e] = gb[e] = 1.f;
+        suma[e] = sumb[e] = 0.f;
     }
-    for (unsigned item = blockIdx.x * (unsigned)teams + threadIdx.x / W.team; item < W.items; item += gridDim.x * (unsigned)teams) {
-        const unsigned token = item / W.groups, group = item - token * W.groups, b = token / W.N, n = token - b * W.N;
+    if (norm) {
+        load_vector<V>(P.gamma + ca, ga);
+        load_vector<V>(P.gamma + cb, gb);
+    }
+    for (unsigned item = block * (unsigned)teams + threadIdx.x / W.team; item < P.items; item += blocks * (unsigned)teams) {
+        const unsigned token = item / P.groups, group = item - token * P.groups, b = token / W.N, n = token - b * W.N;
         float xa[RPT][V], xb[RPT][V], ya[BACK ? RPT : 1][V], yb[BACK ? RPT : 1][V], cos[V], sin[V];
         // rows that do not exist are read in another's place and not written
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
-            const int head = min((int)(group + i * W.groups), W.all - 1);
-            const bool q = head < W.heads;
-            const att::Rows &R = q ? W.I.Q : W.I.K;
+            const int head = min((int)(group + i * P.groups), P.heads - 1);
             if (!BACK || norm) {
-                const char *p = R.p + b * R.batch + n * R.token + (q ? head : head - W.heads) * R.head;
+                const char *p = P.x.p + b * P.x.batch + n * P.x.token + head * P.x.head;
                 load<E, V>(p + ca * sizeof(E), xa[i]);
                 load<E, V>(p + cb * sizeof(E), xb[i]);
             }
             if constexpr (BACK) {
-                const att::Rows &G = q ? W.gQ : W.gK;
-                const char *p = G.p + b * G.batch + n * G.token + (q ? head : head - W.heads) * G.head;
+                const char *p = P.g.p + b * P.g.batch + n * P.g.token + head * P.g.head;
                 load<E, V>(p + ca * sizeof(E), ya[i]);
                 load<E, V>(p + cb * sizeof(E), yb[i]);
             }
         }
         if (turned) {
-            const int at = W.I.positions ? min(max(W.I.positions[token], 0), W.table_rows - 1) : (int)n;
+            const int at = W.positions ? min(max(W.positions[token], 0), W.table_rows - 1) : (int)n;
             const long pair = (long)at * (W.turned / 2) + V * unit;
-            load_vector<V>(W.I.cos + pair, cos);
-            load_vector<V>(W.I.sin + pair, sin);
+            load_vector<V>(W.cos + pair, cos);
+            load_vector<V>(W.sin + pair, sin);
             if (BACK) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) sin[e] = -sin[e];
@@ -188,8 +185,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
         }
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
-            const int head = (int)(group + i * W.groups);
-            const bool q = head < W.heads, live = active && head < W.all;
+            const int head = (int)(group + i * P.groups);
+            const bool live = active && head < P.heads;
             float inv = 1.f;
             if (norm) {
                 float s = 0.f;
@@ -201,8 +198,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
             if constexpr (!BACK) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    oa[e] = norm ? xa[i][e] * inv * (q ? gamma[0][e] : gamma[1][e]) : xa[i][e];
-                    ob[e] = norm ? xb[i][e] * inv * (q ? gamma[0][V + e] : gamma[1][V + e]) : xb[i][e];
+                    oa[e] = norm ? xa[i][e] * inv * ga[e] : xa[i][e];
+                    ob[e] = norm ? xb[i][e] * inv * gb[e] : xb[i][e];
                 }
                 if (turned) turn<V>(oa, ob, cos, sin, W.halves);
             } else {
@@ -215,13 +212,10 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
                     if (!norm) continue;
                     xa[i][e] *= inv;
                     xb[i][e] *= inv;
-                    const float sa = live ? oa[e] * xa[i][e] : 0.f, sb = live ? ob[e] * xb[i][e] : 0.f;
-                    sums[0][e] += q ? sa : 0.f;
-                    sums[1][e] += q ? 0.f : sa;
-                    sums[0][V + e] += q ? sb : 0.f;
-                    sums[1][V + e] += q ? 0.f : sb;
-                    oa[e] *= q ? gamma[0][e] : gamma[1][e];
-                    ob[e] *= q ? gamma[0][V + e] : gamma[1][V + e];
+                    suma[e] += live ? oa[e] * xa[i][e] : 0.f;
+                    sumb[e] += live ? ob[e] * xb[i][e] : 0.f;
+                    oa[e] *= ga[e];
+                    ob[e] *= gb[e];
                     dot = fmaf(oa[e], xa[i][e], fmaf(ob[e], xb[i][e], dot));
                 }
                 if (norm) {
@@ -234,8 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
                 }
             }
             if (live) {
-                const att::Rows &O = q ? W.oQ : W.oK;
-                char *p = O.p + b * O.batch + n * O.token + (q ? head : head - W.heads) * O.head;
+                char *p = P.o.p + b * P.o.batch + n * P.o.token + head * P.o.head;
                 store<E, V>(p + ca * sizeof(E), oa);
                 store<E, V>(p + cb * sizeof(E), ob);
             }
@@ -244,42 +237,40 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
     if constexpr (BACK) {
         if (!norm) return;
         // the workgroup's sums: teams of a wavefront first, then its four wavefronts
-        __shared__ float lds[kThreads / 64][2][128];
+        __shared__ float lds[kThreads / 64][128];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) {
-                float v = sums[k][e];
-                for (int o = W.team; o < 64; o *= 2) v += __shfl_xor(v, o);
-                if (threadIdx.x % 64 < W.team && active) lds[threadIdx.x / 64][k][e < V ? ca + e : cb + e - V] = v;
-            }
+        for (int e = 0; e < 2 * V; ++e) {
+            float v = e < V ? suma[e % V] : sumb[e % V];
+            for (int o = W.team; o < 64; o *= 2) v += __shfl_xor(v, o);
+            if (threadIdx.x % 64 < W.team && active) lds[threadIdx.x / 64][e < V ? ca + e : cb + e - V] = v;
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * W.d; i += kThreads) {
-            const int k = i / W.d, c = i % W.d;
+        for (int c = threadIdx.x; c < W.d; c += kThreads) {
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < kThreads / 64; ++w) v += lds[w][k][c];
-            W.sums[(long)blockIdx.x * 2 * W.d + i] = v;
+            for (int w = 0; w < kThreads / 64; ++w) v += lds[w][c];
+            W.sums[(long)blockIdx.x * W.d + c] = v;
         }
     }
 }
 
-// Sums of the workgroups' sums: 16 columns to a workgroup, 16 shares of the rows.
-__global__ __launch_bounds__(256) void k_qk_norm_sums(const float *sums, int rows, int d, float *dq, float *dk)
+// Sums of the workgroups' sums: 8 columns to a workgroup, 32 shares of the rows; the queries' rows, then the keys'.
+__global__ __launch_bounds__(256) void k_qk_norm_sums(const float *sums, int query_rows, int rows, int d, float *dq, float *dk)
 {
-    __shared__ float lds[16][17];
-    const int col = threadIdx.x % 16, share = threadIdx.x / 16, c = blockIdx.x * 16 + col;
+    __shared__ float lds[32][9];
+    const int each = d / 8, keys = blockIdx.x / each, col = threadIdx.x % 8, share = threadIdx.x / 8, c = blockIdx.x % each * 8 + col;
+    const int first = keys ? query_rows : 0, end = keys ? rows : query_rows;
     float v = 0.f;
-    if (c < 2 * d)
-        for (int r = share; r < rows; r += 16) v += sums[(long)r * 2 * d + c];
+#pragma unroll 8
+    for (int r = first + share; r < end; r += 32) v += sums[(long)r * d + c];
     lds[share][col] = v;
     __syncthreads();
-    if (share || c >= 2 * d) return;
+    if (share) return;
     v = 0.f;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) v += lds[s][col];
-    float *out = c < d ? dq : dk;
-    if (out) out[c < d ? c : c - d] = v;
+    for (int s = 0; s < 32; ++s) v += lds[s][col];
+    float *out = keys ? dk : dq;
+    if (out) out[c] = v;
 }
 
 // Channels of a chunk: whole pairs of the rotated part to a lane, chunks of up to 16 bytes.
@@ -295,21 +286,42 @@ int team_of(const QkNormSizes &S, int V)
     while (2 * V * t < S.d) t *= 2;
     return t;
 }
-// Heads of a token to a team.
-int rows_per_team(const QkNormSizes &S) { return S.tokens * (S.heads + S.kv_heads) >= 16384 ? 4 : 1; }
-long workgroups(const QkNormSizes &S, bool back)
+// Heads of a token to a team: several share the angles and are on their way at once; of few rows each goes to a team of its own.
+int rows_per_team(const QkNormSizes &S)
 {
-    const int rpt = rows_per_team(S), teams = kThreads / team_of(S, chunk(S));
-    const long items = S.tokens * ((S.heads + S.kv_heads + rpt - 1) / rpt), blocks = (items + teams - 1) / teams;
-    return std::min(blocks, back ? 1024L : 1L << 20);
+    if (S.tokens * (S.heads + S.kv_heads) < 16384) return 1;
+    auto fits = [&](int r) {
+        auto waste = [&](int heads) { return 4 * ((heads + r - 1) / r * r) > 5 * heads; };
+        return !waste(S.heads) && !(S.kv_heads && waste(S.kv_heads));
+    };
+    return fits(4) ? 4 : fits(2) ? 2 : 1;
 }
+// Workgroups of the queries and of the keys.
+struct Blocks {
+    long query, key;
+    Blocks(const QkNormSizes &S, bool back)
+    {
+        const int rpt = rows_per_team(S), teams = kThreads / team_of(S, chunk(S));
+        auto all = [&](int heads) { return (S.tokens * ((heads + rpt - 1) / rpt) + teams - 1) / teams; };
+        query = all(S.heads);
+        key = all(S.kv_heads);
+        const long most = back ? 512L : 1L << 20;
+        if (query + key > most) {
+            const long sum = query + key;
+            query = std::max(1L, query * most / sum);
+            key = key ? std::max(1L, key * most / sum) : 0;
+        }
+    }
+};
 
 template <class E, int V, bool BACK>
 int launch(const QkNormSizes &S, const Work &W, int rpt, hipStream_t st)
 {
     const ProfScope scope(st, BACK ? K_QK_NORM_BACKWARD : K_QK_NORM);
-    const unsigned blocks = (unsigned)workgroups(S, BACK);
+    const Blocks n(S, BACK);
+    const unsigned blocks = (unsigned)(n.query + n.key);
     if (rpt == 4) k_qk_norm<E, V, 4, BACK><<<blocks, kThreads, 0, st>>>(W);
+    else if (rpt == 2) k_qk_norm<E, V, 2, BACK><<<blocks, kThreads, 0, st>>>(W);
     else k_qk_norm<E, V, 1, BACK><<<blocks, kThreads, 0, st>>>(W);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
@@ -327,14 +339,21 @@ int pick(const QkNormSizes &S, const Work &W, int rpt, hipStream_t st)
     }
 }
 
-Work make_work(const QkNormSizes &S, const QkNormIn &I, int rpt)
+Work make_work(const QkNormSizes &S, const QkNormIn &I, int rpt, bool back)
 {
     Work W{};
-    W.I = I;
+    for (int k = 0; k < 2; ++k) {
+        Part &P = W.part[k];
+        P.x = k ? I.K : I.Q;
+        P.gamma = k ? I.k_gamma : I.q_gamma;
+        P.heads = k ? S.kv_heads : S.heads;
+        P.groups = (unsigned)((P.heads + rpt - 1) / rpt);
+        P.items = (unsigned)(S.tokens * P.groups);
+    }
+    W.cos = I.cos;
+    W.sin = I.sin;
+    W.positions = I.positions;
     W.N = (unsigned)S.N;
-    W.all = S.heads + S.kv_heads;
-    W.groups = (unsigned)((W.all + rpt - 1) / rpt);
-    W.heads = S.heads;
     W.d = S.d;
     W.turned = S.turned;
     W.table_rows = S.table_rows;
@@ -342,7 +361,7 @@ Work make_work(const QkNormSizes &S, const QkNormIn &I, int rpt)
     W.eps = S.eps;
     W.d_inv = 1.0f / (float)S.d;
     W.halves = S.halves;
-    W.items = (unsigned)(S.tokens * W.groups);
+    W.query_blocks = (unsigned)Blocks(S, back).query;
     return W;
 }
 
@@ -352,23 +371,27 @@ int qk_norm_forward(const QkNormSizes &S, const QkNormIn &I, const att::Rows &Qo
 {
     if (S.tokens == 0) return BRA_OK;
     const int rpt = rows_per_team(S);
-    Work W = make_work(S, I, rpt);
-    W.oQ = Qout;
-    W.oK = Kout;
+    Work W = make_work(S, I, rpt, false);
+    W.part[0].o = Qout;
+    W.part[1].o = Kout;
     return S.f32 ? pick<float, false>(S, W, rpt, st) : pick<bf16_t, false>(S, W, rpt, st);
 }
 
-size_t qk_norm_backward_workspace_bytes(const QkNormSizes &S) { return align256(sizeof(float) * 2 * S.d * workgroups(S, true)); }
+size_t qk_norm_backward_workspace_bytes(const QkNormSizes &S)
+{
+    const Blocks n(S, true);
+    return align256(sizeof(float) * S.d * std::max(n.query + n.key, 1L));
+}
 
 int qk_norm_backward(const QkNormSizes &S, const QkNormIn &I, const att::Rows &gQ, const att::Rows &gK, const att::Rows &dQ, const att::Rows &dK, float *dq_gamma,
                      float *dk_gamma, void *ws, hipStream_t st)
 {
     const int rpt = rows_per_team(S);
-    Work W = make_work(S, I, rpt);
-    W.gQ = gQ;
-    W.gK = gK;
-    W.oQ = dQ;
-    W.oK = dK;
+    Work W = make_work(S, I, rpt, true);
+    W.part[0].g = gQ;
+    W.part[1].g = gK;
+    W.part[0].o = dQ;
+    W.part[1].o = dK;
     W.sums = (float *)ws;
     if (S.tokens > 0) {
         const int rc = S.f32 ? pick<float, true>(S, W, rpt, st) : pick<bf16_t, true>(S, W, rpt, st);
@@ -376,7 +399,8 @@ int qk_norm_backward(const QkNormSizes &S, const QkNormIn &I, const att::Rows &g
     }
     if (!I.q_gamma || (!dq_gamma && !dk_gamma)) return BRA_OK;
     const ProfScope scope(st, K_QK_NORM_SUMS);
-    k_qk_norm_sums<<<(2 * S.d + 15) / 16, 256, 0, st>>>(W.sums, (int)workgroups(S, true), S.d, dq_gamma, dk_gamma);
+    const Blocks n(S, true);
+    k_qk_norm_sums<<<2 * S.d / 8, 256, 0, st>>>(W.sums, (int)n.query, (int)(n.query + n.key), S.d, dq_gamma, dk_gamma);
     return hipGetLastError() == hipSuccess ? BRA_OK : BRA_ERR_LAUNCH;
 }
 
