@@ -58,7 +58,7 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     const int first_row = tile * F::kRows, row = first_row + (FEW ? 0 : 32 * wave) + c;
     const bool valid = row < A.rows;
     const int query = row_query(A, min(row, A.rows - 1)), limit = valid ? seq.limit(query) : 0;
-    const int least = columns_min(limit), most = columns_max(limit);
+    const int least = columns_min(limit);
     // keys that any row of the workgroup sees
     int end = 0;
     if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
 
     f32x16 acc[G::NT];
     clear(acc);
-    Running run;
+    Running run(limit > 0);
     const char *kt = ring, *vt = ring + F::kTile;
     f32x16 s[KT / 32];
     auto scores = [&](int k0) {
@@ -120,35 +120,14 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
             scores(t * KT);
             lds_reads_done();
             if (two) request(false, t + 2 * WAVES, buffer);
-            run.weights(s, A.c, acc);
+#pragma unroll
+            for (int i = 0; i < KT / 32; ++i) run.weights(s[i], A.c, acc);
             if (two) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
             else if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * L) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             outputs();
             lds_reads_done();
             if (two) request(true, t + 2 * WAVES, buffer);
-        }
-    } else {
-        int t = split * share;
-        if (t < last) {
-            request(false, t, 0);
-            request(true, t, 0);
-        }
-        arrived<G>(x);
-        for (int buffer = 0; t < last; ++t, buffer ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (t + 1 < last) {
-                request(false, t + 1, buffer ^ 1);
-                request(true, t + 1, buffer ^ 1);
-            }
-            if (t * KT >= most) continue;
-            kt = lds + buffer * F::kBuffer;
-            vt = kt + F::kTile;
-            scores(t * KT);
-            run.weights(s, A.c, acc);
-            outputs();
         }
     }
 
@@ -181,6 +160,103 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
         }
     }
     if (valid) finish<E, G>(A, b, hk, split, row, h, acc, m, l);
+}
+
+// Many rows: the wavefronts of a workgroup have 32 rows each and share tiles of KT keys and values, the next of which is on its way.
+template <class E, int D>
+struct Main {
+    typedef Geometry<E, D> G;
+    typedef Slots<G> S;
+    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, KT = sizeof(E) == 4 ? 32 : 64;
+    static constexpr int kTile = KT * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile;        // K, V, K, V
+    typedef Walk<G, KT, kThreads> Loads;
+};
+
+template <class E, int D>
+__global__ __launch_bounds__(256, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E) == 2 && D <= 64 ? 3 : 2) void k_attention_rows(Call A)
+{
+    typedef Main<E, D> F;
+    typedef typename F::G G;
+    typedef typename F::S S;
+    constexpr int KT = F::KT;
+    extern __shared__ char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
+    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
+    const Sequence seq(A, b);
+    const int pieces = A.d * (int)sizeof(E) / 16;
+
+    const int first_row = tile * F::kRows, row = first_row + 32 * wave + c;
+    const bool valid = row < A.rows;
+    const int query = row_query(A, min(row, A.rows - 1)), limit = valid ? seq.limit(query) : 0;
+    const int least = columns_min(limit), most = columns_max(limit);
+    // keys that any row of the workgroup sees
+    int end = 0;
+    if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
+    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, first = split * share, last = min(all, first + share);
+
+    const unsigned at = lds_address(lds);
+    typename F::Loads keys(A.K.p + b * A.K.batch + hk * A.K.head + (long)first * KT * A.K.token, A.K.token, seq.nk - first * KT, pieces, threadIdx.x);
+    typename F::Loads values(A.V.p + b * A.V.batch + hk * A.V.head + (long)first * KT * A.V.token, A.V.token, seq.nk - first * KT, pieces, threadIdx.x);
+    typename G::Piece x[G::kSteps];
+    {
+        const int head = hk * A.G + min(row, A.rows - 1) - query * A.G;
+        load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
+    }
+    if (first < last) {
+        keys.request(at, pieces, threadIdx.x);
+        values.request(at + F::kTile, pieces, threadIdx.x);
+    }
+    arrived<G>(x);
+
+    const Reader<G> reader(lane);
+    f32x16 acc[G::NT];
+    clear(acc);
+    Running run(limit > 0);
+    // tile t, which lies in the buffers B
+    auto body = [&](auto B, int t) __attribute__((always_inline)) {
+        constexpr int kMine = decltype(B)::value * 2 * F::kTile, kOther = 2 * F::kTile - kMine;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 1 < last) {
+            keys.request(at + kOther, pieces, threadIdx.x);
+            values.request(at + kOther + F::kTile, pieces, threadIdx.x);
+        }
+        const int k0 = t * KT;
+        if (k0 >= most) return;
+        f32x16 s[KT / 32];
+        unrolled<KT / 32>([&](auto i) __attribute__((always_inline)) {
+            s[i] = f32x16{};
+            unrolled<S::kRows>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_rows(o, lds + kMine + i * F::kSub, reader, f);
+                S::rows(s[i], o, x, f);
+            });
+        });
+        if (k0 + KT > least) {
+#pragma unroll
+            for (int i = 0; i < KT / 32; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[i][r] = k0 + 32 * i + result_row(r, h) < limit ? s[i][r] : -INFINITY;
+        }
+        unrolled<KT / 32>([&](auto i) __attribute__((always_inline)) {
+            run.weights(s[i], A.c, acc);
+            typename S::Weights p;
+            unrolled<8>([&](auto r) __attribute__((always_inline)) { S::keep(p, s[i], 2 * r + 1); });
+            unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_columns(o, lds + kMine + F::kTile + i * F::kSub, reader, f);
+                S::columns(acc, o, p, f);
+            });
+        });
+    };
+    for (int t = first; t < last; t += 2) {
+        body(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < last) body(std::integral_constant<int, 1>{}, t + 1);
+    }
+    if (valid) finish<E, G>(A, b, hk, split, row, h, acc, run.m, pair_sum(run.l));
 }
 
 // The splits' sums put together.  A thread has 8 channels of a row and every `groups`-th of its splits (one after another they took 26 us for
@@ -266,6 +342,20 @@ int launch(Call A, hipStream_t st)
 }
 
 template <class E, int D>
+int launch_rows(Call A, hipStream_t st)
+{
+    typedef Main<E, D> F;
+    const int rc = allow_lds<k_attention_rows<E, D>>(F::kLds);
+    if (rc != BRA_OK) return rc;
+    for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION);
+        k_attention_rows<E, D><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
+}
+
+template <class E, int D>
 int join(Call A, long heads, hipStream_t st)
 {
     constexpr int CH = D / 8;
@@ -287,7 +377,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
     constexpr bool f32 = sizeof(E) == 4;
     int rc;
     if (few(S)) rc = launch<E, D, 32, (f32 && D > 64 ? 2 : 4), true>(A, st);
-    else rc = launch<E, D, (f32 ? 32 : 64), 4, false>(A, st);
+    else rc = launch_rows<E, D>(A, st);
     if (rc == BRA_OK && A.splits > 1) rc = join<E, D>(A, (long)S.B * S.Hk, st);
     return rc;
 }

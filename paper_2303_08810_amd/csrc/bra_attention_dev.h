@@ -225,6 +225,137 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[N])
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
 }
 
+// A wavefront's reads of a tile in LDS, as offsets from its first row, for subtiles of 32 rows from a multiple of 32 on.
+template <class G>
+struct Reader {
+    unsigned row[G::kSteps], column[G::kF32 ? 2 : 2 * G::NT];
+    __device__ __forceinline__ explicit Reader(int lane)
+    {
+        const int h = lane / 32, c = lane % 32;
+#pragma unroll
+        for (int ks = 0; ks < G::kSteps; ++ks) row[ks] = c * G::kPitch + 16 * ((2 * ks + h) ^ G::turn(c));
+        if constexpr (!G::kF32) {
+            const int s = lane % 16, q = lane / 16, col4 = s % 2 * 2 + s % 4 / 2;
+#pragma unroll
+            for (int t = 0; t < G::NT; ++t)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = 8 * half + 4 * h + s / 4, o = 32 * t + 16 * (q % 2) + 4 * col4;
+                    column[2 * t + half] = r * G::kPitch + 16 * ((o / 8) ^ G::turn(r)) + 2 * (o % 8);
+                }
+        } else {
+            // rows 8 a + 4 h + b of a subtile, a channel of 32: turn() of the row is that of 4 h with b in front of it and a % 2 behind
+            const int channel = c / 16 * 16 + c / 4 % 2 * 8 + c / 8 % 2 * 4 + c % 4;
+            column[0] = 4 * h * G::kPitch + 4 * (channel % 4);
+            column[1] = channel / 4 ^ G::turn(4 * h);
+        }
+    }
+};
+
+template <int N, class F, int I = 0>
+__device__ __forceinline__ void unrolled(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<N, F, I + 1>(f);
+    }
+}
+
+// One product of a subtile: slot f of kRowSlots multiplies rows into s, slot f of kColumnSlots columns into acc.  A slot's operand is read some
+// slots before.
+template <class G>
+struct Slots {
+    static constexpr int kRows = G::kSteps, kColumns = G::kF32 ? 16 : 2 * G::NT;
+    struct Operand {
+        typename std::conditional<G::kF32, f32x4, u32x4>::type v;
+    };
+    __device__ static __forceinline__ void read_rows(Operand &o, const char *tile, const Reader<G> &R, const int f) { o.v = *(const decltype(o.v) *)(tile + R.row[f]); }
+    __device__ static __forceinline__ void read_columns(Operand &o, const char *tile, const Reader<G> &R, int f)
+    {
+        if constexpr (G::kF32) {
+            const int row = 8 * (f / 4) + f % 4;            // + 4 h
+#pragma unroll
+            for (int t = 0; t < G::NT; ++t) {
+                const int piece = (8 * t) ^ (R.column[1] ^ G::turn(row));
+                o.v[t] = *(const float *)(tile + R.column[0] + row * G::kPitch + 16 * piece);
+            }
+        } else {
+            const int kk = f / G::NT, t = f % G::NT;
+            u32x2 r[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) r[half] = __builtin_bit_cast(u32x2, lds_read_tr16((const bf16_t *)(tile + 16 * kk * G::kPitch + R.column[2 * t + half])));
+            o.v = u32x4{r[0][0], r[0][1], r[1][0], r[1][1]};
+        }
+    }
+    __device__ static __forceinline__ void rows(f32x16 &s, const Operand &o, const typename G::Piece (&x)[G::kSteps], int f)
+    {
+        if constexpr (G::kF32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = mfma_f32(o.v[e], x[f][e], s);
+        } else s = mfma32(__builtin_bit_cast(bf16x8, o.v), x[f], s);
+    }
+    typedef typename std::conditional<G::kF32, f32x16, u32x4[2]>::type Weights;        // 32 values of the contraction: float32, or bf16 pairs
+    __device__ static __forceinline__ void copy(Weights &p, const Weights &q)
+    {
+        if constexpr (G::kF32) p = q;
+        else {
+            p[0] = q[0];
+            p[1] = q[1];
+        }
+    }
+    // Values r - 1 and r of them.
+    __device__ static __forceinline__ void keep(Weights &p, const f32x16 &s, int r)
+    {
+        if constexpr (G::kF32) {
+            p[r - 1] = s[r - 1];
+            p[r] = s[r];
+        } else p[r / 8][r % 8 / 2] = pack_bf16(s[r - 1], s[r]);
+    }
+    __device__ static __forceinline__ void columns(f32x16 (&acc)[G::NT], const Operand &o, const Weights &p, int f)
+    {
+        if constexpr (G::kF32) {
+#pragma unroll
+            for (int t = 0; t < G::NT; ++t) acc[t] = mfma_f32(o.v[t], p[f], acc[t]);
+        } else acc[f % G::NT] = mfma32(__builtin_bit_cast(bf16x8, o.v), __builtin_bit_cast(bf16x8, p[f / G::NT]), acc[f % G::NT]);
+    }
+};
+
+// Direct loads of a tensor's tiles of ROWS rows one after the other: a lane's pointers go on by a tile each time.
+template <class G, int ROWS, int THREADS>
+struct Walk {
+    static constexpr int L = ROWS * G::kPieces / THREADS;
+    static_assert(L * THREADS == ROWS * G::kPieces, "whole loads");
+    const char *at[L];
+    long step;
+    unsigned wave;          // LDS offset of this wavefront's part
+    int left;               // rows from the next tile on
+    bool whole;             // rows fill the pitch
+    __device__ __forceinline__ Walk(const char *first, long token, int rows, int pieces, int thread) : step(ROWS * token), wave(1024 * __builtin_amdgcn_readfirstlane(thread / 64)), left(rows), whole(pieces == G::kPieces)
+    {
+#pragma unroll
+        for (int u = 0; u < L; ++u) {
+            const int i = thread + THREADS * u, row = i / G::kPieces, piece = i % G::kPieces ^ G::turn(row);
+            at[u] = first + row * token + 16 * piece;
+        }
+    }
+    __device__ __forceinline__ void request(unsigned lds, int pieces, int thread)
+    {
+        if (whole && left >= ROWS) {
+#pragma unroll
+            for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)at[u], lds + wave + 16 * THREADS * u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < L; ++u) {
+                const int i = thread + THREADS * u, row = i / G::kPieces, piece = i % G::kPieces ^ G::turn(row);
+                load_to_lds_untracked((const bf16_t *)(row < left && piece < pieces ? at[u] : (const char *)zeros), lds + wave + 16 * THREADS * u);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < L; ++u) at[u] += step;
+        left -= ROWS;
+    }
+};
+
 // Of the two lanes of a column.
 __device__ __forceinline__ float pair_max(float v)
 {
@@ -252,37 +383,48 @@ __device__ __forceinline__ int columns_max(int v)
     return __builtin_amdgcn_readfirstlane(v);
 }
 
-// Softmax statistics of a column, in powers of two: m so far (the same in both of its lanes), l this lane's share of the sum.
+// Softmax statistics of a column, in powers of two: m, from which its weights are taken (a whole number, the same in both of its lanes), l this lane's
+// share of their sum.
 struct Running {
-    float m = -INFINITY, base = 0.f, l = 0.f;       // base: m, or 0 where there is none yet
-    // S -> P; what is in acc is brought to the new maximum.  The maximum is raised only where it grows by more than 2^8: P stays below 2^8
-    // and its sums are float32.
-    template <int KT, int NT>
-    __device__ __forceinline__ void weights(f32x16 (&s)[KT], float c, f32x16 (&acc)[NT])
+    float m, base, bar, l = 0.f;        // base: m, or 0 where there is none yet; bar: what a lane's weights of 32 keys may sum up to
+    // `sees`: whether any key is visible to the column; one that sees none needs no m
+    __device__ __forceinline__ explicit Running(bool sees) : m(sees ? -INFINITY : 0.f), base(0.f), bar(sees ? -1.f : kMost) {}
+    static constexpr float kMost = 8192.f;
+    // S -> P of 32 keys.  Weights are taken from the m that there is; only where a lane's sum shows that one has grown too large, or where there is none
+    // yet, the maximum is looked for, and m raised to it: what is in acc follows by a power of two, so that nothing is rounded.  Sums are float32
+    // and stay below 2^13 a step.  The maximum of every tile took a sixth of the vector instructions, which bound heads of 64 channels.
+    template <int NT>
+    __device__ __forceinline__ void weights(f32x16 &s, float c, f32x16 (&acc)[NT])
     {
-        float top = s[0][0];
+        f32x16 e;
+        float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+        for (int r = 0; r < 16; ++r) {
+            e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -base));
+            sum += e[r];
+        }
+        if (__builtin_amdgcn_ballot_w64(sum > bar) != 0) {
+            float top = fmaxf(s[0], s[1]);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-        top = pair_max(top) * c;
-        if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {
-            const float next = fmaxf(m, top), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+            for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
+            const float next = fmaxf(m, ceilf(pair_max(top) * c)), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
             m = next;
             base = next == -INFINITY ? 0.f : next;
+            bar = next == -INFINITY ? -1.f : kMost;
             l *= alpha;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[t][r] *= alpha;
-        }
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
+            sum = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], c, -base));
-                l += s[k][r];
+                e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -base));
+                sum += e[r];
             }
+        }
+        l += sum;
+        s = e;
     }
 };
 
