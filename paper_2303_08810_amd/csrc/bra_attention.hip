@@ -163,19 +163,19 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
 }
 
 // Many rows: the wavefronts of a workgroup have 32 rows each and share tiles of KT keys and values, the next of which is on its way.
-template <class E, int D>
+template <class E, int D, int WAVES>
 struct Main {
     typedef Geometry<E, D> G;
     typedef Slots<G> S;
-    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, KT = sizeof(E) == 4 ? 32 : 64;
+    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES, KT = sizeof(E) == 4 ? 32 : 64;
     static constexpr int kTile = KT * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile;        // K, V, K, V
     typedef Walk<G, KT, kThreads> Loads;
 };
 
-template <class E, int D>
-__global__ __launch_bounds__(256, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E) == 2 && D <= 64 ? 3 : 2) void k_attention_rows(Call A)
+template <class E, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E) == 2 && D <= 64 ? 3 : 2) void k_attention_rows(Call A)
 {
-    typedef Main<E, D> F;
+    typedef Main<E, D, WAVES> F;
     typedef typename F::G G;
     typedef typename F::S S;
     constexpr int KT = F::KT;
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 
 bool few(const Sizes &S) { return S.rows() <= 32; }
 int key_tile(const Sizes &S) { return few(S) || S.f32 ? 32 : 64; }
-int waves(const Sizes &S) { return few(S) && S.f32 && S.width() > 64 ? 2 : 4; }
+int waves(const Sizes &S) { return few(S) ? (S.f32 && S.width() > 64 ? 2 : 4) : S.rows() <= 64 ? 2 : 4; }
 long row_tiles(const Sizes &S)
 {
     const int rows = few(S) ? 32 : 32 * waves(S);
@@ -341,15 +341,15 @@ int launch(Call A, hipStream_t st)
     return BRA_OK;
 }
 
-template <class E, int D>
+template <class E, int D, int WAVES>
 int launch_rows(Call A, hipStream_t st)
 {
-    typedef Main<E, D> F;
-    const int rc = allow_lds<k_attention_rows<E, D>>(F::kLds);
+    typedef Main<E, D, WAVES> F;
+    const int rc = allow_lds<k_attention_rows<E, D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION);
-        k_attention_rows<E, D><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        k_attention_rows<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;
@@ -377,7 +377,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
     constexpr bool f32 = sizeof(E) == 4;
     int rc;
     if (few(S)) rc = launch<E, D, 32, (f32 && D > 64 ? 2 : 4), true>(A, st);
-    else rc = launch_rows<E, D>(A, st);
+    else rc = waves(S) == 2 ? launch_rows<E, D, 2>(A, st) : launch_rows<E, D, 4>(A, st);
     if (rc == BRA_OK && A.splits > 1) rc = join<E, D>(A, (long)S.B * S.Hk, st);
     return rc;
 }

@@ -11,19 +11,22 @@ namespace bra {
 namespace att {
 namespace {
 
-template <class E, int D, int TILE, int WAVES>
-struct Backward {
+template <class E, int D, int WAVES>
+struct Queries {
     typedef Geometry<E, D> G;
-    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
-    static constexpr int kTile = TILE * G::kPitch, kBuffer = 2 * kTile, kQueryLds = 2 * kBuffer, kKeyBuffer = kBuffer + 2 * TILE * 4, kKeyLds = 2 * kKeyBuffer;
-    typedef Stage<G, TILE, kThreads> Loads;
+    typedef Slots<G> S;
+    static constexpr int kThreads = 64 * WAVES, kMine = 32 * WAVES, KT = sizeof(E) == 4 ? 32 : 64;
+    static constexpr int kTile = KT * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile;        // K, V, K, V
+    typedef Walk<G, KT, kThreads> Loads;
 };
 
-template <class E, int D, int KT, int WAVES>
+template <class E, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void k_query_grads(Call A)
 {
-    typedef Backward<E, D, KT, WAVES> F;
+    typedef Queries<E, D, WAVES> F;
     typedef typename F::G G;
+    typedef typename F::S S;
+    constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
     const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
@@ -32,24 +35,21 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
-    const int first_row = tile * F::kRows, row = first_row + 32 * wave + c, some = min(row, A.rows - 1);
+    const int first_row = tile * F::kMine, row = first_row + 32 * wave + c, some = min(row, A.rows - 1);
     const bool valid = row < A.rows;
     const int query = row_query(A, some), head = hk * A.G + some - query * A.G, limit = valid ? seq.limit(query) : 0;
     const int least = columns_min(limit), most = columns_max(limit);
     int end = 0;
-    if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
-    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, from = split * share, last = min(all, from + share);
+    if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kMine, A.rows) - 1), seq.nq - 1));
+    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, first = split * share, last = min(all, first + share);
 
-    const unsigned ring_at = lds_address(lds);
-    const char *keys = A.K.p + b * A.K.batch + hk * A.K.head, *values = A.V.p + b * A.V.batch + hk * A.V.head;
-    auto request = [&](int t, int buffer) {
-        const int k0 = t * KT;
-        const char *k = keys + k0 * A.K.token, *v = values + k0 * A.V.token;
-        F::Loads::request([&](int r) { return k + r * A.K.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer, threadIdx.x);
-        F::Loads::request([&](int r) { return v + r * A.V.token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + F::kTile, threadIdx.x);
-    };
-    if (from < last) request(from, 0);
-
+    const unsigned at = lds_address(lds);
+    typename F::Loads keys(A.K.p + b * A.K.batch + hk * A.K.head + (long)first * KT * A.K.token, A.K.token, seq.nk - first * KT, pieces, threadIdx.x);
+    typename F::Loads values(A.V.p + b * A.V.batch + hk * A.V.head + (long)first * KT * A.V.token, A.V.token, seq.nk - first * KT, pieces, threadIdx.x);
+    if (first < last) {
+        keys.request(at, pieces, threadIdx.x);
+        values.request(at + F::kTile, pieces, threadIdx.x);
+    }
     typename G::Piece x[G::kSteps], g[G::kSteps];
     load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
     load_columns<G>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, limit > 0, pieces, h, g);
@@ -57,59 +57,207 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     {
         typename G::Piece o[G::kSteps];
         load_columns<G>(A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces, h, o);
+        if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
 #pragma unroll
         for (int ks = 0; ks < G::kSteps; ++ks)
 #pragma unroll
             for (int e = 0; e < 16 / (int)sizeof(E); ++e) delta = fmaf((float)g[ks][e], (float)o[ks][e], delta);
         delta = pair_sum(delta);
-        if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
         if (valid && h == 0 && split == 0) {
             A.row_lse[(long)hb * A.rows + row] = lse;
             A.row_delta[(long)hb * A.rows + row] = delta;
         }
     }
-
     arrived<G>(x);
     arrived<G>(g);
 
+    const Reader<G> reader(lane);
     f32x16 acc[G::NT];
     clear(acc);
-    for (int t = from, buffer = 0; t < last; ++t, buffer ^= 1) {
+    // tile t, which lies in the buffers B
+    auto body = [&](auto B, int t) __attribute__((always_inline)) {
+        constexpr int kMine = decltype(B)::value * 2 * F::kTile, kOther = 2 * F::kTile - kMine;
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t + 1 < last) request(t + 1, buffer ^ 1);
+        if (t + 1 < last) {
+            keys.request(at + kOther, pieces, threadIdx.x);
+            values.request(at + kOther + F::kTile, pieces, threadIdx.x);
+        }
         const int k0 = t * KT;
-        if (k0 >= most) continue;
-        const char *kt = lds + buffer * F::kBuffer, *vt = kt + F::kTile;
+        if (k0 >= most) return;
         const bool masked = k0 + KT > least;
-#pragma unroll
-        for (int i = 0; i < KT / 32; ++i) {
-            f32x16 s[2];
-            clear(s);
-            multiply_rows<G>(s[0], kt, 32 * i, x, lane);
-            multiply_rows<G>(s[1], vt, 32 * i, g, lane);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], A.c, -lse)) * (s[1][r] - delta);
+        unrolled<KT / 32>([&](auto i) __attribute__((always_inline)) {
+            const char *kt = lds + kMine + i * F::kSub, *vt = kt + F::kTile;
+            f32x16 s{}, d{};
+            unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_rows(o, f % 2 ? vt : kt, reader, f / 2);
+                S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
+            });
             if (masked) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[0][r] = k0 + 32 * i + result_row(r, h) < limit ? s[0][r] : 0.f;
+                for (int r = 0; r < 16; ++r) s[r] = k0 + 32 * i + result_row(r, h) < limit ? s[r] : -INFINITY;
             }
-            multiply_columns<G>(acc, kt, 32 * i, s[0], lane);
-        }
+            typename S::Weights w;
+            unrolled<16>([&](auto i) __attribute__((always_inline)) {
+                constexpr int r = i;
+                d[r] = __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -lse)) * (d[r] - delta);
+                if constexpr (r % 2) S::keep(w, d, r);
+            });
+            unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_columns(o, kt, reader, f);
+                S::columns(acc, o, w, f);
+            });
+        });
+    };
+    for (int t = first; t < last; t += 2) {
+        body(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < last) body(std::integral_constant<int, 1>{}, t + 1);
     }
-    if (A.splits > 1) {
-        if (valid) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, D, h);
-    } else if (valid) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
+    if (!valid) return;
+    if (A.splits > 1) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, D, h);
+    else store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
 }
 
-template <class E, int D, int RT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 1 : 2) void k_key_grads(Call A)
+// k_key_grads walks over subtiles of 32 rows, kRing of which are in LDS: while the weights of one are formed, the products of the one before with its
+// weights are on their way, a product between every few of the other instructions; then come the products of the next one with what the wavefront keeps
+// in registers.
+template <class E, int D, int WAVES>
+struct Backward {
+    typedef Geometry<E, D> G;
+    typedef Slots<G> S;
+    static constexpr int kThreads = 64 * WAVES, kMine = 32 * WAVES;
+    static constexpr int kRing = sizeof(E) == 4 && D > 64 ? 4 : 5;
+    static constexpr int kTile = 32 * G::kPitch, kSlot = 2 * kTile + 256, kLds = kRing * kSlot;      // two tensors, lse and delta
+    typedef Tiles<G, 32, kThreads> Loads;
+};
+
+// A wavefront's registers over the subtiles.
+template <class G, bool KEYS>
+struct Pipe {
+    typedef Slots<G> S;
+    static constexpr int kColumns = (KEYS ? 2 : 1) * S::kColumns, kReadAhead = 2 * S::kRows < 8 ? 2 * S::kRows : 8;
+    f32x16 s[2];                                // scores and dP of a subtile
+    typename S::Weights p, ds;                  // of the subtile before
+    f32x16 sum[KEYS ? 2 : 1][G::NT];            // dV and dK, or dQ
+
+    // s of a subtile
+    __device__ __forceinline__ void scores(const char *t0, const char *t1, const Reader<G> &R, const typename G::Piece (&x)[G::kSteps], const typename G::Piece (&g)[G::kSteps])
+    {
+        s[0] = s[1] = f32x16{};
+        unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_rows(o, f % 2 ? t1 : t0, R, f / 2);
+            S::rows(s[f % 2], o, f % 2 ? g : x, f / 2);
+        });
+    }
+    // one product of the sums of the subtile before, whose tiles are t0 and t1
+    template <int F>
+    __device__ __forceinline__ void read_column(typename S::Operand &o, const char *t0, const char *t1, const Reader<G> &R)
+    {
+        S::read_columns(o, KEYS && F % 2 == 0 ? t1 : t0, R, KEYS ? F / 2 : F);
+    }
+    template <int F>
+    __device__ __forceinline__ void product(const typename S::Operand &o)
+    {
+        if constexpr (!KEYS) S::columns(sum[0], o, ds, F);
+        else if constexpr (F % 2 == 0) S::columns(sum[0], o, p, F / 2);
+        else S::columns(sum[1], o, ds, F / 2);
+    }
+    __device__ __forceinline__ void sums(const char *t0, const char *t1, const Reader<G> &R)
+    {
+        unrolled<kColumns>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            this->template read_column<f>(o, t0, t1, R);
+            this->template product<f>(o);
+        });
+    }
+    // s -> p, ds; with COLUMNS the sums of the subtile before, in b0, b1, on the way; then s of the next one, in n0, n1.  weights(r): value r's
+    // -lse log2 e and delta.  Operands are read kBefore products ahead.
+    template <bool COLUMNS, class W>
+    __device__ __forceinline__ void step(const char *b0, const char *b1, const char *n0, const char *n1, const Reader<G> &R, const typename G::Piece (&x)[G::kSteps],
+                                         const typename G::Piece (&g)[G::kSteps], float c, W weights)
+    {
+        constexpr int N = COLUMNS ? kColumns : 1, all = N + 2 * S::kRows, kBefore = kReadAhead;
+        typename S::Operand o[all];
+        typename S::Weights np, nds;
+        auto read = [&](auto f) __attribute__((always_inline)) {
+            if constexpr (f >= N) S::read_rows(o[f], (f - N) % 2 ? n1 : n0, R, (f - N) / 2);
+            else if constexpr (COLUMNS) this->template read_column<f>(o[f], b0, b1, R);
+        };
+        unrolled<kBefore>(read);
+        __builtin_amdgcn_sched_barrier(0);
+        unrolled<N>([&](auto f) __attribute__((always_inline)) {
+            if constexpr (f + kBefore < all) read(std::integral_constant<int, f + kBefore>{});
+            if constexpr (COLUMNS) this->template product<f>(o[f]);
+            unrolled<16 * (f + 1) / N - 16 * f / N>([&](auto i) __attribute__((always_inline)) {
+                constexpr int r = 16 * f / N + i;
+                float minus_lse, delta;
+                weights(std::integral_constant<int, r>{}, minus_lse, delta);
+                s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, minus_lse));
+                s[1][r] = s[0][r] * (s[1][r] - delta);
+                if constexpr (r % 2) {
+                    if (KEYS) S::keep(np, s[0], r);
+                    S::keep(nds, s[1], r);
+                }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (KEYS) S::copy(p, np);
+        S::copy(ds, nds);
+        s[0] = s[1] = f32x16{};
+        unrolled<2 * S::kRows>([&](auto i) __attribute__((always_inline)) {
+            constexpr int f = N + i;
+            if constexpr (f + kBefore < all) read(std::integral_constant<int, f + kBefore>{});
+            S::rows(s[i % 2], o[f], i % 2 ? g : x, i / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    }
+};
+
+// A workgroup's subtiles [0, n), of which this wavefront works on [from, to).  Turn j has the subtiles j - 1 to j + 1 in LDS; before it, what was asked
+// for in turn j - 3 (j - 2 with the shorter ring) has arrived everywhere, and then subtile j + kRing - 2 is asked for, where j - 2 lay.  `own`: this wavefront's
+// loads of a subtile.
+template <class F, class Scores, class Weights, class Sums, class Request>
+__device__ __forceinline__ void take_turns(int n, int from, int to, bool one_more, bool loads, Scores scores, Weights weights, Sums sums, Request request)
 {
-    typedef Backward<E, D, RT, WAVES> F;
+    if (n <= 0) return;
+    for (int j = 0; j < min(n, F::kRing - 3); ++j) request(j);
+    auto turn = [&](int j) __attribute__((always_inline)) {
+        // (fewer loads than this are on their way in the last turns: all of them are waited for)
+        if (F::kRing == 4 || j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else if (one_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L + 1) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (j + F::kRing - 2 < n) request(j + F::kRing - 2);
+    };
+    // every wavefront meets the others at n + 2 barriers; what it does between them differs at its ends alone, so that its sums stay where they are
+    int j = -1;
+    if (from < to) {
+        for (; j < from - 1; ++j) turn(j);
+        turn(j++);
+        scores(from);
+        turn(j++);
+        weights(std::false_type{}, from);
+        for (; j < to; ++j) {
+            turn(j);
+            weights(std::true_type{}, j);
+        }
+        turn(j++);
+        sums(to - 1);
+    }
+    for (; j <= n; ++j) turn(j);
+}
+
+template <class E, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 64 || sizeof(E) == 4 ? 1 : 2) void k_key_grads(Call A)
+{
+    typedef Backward<E, D, WAVES> F;
     typedef typename F::G G;
-    static_assert(RT == 64 && WAVES >= 2, "a wavefront each loads a tile's lse and delta");
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
     const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
@@ -119,83 +267,85 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || (sizeof(E) == 4 && D > 32) ? 
     const int pieces = A.d * (int)sizeof(E) / 16;
 
     // rows begin .. end - 1 see this lane's key
-    const int first_key = tile * F::kRows, key = first_key + 32 * wave + c, end = seq.nq * A.G;
-    auto begin_of = [&](int k) { return seq.causal ? min(max(k - seq.off, 0), seq.nq) * A.G : 0; };
+    const int first_key = tile * F::kMine, key = first_key + 32 * wave + c, end = seq.nq * A.G;
+    auto begin_of = [&](int j) { return seq.causal ? min(max(j - seq.off, 0), seq.nq) * A.G : 0; };
     const bool live = key < seq.nk;
     const int begin = live ? begin_of(key) : end;
     const int wave_key = first_key + 32 * wave, least = begin_of(wave_key), most = wave_key + 31 < seq.nk ? begin_of(wave_key + 31) : end;
+    const int front = begin_of(first_key) / 32, all = first_key < seq.nk ? max((end + 31) / 32 - front, 0) : 0, share = (all + A.splits - 1) / A.splits;
+    const int first = front + split * share, n = min(all, (split + 1) * share) - split * share, row0 = 32 * first;
 
-    typename G::Piece kx[G::kSteps], vx[G::kSteps];
+    typename G::Piece x[G::kSteps], g[G::kSteps];
     const int some = live ? key : 0;
-    load_columns<G>(A.K.p + b * A.K.batch + some * A.K.token + hk * A.K.head, live, pieces, h, kx);
-    load_columns<G>(A.V.p + b * A.V.batch + some * A.V.token + hk * A.V.head, live, pieces, h, vx);
+    load_columns<G>(A.K.p + b * A.K.batch + some * A.K.token + hk * A.K.head, live, pieces, h, x);
+    load_columns<G>(A.V.p + b * A.V.batch + some * A.V.token + hk * A.V.head, live, pieces, h, g);
+    arrived<G>(x);
+    arrived<G>(g);
 
-    const unsigned ring_at = lds_address(lds);
-    const char *queries = A.Q.p + b * A.Q.batch + hk * A.G * A.Q.head, *grads = A.dO.p + b * A.dO.batch + hk * A.G * A.dO.head;
-    const float *row_lse = A.row_lse + (long)hb * A.rows, *row_delta = A.row_delta + (long)hb * A.rows;
-    auto request = [&](int t, int buffer) {
-        const int r0 = t * RT;
-        const unsigned at = ring_at + buffer * F::kKeyBuffer;
-        F::Loads::request([&](int r) { const int q = row_query(A, r0 + r); return queries + q * A.Q.token + (r0 + r - q * A.G) * A.Q.head; }, end - r0, pieces, at, threadIdx.x);
-        F::Loads::request([&](int r) { const int q = row_query(A, r0 + r); return grads + q * A.dO.token + (r0 + r - q * A.G) * A.dO.head; }, end - r0, pieces, at + F::kTile,
-                          threadIdx.x);
-        if (wave < 2) load4_to_lds_untracked((wave ? row_delta : row_lse) + min(r0 + lane, A.rows - 1), at + F::kBuffer + 4 * RT * wave);
+    const unsigned at = lds_address(lds);
+    const char *q = A.Q.p + b * A.Q.batch + hk * A.G * A.Q.head, *o = A.dO.p + b * A.dO.batch + hk * A.G * A.dO.head;
+    auto query_at = [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return q + i * A.Q.token + (r - i * A.G) * A.Q.head; };
+    auto grad_at = [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return o + i * A.dO.token + (r - i * A.G) * A.dO.head; };
+    // 32 rows on are as many heads and whole tokens on, where they are whole tokens
+    const long tokens = 32 % A.G == 0 ? 32 / A.G : 0;
+    typename F::Loads queries(query_at, tokens * A.Q.token, row0, end, pieces, threadIdx.x), grads(grad_at, tokens * A.dO.token, row0, end, pieces, threadIdx.x);
+    const float *row_sums = (h ? A.row_delta : A.row_lse) + (long)hb * A.rows;
+
+    const Reader<G> reader(lane);
+    Pipe<G, true> pipe;
+    clear(pipe.sum[0]);
+    clear(pipe.sum[1]);
+    auto slot = [&](int j) __attribute__((always_inline)) {
+        unsigned o = (unsigned)j % F::kRing * F::kSlot;
+        asm("" : "+s"(o));          // (a scalar, or the compiler forms it again for every lane and read)
+        return o;
     };
-    const int front = begin_of(first_key) / RT, all = first_key < seq.nk ? max((end + RT - 1) / RT - front, 0) : 0, share = (all + A.splits - 1) / A.splits;
-    const int from = front + split * share, last = front + min(all, (split + 1) * share);
-    f32x16 dk[G::NT], dv[G::NT];
-    clear(dk);
-    clear(dv);
-    if (from < last) request(from, 0);
-    arrived<G>(kx);
-    arrived<G>(vx);
-    for (int t = from, buffer = 0; t < last; ++t, buffer ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (t + 1 < last) request(t + 1, buffer ^ 1);
-        const int r0 = t * RT;
-        if (r0 + RT <= least || wave_key >= seq.nk) continue;
-        const char *qt = lds + buffer * F::kKeyBuffer, *gt = qt + F::kTile;
-        const float *ls = (const float *)(qt + F::kBuffer), *ds = ls + RT;
-        const bool masked = r0 < most || r0 + RT > end;
-#pragma unroll
-        for (int i = 0; i < RT / 32; ++i) {
-            f32x16 s[2];
-            clear(s);
-            multiply_rows<G>(s[0], qt, 32 * i, kx, lane);
-            multiply_rows<G>(s[1], gt, 32 * i, vx, lane);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 l4 = *(const f32x4 *)(ls + 32 * i + 8 * q + 4 * h), d4 = *(const f32x4 *)(ds + 32 * i + 8 * q + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * q + e;
-                    s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], A.c, -l4[e]));
-                    s[1][r] = s[0][r] * (s[1][r] - d4[e]);
-                }
-            }
-            if (masked) {
+    take_turns<F>(
+        n, max(least / 32 - first, 0), wave_key < seq.nk ? n : 0, wave == 0, wave < F::Loads::kLoaders,
+        [&](int j) __attribute__((always_inline)) { pipe.scores(lds + slot(j), lds + slot(j) + F::kTile, reader, x, g); },
+        [&](auto columns, int j) __attribute__((always_inline)) {
+            const int r0 = row0 + 32 * j;
+            if (r0 < most || r0 + 32 > end) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int at = r0 + 32 * i + result_row(r, h);
-                    const bool see = at >= begin && at < end;
-                    s[0][r] = see ? s[0][r] : 0.f;
-                    s[1][r] = see ? s[1][r] : 0.f;
+                    const int i = r0 + result_row(r, h);
+                    const bool see = i >= begin && i < end;
+                    pipe.s[0][r] = see ? pipe.s[0][r] : -INFINITY;
+                    pipe.s[1][r] = see ? pipe.s[1][r] : 0.f;
                 }
             }
-            multiply_columns<G>(dv, gt, 32 * i, s[0], lane);
-            multiply_columns<G>(dk, qt, 32 * i, s[1], lane);
-        }
-    }
+            const char *before = lds + slot(j + F::kRing - 1), *next = lds + slot(j + 1);        // (behind the last one: what is there, whose scores nobody uses)
+            const float *mine = (const float *)(lds + slot(j) + 2 * F::kTile) + 4 * h;
+            f32x4 l[2], d[2];
+            l[0] = *(const f32x4 *)mine;
+            d[0] = *(const f32x4 *)(mine + 32);
+            pipe.template step<decltype(columns)::value>(before, before + F::kTile, next, next + F::kTile, reader, x, g, A.c, [&](auto r, float &ml, float &dl) __attribute__((always_inline)) {
+                if constexpr (r % 4 == 0 && r < 12) {
+                    l[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 8);
+                    d[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 40);
+                }
+                ml = -l[r / 4 % 2][r % 4];
+                dl = d[r / 4 % 2][r % 4];
+            });
+        },
+        [&](int j) __attribute__((always_inline)) { pipe.sums(lds + slot(j), lds + slot(j) + F::kTile, reader); },
+        [&](int j) __attribute__((always_inline)) {
+            queries.request(at + slot(j), pieces, threadIdx.x, query_at);
+            grads.request(at + slot(j) + F::kTile, pieces, threadIdx.x, grad_at);
+            if (wave == 0) load4_to_lds_untracked(row_sums + min(row0 + 32 * j + c, A.rows - 1), at + slot(j) + 2 * F::kTile);
+        });
     if (key >= A.Nk) return;
+    if (!live) {
+        clear(pipe.sum[0]);
+        clear(pipe.sum[1]);
+    }
     if (A.splits > 1) {
         float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
-        store_columns<float, G>((char *)part, dk, A.scale, D, h);
-        store_columns<float, G>((char *)(part + D), dv, 1.f, D, h);
+        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, D, h);
+        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, D, h);
     } else {
-        store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, dk, A.scale, A.d, h);
-        store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, dv, 1.f, A.d, h);
+        store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, pipe.sum[1], A.scale, A.d, h);
+        store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, pipe.sum[0], 1.f, A.d, h);
     }
 }
 
@@ -229,14 +379,14 @@ __global__ __launch_bounds__(256) void k_grads_join(Call A)
     }
 }
 
-constexpr int kWaves = 4, kRowTile = 64;
-int key_tile(const Sizes &S) { return S.f32 ? 32 : 64; }
+// Wavefronts of a workgroup, of 32 rows (keys) each.
+int waves_of(long mine) { return mine <= 64 ? 2 : 4; }
 
 // Shares of the keys (of the rows) that workgroups walk over, where there are few of them, or a causal mask makes them of different lengths.
 int splits_of(const Sizes &S, bool keys)
 {
     const long mine = keys ? S.Nk : S.rows(), walked = keys ? S.rows() : S.Nk;
-    const long blocks = (mine + 32 * kWaves - 1) / (32 * kWaves) * S.B * S.Hk, tiles = (walked + (keys ? kRowTile : key_tile(S)) - 1) / (keys ? kRowTile : key_tile(S));
+    const long each = 32 * waves_of(mine), blocks = (mine + each - 1) / each * S.B * S.Hk, tiles = (walked + 63) / 64;
     if (blocks == 0) return 1;
     const long want = S.causal ? 1024 : 512;
     return (int)std::max(1L, std::min({want / blocks, tiles / 4, 16L}));
@@ -260,34 +410,47 @@ int join(Call A, long heads, hipStream_t st)
     return BRA_OK;
 }
 
-template <class E, int D>
-int run(const Sizes &S, Call A, hipStream_t st)
+template <class E, int D, int WAVES>
+int query_grads(const Sizes &S, Call A, long heads, hipStream_t st)
 {
-    constexpr int KT = sizeof(E) == 4 ? 32 : 64;
-    typedef Backward<E, D, KT, kWaves> FQ;
-    typedef Backward<E, D, kRowTile, kWaves> FK;
-    const long heads = (long)S.B * S.Hk;
-    int rc = allow_lds<k_query_grads<E, D, KT, kWaves>>(FQ::kQueryLds);
-    if (rc == BRA_OK) rc = allow_lds<k_key_grads<E, D, kRowTile, kWaves>>(FK::kKeyLds);
+    typedef Queries<E, D, WAVES> F;
+    const int rc = allow_lds<k_query_grads<E, D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
-    A.tiles = (A.rows + FQ::kRows - 1) / FQ::kRows;
+    A.tiles = (A.rows + F::kMine - 1) / F::kMine;
     A.splits = splits_of(S, false);
     A.blocks = A.tiles * A.splits * heads;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_QUERY_GRADS);
-        k_query_grads<E, D, KT, kWaves><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FQ::kThreads, FQ::kQueryLds, st>>>(A);
+        k_query_grads<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
-    if (A.splits > 1 && (rc = join<E, D, false>(A, heads, st)) != BRA_OK) return rc;
-    A.tiles = (A.Nk + FK::kRows - 1) / FK::kRows;
+    return A.splits > 1 ? join<E, D, false>(A, heads, st) : BRA_OK;
+}
+
+template <class E, int D, int WAVES>
+int key_grads(const Sizes &S, Call A, long heads, hipStream_t st)
+{
+    typedef Backward<E, D, WAVES> F;
+    const int rc = allow_lds<k_key_grads<E, D, WAVES>>(F::kLds);
+    if (rc != BRA_OK) return rc;
+    A.tiles = (A.Nk + F::kMine - 1) / F::kMine;
     A.splits = splits_of(S, true);
     A.blocks = A.tiles * A.splits * heads;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_KEY_GRADS);
-        k_key_grads<E, D, kRowTile, kWaves><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), FK::kThreads, FK::kKeyLds, st>>>(A);
+        k_key_grads<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return A.splits > 1 ? join<E, D, true>(A, heads, st) : BRA_OK;
+}
+
+template <class E, int D>
+int run(const Sizes &S, const Call &A, hipStream_t st)
+{
+    const long heads = (long)S.B * S.Hk;
+    const int rc = waves_of(S.rows()) == 2 ? query_grads<E, D, 2>(S, A, heads, st) : query_grads<E, D, 4>(S, A, heads, st);
+    if (rc != BRA_OK) return rc;
+    return waves_of(S.Nk) == 2 ? key_grads<E, D, 2>(S, A, heads, st) : key_grads<E, D, 4>(S, A, heads, st);
 }
 
 template <class E>

@@ -356,6 +356,45 @@ struct Walk {
     }
 };
 
+// The same for rows whose places are at(row), `step` bytes further on with every tile, or (0) anywhere.
+template <class G, int ROWS, int THREADS>
+struct Tiles {
+    static constexpr int kLoads = ROWS * G::kPieces, L = (kLoads + THREADS - 1) / THREADS;
+    static_assert(kLoads % THREADS == 0 || (kLoads < THREADS && kLoads % 64 == 0), "whole loads of a wavefront");
+    static constexpr int kLoaders = kLoads < THREADS ? kLoads / 64 : THREADS / 64;      // wavefronts that load
+    const char *place[L];
+    long step;
+    int wave, row, end;     // this wavefront; the next tile's first row, where rows end
+    bool whole;             // rows fill the pitch
+    __device__ static __forceinline__ int row_of(int u, int thread) { return (thread + THREADS * u) / G::kPieces; }
+    __device__ static __forceinline__ int piece_of(int u, int thread) { return (thread + THREADS * u) % G::kPieces ^ G::turn(row_of(u, thread)); }
+    template <class F>
+    __device__ __forceinline__ Tiles(F at, long step_, int first, int end_, int pieces, int thread)
+        : step(step_), wave(__builtin_amdgcn_readfirstlane(thread / 64)), row(first), end(end_), whole(pieces == G::kPieces)
+    {
+#pragma unroll
+        for (int u = 0; u < L; ++u) place[u] = at(first + row_of(u, thread)) + 16 * piece_of(u, thread);
+    }
+    template <class F>
+    __device__ __forceinline__ void request(unsigned lds, int pieces, int thread, F at)
+    {
+        const unsigned to = lds + 1024 * wave;
+        if (wave < kLoaders) {
+            if (whole && row + ROWS <= end) {
+#pragma unroll
+                for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)place[u], to + 16 * THREADS * u);
+            } else {
+#pragma unroll
+                for (int u = 0; u < L; ++u)
+                    load_to_lds_untracked((const bf16_t *)(row + row_of(u, thread) < end && piece_of(u, thread) < pieces ? place[u] : (const char *)zeros), to + 16 * THREADS * u);
+            }
+        }
+        row += ROWS;
+#pragma unroll
+        for (int u = 0; u < L; ++u) place[u] = step ? place[u] + step : at(row + row_of(u, thread)) + 16 * piece_of(u, thread);
+    }
+};
+
 // Of the two lanes of a column.
 __device__ __forceinline__ float pair_max(float v)
 {
