@@ -165,15 +165,15 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
 // Many rows: the wavefronts of a workgroup have 32 rows each and share tiles of KT keys and values, the next of which is on its way.
 template <class E, int D, int WAVES>
 struct Main {
-    typedef Geometry<E, D> G;
-    typedef Slots<G> S;
-    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES, KT = sizeof(E) == 4 ? 32 : 64;
-    static constexpr int kTile = KT * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile;        // K, V, K, V
-    typedef Walk<G, KT, kThreads> Loads;
+    static constexpr int T = sizeof(E) == 4 ? 3 : 1, kThreads = 64 * WAVES, kRows = 32 * WAVES, KT = T == 3 ? 32 : 64;
+    typedef Geometry<bf16_t, D> G;
+    static constexpr int kPlane = KT * G::kPitch, kTile = T * kPlane, kSub = 32 * G::kPitch, kLds = 4 * kTile;       // K, V, K, V
+    typedef Slots<G, T, kPlane> S;
+    typedef Walk<G, T, KT, kThreads> Loads;
 };
 
 template <class E, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E) == 2 && D <= 64 ? 3 : 2) void k_attention_rows(Call A)
+__global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : sizeof(E) == 2 && D <= 64 ? 3 : 2) void k_attention_rows(Call A)
 {
     typedef Main<E, D, WAVES> F;
     typedef typename F::G G;
@@ -185,7 +185,6 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
-    const int pieces = A.d * (int)sizeof(E) / 16;
 
     const int first_row = tile * F::kRows, row = first_row + 32 * wave + c;
     const bool valid = row < A.rows;
@@ -197,18 +196,17 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E
     const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, first = split * share, last = min(all, first + share);
 
     const unsigned at = lds_address(lds);
-    typename F::Loads keys(A.K.p + b * A.K.batch + hk * A.K.head + (long)first * KT * A.K.token, A.K.token, seq.nk - first * KT, pieces, threadIdx.x);
-    typename F::Loads values(A.V.p + b * A.V.batch + hk * A.V.head + (long)first * KT * A.V.token, A.V.token, seq.nk - first * KT, pieces, threadIdx.x);
-    typename G::Piece x[G::kSteps];
+    typename F::Loads keys(key_source<G, F::T>(A, A.K, A.pK, b, hb, seq.nk), first * KT, threadIdx.x), values(key_source<G, F::T>(A, A.V, A.pV, b, hb, seq.nk), first * KT, threadIdx.x);
+    typename S::Columns x;
     {
         const int head = hk * A.G + min(row, A.rows - 1) - query * A.G;
-        load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
+        S::template load<E>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, A.d / 8, h, x);
     }
     if (first < last) {
-        keys.request(at, pieces, threadIdx.x);
-        values.request(at + F::kTile, pieces, threadIdx.x);
+        keys.request(at, threadIdx.x);
+        values.request(at + F::kTile, threadIdx.x);
     }
-    arrived<G>(x);
+    S::arrived(x);
 
     const Reader<G> reader(lane);
     f32x16 acc[G::NT];
@@ -221,8 +219,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 96 ? 1 : sizeof(E
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (t + 1 < last) {
-            keys.request(at + kOther, pieces, threadIdx.x);
-            values.request(at + kOther + F::kTile, pieces, threadIdx.x);
+            keys.request(at + kOther, threadIdx.x);
+            values.request(at + kOther + F::kTile, threadIdx.x);
         }
         const int k0 = t * KT;
         if (k0 >= most) return;
@@ -421,7 +419,7 @@ using namespace att;
 size_t attention_workspace_bytes(const Sizes &S)
 {
     const long splits = splits_of(S), rows = S.rows() * S.B * S.Hk;
-    return splits > 1 ? align256(sizeof(float) * splits * rows * S.width()) + align256(2 * sizeof(float) * splits * rows) : 0;
+    return (S.f32 && !few(S) ? terms_bytes(S, false) : 0) + (splits > 1 ? align256(sizeof(float) * splits * rows * S.width()) + align256(2 * sizeof(float) * splits * rows) : 0);
 }
 
 int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, float *lse, void *ws, hipStream_t st)
@@ -435,6 +433,11 @@ int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &
     A.tiles = (int)row_tiles(S);
     A.splits = splits_of(S);
     A.blocks = (long)A.tiles * A.splits * S.B * S.Hk;
+    if (S.f32 && !few(S)) {
+        const int rc = make_terms(S, A, false, ws, st);
+        if (rc != BRA_OK) return rc;
+        ws = (char *)ws + terms_bytes(S, false);
+    }
     if (A.splits > 1) {
         A.part = (float *)ws;
         A.part_ml = (float *)((char *)ws + align256(sizeof(float) * A.splits * S.rows() * S.B * S.Hk * S.width()));

@@ -13,11 +13,11 @@ namespace {
 
 template <class E, int D, int WAVES>
 struct Queries {
-    typedef Geometry<E, D> G;
-    typedef Slots<G> S;
-    static constexpr int kThreads = 64 * WAVES, kMine = 32 * WAVES, KT = sizeof(E) == 4 ? 32 : 64;
-    static constexpr int kTile = KT * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile;        // K, V, K, V
-    typedef Walk<G, KT, kThreads> Loads;
+    static constexpr int T = sizeof(E) == 4 ? 3 : 1, kThreads = 64 * WAVES, kMine = 32 * WAVES, KT = T == 3 ? 32 : 64;
+    typedef Geometry<bf16_t, D> G;
+    static constexpr int kPlane = KT * G::kPitch, kTile = T * kPlane, kSub = 32 * G::kPitch, kLds = 4 * kTile;       // K, V, K, V
+    typedef Slots<G, T, kPlane> S;
+    typedef Walk<G, T, KT, kThreads> Loads;
 };
 
 template <class E, int D, int WAVES>
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
-    const int pieces = A.d * (int)sizeof(E) / 16;
+    const int pieces = A.d / 8;
 
     const int first_row = tile * F::kMine, row = first_row + 32 * wave + c, some = min(row, A.rows - 1);
     const bool valid = row < A.rows;
@@ -44,24 +44,19 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, first = split * share, last = min(all, first + share);
 
     const unsigned at = lds_address(lds);
-    typename F::Loads keys(A.K.p + b * A.K.batch + hk * A.K.head + (long)first * KT * A.K.token, A.K.token, seq.nk - first * KT, pieces, threadIdx.x);
-    typename F::Loads values(A.V.p + b * A.V.batch + hk * A.V.head + (long)first * KT * A.V.token, A.V.token, seq.nk - first * KT, pieces, threadIdx.x);
+    typename F::Loads keys(key_source<G, F::T>(A, A.K, A.pK, b, hb, seq.nk), first * KT, threadIdx.x), values(key_source<G, F::T>(A, A.V, A.pV, b, hb, seq.nk), first * KT, threadIdx.x);
     if (first < last) {
-        keys.request(at, pieces, threadIdx.x);
-        values.request(at + F::kTile, pieces, threadIdx.x);
+        keys.request(at, threadIdx.x);
+        values.request(at + F::kTile, threadIdx.x);
     }
-    typename G::Piece x[G::kSteps], g[G::kSteps];
-    load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
-    load_columns<G>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, limit > 0, pieces, h, g);
+    typename S::Columns x, g;
+    const char *dO = A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head;
+    S::template load<E>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
+    S::template load<E>(dO, limit > 0, pieces, h, g);
     float delta = 0.f, lse = 0.f;
     {
-        typename G::Piece o[G::kSteps];
-        load_columns<G>(A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces, h, o);
+        delta = row_product<E>(dO, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces, G::kSteps, h);
         if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
-#pragma unroll
-        for (int ks = 0; ks < G::kSteps; ++ks)
-#pragma unroll
-            for (int e = 0; e < 16 / (int)sizeof(E); ++e) delta = fmaf((float)g[ks][e], (float)o[ks][e], delta);
         delta = pair_sum(delta);
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
         if (valid && h == 0 && split == 0) {
@@ -69,8 +64,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
             A.row_delta[(long)hb * A.rows + row] = delta;
         }
     }
-    arrived<G>(x);
-    arrived<G>(g);
+    S::arrived(x);
+    S::arrived(g);
 
     const Reader<G> reader(lane);
     f32x16 acc[G::NT];
@@ -82,8 +77,8 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (t + 1 < last) {
-            keys.request(at + kOther, pieces, threadIdx.x);
-            values.request(at + kOther + F::kTile, pieces, threadIdx.x);
+            keys.request(at + kOther, threadIdx.x);
+            values.request(at + kOther + F::kTile, threadIdx.x);
         }
         const int k0 = t * KT;
         if (k0 >= most) return;
@@ -125,12 +120,12 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
 // k_key_grads walks over subtiles of 32 rows, kRing of which are in LDS: while the weights of one are formed, the products of the one before with its
 // weights are on their way, a product between every few of the other instructions; then come the products of the next one with what the wavefront keeps
 // in registers.
-template <class E, int D, int WAVES>
+template <int D, int WAVES>
 struct Backward {
-    typedef Geometry<E, D> G;
-    typedef Slots<G> S;
+    typedef Geometry<bf16_t, D> G;
+    typedef Slots<G, 1, 0> S;
     static constexpr int kThreads = 64 * WAVES, kMine = 32 * WAVES;
-    static constexpr int kRing = sizeof(E) == 4 && D > 64 ? 4 : 5;
+    static constexpr int kRing = 5;
     static constexpr int kTile = 32 * G::kPitch, kSlot = 2 * kTile + 256, kLds = kRing * kSlot;      // two tensors, lse and delta
     typedef Tiles<G, 32, kThreads> Loads;
 };
@@ -138,14 +133,15 @@ struct Backward {
 // A wavefront's registers over the subtiles.
 template <class G, bool KEYS>
 struct Pipe {
-    typedef Slots<G> S;
+    typedef Slots<G, 1, 0> S;
+    typedef typename S::Columns X;
     static constexpr int kColumns = (KEYS ? 2 : 1) * S::kColumns, kReadAhead = 2 * S::kRows < 8 ? 2 * S::kRows : 8;
     f32x16 s[2];                                // scores and dP of a subtile
     typename S::Weights p, ds;                  // of the subtile before
     f32x16 sum[KEYS ? 2 : 1][G::NT];            // dV and dK, or dQ
 
     // s of a subtile
-    __device__ __forceinline__ void scores(const char *t0, const char *t1, const Reader<G> &R, const typename G::Piece (&x)[G::kSteps], const typename G::Piece (&g)[G::kSteps])
+    __device__ __forceinline__ void scores(const char *t0, const char *t1, const Reader<G> &R, const X &x, const X &g)
     {
         s[0] = s[1] = f32x16{};
         unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
@@ -178,8 +174,7 @@ struct Pipe {
     // s -> p, ds; with COLUMNS the sums of the subtile before, in b0, b1, on the way; then s of the next one, in n0, n1.  weights(r): value r's
     // -lse log2 e and delta.  Operands are read kBefore products ahead.
     template <bool COLUMNS, class W>
-    __device__ __forceinline__ void step(const char *b0, const char *b1, const char *n0, const char *n1, const Reader<G> &R, const typename G::Piece (&x)[G::kSteps],
-                                         const typename G::Piece (&g)[G::kSteps], float c, W weights)
+    __device__ __forceinline__ void step(const char *b0, const char *b1, const char *n0, const char *n1, const Reader<G> &R, const X &x, const X &g, float c, W weights)
     {
         constexpr int N = COLUMNS ? kColumns : 1, all = N + 2 * S::kRows, kBefore = kReadAhead;
         typename S::Operand o[all];
@@ -206,8 +201,8 @@ struct Pipe {
             });
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (KEYS) S::copy(p, np);
-        S::copy(ds, nds);
+        if (KEYS) p = np;
+        ds = nds;
         s[0] = s[1] = f32x16{};
         unrolled<2 * S::kRows>([&](auto i) __attribute__((always_inline)) {
             constexpr int f = N + i;
@@ -219,7 +214,7 @@ struct Pipe {
 };
 
 // A workgroup's subtiles [0, n), of which this wavefront works on [from, to).  Turn j has the subtiles j - 1 to j + 1 in LDS; before it, what was asked
-// for in turn j - 3 (j - 2 with the shorter ring) has arrived everywhere, and then subtile j + kRing - 2 is asked for, where j - 2 lay.  `own`: this wavefront's
+// for in turn j - 3 has arrived everywhere, and then subtile j + kRing - 2 is asked for, where j - 2 lay.  `own`: this wavefront's
 // loads of a subtile.
 template <class F, class Scores, class Weights, class Sums, class Request>
 __device__ __forceinline__ void take_turns(int n, int from, int to, bool one_more, bool loads, Scores scores, Weights weights, Sums sums, Request request)
@@ -228,7 +223,7 @@ __device__ __forceinline__ void take_turns(int n, int from, int to, bool one_mor
     for (int j = 0; j < min(n, F::kRing - 3); ++j) request(j);
     auto turn = [&](int j) __attribute__((always_inline)) {
         // (fewer loads than this are on their way in the last turns: all of them are waited for)
-        if (F::kRing == 4 || j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         else if (one_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L + 1) : "memory");
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L) : "memory");
         __builtin_amdgcn_s_barrier();
@@ -253,10 +248,12 @@ __device__ __forceinline__ void take_turns(int n, int from, int to, bool one_mor
     for (; j <= n; ++j) turn(j);
 }
 
-template <class E, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D > 64 || sizeof(E) == 4 ? 1 : 2) void k_key_grads(Call A)
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A)
 {
-    typedef Backward<E, D, WAVES> F;
+    typedef bf16_t E;
+    typedef Backward<D, WAVES> F;
+    typedef typename F::S S;
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
@@ -264,7 +261,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || sizeof(E) == 4 ? 1 : 2) void 
     const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
-    const int pieces = A.d * (int)sizeof(E) / 16;
+    const int pieces = A.d / 8;
 
     // rows begin .. end - 1 see this lane's key
     const int first_key = tile * F::kMine, key = first_key + 32 * wave + c, end = seq.nq * A.G;
@@ -275,12 +272,12 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || sizeof(E) == 4 ? 1 : 2) void 
     const int front = begin_of(first_key) / 32, all = first_key < seq.nk ? max((end + 31) / 32 - front, 0) : 0, share = (all + A.splits - 1) / A.splits;
     const int first = front + split * share, n = min(all, (split + 1) * share) - split * share, row0 = 32 * first;
 
-    typename G::Piece x[G::kSteps], g[G::kSteps];
+    typename S::Columns x, g;
     const int some = live ? key : 0;
-    load_columns<G>(A.K.p + b * A.K.batch + some * A.K.token + hk * A.K.head, live, pieces, h, x);
-    load_columns<G>(A.V.p + b * A.V.batch + some * A.V.token + hk * A.V.head, live, pieces, h, g);
-    arrived<G>(x);
-    arrived<G>(g);
+    S::template load<E>(A.K.p + b * A.K.batch + some * A.K.token + hk * A.K.head, live, pieces, h, x);
+    S::template load<E>(A.V.p + b * A.V.batch + some * A.V.token + hk * A.V.head, live, pieces, h, g);
+    S::arrived(x);
+    S::arrived(g);
 
     const unsigned at = lds_address(lds);
     const char *q = A.Q.p + b * A.Q.batch + hk * A.G * A.Q.head, *o = A.dO.p + b * A.dO.batch + hk * A.G * A.dO.head;
@@ -334,6 +331,125 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 || sizeof(E) == 4 ? 1 : 2) void 
             grads.request(at + slot(j) + F::kTile, pieces, threadIdx.x, grad_at);
             if (wave == 0) load4_to_lds_untracked(row_sums + min(row0 + 32 * j + c, A.rows - 1), at + slot(j) + 2 * F::kTile);
         });
+    if (key >= A.Nk) return;
+    if (!live) {
+        clear(pipe.sum[0]);
+        clear(pipe.sum[1]);
+    }
+    if (A.splits > 1) {
+        float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
+        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, D, h);
+        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, D, h);
+    } else {
+        store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, pipe.sum[1], A.scale, A.d, h);
+        store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, pipe.sum[0], 1.f, A.d, h);
+    }
+}
+
+// float32: subtiles of 32 rows, the next of which is on its way.
+template <int D, int WAVES>
+struct BackwardF32 {
+    static constexpr int T = 3, kThreads = 64 * WAVES, kMine = 32 * WAVES;
+    typedef Geometry<bf16_t, D> G;
+    static constexpr int kPlane = 32 * G::kPitch, kTile = T * kPlane, kSlot = 2 * kTile + 256, kLds = 2 * kSlot;     // Q, dO, lse and delta
+    typedef Slots<G, T, kPlane> S;
+    typedef Walk<G, T, 32, kThreads> Loads;
+};
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Call A)
+{
+    typedef float E;
+    typedef BackwardF32<D, WAVES> F;
+    typedef typename F::S S;
+    typedef typename F::G G;
+    extern __shared__ char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
+    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
+    const Sequence seq(A, b);
+    const int pieces = A.d / 8;
+
+    // rows begin .. end - 1 see this lane's key
+    const int first_key = tile * F::kMine, key = first_key + 32 * wave + c, end = seq.nq * A.G;
+    auto begin_of = [&](int j) { return seq.causal ? min(max(j - seq.off, 0), seq.nq) * A.G : 0; };
+    const bool live = key < seq.nk;
+    const int begin = live ? begin_of(key) : end;
+    const int wave_key = first_key + 32 * wave, least = begin_of(wave_key), most = wave_key + 31 < seq.nk ? begin_of(wave_key + 31) : end;
+    const int front = begin_of(first_key) / 32, all = first_key < seq.nk ? max((end + 31) / 32 - front, 0) : 0, share = (all + A.splits - 1) / A.splits;
+    const int first = front + min(all, split * share), last = front + min(all, (split + 1) * share);
+
+    const unsigned at = lds_address(lds);
+    typename F::Loads queries(row_source<G>(A, A.pQ, hb), 32 * first, threadIdx.x), grads(row_source<G>(A, A.pG, hb), 32 * first, threadIdx.x);
+    const float *row_sums = (h ? A.row_delta : A.row_lse) + (long)hb * A.rows;
+    auto request = [&](int t, int slot) __attribute__((always_inline)) {
+        queries.request(at + slot, threadIdx.x);
+        grads.request(at + slot + F::kTile, threadIdx.x);
+        if (wave == 0) load4_to_lds_untracked(row_sums + min(32 * t + c, A.rows - 1), at + slot + 2 * F::kTile);
+    };
+    if (first < last) request(first, 0);
+    typename S::Columns x, g;
+    const int some = live ? key : 0;
+    S::template load<E>(A.K.p + b * A.K.batch + some * A.K.token + hk * A.K.head, live, pieces, h, x);
+    S::template load<E>(A.V.p + b * A.V.batch + some * A.V.token + hk * A.V.head, live, pieces, h, g);
+    S::arrived(x);
+    S::arrived(g);
+
+    const Reader<G> reader(lane);
+    struct {
+        f32x16 sum[2][G::NT];           // dV and dK
+    } pipe;
+    clear(pipe.sum[0]);
+    clear(pipe.sum[1]);
+    auto body = [&](auto B, int t) __attribute__((always_inline)) {
+        constexpr int kMine = decltype(B)::value * F::kSlot, kOther = F::kSlot - kMine;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 1 < last) request(t + 1, kOther);
+        const int r0 = 32 * t;
+        if (r0 + 32 <= least || wave_key >= seq.nk) return;
+        const char *qt = lds + kMine, *gt = qt + F::kTile;
+        const float *ls = (const float *)(gt + F::kTile) + 4 * h;
+        f32x16 s{}, d{};
+        unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_rows(o, f % 2 ? gt : qt, reader, f / 2);
+            S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
+        });
+        if (r0 < most || r0 + 32 > end) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = r0 + result_row(r, h);
+                const bool see = i >= begin && i < end;
+                s[r] = see ? s[r] : -INFINITY;
+                d[r] = see ? d[r] : 0.f;
+            }
+        }
+        typename S::Weights p, ds;
+        unrolled<4>([&](auto q) __attribute__((always_inline)) {
+            const f32x4 l4 = *(const f32x4 *)(ls + 8 * q), d4 = *(const f32x4 *)(ls + 32 + 8 * q);
+            unrolled<4>([&](auto e) __attribute__((always_inline)) {
+                constexpr int i = e, r = 4 * decltype(q)::value + i;
+                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -l4[i]));
+                d[r] = s[r] * (d[r] - d4[i]);
+                if constexpr (r % 2) {
+                    S::keep(p, s, r);
+                    S::keep(ds, d, r);
+                }
+            });
+        });
+        unrolled<2 * S::kColumns>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_columns(o, f % 2 ? qt : gt, reader, f / 2);
+            S::columns(pipe.sum[f % 2], o, f % 2 ? ds : p, f / 2);
+        });
+    };
+    for (int t = first; t < last; t += 2) {
+        body(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < last) body(std::integral_constant<int, 1>{}, t + 1);
+    }
     if (key >= A.Nk) return;
     if (!live) {
         clear(pipe.sum[0]);
@@ -430,15 +546,20 @@ int query_grads(const Sizes &S, Call A, long heads, hipStream_t st)
 template <class E, int D, int WAVES>
 int key_grads(const Sizes &S, Call A, long heads, hipStream_t st)
 {
-    typedef Backward<E, D, WAVES> F;
-    const int rc = allow_lds<k_key_grads<E, D, WAVES>>(F::kLds);
+    constexpr bool f32 = sizeof(E) == 4;
+    typedef typename std::conditional<f32, BackwardF32<D, WAVES>, Backward<D, WAVES>>::type F;
+    int rc;
+    if constexpr (f32) rc = allow_lds<k_key_grads_f32<D, WAVES>>(F::kLds);
+    else rc = allow_lds<k_key_grads<D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
     A.tiles = (A.Nk + F::kMine - 1) / F::kMine;
     A.splits = splits_of(S, true);
     A.blocks = A.tiles * A.splits * heads;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_KEY_GRADS);
-        k_key_grads<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        const unsigned n = (unsigned)std::min(kMaxBlocks, A.blocks - A.first);
+        if constexpr (f32) k_key_grads_f32<D, WAVES><<<n, F::kThreads, F::kLds, st>>>(A);
+        else k_key_grads<D, WAVES><<<n, F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return A.splits > 1 ? join<E, D, true>(A, heads, st) : BRA_OK;
@@ -469,7 +590,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
 
 using namespace att;
 
-size_t attention_backward_workspace_bytes(const Sizes &S) { return 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)); }
+size_t attention_backward_workspace_bytes(const Sizes &S) { return 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)) + (S.f32 ? terms_bytes(S, true) : 0); }
 
 int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, const float *lse, const Rows &dO, const Rows &dQ, const Rows &dK,
                        const Rows &dV, void *ws, hipStream_t st)
@@ -487,6 +608,10 @@ int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows 
     A.row_lse = (float *)ws;
     A.row_delta = (float *)((char *)ws + align256(sizeof(float) * S.rows() * S.B * S.Hk));
     A.part = (float *)((char *)A.row_delta + align256(sizeof(float) * S.rows() * S.B * S.Hk));
+    if (S.f32) {
+        const int rc = make_terms(S, A, true, (char *)A.part + align256(part_bytes(S)), st);
+        if (rc != BRA_OK) return rc;
+    }
     return S.f32 ? run<float>(S, A, st) : run<bf16_t>(S, A, st);
 }
 

@@ -4,7 +4,9 @@
 // the keys, four and four), O^T = V^T P^T takes that result as its right operand as it stands in the registers, since the order of the contraction
 // is free: step kk takes the keys 16 kk + 4 h + 0..3 and 16 kk + 8 + 4 h + 0..3 from half h of the wavefront, and V^T is read from LDS in
 // the same order.  No value of S or P moves between lanes.  The backward pass does the same with keys in the columns.
-// bf16: 32x32x16 instructions, the transposed operand by the transposing LDS read.  float32: 32x32x2 instructions, the same layouts.
+// bf16: 32x32x16 instructions, the transposed operand by the transposing LDS read.  float32 with many rows: three bf16 terms to a value, x = hi + mid +
+// lo, and the six products of terms that matter (2^-23 of a product is left out), the small ones first: on the float32 instruction, which few rows take, a
+// product takes 16 bf16 ones' time, this way 6.
 #pragma once
 
 #include "bra_attention.h"
@@ -38,6 +40,10 @@ struct Call {
     Rows dO, dQ, dK, dV;
     const float *lse_in;
     float *row_lse, *row_delta;     // [B Hk, rows]: lse log2 e, and sum of dO O
+    // float32 as three planes of bf16 terms, [B Hk][rows rounded up to 64][pitch] each, zero behind lengths and widths
+    const char *pK, *pV, *pQ, *pG;
+    long key_plane, row_plane;      // bytes from a plane to the next
+    int key_rows, row_rows;         // of a head in a plane
 };
 
 // row / G: the product with 2^32 / G, rounded up, is too large by one at most.
@@ -228,27 +234,19 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[N])
 // A wavefront's reads of a tile in LDS, as offsets from its first row, for subtiles of 32 rows from a multiple of 32 on.
 template <class G>
 struct Reader {
-    unsigned row[G::kSteps], column[G::kF32 ? 2 : 2 * G::NT];
+    unsigned row[G::kSteps], column[2 * G::NT];
     __device__ __forceinline__ explicit Reader(int lane)
     {
-        const int h = lane / 32, c = lane % 32;
+        const int h = lane / 32, c = lane % 32, s = lane % 16, q = lane / 16, col4 = s % 2 * 2 + s % 4 / 2;
 #pragma unroll
         for (int ks = 0; ks < G::kSteps; ++ks) row[ks] = c * G::kPitch + 16 * ((2 * ks + h) ^ G::turn(c));
-        if constexpr (!G::kF32) {
-            const int s = lane % 16, q = lane / 16, col4 = s % 2 * 2 + s % 4 / 2;
 #pragma unroll
-            for (int t = 0; t < G::NT; ++t)
+        for (int t = 0; t < G::NT; ++t)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int r = 8 * half + 4 * h + s / 4, o = 32 * t + 16 * (q % 2) + 4 * col4;
-                    column[2 * t + half] = r * G::kPitch + 16 * ((o / 8) ^ G::turn(r)) + 2 * (o % 8);
-                }
-        } else {
-            // rows 8 a + 4 h + b of a subtile, a channel of 32: turn() of the row is that of 4 h with b in front of it and a % 2 behind
-            const int channel = c / 16 * 16 + c / 4 % 2 * 8 + c / 8 % 2 * 4 + c % 4;
-            column[0] = 4 * h * G::kPitch + 4 * (channel % 4);
-            column[1] = channel / 4 ^ G::turn(4 * h);
-        }
+            for (int half = 0; half < 2; ++half) {
+                const int r = 8 * half + 4 * h + s / 4, o = 32 * t + 16 * (q % 2) + 4 * col4;
+                column[2 * t + half] = r * G::kPitch + 16 * ((o / 8) ^ G::turn(r)) + 2 * (o % 8);
+            }
     }
 };
 
@@ -261,88 +259,172 @@ __device__ __forceinline__ void unrolled(F f)
     }
 }
 
-// One product of a subtile: slot f of kRowSlots multiplies rows into s, slot f of kColumnSlots columns into acc.  A slot's operand is read some
-// slots before.
-template <class G>
+// One product of a subtile: slot f of kRows multiplies rows into s, slot f of kColumns columns into acc.  T terms to a value, whose tiles are PLANE bytes apart.
+template <class G, int T, int PLANE>
 struct Slots {
-    static constexpr int kRows = G::kSteps, kColumns = G::kF32 ? 16 : 2 * G::NT;
+    static constexpr int kRows = G::kSteps, kColumns = 2 * G::NT;
     struct Operand {
-        typename std::conditional<G::kF32, f32x4, u32x4>::type v;
+        u32x4 v[T];
     };
-    __device__ static __forceinline__ void read_rows(Operand &o, const char *tile, const Reader<G> &R, const int f) { o.v = *(const decltype(o.v) *)(tile + R.row[f]); }
+    struct Columns {            // what a wavefront keeps: 32 rows as column operands
+        bf16x8 v[T][G::kSteps];
+    };
+    struct Weights {            // 32 values of the contraction
+        u32x4 v[T][2];
+    };
+    __device__ static __forceinline__ f32x16 product(const Operand &a, const bf16x8 (&b)[T], f32x16 c)
+    {
+        auto one = [&](int i, int j) __attribute__((always_inline)) { c = mfma32(__builtin_bit_cast(bf16x8, a.v[i]), b[j], c); };
+        if constexpr (T == 3) {
+            one(2, 0);
+            one(0, 2);
+            one(1, 1);
+            one(1, 0);
+            one(0, 1);
+        }
+        one(0, 0);
+        return c;
+    }
+    __device__ static __forceinline__ void read_rows(Operand &o, const char *tile, const Reader<G> &R, int f)
+    {
+#pragma unroll
+        for (int t = 0; t < T; ++t) o.v[t] = *(const u32x4 *)(tile + t * PLANE + R.row[f]);
+    }
     __device__ static __forceinline__ void read_columns(Operand &o, const char *tile, const Reader<G> &R, int f)
     {
-        if constexpr (G::kF32) {
-            const int row = 8 * (f / 4) + f % 4;            // + 4 h
+        const int kk = f / G::NT, n = f % G::NT;
 #pragma unroll
-            for (int t = 0; t < G::NT; ++t) {
-                const int piece = (8 * t) ^ (R.column[1] ^ G::turn(row));
-                o.v[t] = *(const float *)(tile + R.column[0] + row * G::kPitch + 16 * piece);
-            }
-        } else {
-            const int kk = f / G::NT, t = f % G::NT;
+        for (int t = 0; t < T; ++t) {
             u32x2 r[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) r[half] = __builtin_bit_cast(u32x2, lds_read_tr16((const bf16_t *)(tile + 16 * kk * G::kPitch + R.column[2 * t + half])));
-            o.v = u32x4{r[0][0], r[0][1], r[1][0], r[1][1]};
+            for (int half = 0; half < 2; ++half) r[half] = __builtin_bit_cast(u32x2, lds_read_tr16((const bf16_t *)(tile + t * PLANE + 16 * kk * G::kPitch + R.column[2 * n + half])));
+            o.v[t] = u32x4{r[0][0], r[0][1], r[1][0], r[1][1]};
         }
     }
-    __device__ static __forceinline__ void rows(f32x16 &s, const Operand &o, const typename G::Piece (&x)[G::kSteps], int f)
+    __device__ static __forceinline__ void rows(f32x16 &s, const Operand &o, const Columns &x, int f)
     {
-        if constexpr (G::kF32) {
+        bf16x8 b[T];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = mfma_f32(o.v[e], x[f][e], s);
-        } else s = mfma32(__builtin_bit_cast(bf16x8, o.v), x[f], s);
-    }
-    typedef typename std::conditional<G::kF32, f32x16, u32x4[2]>::type Weights;        // 32 values of the contraction: float32, or bf16 pairs
-    __device__ static __forceinline__ void copy(Weights &p, const Weights &q)
-    {
-        if constexpr (G::kF32) p = q;
-        else {
-            p[0] = q[0];
-            p[1] = q[1];
-        }
-    }
-    // Values r - 1 and r of them.
-    __device__ static __forceinline__ void keep(Weights &p, const f32x16 &s, int r)
-    {
-        if constexpr (G::kF32) {
-            p[r - 1] = s[r - 1];
-            p[r] = s[r];
-        } else p[r / 8][r % 8 / 2] = pack_bf16(s[r - 1], s[r]);
+        for (int t = 0; t < T; ++t) b[t] = x.v[t][f];
+        s = product(o, b, s);
     }
     __device__ static __forceinline__ void columns(f32x16 (&acc)[G::NT], const Operand &o, const Weights &p, int f)
     {
-        if constexpr (G::kF32) {
+        bf16x8 b[T];
 #pragma unroll
-            for (int t = 0; t < G::NT; ++t) acc[t] = mfma_f32(o.v[t], p[f], acc[t]);
-        } else acc[f % G::NT] = mfma32(__builtin_bit_cast(bf16x8, o.v), __builtin_bit_cast(bf16x8, p[f / G::NT]), acc[f % G::NT]);
+        for (int t = 0; t < T; ++t) b[t] = __builtin_bit_cast(bf16x8, p.v[t][f / G::NT]);
+        acc[f % G::NT] = product(o, b, acc[f % G::NT]);
+    }
+    // Values r - 1 and r of the weights.
+    __device__ static __forceinline__ void keep(Weights &p, const f32x16 &s, int r)
+    {
+        float a = s[r - 1], b = s[r];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const unsigned u = pack_bf16(a, b);
+            p.v[t][r / 8][r % 8 / 2] = u;
+            a -= bf16_lo(u);
+            b -= bf16_hi(u);
+        }
+    }
+    // A row of a tensor (or zeros), pieces 2 ks + h of 8 channels of `pieces`.
+    template <class E>
+    __device__ static __forceinline__ void load(const char *p, bool valid, int pieces, int h, Columns &x)
+    {
+#pragma unroll
+        for (int ks = 0; ks < G::kSteps; ++ks) {
+            const int piece = 2 * ks + h;
+            const bool there = valid && piece < pieces;
+            if constexpr (T == 1) x.v[0][ks] = *(const bf16x8 *)(there ? p + 16 * piece : (const char *)zeros);
+            else {
+                const f32x4 v0 = *(const f32x4 *)(there ? p + 32 * piece : (const char *)zeros), v1 = *(const f32x4 *)(there ? p + 32 * piece + 16 : (const char *)zeros);
+                const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                bf16x8 t[3];
+                split3(v, t);
+#pragma unroll
+                for (int i = 0; i < T; ++i) x.v[i][ks] = t[i];
+            }
+        }
+    }
+    // The operands have arrived.  Without it the compiler, which does not count the direct loads, waits for the registers' loads at their first use in
+    // the loop over the tiles, and with them for the tile that is on its way, every time.
+    __device__ static __forceinline__ void arrived(Columns &x)
+    {
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int ks = 0; ks < G::kSteps; ++ks) asm volatile("" : "+v"(x.v[t][ks]));
     }
 };
 
-// Direct loads of a tensor's tiles of ROWS rows one after the other: a lane's pointers go on by a tile each time.
-template <class G, int ROWS, int THREADS>
+// sum over a row's channels of a b, this lane's pieces of them
+template <class E>
+__device__ __forceinline__ float row_product(const char *a, const char *b, bool valid, int pieces, int steps, int h)
+{
+    float sum = 0.f;
+    for (int ks = 0; ks < steps; ++ks) {
+        const int piece = 2 * ks + h;
+        if (!valid || piece >= pieces) continue;
+        if constexpr (sizeof(E) == 2) {
+            const bf16x8 x = *(const bf16x8 *)(a + 16 * piece), y = *(const bf16x8 *)(b + 16 * piece);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 x = *(const f32x4 *)(a + 32 * piece + 16 * i), y = *(const f32x4 *)(b + 32 * piece + 16 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = fmaf(x[e], y[e], sum);
+            }
+        }
+    }
+    return sum;
+}
+
+// Where tiles of keys (rows) of a head come from: the tensor itself, or its planes of terms, which have whole rows and zeros behind the end.
+struct Source {
+    const char *p;
+    long token, plane;
+    int rows, pieces;
+};
+template <class G, int T>
+__device__ __forceinline__ Source key_source(const Call &A, const Rows &R, const char *planes, int b, int hb, int nk)
+{
+    if constexpr (T == 1) return Source{R.p + b * R.batch + (hb - b * A.Hk) * R.head, R.token, 0, nk, A.d / 8};
+    else return Source{planes + (long)hb * A.key_rows * G::kPitch, G::kPitch, A.key_plane, A.key_rows, G::kPieces};
+}
+template <class G>
+__device__ __forceinline__ Source row_source(const Call &A, const char *planes, int hb)
+{
+    return Source{planes + (long)hb * A.row_rows * G::kPitch, G::kPitch, A.row_plane, A.row_rows, G::kPieces};
+}
+
+// Direct loads of its tiles of ROWS rows one after the other, from row `first` on: a lane's pointers go on by a tile each time.
+template <class G, int T, int ROWS, int THREADS>
 struct Walk {
-    static constexpr int L = ROWS * G::kPieces / THREADS;
-    static_assert(L * THREADS == ROWS * G::kPieces, "whole loads");
+    static constexpr int kLoads = ROWS * G::kPieces, L = (kLoads + THREADS - 1) / THREADS, kTile = ROWS * G::kPitch;
+    static_assert(kLoads % THREADS == 0 || (kLoads < THREADS && kLoads % 64 == 0), "whole loads of a wavefront");
     const char *at[L];
-    long step;
+    long step, plane;
     unsigned wave;          // LDS offset of this wavefront's part
-    int left;               // rows from the next tile on
-    bool whole;             // rows fill the pitch
-    __device__ __forceinline__ Walk(const char *first, long token, int rows, int pieces, int thread) : step(ROWS * token), wave(1024 * __builtin_amdgcn_readfirstlane(thread / 64)), left(rows), whole(pieces == G::kPieces)
+    int left, pieces;       // rows from the next tile on; pieces of a row
+    __device__ __forceinline__ Walk(const Source &S, int first, int thread)
+        : step(ROWS * S.token), plane(S.plane), wave(1024 * __builtin_amdgcn_readfirstlane(thread / 64)), left(S.rows - first), pieces(S.pieces)
     {
 #pragma unroll
         for (int u = 0; u < L; ++u) {
             const int i = thread + THREADS * u, row = i / G::kPieces, piece = i % G::kPieces ^ G::turn(row);
-            at[u] = first + row * token + 16 * piece;
+            at[u] = S.p + (first + row) * S.token + 16 * piece;
         }
     }
-    __device__ __forceinline__ void request(unsigned lds, int pieces, int thread)
+    __device__ __forceinline__ void request(unsigned lds, int thread)
     {
-        if (whole && left >= ROWS) {
+        if (kLoads < THREADS && wave >= kLoads * 16) return;        // the first wavefronts load it all
+        if (T > 1 || (pieces == G::kPieces && left >= ROWS)) {
 #pragma unroll
-            for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)at[u], lds + wave + 16 * THREADS * u);
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)(at[u] + t * plane), lds + wave + t * kTile + 16 * THREADS * u);
         } else {
 #pragma unroll
             for (int u = 0; u < L; ++u) {
@@ -356,7 +438,7 @@ struct Walk {
     }
 };
 
-// The same for rows whose places are at(row), `step` bytes further on with every tile, or (0) anywhere.
+// The same for one term and rows whose places are at(row), `step` bytes further on with every tile, or (0) anywhere.
 template <class G, int ROWS, int THREADS>
 struct Tiles {
     static constexpr int kLoads = ROWS * G::kPieces, L = (kLoads + THREADS - 1) / THREADS;
@@ -471,6 +553,10 @@ struct Running {
 __device__ __forceinline__ int result_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
 Call make_call(const Sizes &S);
+
+// float32: the planes of terms of keys and values, in the backward pass of queries and dO too (bra_attention_terms.hip).
+size_t terms_bytes(const Sizes &S, bool backward);
+int make_terms(const Sizes &S, Call &A, bool backward, void *ws, hipStream_t st);
 
 constexpr long kMaxBlocks = 1L << 22;       // of a launch: fewer than 2^32 threads
 
