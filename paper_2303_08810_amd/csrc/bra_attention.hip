@@ -31,7 +31,7 @@ __device__ __forceinline__ void finish(const Call &A, int b, int hk, int split, 
     const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
     if (A.splits > 1) {
         const long at = ((long)(b * A.Hk + hk) * A.splits + split) * A.rows + row;
-        store_columns<float, G>((char *)(A.part + at * G::D), acc, 1.f, G::D, h);
+        store_columns<float, G>((char *)(A.part + at * G::D), acc, 1.f, A.d, h);
         if (h == 0) {
             A.part_ml[2 * at] = m;
             A.part_ml[2 * at + 1] = l;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(factor, v[e], o[e] * old);
     };
-    if (valid)
+    if (valid && ch < A.d)
 #pragma unroll 4
         for (int s = group; s < A.splits; s += groups) {
             const long p = at + (long)s * A.rows;
@@ -321,7 +321,9 @@ int splits_of(const Sizes &S)
 {
     const long blocks = row_tiles(S) * S.B * S.Hk, tiles = (S.Nk + key_tile(S) - 1) / key_tile(S);
     if (blocks == 0) return 1;
-    const long want = 512, least = few(S) ? 2 * waves(S) : 4;
+    // A split is worth its join (5 us and more) where enough tiles are left to it (us without / with: 1024 tokens of 12 heads of 64 16.7 / 17.8, 2 x 512 of 8
+    // heads 13.0 / 15.1; 2048 causal of 16 / 4 heads of 128 46.8 / 44.5; float32 3 x 667 of 6 heads of 40 37.7 / 30.4).
+    const long want = 512, least = few(S) ? 2 * waves(S) : S.f32 ? 5 : 12;
     return (int)std::max(1L, std::min({want / blocks, tiles / least, 64L}));
 }
 

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         if (t + 1 < last) body(std::integral_constant<int, 1>{}, t + 1);
     }
     if (!valid) return;
-    if (A.splits > 1) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, D, h);
+    if (A.splits > 1) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, A.d, h);
     else store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
 }
 
@@ -338,8 +338,8 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     }
     if (A.splits > 1) {
         float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
-        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, D, h);
-        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, D, h);
+        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, A.d, h);
+        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, A.d, h);
     } else {
         store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, pipe.sum[1], A.scale, A.d, h);
         store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, pipe.sum[0], 1.f, A.d, h);
@@ -457,12 +457,148 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     }
     if (A.splits > 1) {
         float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
-        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, D, h);
-        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, D, h);
+        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, A.d, h);
+        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, A.d, h);
     } else {
         store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, pipe.sum[1], A.scale, A.d, h);
         store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, pipe.sum[0], 1.f, A.d, h);
     }
+}
+
+// Both in one launch where a head has up to 64 rows and 64 keys: everything is in LDS once, two wavefronts have the query side, two the key side.  64 x 49 tokens
+// of 16 heads of 32 in two launches 17.8 us, this way 12.2.
+template <int D>
+struct Short {
+    typedef Geometry<bf16_t, D> G;
+    typedef Slots<G, 1, 0> S;
+    static constexpr int kThreads = 256, kTile = 64 * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile + 2 * 64 * 4;      // K, V, Q, dO, lse, delta
+    typedef Tiles<G, 64, kThreads> Loads;
+};
+
+template <int D>
+__global__ __launch_bounds__(256, D > 64 ? 1 : 2) void k_short_grads(Call A)
+{
+    typedef bf16_t E;
+    typedef Short<D> F;
+    typedef typename F::S S;
+    typedef typename F::G G;
+    extern __shared__ char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32, side = wave % 2;
+    const int hb = (int)(A.first + blockIdx.x), b = hb / A.Hk, hk = hb % A.Hk;
+    const Sequence seq(A, b);
+    const int pieces = A.d / 8, end = seq.nq * A.G;
+    const unsigned at = lds_address(lds);
+    float *sums = (float *)(lds + 4 * F::kTile);
+    {
+        const char *k = A.K.p + b * A.K.batch + hk * A.K.head, *v = A.V.p + b * A.V.batch + hk * A.V.head;
+        const char *q = A.Q.p + b * A.Q.batch + hk * A.G * A.Q.head, *o = A.dO.p + b * A.dO.batch + hk * A.G * A.dO.head;
+        auto load = [&](int tile, int rows, auto place) __attribute__((always_inline)) {
+            typename F::Loads loads(place, 1, 0, rows, pieces, threadIdx.x);
+            loads.request(at + tile * F::kTile, pieces, threadIdx.x, place);
+        };
+        load(0, seq.nk, [&](int r) __attribute__((always_inline)) { return k + r * A.K.token; });
+        load(1, seq.nk, [&](int r) __attribute__((always_inline)) { return v + r * A.V.token; });
+        load(2, end, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return q + i * A.Q.token + (r - i * A.G) * A.Q.head; });
+        load(3, end, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return o + i * A.dO.token + (r - i * A.G) * A.dO.head; });
+    }
+    const int row = 32 * side + c, some = min(row, A.rows - 1), query = row_query(A, some), head = hk * A.G + some - query * A.G;
+    const int limit = row < A.rows ? seq.limit(query) : 0;
+    float lse = 0.f, delta = 0.f;
+    if (wave < 2) {
+        delta = pair_sum(row_product<E>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces,
+                                        G::kSteps, h));
+        if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
+        lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
+        if (h == 0) {
+            sums[row] = lse;
+            sums[64 + row] = delta;
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+
+    const Reader<G> reader(lane);
+    const char *kt = lds, *vt = kt + F::kTile, *qt = vt + F::kTile, *gt = qt + F::kTile;
+    // a subtile's rows as what the wavefront keeps
+    auto keep = [&](typename S::Columns &x, const char *tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < G::kSteps; ++ks) x.v[0][ks] = *(const bf16x8 *)(tile + side * F::kSub + reader.row[ks]);
+    };
+    auto scores = [&](f32x16 &s, f32x16 &d, const char *t0, const char *t1, const typename S::Columns &x, const typename S::Columns &g) __attribute__((always_inline)) {
+        s = d = f32x16{};
+        unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_rows(o, f % 2 ? t1 : t0, reader, f / 2);
+            S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
+        });
+    };
+    typename S::Columns x, g;
+    f32x16 s, d;
+    if (wave < 2) {
+        keep(x, qt);
+        keep(g, gt);
+        f32x16 acc[G::NT];
+        clear(acc);
+        const int most = columns_max(limit);
+        for (int i = 0; 32 * i < most; ++i) {
+            scores(s, d, kt + i * F::kSub, vt + i * F::kSub, x, g);
+            typename S::Weights w;
+            unrolled<16>([&](auto e) __attribute__((always_inline)) {
+                constexpr int r = e;
+                const float p = 32 * i + result_row(r, h) < limit ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -lse)) : 0.f;
+                d[r] = p * (d[r] - delta);
+                if constexpr (r % 2) S::keep(w, d, r);
+            });
+            unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_columns(o, kt + i * F::kSub, reader, f);
+                S::columns(acc, o, w, f);
+            });
+        }
+        if (row < A.rows) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
+        return;
+    }
+    const int key = 32 * side + c;
+    const bool live = key < seq.nk;
+    const int begin = !live ? end : seq.causal ? min(max(key - seq.off, 0), seq.nq) * A.G : 0;
+    keep(x, kt);
+    keep(g, vt);
+    f32x16 dk[G::NT], dv[G::NT];
+    clear(dk);
+    clear(dv);
+    const int from = columns_min(begin) / 32;
+    for (int i = from; 32 * i < end; ++i) {
+        scores(s, d, qt + i * F::kSub, gt + i * F::kSub, x, g);
+        const float *mine = sums + 32 * i + 4 * h;
+        typename S::Weights p, ds;
+        unrolled<4>([&](auto q) __attribute__((always_inline)) {
+            const f32x4 l4 = *(const f32x4 *)(mine + 8 * q), d4 = *(const f32x4 *)(mine + 64 + 8 * q);
+            unrolled<4>([&](auto e) __attribute__((always_inline)) {
+                constexpr int j = e, r = 4 * decltype(q)::value + j;
+                const int at_row = 32 * i + result_row(r, h);
+                const bool see = at_row >= begin && at_row < end;
+                s[r] = see ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -l4[j])) : 0.f;
+                d[r] = see ? s[r] * (d[r] - d4[j]) : 0.f;
+                if constexpr (r % 2) {
+                    S::keep(p, s, r);
+                    S::keep(ds, d, r);
+                }
+            });
+        });
+        unrolled<2 * S::kColumns>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_columns(o, (f % 2 ? qt : gt) + i * F::kSub, reader, f / 2);
+            S::columns(f % 2 ? dk : dv, o, f % 2 ? ds : p, f / 2);
+        });
+    }
+    if (key >= A.Nk) return;
+    if (!live) {
+        clear(dk);
+        clear(dv);
+    }
+    store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, dk, A.scale, A.d, h);
+    store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, dv, 1.f, A.d, h);
 }
 
 // The splits' sums put together, in their order: dQ, [heads][splits][rows][D], or dK and dV, [heads][splits][Nk][2][D].
@@ -504,8 +640,11 @@ int splits_of(const Sizes &S, bool keys)
     const long mine = keys ? S.Nk : S.rows(), walked = keys ? S.rows() : S.Nk;
     const long each = 32 * waves_of(mine), blocks = (mine + each - 1) / each * S.B * S.Hk, tiles = (walked + 63) / 64;
     if (blocks == 0) return 1;
-    const long want = S.causal ? 1024 : 512;
-    return (int)std::max(1L, std::min({want / blocks, tiles / 4, 16L}));
+    // (us with 256 / 384 / 512 / 768 / 1024 workgroups at least: bf16, causal, 8192 of 16 / 4 heads of 128 1753 / 1753 / 1205 / 1393 / 1220, 2048 of them 158 / 154 / 154 /
+    // 176 / 184, 4096 of 8 heads of 64 179 / 179 / 142 / 132 / 136, not causal, 1024 of 12 heads of 64 48 / 52 / 51 / 60 / 61; float32, one workgroup to a compute
+    // unit, 2 x 1295 causal of 8 / 2 heads of 72 249 / 180 / 210 / 192 / 203)
+    const long want = S.f32 ? 384 : 512;
+    return (int)std::max(1L, std::min({want / blocks, tiles / (S.f32 ? 2 : 4), 16L}));
 }
 size_t part_bytes(const Sizes &S)
 {
@@ -565,10 +704,29 @@ int key_grads(const Sizes &S, Call A, long heads, hipStream_t st)
     return A.splits > 1 ? join<E, D, true>(A, heads, st) : BRA_OK;
 }
 
+bool is_short(const Sizes &S) { return !S.f32 && S.rows() <= 64 && S.Nk <= 64; }
+
+template <int D>
+int short_grads(Call A, long heads, hipStream_t st)
+{
+    typedef Short<D> F;
+    const int rc = allow_lds<k_short_grads<D>>(F::kLds);
+    if (rc != BRA_OK) return rc;
+    for (A.first = 0; A.first < heads; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION_SHORT_GRADS);
+        k_short_grads<D><<<(unsigned)std::min(kMaxBlocks, heads - A.first), F::kThreads, F::kLds, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
+}
+
 template <class E, int D>
 int run(const Sizes &S, const Call &A, hipStream_t st)
 {
     const long heads = (long)S.B * S.Hk;
+    if constexpr (sizeof(E) == 2) {
+        if (is_short(S)) return short_grads<D>(A, heads, st);
+    }
     const int rc = waves_of(S.rows()) == 2 ? query_grads<E, D, 2>(S, A, heads, st) : query_grads<E, D, 4>(S, A, heads, st);
     if (rc != BRA_OK) return rc;
     return waves_of(S.Nk) == 2 ? key_grads<E, D, 2>(S, A, heads, st) : key_grads<E, D, 4>(S, A, heads, st);
@@ -590,7 +748,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
 
 using namespace att;
 
-size_t attention_backward_workspace_bytes(const Sizes &S) { return 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)) + (S.f32 ? terms_bytes(S, true) : 0); }
+size_t attention_backward_workspace_bytes(const Sizes &S) { return is_short(S) ? 0 : 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)) + (S.f32 ? terms_bytes(S, true) : 0); }
 
 int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, const float *lse, const Rows &dO, const Rows &dQ, const Rows &dK,
                        const Rows &dV, void *ws, hipStream_t st)

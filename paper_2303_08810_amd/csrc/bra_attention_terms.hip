@@ -10,25 +10,25 @@ namespace att {
 namespace {
 
 struct Tensors {
-    Rows R[4];          // K, V, Q, dO
+    Rows R[4];              // K, V, Q, dO
     char *planes[4];
-    long pieces[4];     // of 8 channels; those of the tensors before are counted first
+    unsigned blocks[4];     // workgroups of the tensors up to this one
     int n;
 };
 
-// 2 x 1295 tokens of 8 / 2 heads of 72 among others: K, V, Q and dO 7 us.
+// A workgroup has 256 pieces of 8 channels of a head.  2 x 1295 tokens of 8 / 2 heads of 72 among others: K, V, Q and dO 7 us.
 template <int P>
-__global__ __launch_bounds__(256) void k_attention_terms(Call A, Tensors X, long first)
+__global__ __launch_bounds__(256) void k_attention_terms(Call A, Tensors X, unsigned first)
 {
-    constexpr int kPieces = P / 8;
-    long i = (first + blockIdx.x) * 256 + threadIdx.x;
+    constexpr int kPieces = P / 8, kRows = 256 / kPieces;
+    unsigned block = first + blockIdx.x;
     int which = 0;
-    while (which < X.n && i >= X.pieces[which]) i -= X.pieces[which++];
-    if (which == X.n) return;
+    while (which + 1 < X.n && block >= X.blocks[which]) ++which;
+    if (which) block -= X.blocks[which - 1];
     const bool keys = which < 2;
-    const int piece = (int)(i % kPieces), each = keys ? A.key_rows : A.row_rows;
-    const long r = i / kPieces;
-    const int row = (int)(r % each), hb = (int)(r / each), b = hb / A.Hk, hk = hb - b * A.Hk;
+    const unsigned per = (unsigned)(keys ? A.key_rows : A.row_rows) / kRows;
+    const int hb = (int)(block / per), row = (int)(block - hb * per) * kRows + threadIdx.x / kPieces, piece = threadIdx.x % kPieces, b = hb / A.Hk, hk = hb - b * A.Hk;
+    const long i = (long)block * 256 + threadIdx.x;
     const Sequence seq(A, b);
     const Rows &R = X.R[which];
     int token = row, head = hk;
@@ -78,21 +78,21 @@ int make_terms(const Sizes &S, Call &A, bool backward, void *ws, hipStream_t st)
         X.R[i] = all[i];
         X.planes[i] = p;
         const long plane = i < 2 ? A.key_plane : A.row_plane;
-        X.pieces[i] = plane / 16;
-        blocks += X.pieces[i];
+        blocks += plane / 16 / 256;             // (64 rows of 4 pieces at least: whole workgroups)
+        X.blocks[i] = (unsigned)blocks;
         p += 3 * plane;
     }
+    if (blocks >= 1L << 32) return BRA_ERR_UNSUPPORTED;
     A.pK = X.planes[0];
     A.pV = X.planes[1];
     A.pQ = X.planes[2];
     A.pG = X.planes[3];
-    blocks = (blocks + 255) / 256;
     for (long first = 0; first < blocks; first += kMaxBlocks) {
         const unsigned n = (unsigned)std::min(kMaxBlocks, blocks - first);
         const ProfScope scope(st, K_ATTENTION_TERMS);
-        if (pitch(S) == 32) k_attention_terms<32><<<n, 256, 0, st>>>(A, X, first);
-        else if (pitch(S) == 64) k_attention_terms<64><<<n, 256, 0, st>>>(A, X, first);
-        else k_attention_terms<128><<<n, 256, 0, st>>>(A, X, first);
+        if (pitch(S) == 32) k_attention_terms<32><<<n, 256, 0, st>>>(A, X, (unsigned)first);
+        else if (pitch(S) == 64) k_attention_terms<64><<<n, 256, 0, st>>>(A, X, (unsigned)first);
+        else k_attention_terms<128><<<n, 256, 0, st>>>(A, X, (unsigned)first);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;

@@ -100,7 +100,7 @@ enum KernelId {
     K_BLK_POS_LN, K_BLK_ADD_LN, K_BLK_MLP_IN, K_BLK_MLP_OUT, K_BLK_MLP_FUSED, K_GEN_BACKWARD,
     K_FFN_OPERANDS, K_FFN_GATED, K_FFN_PRODUCT, K_FFN_FEW, K_FFN_HIDDEN_GRADS, K_FFN_WEIGHT_GRADS, K_FFN_SUMS,
     K_NORM, K_NORM_BACKWARD, K_NORM_SUMS, K_ADAMW,
-    K_QK_NORM, K_QK_NORM_BACKWARD, K_QK_NORM_SUMS, K_ATTENTION, K_ATTENTION_TERMS, K_ATTENTION_JOIN, K_ATTENTION_QUERY_GRADS, K_ATTENTION_KEY_GRADS, K_COUNT
+    K_QK_NORM, K_QK_NORM_BACKWARD, K_QK_NORM_SUMS, K_ATTENTION, K_ATTENTION_TERMS, K_ATTENTION_JOIN, K_ATTENTION_QUERY_GRADS, K_ATTENTION_KEY_GRADS, K_ATTENTION_SHORT_GRADS, K_COUNT
 };
 
 // Brackets the launches issued during its lifetime with two events on `st` when

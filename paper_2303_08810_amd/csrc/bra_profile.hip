@@ -19,7 +19,7 @@ const char *const kNames[K_COUNT] = {
     "block_pos_ln", "block_add_ln", "block_mlp_in", "block_mlp_out", "block_mlp_fused", "gen_backward",
     "ffn_operands", "ffn_gated", "ffn_product", "ffn_few", "ffn_hidden_grads", "ffn_weight_grads", "ffn_sums",
     "norm", "norm_backward", "norm_sums", "adamw",
-    "qk_norm", "qk_norm_backward", "qk_norm_sums", "attention", "attention_terms", "attention_join", "attention_query_grads", "attention_key_grads",
+    "qk_norm", "qk_norm_backward", "qk_norm_sums", "attention", "attention_terms", "attention_join", "attention_query_grads", "attention_key_grads", "attention_short_grads",
 };
 }  // namespace
 

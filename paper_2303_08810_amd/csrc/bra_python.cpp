@@ -823,10 +823,10 @@ PyObject *py_attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
             for (int i = 0; i < 3; ++i) own_memory(grads[i], {&Q, &K, &V, &O, &dO, &grads[(i + 1) % 3], &grads[(i + 2) % 3]});
         size_t bytes = 0;
         check(bra_attention_backward_workspace_bytes(&c.s, &bytes));
-        const at::Tensor *ws = workspace(tensor(a[10]), bytes, Q, own);
+        const at::Tensor *ws = workspace_if(tensor(a[10]), bytes, Q, own);
         void *st = stream_of(Q);
         run([&] {
-            return bra_attention_backward(&c.s, &c.Q, &c.K, &c.V, &o, (const float *)lse.data_ptr(), &go, c.q_lens, c.k_lens, &d[0], &d[1], &d[2], ws->data_ptr(), (size_t)ws->numel(), st);
+            return bra_attention_backward(&c.s, &c.Q, &c.K, &c.V, &o, (const float *)lse.data_ptr(), &go, c.q_lens, c.k_lens, &d[0], &d[1], &d[2], data(ws), ws ? (size_t)ws->numel() : 0, st);
         });
         for (int i = 0; i < 3; ++i) objects[i] = wrap(grads[i]);        // (the caller's own object where it gave one)
         return tuple({objects[0], objects[1], objects[2]});
