@@ -346,12 +346,13 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
  * A tensor [B, N, heads, d] is given by a bra_rows: its element (b, n, h, c) lies at data + b batch + n token + h head + c, in elements, so that
  * parts of one buffer, or a cache with the heads outside, are taken as they lie.  Pointers, and strides in bytes, are multiples of 16 (the stride
  * of a dimension of one entry is not looked at); inputs may have strides of 0.  What is written overlaps neither itself nor an input.
- * d: a multiple of 8 up to 128 (heads that are no multiple of 32 wide take the time of the next one).  bf16 tensors: bf16 matrix instructions, P
- * rounded to bf16 before its product with V, everything else float32.  float32 tensors: the float32 matrix instruction.
+ * d: a multiple of 8 up to 128 (heads that are no multiple of 32 wide take the time of the next one).  bf16 tensors: P is rounded to bf16 before its product
+ * with V, everything else is float32.  float32 tensors: products of three bf16 terms per operand (relative error of a product 2^-23; a value that is not
+ * finite, or above 3.3e38, makes NaN of what depends on it), up to 32 rows (queries times heads / kv_heads) forward the float32 matrix instruction.
  * scale <= 0 selects 1 / sqrt(d).  No atomic adds: a repeat gives the same bits.  Nothing else than `ws` is needed; its size depends on the shape and
  * may be 0.
  * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite, negative
- * strides, B heads or Nq heads above 2^30); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; LAUNCH. */
+ * strides, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; LAUNCH. */
 typedef struct bra_attention_shape {
     int32_t B, Nq, Nk;        /* sequences; queries and keys of each, at most */
     int32_t heads, kv_heads;  /* heads of the queries, of keys and values */

@@ -133,6 +133,7 @@ static int make_attention_sizes(const bra_attention_shape *s, att::Sizes &S)
         s->d < 1 || !std::isfinite(s->scale))
         return BRA_ERR_SHAPE;
     if ((long)s->B * s->heads > (1L << 30) || (long)s->Nq * s->heads > (1L << 30)) return BRA_ERR_SHAPE;
+    if ((long)s->B * s->heads > (1L << 40) / std::max({s->Nq, s->Nk, 1})) return BRA_ERR_SHAPE;
     if (s->dtype != BRA_F32 && s->dtype != BRA_BF16) return BRA_ERR_DTYPE;
     if (s->d % 8 || s->d > 128) return BRA_ERR_UNSUPPORTED;
     S = att::Sizes{s->B, s->Nq, s->Nk, s->heads, s->kv_heads, s->d, s->dtype == BRA_F32, s->causal != 0, s->scale > 0.f ? s->scale : 1.0f / sqrtf((float)s->d), nullptr, nullptr};

@@ -40,7 +40,7 @@ struct Call {
     Rows dO, dQ, dK, dV;
     const float *lse_in;
     float *row_lse, *row_delta;     // [B Hk, rows]: lse log2 e, and sum of dO O
-    // float32 as three planes of bf16 terms, [B Hk][rows rounded up to 64][pitch] each, zero behind lengths and widths
+    // float32 as three planes of bf16 terms, [B Hk][rows rounded up to 32][pitch] each, zero behind lengths and widths
     const char *pK, *pV, *pQ, *pG;
     long key_plane, row_plane;      // bytes from a plane to the next
     int key_rows, row_rows;         // of a head in a plane

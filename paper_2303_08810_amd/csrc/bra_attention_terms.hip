@@ -1,5 +1,5 @@
 // float32 operands of attention as three bf16 terms each, hi + mid + lo, in planes that the products' tiles are loaded from: keys and values a head after
-// the other, queries and dO as rows (query, head) of a key head.  Zero behind the lengths, behind the last row up to a multiple of 64, and behind a head's
+// the other, queries and dO as rows (query, head) of a key head.  Zero behind the lengths, behind the last row up to a multiple of 32, and behind a head's
 // channels up to the pitch, so that the tiles need no bounds.  Bound by memory.
 #include "bra_attention_dev.h"
 
@@ -16,11 +16,11 @@ struct Tensors {
     int n;
 };
 
-// A workgroup has 256 pieces of 8 channels of a head.  2 x 1295 tokens of 8 / 2 heads of 72 among others: K, V, Q and dO 7 us.
+// A workgroup has 128 pieces of 8 channels of a head.  2 x 1295 tokens of 8 / 2 heads of 72 among others: K, V, Q and dO 7 us.
 template <int P>
-__global__ __launch_bounds__(256) void k_attention_terms(Call A, Tensors X, unsigned first)
+__global__ __launch_bounds__(128) void k_attention_terms(Call A, Tensors X, unsigned first)
 {
-    constexpr int kPieces = P / 8, kRows = 256 / kPieces;
+    constexpr int kPieces = P / 8, kRows = 128 / kPieces;
     unsigned block = first + blockIdx.x;
     int which = 0;
     while (which + 1 < X.n && block >= X.blocks[which]) ++which;
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void k_attention_terms(Call A, Tensors X, unsi
     const bool keys = which < 2;
     const unsigned per = (unsigned)(keys ? A.key_rows : A.row_rows) / kRows;
     const int hb = (int)(block / per), row = (int)(block - hb * per) * kRows + threadIdx.x / kPieces, piece = threadIdx.x % kPieces, b = hb / A.Hk, hk = hb - b * A.Hk;
-    const long i = (long)block * 256 + threadIdx.x;
+    const long i = (long)block * 128 + threadIdx.x;
     const Sequence seq(A, b);
     const Rows &R = X.R[which];
     int token = row, head = hk;
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void k_attention_terms(Call A, Tensors X, unsi
 }
 
 int pitch(const Sizes &S) { return S.width() <= 32 ? 32 : S.width() <= 64 ? 64 : 128; }
-long padded(long rows) { return (rows + 63) / 64 * 64; }
+long padded(long rows) { return (rows + 31) / 32 * 32; }
 long plane_bytes(const Sizes &S, long rows) { return (long)S.B * S.Hk * padded(rows) * pitch(S) * 2; }
 
 }  // namespace
@@ -78,7 +78,7 @@ int make_terms(const Sizes &S, Call &A, bool backward, void *ws, hipStream_t st)
         X.R[i] = all[i];
         X.planes[i] = p;
         const long plane = i < 2 ? A.key_plane : A.row_plane;
-        blocks += plane / 16 / 256;             // (64 rows of 4 pieces at least: whole workgroups)
+        blocks += plane / 16 / 128;             // (32 rows of 4 pieces at least: whole workgroups)
         X.blocks[i] = (unsigned)blocks;
         p += 3 * plane;
     }
@@ -90,9 +90,9 @@ int make_terms(const Sizes &S, Call &A, bool backward, void *ws, hipStream_t st)
     for (long first = 0; first < blocks; first += kMaxBlocks) {
         const unsigned n = (unsigned)std::min(kMaxBlocks, blocks - first);
         const ProfScope scope(st, K_ATTENTION_TERMS);
-        if (pitch(S) == 32) k_attention_terms<32><<<n, 256, 0, st>>>(A, X, (unsigned)first);
-        else if (pitch(S) == 64) k_attention_terms<64><<<n, 256, 0, st>>>(A, X, (unsigned)first);
-        else k_attention_terms<128><<<n, 256, 0, st>>>(A, X, (unsigned)first);
+        if (pitch(S) == 32) k_attention_terms<32><<<n, 128, 0, st>>>(A, X, (unsigned)first);
+        else if (pitch(S) == 64) k_attention_terms<64><<<n, 128, 0, st>>>(A, X, (unsigned)first);
+        else k_attention_terms<128><<<n, 128, 0, st>>>(A, X, (unsigned)first);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;

@@ -1,0 +1,231 @@
+"""Attention between whole sequences where it can go wrong: steep and far scores, lengths out of range, what lies around the outputs, strides and offsets, refusals, streams and
+graphs, NaN, many heads."""
+import math
+
+import pytest
+import torch
+
+import paper_2303_08810_amd as bra
+from attention_util import Attention, check
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def make(B, Nq, Nk, H, Hk, d, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, generator=g).to(dtype).cuda()
+    return randn(B, Nq, H, d), randn(B, Nk, Hk, d), randn(B, Nk, Hk, d), randn(B, Nq, H, d)
+
+
+def verify(Q, K, V, dO, **rule):
+    """Both passes against the 64-bit form, and what a repeat gives."""
+    ref = Attention(Q, K, V, **rule)
+    O_ref, lse_ref, O_off, lse_off = ref.forward()
+    O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True, **rule)
+    check(O, O_ref, O_off, "O")
+    check(lse, lse_ref, lse_off, "lse")
+    O_in, lse_in = O_ref.to(Q.dtype), lse_ref.float()
+    grads = bra.bra_attention_backward(Q, K, V, O_in, lse_in, dO, **rule)
+    for name, got, (want, off) in zip(("dQ", "dK", "dV"), grads, ref.backward(O_in, lse_in, dO)):
+        check(got, want, off, name)
+    return O, lse, grads
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Nq,Nk,causal", [(1, 900, False), (70, 900, False), (300, 300, True)])
+@pytest.mark.parametrize("kind", ["rising", "falling", "low", "high", "spike"])
+def test_steep_scores(kind, Nq, Nk, causal, dtype):
+    """Scores that rise or fall along the keys by hundreds, that are all far below or above 0, one that is far above the others."""
+    Q, K, V, dO = make(2, Nq, Nk, 2, 1, 64, dtype, seed=3)
+    ramp = torch.linspace(0, 1, Nk, device="cuda")[None, :, None]
+    Q[..., 0] = 8.0
+    K[..., 0] = {"rising": 400 * ramp, "falling": -400 * ramp, "low": -900 + 0 * ramp, "high": 900 + 0 * ramp,
+                 "spike": torch.where(torch.arange(Nk, device="cuda")[None, :, None] == Nk - 7, 300.0, 0.0)}[kind].to(dtype)
+    verify(Q, K, V, dO, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_lengths_out_of_range(dtype):
+    Q, K, V, dO = make(4, 50, 90, 2, 2, 40, dtype)
+    lens = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    rule = dict(q_lens=lens(-5, 51, 2 ** 31 - 1, 7), k_lens=lens(90, -2 ** 31, 1000, 0))
+    O, lse, grads = verify(Q, K, V, dO, **rule)
+    assert not O[0].any() and not O[1].any() and not O[3].any() and bool((lse[1] == -math.inf).all())
+    clamped = dict(q_lens=lens(0, 50, 50, 7), k_lens=lens(90, 0, 90, 0))
+    assert torch.equal(O, bra.bra_attention_forward(Q, K, V, **clamped))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [49, 300])
+def test_outputs_leave_what_is_around_them(N, dtype):
+    """Gradients into the parts of a packed buffer, O into every other head of one: the rest keeps its values, rows behind the lengths become zero."""
+    B, H, Hk, d = 3, 4, 2, 56
+    X = torch.randn(B, N, H + 2 * Hk, d, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    Q, K, V = X[:, :, :H], X[:, :, H:H + Hk], X[:, :, H + Hk:]
+    lens = torch.tensor([N, 5, 0], dtype=torch.int32, device="cuda")
+    rule = dict(causal=True, q_lens=lens, k_lens=lens)
+    wide = torch.full((B, N, 2 * H, d + 8), 7.0, dtype=dtype, device="cuda")
+    place = wide[:, :, ::2, :d]
+    out, lse = bra.bra_attention_forward(Q, K, V, want_lse=True, out=place, **rule)
+    assert out is place
+    O = bra.bra_attention_forward(Q, K, V, **rule)
+    assert torch.equal(place, O) and bool((wide[:, :, 1::2] == 7).all()) and bool((wide[..., d:] == 7).all())
+    assert not O[1, 5:].any() and not O[2].any()
+    dO = torch.randn(B, N, H, d, generator=torch.Generator().manual_seed(2)).to(dtype).cuda()
+    buffer = torch.full((B, N, H + 2 * Hk + 1, d), math.nan, dtype=dtype, device="cuda")
+    parts = buffer[:, :, :H], buffer[:, :, H:H + Hk], buffer[:, :, H + Hk:-1]
+    got = bra.bra_attention_backward(Q, K, V, O, lse, dO, out=parts, **rule)
+    assert all(a is b for a, b in zip(got, parts))
+    for a, b in zip(parts, bra.bra_attention_backward(Q, K, V, O, lse, dO, **rule)):
+        assert torch.equal(a, b) and not a[1, 5:].any() and not a[2].any()
+    assert bool(buffer[:, :, -1].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_broadcast_inputs(dtype):
+    """Strides of 0: one key head and one sequence's keys for all, a constant dO."""
+    Q, K, V, dO = make(3, 40, 77, 4, 1, 32, dtype)
+    K, V = K[:1].expand(3, -1, 4, -1), V[:, :, :1].expand(-1, -1, 4, -1)
+    dO = dO[:, :1, :1].expand(3, 40, 4, 32)
+    verify(Q, K, V, dO)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_beyond_32_bits(dtype):
+    """A cache whose tokens lie 16 MB apart."""
+    Nk, far = 300, (16 << 20) // (2 if dtype == BF16 else 4)
+    store = torch.empty(far * (Nk + 1), dtype=dtype, device="cuda")
+    g = torch.Generator().manual_seed(4)
+    place = store.as_strided((1, Nk, 2, 64), (0, far, 64, 1))
+    K = torch.randn(1, Nk, 2, 64, generator=g).to(dtype).cuda()
+    place.copy_(K)
+    for Nq in (1, 100):
+        Q, V, dO = (torch.randn(1, n, h, 64, generator=g).to(dtype).cuda() for n, h in ((Nq, 4), (Nk, 2), (Nq, 4)))
+        for a, b in ((place, V), (V, place)):
+            O, lse = bra.bra_attention_forward(Q, a, b, want_lse=True)
+            assert torch.equal(O, bra.bra_attention_forward(Q, a.contiguous(), b.contiguous()))
+            for x, y in zip(bra.bra_attention_backward(Q, a, b, O, lse, dO), bra.bra_attention_backward(Q, a.contiguous(), b.contiguous(), O, lse, dO)):
+                assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("N,dtype", [(1, BF16), (40, BF16), (1, F32)])
+def test_more_heads_than_a_launch_has_workgroups(N, dtype):
+    """2^22 workgroups and more in several launches: the last heads as they come out on their own.  (In float32 the gradients' planes of terms for as many heads would take 100 GB.)"""
+    B, H = (1 << 22) // 8 + 3, 8
+    Q, K, V, dO = (torch.randn(B, N, H, 8, dtype=dtype, device="cuda") for _ in range(4))
+    print("many heads", N, dtype, flush=True)
+    O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+    grads = bra.bra_attention_backward(Q, K, V, O, lse, dO) if dtype == BF16 else ()
+    for part in (slice(0, 3), slice(B // 2, B // 2 + 3), slice(B - 4, B)):
+        q, k, v, o = Q[part], K[part], V[part], dO[part]
+        ref = Attention(q, k, v)
+        O_ref, lse_ref, O_off, lse_off = ref.forward()
+        check(O[part], O_ref, O_off, "O")
+        check(lse[part], lse_ref, lse_off, "lse")
+        for name, got, (want, off) in zip(("dQ", "dK", "dV"), grads, ref.backward(O[part], lse[part], o)):
+            check(got[part], want, off, name)
+
+
+@pytest.mark.parametrize("H,Hk", [(64, 1), (40, 8), (33, 3)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_heads_to_a_key_head(H, Hk, dtype):
+    Q, K, V, dO = make(2, 11, 150, H, Hk, 48, dtype)
+    verify(Q, K, V, dO, causal=True, k_lens=torch.tensor([150, 9], dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [40, 200])
+def test_nan_stays_in_its_sequence_and_head(N, dtype):
+    Q, K, V, dO = make(2, N, N, 4, 2, 64, dtype)
+    O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+    grads = bra.bra_attention_backward(Q, K, V, O, lse, dO)
+    K2 = K.clone()
+    K2[1, 3, 1, 5] = math.nan
+    O2, lse2 = bra.bra_attention_forward(Q, K2, V, want_lse=True)
+    assert bool(O2[1, :, 2:].isnan().all()) and bool(lse2[1, 2:].isnan().all())
+    assert torch.equal(O2[0], O[0]) and torch.equal(O2[1, :, :2], O[1, :, :2]) and torch.equal(lse2[1, :2], lse[1, :2])
+    got = bra.bra_attention_backward(Q, K2, V, O2, lse2, dO)
+    for a, b in zip(got, grads):
+        half = a.shape[2] // 2
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1, :, :half], b[1, :, :half]) and bool(a[1, :, half:].isnan().all())
+
+
+def test_refusals():
+    Q, K, V, dO = make(2, 20, 30, 4, 2, 64, BF16)
+    O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+    back = lambda **k: bra.bra_attention_backward(**{**dict(Q=Q, K=K, V=V, O=O, lse=lse, dO=dO), **k})
+    odd = torch.zeros(2, 20, 4, 68, dtype=BF16, device="cuda")[..., 1:65]
+    lens = torch.tensor([3, 4], dtype=torch.int32, device="cuda")
+    for bad in (dict(q_lens=lens.long()), dict(k_lens=lens[:1]), dict(k_lens=lens.cpu()), dict(out=odd), dict(out=Q), dict(out=K[:, :20].expand(2, 20, 2, 64)), dict(out=O.float()),
+                dict(out=O[:, :1].expand(2, 20, 4, 64))):
+        with pytest.raises(ValueError):
+            bra.bra_attention_forward(Q, K, V, **bad)
+    for q, k, v in ((odd, K, V), (Q, K.float(), V), (Q, K, V[:, :29]), (Q.transpose(2, 3), K, V), (Q, K.cpu(), V)):
+        with pytest.raises(ValueError):
+            bra.bra_attention_forward(q, k, v)
+    for bad in (dict(lse=lse[:, :2]), dict(lse=lse.double()), dict(lse=lse.transpose(1, 2).contiguous().transpose(1, 2)), dict(dO=odd), dict(O=O[:, :19]), dict(out=(O,)), dict(out=(Q, K, V)),
+                dict(out=(torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)[:, :1].expand(2, 30, 2, 64)))):
+        with pytest.raises(ValueError):
+            back(**bad)
+    same = torch.empty_like(K)
+    with pytest.raises(ValueError):
+        back(out=(torch.empty_like(Q), same, same))
+    with pytest.raises(TypeError):
+        bra.bra_attention_forward(Q, K, V, scale=[1.0])
+    big = torch.zeros(1, 70000, 2, 64, dtype=BF16, device="cuda")
+    with pytest.raises(bra.BraError):
+        bra.bra_attention_forward(Q[:1, :1], big, big, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    # a scale that is given
+    check(bra.bra_attention_forward(Q, K, V, scale=0.3), *[Attention(Q, K, V, scale=0.3).forward()[i] for i in (0, 2)], "O")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Nq,Nk", [(1, 2500), (49, 49), (130, 1100)])
+def test_graphs_and_streams(Nq, Nk, dtype):
+    """Both passes captured with workspaces of their own and replayed with new inputs, eager calls between the replays; two streams at once."""
+    H, Hk, d = 4, 2, 64
+    sets = [make(2, Nq, Nk, H, Hk, d, dtype, seed=s) for s in range(3)]
+    lens = torch.tensor([Nk, Nk // 3], dtype=torch.int32, device="cuda")
+    rule = dict(k_lens=lens)
+
+    def both(Q, K, V, dO):
+        O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True, **rule)
+        return (O, lse) + bra.bra_attention_backward(Q, K, V, O, lse, dO, **rule)
+
+    want = [[t.clone() for t in both(*s)] for s in sets]
+    graphs = []
+    for s in range(2):
+        held = [t.clone() for t in sets[s]]
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            both(*held)
+        torch.cuda.current_stream().wait_stream(stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = both(*held)
+        graphs.append((graph, held, out))
+    for turn in range(3):
+        for i, (graph, held, out) in enumerate(graphs):
+            source = (turn + i) % 3
+            for a, b in zip(held, sets[source]):
+                a.copy_(b)
+            graph.replay()
+            eager = both(*sets[(source + 1) % 3])
+            torch.cuda.synchronize()
+            for a, b in zip(out, want[source]):
+                assert torch.equal(a, b)
+            for a, b in zip(eager, want[(source + 1) % 3]):
+                assert torch.equal(a, b)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                results.append((i, both(*sets[i])))
+    torch.cuda.synchronize()
+    for i, got in results:
+        for a, b in zip(got, want[i]):
+            assert torch.equal(a, b)
