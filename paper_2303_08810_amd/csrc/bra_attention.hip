@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : sizeof(E
     constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     S::template load<E>(dO, limit > 0, pieces, h, g);
     float delta = 0.f, lse = 0.f;
     {
-        delta = row_product<E>(dO, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces, G::kSteps, h);
+        delta = row_product<E, G::kSteps>(dO, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces, h);
         if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
         delta = pair_sum(delta);
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
     const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A.first + blockIdx.x, A.blocks, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
     const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -505,8 +505,8 @@ __global__ __launch_bounds__(256, D > 64 ? 1 : 2) void k_short_grads(Call A)
     const int limit = row < A.rows ? seq.limit(query) : 0;
     float lse = 0.f, delta = 0.f;
     if (wave < 2) {
-        delta = pair_sum(row_product<E>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0, pieces,
-                                        G::kSteps, h));
+        delta = pair_sum(row_product<E, G::kSteps>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0,
+                                                    pieces, h));
         if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
         if (h == 0) {

@@ -64,18 +64,19 @@ struct Sequence {
 };
 
 // What workgroup `block` works on: `per` workgroups to a head, those of a head on one XCD, where they meet in its L2, heads next to each other on
-// different ones, since those of a batch's long sequences would otherwise come to one.  The workgroups of the last heads, fewer than XCDs, are dealt out evenly.
+// different ones, since those of a batch's long sequences would otherwise come to one.  The last heads, fewer than XCDs, are dealt out evenly, a part of a head
+// to an XCD, or, where sequences have lengths of their own, every head to all of them.
 struct Place {
     int head, inner;
-    __device__ __forceinline__ Place(long block, long blocks, long per)
+    __device__ __forceinline__ Place(const Call &A, long block, long per)
     {
-        const long whole = blocks / per / 8 * 8 * per;
-        long i;
+        const long whole = A.blocks / per / 8 * 8 * per;
+        long i = block;
         if (block < whole) {
             const long j = block / 8;
             i = (j / per * 8 + block % 8) * per + j % per;
-        } else {
-            const long left = blocks - whole, j = block - whole, xcd = j % 8, each = left / 8, rest = left % 8;
+        } else if (!A.q_lens && !A.k_lens) {
+            const long left = A.blocks - whole, j = block - whole, xcd = j % 8, each = left / 8, rest = left % 8;
             i = whole + xcd * each + min(xcd, rest) + j / 8;
         }
         head = (int)(i / per);
@@ -357,27 +358,27 @@ struct Slots {
     }
 };
 
-// sum over a row's channels of a b, this lane's pieces of them
-template <class E>
-__device__ __forceinline__ float row_product(const char *a, const char *b, bool valid, int pieces, int steps, int h)
+// sum over a row's channels of a b, this lane's pieces of them; all loads are on their way at once
+template <class E, int STEPS>
+__device__ __forceinline__ float row_product(const char *a, const char *b, bool valid, int pieces, int h)
 {
-    float sum = 0.f;
-    for (int ks = 0; ks < steps; ++ks) {
-        const int piece = 2 * ks + h;
-        if (!valid || piece >= pieces) continue;
-        if constexpr (sizeof(E) == 2) {
-            const bf16x8 x = *(const bf16x8 *)(a + 16 * piece), y = *(const bf16x8 *)(b + 16 * piece);
+    constexpr int W = sizeof(E) == 2 ? 1 : 2;       // loads of 16 bytes to 8 channels
+    u32x4 x[STEPS * W], y[STEPS * W];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f32x4 x = *(const f32x4 *)(a + 32 * piece + 16 * i), y = *(const f32x4 *)(b + 32 * piece + 16 * i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum = fmaf(x[e], y[e], sum);
-            }
-        }
+    for (int i = 0; i < STEPS * W; ++i) {
+        const int piece = 2 * (i / W) + h;
+        const bool there = valid && piece < pieces;
+        x[i] = *(const u32x4 *)(there ? a + 16 * (W * piece + i % W) : (const char *)zeros);
+        y[i] = *(const u32x4 *)(there ? b + 16 * (W * piece + i % W) : (const char *)zeros);
     }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < STEPS * W; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (W == 1) sum = fmaf(bf16_lo(x[i][e]), bf16_lo(y[i][e]), fmaf(bf16_hi(x[i][e]), bf16_hi(y[i][e]), sum));
+            else sum = fmaf(__builtin_bit_cast(f32x4, x[i])[e], __builtin_bit_cast(f32x4, y[i])[e], sum);
+        }
     return sum;
 }
 
