@@ -640,11 +640,11 @@ int splits_of(const Sizes &S, bool keys)
     const long mine = keys ? S.Nk : S.rows(), walked = keys ? S.rows() : S.Nk;
     const long each = 32 * waves_of(mine), blocks = (mine + each - 1) / each * S.B * S.Hk, tiles = (walked + 63) / 64;
     if (blocks == 0) return 1;
-    // (us with 256 / 384 / 512 / 768 / 1024 workgroups at least: bf16, causal, 8192 of 16 / 4 heads of 128 1753 / 1753 / 1205 / 1393 / 1220, 2048 of them 158 / 154 / 154 /
-    // 176 / 184, 4096 of 8 heads of 64 179 / 179 / 142 / 132 / 136, not causal, 1024 of 12 heads of 64 48 / 52 / 51 / 60 / 61; float32, one workgroup to a compute
-    // unit, 2 x 1295 causal of 8 / 2 heads of 72 249 / 180 / 210 / 192 / 203)
-    const long want = S.f32 ? 384 : 512;
-    return (int)std::max(1L, std::min({want / blocks, tiles / (S.f32 ? 2 : 4), 16L}));
+    // (us with 256 / 384 / 512 / 768 / 1024 workgroups at least: causal, 8192 of 16 / 4 heads of 128 1685 / 1682 / 1146 / 1347 / 1170, 2048 of them 156 / 152 / 149 / 171 /
+    // 177, 4096 of 8 heads of 64 179 / 179 / 138 / 127 / 129, 3 x 2048 of lengths from a third on of 4 / 2 heads of 128 151 / 124 / 126 / 132 / 158; not causal, 1024 of
+    // 12 heads of 64 48 / 50 / 49 / 58 / 58; float32, 2 x 1295 causal of lengths from a half on of 8 / 2 heads of 72 245 / 168 / 152 / 155 / 168)
+    const long want = 512;
+    return (int)std::max(1L, std::min({want / blocks, tiles / 2, 16L}));
 }
 size_t part_bytes(const Sizes &S)
 {
