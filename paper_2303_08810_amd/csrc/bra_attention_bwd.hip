@@ -465,53 +465,72 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     }
 }
 
-// Both in one launch where a head has up to 64 rows and 64 keys: everything is in LDS once, two wavefronts have the query side, two the key side.  64 x 49 tokens
-// of 16 heads of 32 in two launches 17.8 us, this way 12.2.
-template <int D>
+// Both in one launch where a head has up to R rows and R keys: everything is in LDS once, in float32 as terms formed on the way there; half of the wavefronts
+// have the query side, half the key side, 32 or 64 rows (keys) each.
+template <class E, int D, int R>
 struct Short {
+    static constexpr int T = sizeof(E) == 4 ? 3 : 1, kGroups = R / 32, kSide = kGroups < 4 ? kGroups : 4, kThreads = 128 * kSide;
     typedef Geometry<bf16_t, D> G;
-    typedef Slots<G, 1, 0> S;
-    static constexpr int kThreads = 256, kTile = 64 * G::kPitch, kSub = 32 * G::kPitch, kLds = 4 * kTile + 2 * 64 * 4;      // K, V, Q, dO, lse, delta
-    typedef Tiles<G, 64, kThreads> Loads;
+    static constexpr int kPlane = R * G::kPitch, kTile = T * kPlane, kSub = 32 * G::kPitch, kLds = 4 * kTile + 2 * R * 4;        // K, V, Q, dO, lse, delta
+    typedef Slots<G, T, kPlane> S;
 };
 
-template <int D>
-__global__ __launch_bounds__(256, D > 64 ? 1 : 2) void k_short_grads(Call A)
+// A head's rows, which lie at place(row), to LDS; zeros behind `rows`.
+template <class E, class F, class P>
+__device__ __forceinline__ void load_short(char *tile, int rows, int pieces, P place)
 {
-    typedef bf16_t E;
-    typedef Short<D> F;
+    typedef typename F::G G;
+    constexpr int kLoads = F::kPlane / 16, L = (kLoads + F::kThreads - 1) / F::kThreads;
+    const unsigned at = lds_address(tile) + 1024 * __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+        const int i = threadIdx.x + F::kThreads * u, row = i / G::kPieces, piece = i % G::kPieces ^ G::turn(row);
+        if (kLoads % F::kThreads != 0 && i >= kLoads) break;         // (whole wavefronts)
+        const bool there = row < rows && piece < pieces;
+        const char *p = there ? place(row) + (int)sizeof(E) * 8 * piece : (const char *)zeros;
+        if constexpr (F::T == 1) load_to_lds_untracked((const bf16_t *)p, at + 16 * F::kThreads * u);
+        else {
+            const f32x4 v0 = *(const f32x4 *)p, v1 = *(const f32x4 *)(there ? p + 16 : p);
+            const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            bf16x8 t[3];
+            split3(v, t);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(bf16x8 *)(tile + k * F::kPlane + 16 * i) = t[k];
+        }
+    }
+}
+
+template <class E, int D, int R>
+__global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 : 2) void k_short_grads(Call A)
+{
+    typedef Short<E, D, R> F;
     typedef typename F::S S;
     typedef typename F::G G;
     extern __shared__ char lds[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32, side = wave % 2;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
     const int hb = (int)(A.first + blockIdx.x), b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d / 8, end = seq.nq * A.G;
-    const unsigned at = lds_address(lds);
-    float *sums = (float *)(lds + 4 * F::kTile);
+    char *kt = lds, *vt = kt + F::kTile, *qt = vt + F::kTile, *gt = qt + F::kTile;
+    float *sums = (float *)(gt + F::kTile);
     {
         const char *k = A.K.p + b * A.K.batch + hk * A.K.head, *v = A.V.p + b * A.V.batch + hk * A.V.head;
         const char *q = A.Q.p + b * A.Q.batch + hk * A.G * A.Q.head, *o = A.dO.p + b * A.dO.batch + hk * A.G * A.dO.head;
-        auto load = [&](int tile, int rows, auto place) __attribute__((always_inline)) {
-            typename F::Loads loads(place, 1, 0, rows, pieces, threadIdx.x);
-            loads.request(at + tile * F::kTile, pieces, threadIdx.x, place);
-        };
-        load(0, seq.nk, [&](int r) __attribute__((always_inline)) { return k + r * A.K.token; });
-        load(1, seq.nk, [&](int r) __attribute__((always_inline)) { return v + r * A.V.token; });
-        load(2, end, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return q + i * A.Q.token + (r - i * A.G) * A.Q.head; });
-        load(3, end, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return o + i * A.dO.token + (r - i * A.G) * A.dO.head; });
+        load_short<E, F>(kt, seq.nk, pieces, [&](int r) __attribute__((always_inline)) { return k + r * A.K.token; });
+        load_short<E, F>(vt, seq.nk, pieces, [&](int r) __attribute__((always_inline)) { return v + r * A.V.token; });
+        load_short<E, F>(qt, end, pieces, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return q + i * A.Q.token + (r - i * A.G) * A.Q.head; });
+        load_short<E, F>(gt, end, pieces, [&](int r) __attribute__((always_inline)) { const int i = row_query(A, r); return o + i * A.dO.token + (r - i * A.G) * A.dO.head; });
     }
-    const int row = 32 * side + c, some = min(row, A.rows - 1), query = row_query(A, some), head = hk * A.G + some - query * A.G;
-    const int limit = row < A.rows ? seq.limit(query) : 0;
-    float lse = 0.f, delta = 0.f;
-    if (wave < 2) {
-        delta = pair_sum(row_product<E, G::kSteps>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, limit > 0,
-                                                    pieces, h));
-        if (limit > 0) lse = A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query];
+    // lse log2 e and delta of every row: two lanes to a row
+    for (int row = 32 * wave + c; row < R; row += F::kThreads / 2) {
+        const int some = min(row, A.rows - 1), query = row_query(A, some), head = hk * A.G + some - query * A.G;
+        const bool there = row < end;
+        const float delta = pair_sum(row_product<E, G::kSteps>(A.dO.p + b * A.dO.batch + query * A.dO.token + head * A.dO.head, A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head, there, pieces, h));
+        float lse = there ? A.lse_in[((long)b * A.Hk * A.G + head) * A.Nq + query] : 0.f;
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;       // (no weight at all)
         if (h == 0) {
             sums[row] = lse;
-            sums[64 + row] = delta;
+            sums[R + row] = delta;
         }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -519,11 +538,12 @@ __global__ __launch_bounds__(256, D > 64 ? 1 : 2) void k_short_grads(Call A)
     asm volatile("" ::: "memory");
 
     const Reader<G> reader(lane);
-    const char *kt = lds, *vt = kt + F::kTile, *qt = vt + F::kTile, *gt = qt + F::kTile;
     // a subtile's rows as what the wavefront keeps
     auto keep = [&](typename S::Columns &x, const char *tile) __attribute__((always_inline)) {
 #pragma unroll
-        for (int ks = 0; ks < G::kSteps; ++ks) x.v[0][ks] = *(const bf16x8 *)(tile + side * F::kSub + reader.row[ks]);
+        for (int t = 0; t < F::T; ++t)
+#pragma unroll
+            for (int ks = 0; ks < G::kSteps; ++ks) x.v[t][ks] = *(const bf16x8 *)(tile + t * F::kPlane + reader.row[ks]);
     };
     auto scores = [&](f32x16 &s, f32x16 &d, const char *t0, const char *t1, const typename S::Columns &x, const typename S::Columns &g) __attribute__((always_inline)) {
         s = d = f32x16{};
@@ -535,86 +555,105 @@ __global__ __launch_bounds__(256, D > 64 ? 1 : 2) void k_short_grads(Call A)
     };
     typename S::Columns x, g;
     f32x16 s, d;
-    if (wave < 2) {
-        keep(x, qt);
-        keep(g, gt);
-        f32x16 acc[G::NT];
-        clear(acc);
-        const int most = columns_max(limit);
-        for (int i = 0; 32 * i < most; ++i) {
-            scores(s, d, kt + i * F::kSub, vt + i * F::kSub, x, g);
-            typename S::Weights w;
-            unrolled<16>([&](auto e) __attribute__((always_inline)) {
-                constexpr int r = e;
-                const float p = 32 * i + result_row(r, h) < limit ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -lse)) : 0.f;
-                d[r] = p * (d[r] - delta);
-                if constexpr (r % 2) S::keep(w, d, r);
-            });
-            unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
-                typename S::Operand o;
-                S::read_columns(o, kt + i * F::kSub, reader, f);
-                S::columns(acc, o, w, f);
-            });
+    if (wave < F::kSide) {
+        for (int group = wave;; group += F::kSide) {
+            const int row = 32 * group + c, some = min(row, A.rows - 1), query = row_query(A, some), head = hk * A.G + some - query * A.G;
+            if (32 * group >= A.rows) return;
+            const int limit = row < A.rows ? seq.limit(query) : 0, most = columns_max(limit);
+            const float lse = sums[row], delta = sums[R + row];
+            keep(x, qt + group * F::kSub);
+            keep(g, gt + group * F::kSub);
+            f32x16 acc[G::NT];
+            clear(acc);
+            for (int i = 0; 32 * i < most; ++i) {
+                scores(s, d, kt + i * F::kSub, vt + i * F::kSub, x, g);
+                typename S::Weights w;
+                unrolled<16>([&](auto e) __attribute__((always_inline)) {
+                    constexpr int r = e;
+                    const float p = 32 * i + result_row(r, h) < limit ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -lse)) : 0.f;
+                    d[r] = p * (d[r] - delta);
+                    if constexpr (r % 2) S::keep(w, d, r);
+                });
+                unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
+                    typename S::Operand o;
+                    S::read_columns(o, kt + i * F::kSub, reader, f);
+                    S::columns(acc, o, w, f);
+                });
+            }
+            if (row < A.rows) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
+            if (F::kGroups == F::kSide || group + F::kSide >= F::kGroups) return;
         }
-        if (row < A.rows) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
-        return;
     }
-    const int key = 32 * side + c;
-    const bool live = key < seq.nk;
-    const int begin = !live ? end : seq.causal ? min(max(key - seq.off, 0), seq.nq) * A.G : 0;
-    keep(x, kt);
-    keep(g, vt);
-    f32x16 dk[G::NT], dv[G::NT];
-    clear(dk);
-    clear(dv);
-    const int from = columns_min(begin) / 32;
-    for (int i = from; 32 * i < end; ++i) {
-        scores(s, d, qt + i * F::kSub, gt + i * F::kSub, x, g);
-        const float *mine = sums + 32 * i + 4 * h;
-        typename S::Weights p, ds;
-        unrolled<4>([&](auto q) __attribute__((always_inline)) {
-            const f32x4 l4 = *(const f32x4 *)(mine + 8 * q), d4 = *(const f32x4 *)(mine + 64 + 8 * q);
-            unrolled<4>([&](auto e) __attribute__((always_inline)) {
-                constexpr int j = e, r = 4 * decltype(q)::value + j;
-                const int at_row = 32 * i + result_row(r, h);
-                const bool see = at_row >= begin && at_row < end;
-                s[r] = see ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -l4[j])) : 0.f;
-                d[r] = see ? s[r] * (d[r] - d4[j]) : 0.f;
-                if constexpr (r % 2) {
-                    S::keep(p, s, r);
-                    S::keep(ds, d, r);
-                }
-            });
-        });
-        unrolled<2 * S::kColumns>([&](auto f) __attribute__((always_inline)) {
-            typename S::Operand o;
-            S::read_columns(o, (f % 2 ? qt : gt) + i * F::kSub, reader, f / 2);
-            S::columns(f % 2 ? dk : dv, o, f % 2 ? ds : p, f / 2);
-        });
-    }
-    if (key >= A.Nk) return;
-    if (!live) {
+    for (int group = wave - F::kSide;; group += F::kSide) {
+        const int key = 32 * group + c;
+        if (32 * group >= A.Nk) return;
+        const bool live = key < seq.nk;
+        const int begin = !live ? end : seq.causal ? min(max(key - seq.off, 0), seq.nq) * A.G : 0;
+        keep(x, kt + group * F::kSub);
+        keep(g, vt + group * F::kSub);
+        f32x16 dk[G::NT], dv[G::NT];
         clear(dk);
         clear(dv);
+        for (int i = columns_min(begin) / 32; 32 * i < end; ++i) {
+            scores(s, d, qt + i * F::kSub, gt + i * F::kSub, x, g);
+            const float *mine = sums + 32 * i + 4 * h;
+            typename S::Weights p, ds;
+            unrolled<4>([&](auto q) __attribute__((always_inline)) {
+                const f32x4 l4 = *(const f32x4 *)(mine + 8 * q), d4 = *(const f32x4 *)(mine + R + 8 * q);
+                unrolled<4>([&](auto e) __attribute__((always_inline)) {
+                    constexpr int j = e, r = 4 * decltype(q)::value + j;
+                    const int at_row = 32 * i + result_row(r, h);
+                    const bool see = at_row >= begin && at_row < end;
+                    s[r] = see ? __builtin_amdgcn_exp2f(fmaf(s[r], A.c, -l4[j])) : 0.f;
+                    d[r] = see ? s[r] * (d[r] - d4[j]) : 0.f;
+                    if constexpr (r % 2) {
+                        S::keep(p, s, r);
+                        S::keep(ds, d, r);
+                    }
+                });
+            });
+            unrolled<2 * S::kColumns>([&](auto f) __attribute__((always_inline)) {
+                typename S::Operand o;
+                S::read_columns(o, (f % 2 ? qt : gt) + i * F::kSub, reader, f / 2);
+                S::columns(f % 2 ? dk : dv, o, f % 2 ? ds : p, f / 2);
+            });
+        }
+        if (!live) {
+            clear(dk);
+            clear(dv);
+        }
+        if (key < A.Nk) {
+            store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, dk, A.scale, A.d, h);
+            store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, dv, 1.f, A.d, h);
+        }
+        if (F::kGroups == F::kSide || group + F::kSide >= F::kGroups) return;
     }
-    store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, dk, A.scale, A.d, h);
-    store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, dv, 1.f, A.d, h);
 }
 
-// The splits' sums put together, in their order: dQ, [heads][splits][rows][D], or dK and dV, [heads][splits][Nk][2][D].
-template <class E, int D, bool KEYS>
-__global__ __launch_bounds__(256) void k_grads_join(Call A)
+// What k_grads_join puts together: dQ, [heads][splits][rows][D], and dK and dV, [heads][splits][Nk][2][D], whichever have splits.
+struct Joins {
+    const float *query, *key;
+    int query_splits, key_splits;
+    long query_pieces, key_pieces;              // of 8 channels of a result; 0 where there are no splits
+};
+
+// The splits' sums put together, in their order.
+template <class E, int D>
+__global__ __launch_bounds__(256) void k_grads_join(Call A, Joins J, long first)
 {
-    constexpr int CH = D / 8, W = KEYS ? 2 : 1;
-    const long i = (A.first + blockIdx.x) * 256 + threadIdx.x, each = KEYS ? A.Nk : A.rows, n = A.blocks * each * W;      // here blocks: sequences x key heads
-    const int ch = 8 * (int)(i % CH);
-    const long r = i / CH;
-    if (r >= n || ch >= A.d) return;
-    const int which = (int)(r % W), row = (int)(r / W % each), hb = (int)(r / W / each), b = hb / A.Hk, hk = hb % A.Hk;
-    const float *p = A.part + (((long)hb * A.splits * each + row) * W + which) * D + ch;
+    constexpr int CH = D / 8;
+    long i = (first + blockIdx.x) * 256 + threadIdx.x;
+    const bool keys = i >= J.query_pieces;
+    if (keys) i -= J.query_pieces;
+    if (keys && i >= J.key_pieces) return;
+    const int ch = 8 * (int)(i % CH), splits = keys ? J.key_splits : J.query_splits, W = keys ? 2 : 1;
+    if (ch >= A.d) return;
+    const long r = i / CH, each = keys ? A.Nk : A.rows;
+    const int which = keys ? (int)(r & 1) : 0, row = (int)((keys ? r >> 1 : r) % each), hb = (int)((keys ? r >> 1 : r) / each), b = hb / A.Hk, hk = hb % A.Hk;
+    const float *p = (keys ? J.key : J.query) + (((long)hb * splits * each + row) * W + which) * D + ch;
     float v[8] = {};
 #pragma unroll 4
-    for (int s = 0; s < A.splits; ++s, p += each * W * D) {
+    for (int s = 0; s < splits; ++s, p += each * W * D) {
         const f32x4 v0 = *(const f32x4 *)p, v1 = *(const f32x4 *)(p + 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -622,7 +661,7 @@ __global__ __launch_bounds__(256) void k_grads_join(Call A)
             v[4 + e] += v1[e];
         }
     }
-    if (KEYS) {
+    if (keys) {
         const Rows &R = which ? A.dV : A.dK;
         store8<E>(R.p + b * R.batch + row * R.token + hk * R.head + ch * sizeof(E), v);
     } else {
@@ -646,20 +685,19 @@ int splits_of(const Sizes &S, bool keys)
     const long want = 512;
     return (int)std::max(1L, std::min({want / blocks, tiles / 2, 16L}));
 }
-size_t part_bytes(const Sizes &S)
+size_t part_bytes(const Sizes &S, bool keys)
 {
-    const size_t q = splits_of(S, false), k = splits_of(S, true), row = sizeof(float) * S.width() * S.B * S.Hk;
-    return std::max(q > 1 ? q * S.rows() * row : 0, k > 1 ? k * S.Nk * 2 * row : 0);
+    const size_t n = splits_of(S, keys), row = sizeof(float) * S.width() * S.B * S.Hk;
+    return n > 1 ? align256(n * (keys ? 2 * (size_t)S.Nk : S.rows()) * row) : 0;
 }
 
-template <class E, int D, bool KEYS>
-int join(Call A, long heads, hipStream_t st)
+template <class E, int D>
+int join(const Call &A, const Joins &J, hipStream_t st)
 {
-    A.blocks = heads;
-    const long blocks = (heads * (KEYS ? 2L * A.Nk : (long)A.rows) * (D / 8) + 255) / 256;
-    for (A.first = 0; A.first < blocks; A.first += kMaxBlocks) {
+    const long blocks = (J.query_pieces + J.key_pieces + 255) / 256;
+    for (long first = 0; first < blocks; first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_JOIN);
-        k_grads_join<E, D, KEYS><<<(unsigned)std::min(kMaxBlocks, blocks - A.first), 256, 0, st>>>(A);
+        k_grads_join<E, D><<<(unsigned)std::min(kMaxBlocks, blocks - first), 256, 0, st>>>(A, J, first);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;
@@ -679,7 +717,7 @@ int query_grads(const Sizes &S, Call A, long heads, hipStream_t st)
         k_query_grads<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
-    return A.splits > 1 ? join<E, D, false>(A, heads, st) : BRA_OK;
+    return BRA_OK;
 }
 
 template <class E, int D, int WAVES>
@@ -701,20 +739,28 @@ int key_grads(const Sizes &S, Call A, long heads, hipStream_t st)
         else k_key_grads<D, WAVES><<<n, F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
-    return A.splits > 1 ? join<E, D, true>(A, heads, st) : BRA_OK;
+    return BRA_OK;
 }
 
-bool is_short(const Sizes &S) { return !S.f32 && S.rows() <= 64 && S.Nk <= 64; }
+// Rows and keys that a call of k_short_grads takes, 0 where it is not the one.
+int short_side(const Sizes &S)
+{
+    const long most = std::max(S.rows(), (long)S.Nk);
+    const int fits = S.f32 ? (S.width() <= 32 ? 128 : S.width() <= 64 ? 64 : 32) : S.width() <= 64 ? 256 : 128;      // in LDS
+    for (int side = 32; side <= fits; side *= 2)
+        if (most <= side) return S.f32 || side >= 64 ? side : 64;
+    return 0;
+}
 
-template <int D>
+template <class E, int D, int R>
 int short_grads(Call A, long heads, hipStream_t st)
 {
-    typedef Short<D> F;
-    const int rc = allow_lds<k_short_grads<D>>(F::kLds);
+    typedef Short<E, D, R> F;
+    const int rc = allow_lds<k_short_grads<E, D, R>>(F::kLds);
     if (rc != BRA_OK) return rc;
     for (A.first = 0; A.first < heads; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_SHORT_GRADS);
-        k_short_grads<D><<<(unsigned)std::min(kMaxBlocks, heads - A.first), F::kThreads, F::kLds, st>>>(A);
+        k_short_grads<E, D, R><<<(unsigned)std::min(kMaxBlocks, heads - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;
@@ -724,12 +770,30 @@ template <class E, int D>
 int run(const Sizes &S, const Call &A, hipStream_t st)
 {
     const long heads = (long)S.B * S.Hk;
-    if constexpr (sizeof(E) == 2) {
-        if (is_short(S)) return short_grads<D>(A, heads, st);
+    constexpr bool f32 = sizeof(E) == 4;
+    switch (short_side(S)) {
+    case 32:
+        if constexpr (f32) return short_grads<E, D, 32>(A, heads, st);
+        break;
+    case 64:
+        if constexpr (!f32 || D <= 64) return short_grads<E, D, 64>(A, heads, st);
+        break;
+    case 128:
+        if constexpr (!f32 || D <= 32) return short_grads<E, D, 128>(A, heads, st);
+        break;
+    case 256:
+        if constexpr (!f32 && D <= 64) return short_grads<E, D, 256>(A, heads, st);
+        break;
     }
-    const int rc = waves_of(S.rows()) == 2 ? query_grads<E, D, 2>(S, A, heads, st) : query_grads<E, D, 4>(S, A, heads, st);
+    Call Q = A, K = A;
+    K.part = A.part + part_bytes(S, false) / sizeof(float);
+    int rc = waves_of(S.rows()) == 2 ? query_grads<E, D, 2>(S, Q, heads, st) : query_grads<E, D, 4>(S, Q, heads, st);
+    if (rc == BRA_OK) rc = waves_of(S.Nk) == 2 ? key_grads<E, D, 2>(S, K, heads, st) : key_grads<E, D, 4>(S, K, heads, st);
     if (rc != BRA_OK) return rc;
-    return waves_of(S.Nk) == 2 ? key_grads<E, D, 2>(S, A, heads, st) : key_grads<E, D, 4>(S, A, heads, st);
+    Joins J{Q.part, K.part, splits_of(S, false), splits_of(S, true), 0, 0};
+    if (J.query_splits > 1) J.query_pieces = heads * A.rows * (D / 8);
+    if (J.key_splits > 1) J.key_pieces = heads * A.Nk * 2 * (D / 8);
+    return join<E, D>(A, J, st);
 }
 
 template <class E>
@@ -748,7 +812,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
 
 using namespace att;
 
-size_t attention_backward_workspace_bytes(const Sizes &S) { return is_short(S) ? 0 : 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + align256(part_bytes(S)) + (S.f32 ? terms_bytes(S, true) : 0); }
+size_t attention_backward_workspace_bytes(const Sizes &S) { return short_side(S) ? 0 : 2 * align256(sizeof(float) * S.rows() * S.B * S.Hk) + part_bytes(S, false) + part_bytes(S, true) + (S.f32 ? terms_bytes(S, true) : 0); }
 
 int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, const float *lse, const Rows &dO, const Rows &dQ, const Rows &dK,
                        const Rows &dV, void *ws, hipStream_t st)
@@ -766,8 +830,8 @@ int attention_backward(const Sizes &S, const Rows &Q, const Rows &K, const Rows 
     A.row_lse = (float *)ws;
     A.row_delta = (float *)((char *)ws + align256(sizeof(float) * S.rows() * S.B * S.Hk));
     A.part = (float *)((char *)A.row_delta + align256(sizeof(float) * S.rows() * S.B * S.Hk));
-    if (S.f32) {
-        const int rc = make_terms(S, A, true, (char *)A.part + align256(part_bytes(S)), st);
+    if (S.f32 && !short_side(S)) {
+        const int rc = make_terms(S, A, true, (char *)A.part + part_bytes(S, false) + part_bytes(S, true), st);
         if (rc != BRA_OK) return rc;
     }
     return S.f32 ? run<float>(S, A, st) : run<bf16_t>(S, A, st);

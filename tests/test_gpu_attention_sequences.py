@@ -26,6 +26,12 @@ CASES = [
     (1, 333, 333, 6, 3, 64, False, None, None, "packed"),
     (1, 40, 2500, 4, 4, 64, True, None, None, "cache"),             # keys shared out, many rows
     (2, 40, 1500, 3, 3, 128, False, [40, 39], [1500, 700], "cache"),
+    (2, 100, 128, 3, 3, 128, True, [100, 31], [128, 77], "apart"),     # gradients in one launch, sides of 128, 256, (float32) 128, 64 and 32
+    (2, 50, 256, 4, 1, 24, True, [50, 9], [256, 1], "cache"),
+    (2, 200, 250, 2, 2, 64, False, None, [250, 0], "apart"),
+    (3, 30, 90, 3, 1, 16, False, None, [90, 0, 33], "apart"),
+    (2, 30, 60, 2, 1, 64, True, [30, 0], [60, 7], "apart"),
+    (2, 16, 32, 4, 2, 120, True, None, [32, 20], "apart"),
     (1, 3, 0, 2, 1, 32, False, None, None, "apart"),
     (2, 0, 5, 2, 1, 32, False, None, None, "apart"),
 ]
