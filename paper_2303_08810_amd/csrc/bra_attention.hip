@@ -19,7 +19,8 @@ struct Forward {
     static constexpr int kThreads = 64 * WAVES, kLoaders = FEW ? 64 : kThreads, kRows = FEW ? 32 : 32 * WAVES;
     static constexpr int kTile = KT * G::kPitch, kBuffer = 2 * kTile, kKeyTile = KT;
     static constexpr int kRings = 2 * kBuffer * (FEW ? WAVES : 1);
-    static constexpr int kJoin = FEW ? WAVES * 32 * (D + 2) * 4 : 0;
+    static constexpr int kColumn = D + 4;       // floats of a column's sums: the lanes of a wavefront begin in different banks
+    static constexpr int kJoin = FEW ? WAVES * 32 * (kColumn + 2) * 4 : 0;
     static constexpr int kLds = kRings > kJoin ? kRings : kJoin;
     typedef Stage<G, KT, kLoaders> Loads;
 };
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -131,35 +132,51 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
         }
     }
 
-    float l = pair_sum(run.l), m = run.m;
-    if constexpr (FEW) {
-        // the wavefronts' shares: [wave][column][D] sums, then [wave][column] m and l
-        float *sums = (float *)lds, *ml = sums + WAVES * 32 * D;
-        __syncthreads();
-        store_columns<float, G>((char *)(sums + (wave * 32 + c) * D), acc, 1.f, D, h);
-        if (h == 0) {
-            ml[2 * (32 * wave + c)] = m;
-            ml[2 * (32 * wave + c) + 1] = l;
-        }
-        __syncthreads();
-        if (wave != 0) return;
-        float top = -INFINITY;
+    // the wavefronts' shares: [wave][column][kColumn] sums, then [wave][column] m and l; every wavefront puts some of the channels together
+    const float share_l = pair_sum(run.l);
+    float *sums = (float *)lds, *ml = sums + WAVES * 32 * F::kColumn;
+    __syncthreads();
+    if (limit > 0) store_columns<float, G>((char *)(sums + (wave * 32 + c) * F::kColumn), acc, 1.f, D, h);
+    if (h == 0) {
+        ml[2 * (32 * wave + c)] = run.m;
+        ml[2 * (32 * wave + c) + 1] = share_l;
+    }
+    __syncthreads();
+    if (!valid) return;
+    float m = -INFINITY, l = 0.f, factor[WAVES];
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[2 * (32 * w + c)]);
-        clear(acc);
-        l = 0.f;
-        m = top;
-        for (int w = 0; w < WAVES; ++w) {
-            const float mw = ml[2 * (32 * w + c)], factor = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-            l = fmaf(factor, ml[2 * (32 * w + c) + 1], l);
-            const float *from = sums + (w * 32 + c) * D;
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml[2 * (32 * w + c)]);
 #pragma unroll
-            for (int n = 0; n < G::NT; ++n)
+    for (int w = 0; w < WAVES; ++w) {
+        const float mw = ml[2 * (32 * w + c)];
+        factor[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - m);
+        l = fmaf(factor[w], ml[2 * (32 * w + c) + 1], l);
+    }
+    const int head = hk * A.G + row - query * A.G;
+    const long at = (long)(hb * (long)A.splits + split) * A.rows + row;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    for (int piece = 2 * wave + h; piece < D / 8; piece += 2 * WAVES) {
+        if (8 * piece >= A.d) break;
+        float v[8] = {};
+        if (limit > 0)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[n][e] = fmaf(factor, from[32 * n + 16 * (e / 8) + 8 * h + e % 8], acc[n][e]);
+            for (int w = 0; w < WAVES; ++w) {
+                const float *from = sums + (w * 32 + c) * F::kColumn + 8 * piece;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(factor[w], from[e], v[e]);
+            }
+        if (A.splits > 1) store8<float>((char *)(A.part + at * D + 8 * piece), v);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= inv;
+            store8<E>(A.O.p + b * A.O.batch + query * A.O.token + head * A.O.head + 8 * piece * (int)sizeof(E), v);
         }
     }
-    if (valid) finish<E, G>(A, b, hk, split, row, h, acc, m, l);
+    if (wave || h) return;
+    if (A.splits > 1) {
+        A.part_ml[2 * at] = m;
+        A.part_ml[2 * at + 1] = l;
+    } else if (A.lse) A.lse[((long)b * A.Hk * A.G + head) * A.Nq + query] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Many rows: the wavefronts of a workgroup have 32 rows each and share tiles of KT keys and values, the next of which is on its way.
@@ -181,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : sizeof(E
     constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -432,9 +449,7 @@ int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &
     A.V = V;
     A.O = O;
     A.lse = lse;
-    A.tiles = (int)row_tiles(S);
-    A.splits = splits_of(S);
-    A.blocks = (long)A.tiles * A.splits * S.B * S.Hk;
+    set_grid(A, (long)S.B * S.Hk, row_tiles(S), splits_of(S));
     if (S.f32 && !few(S)) {
         const int rc = make_terms(S, A, false, ws, st);
         if (rc != BRA_OK) return rc;

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
     constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
     const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
     const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     typedef typename F::G G;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, (long)A.tiles * A.splits);
+    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
     const int tile = place.inner % A.tiles, split = place.inner / A.tiles;      // those of a causal mask's long columns first
     const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
@@ -709,9 +709,7 @@ int query_grads(const Sizes &S, Call A, long heads, hipStream_t st)
     typedef Queries<E, D, WAVES> F;
     const int rc = allow_lds<k_query_grads<E, D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
-    A.tiles = (A.rows + F::kMine - 1) / F::kMine;
-    A.splits = splits_of(S, false);
-    A.blocks = A.tiles * A.splits * heads;
+    set_grid(A, heads, (A.rows + F::kMine - 1) / F::kMine, splits_of(S, false));
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_QUERY_GRADS);
         k_query_grads<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
@@ -729,9 +727,7 @@ int key_grads(const Sizes &S, Call A, long heads, hipStream_t st)
     if constexpr (f32) rc = allow_lds<k_key_grads_f32<D, WAVES>>(F::kLds);
     else rc = allow_lds<k_key_grads<D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
-    A.tiles = (A.Nk + F::kMine - 1) / F::kMine;
-    A.splits = splits_of(S, true);
-    A.blocks = A.tiles * A.splits * heads;
+    set_grid(A, heads, (A.Nk + F::kMine - 1) / F::kMine, splits_of(S, true));
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION_KEY_GRADS);
         const unsigned n = (unsigned)std::min(kMaxBlocks, A.blocks - A.first);

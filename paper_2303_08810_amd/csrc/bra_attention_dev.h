@@ -34,6 +34,8 @@ struct Call {
     float scale, c;                 // c = scale log2 e
     int tiles, splits;
     long first, blocks;             // this launch's first workgroup, and how many there are over all launches
+    long whole;                     // workgroups of the heads in whole groups of 8
+    int whole_heads;                // those heads
     float *lse;                     // [B, heads, Nq]
     float *part, *part_ml;          // of the splits
     // the backward pass
@@ -68,19 +70,25 @@ struct Sequence {
 // to an XCD, or, where sequences have lengths of their own, every head to all of them.
 struct Place {
     int head, inner;
-    __device__ __forceinline__ Place(const Call &A, long block, long per)
+    __device__ __forceinline__ Place(const Call &A, long block, int per)
     {
-        const long whole = A.blocks / per / 8 * 8 * per;
         long i = block;
-        if (block < whole) {
+        if (block < A.whole) {
+            const unsigned xcd = (unsigned)block % 8;
             const long j = block / 8;
-            i = (j / per * 8 + block % 8) * per + j % per;
-        } else if (!A.q_lens && !A.k_lens) {
-            const long left = A.blocks - whole, j = block - whole, xcd = j % 8, each = left / 8, rest = left % 8;
-            i = whole + xcd * each + min(xcd, rest) + j / 8;
+            const long group = j >> 32 ? j / per : (unsigned)j / (unsigned)per;        // (the long division takes 0.3 us)
+            head = (int)(group * 8 + xcd);
+            inner = (int)(j - group * per);
+            return;
         }
-        head = (int)(i / per);
-        inner = (int)(i - head * per);
+        if (!A.q_lens && !A.k_lens) {
+            const unsigned left = (unsigned)(A.blocks - A.whole), j = (unsigned)(block - A.whole), xcd = j % 8;
+            i = A.whole + xcd * (left / 8) + min(xcd, left % 8) + j / 8;
+        }
+        const unsigned rest = (unsigned)(i - A.whole);          // of fewer than 8 heads
+        head = (int)(rest / (unsigned)per);
+        inner = (int)(rest - head * (unsigned)per);
+        head += A.whole_heads;
     }
 };
 
@@ -554,6 +562,16 @@ struct Running {
 __device__ __forceinline__ int result_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
 Call make_call(const Sizes &S);
+
+// The grid: `tiles` x `splits` workgroups to a head.
+inline void set_grid(Call &A, long heads, long tiles, int splits)
+{
+    A.tiles = (int)tiles;
+    A.splits = splits;
+    A.blocks = tiles * splits * heads;
+    A.whole_heads = (int)(heads / 8 * 8);
+    A.whole = tiles * splits * A.whole_heads;
+}
 
 // float32: the planes of terms of keys and values, in the backward pass of queries and dO too (bra_attention_terms.hip).
 size_t terms_bytes(const Sizes &S, bool backward);

@@ -238,12 +238,18 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
         if (!norm) return;
         // the workgroup's sums: teams of a wavefront first, then its four wavefronts
         __shared__ float lds[kThreads / 64][128];
+        for (int o = W.team; o < 64; o *= 2)
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-            float v = e < V ? suma[e % V] : sumb[e % V];
-            for (int o = W.team; o < 64; o *= 2) v += __shfl_xor(v, o);
-            if (threadIdx.x % 64 < W.team && active) lds[threadIdx.x / 64][e < V ? ca + e : cb + e - V] = v;
-        }
+            for (int e = 0; e < V; ++e) {
+                suma[e] += __shfl_xor(suma[e], o);
+                sumb[e] += __shfl_xor(sumb[e], o);
+            }
+        if (threadIdx.x % 64 < W.team && active)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                lds[threadIdx.x / 64][ca + e] = suma[e];
+                lds[threadIdx.x / 64][cb + e] = sumb[e];
+            }
         __syncthreads();
         for (int c = threadIdx.x; c < W.d; c += kThreads) {
             float v = 0.f;
