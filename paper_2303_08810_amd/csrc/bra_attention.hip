@@ -274,6 +274,66 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : sizeof(E
     if (valid) finish<E, G>(A, b, hk, split, row, h, acc, run.m, pair_sum(run.l));
 }
 
+// float32 and up to R keys, which lie in LDS at once as terms that are formed on the way there: no planes of terms in memory, no launch for them.
+template <int D, int R, int WAVES>
+struct ShortKeys {
+    static constexpr int T = 3, kThreads = 64 * WAVES, kRows = 32 * WAVES;
+    typedef Geometry<bf16_t, D> G;
+    static constexpr int kPlane = R * G::kPitch, kTile = T * kPlane, kSub = 32 * G::kPitch, kLds = 2 * kTile;
+    typedef Slots<G, T, kPlane> S;
+};
+
+template <int D, int R, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_short_f32(Call A)
+{
+    typedef float E;
+    typedef ShortKeys<D, R, WAVES> F;
+    typedef typename F::G G;
+    typedef typename F::S S;
+    extern __shared__ char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
+    const Place place(A, A.first + blockIdx.x, A.tiles);
+    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
+    const Sequence seq(A, b);
+    const int row = place.inner * F::kRows + 32 * wave + c;
+    const bool valid = row < A.rows;
+    const int query = row_query(A, min(row, A.rows - 1)), head = hk * A.G + min(row, A.rows - 1) - query * A.G, limit = valid ? seq.limit(query) : 0, pieces = A.d / 8;
+    char *kt = lds, *vt = kt + F::kTile;
+    {
+        const char *k = A.K.p + b * A.K.batch + hk * A.K.head, *v = A.V.p + b * A.V.batch + hk * A.V.head;
+        load_short<E, F>(kt, seq.nk, pieces, [&](int r) __attribute__((always_inline)) { return k + r * A.K.token; });
+        load_short<E, F>(vt, seq.nk, pieces, [&](int r) __attribute__((always_inline)) { return v + r * A.V.token; });
+    }
+    typename S::Columns x;
+    S::template load<E>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
+    __syncthreads();
+
+    const Reader<G> reader(lane);
+    const int most = columns_max(limit);
+    f32x16 acc[G::NT];
+    clear(acc);
+    Running run(limit > 0);
+    for (int i = 0; 32 * i < most; ++i) {
+        f32x16 s{};
+        unrolled<S::kRows>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_rows(o, kt + i * F::kSub, reader, f);
+            S::rows(s, o, x, f);
+        });
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 32 * i + result_row(r, h) < limit ? s[r] : -INFINITY;
+        run.weights(s, A.c, acc);
+        typename S::Weights p;
+        unrolled<8>([&](auto r) __attribute__((always_inline)) { S::keep(p, s, 2 * r + 1); });
+        unrolled<S::kColumns>([&](auto f) __attribute__((always_inline)) {
+            typename S::Operand o;
+            S::read_columns(o, vt + i * F::kSub, reader, f);
+            S::columns(acc, o, p, f);
+        });
+    }
+    if (valid) finish<E, G>(A, b, hk, 0, row, h, acc, run.m, pair_sum(run.l));
+}
+
 // The splits' sums put together.  A thread has 8 channels of a row and every `groups`-th of its splits (one after another they took 26 us for
 // 32 splits of 256 rows, this way 6); the groups meet in LDS.
 template <class E, int D>
@@ -334,8 +394,15 @@ long row_tiles(const Sizes &S)
     const int rows = few(S) ? 32 : 32 * waves(S);
     return (S.rows() + rows - 1) / rows;
 }
+// Keys that k_attention_short_f32 has in LDS, 0 where it is not the one.
+int short_keys(const Sizes &S)
+{
+    const int fits = S.width() <= 32 ? 256 : S.width() <= 64 ? 128 : 64;
+    return !S.f32 || few(S) || S.Nk > fits ? 0 : S.Nk > fits / 2 || fits == 64 ? fits : fits / 2;
+}
 int splits_of(const Sizes &S)
 {
+    if (short_keys(S)) return 1;
     const long blocks = row_tiles(S) * S.B * S.Hk, tiles = (S.Nk + key_tile(S) - 1) / key_tile(S);
     if (blocks == 0) return 1;
     // A split is worth its join (5 us and more) where enough tiles are left to it (us without / with: 1024 tokens of 12 heads of 64 16.7 / 17.8, 2 x 512 of 8
@@ -388,11 +455,33 @@ int join(Call A, long heads, hipStream_t st)
     return BRA_OK;
 }
 
+template <int D, int R, int WAVES>
+int launch_short(Call A, hipStream_t st)
+{
+    typedef ShortKeys<D, R, WAVES> F;
+    const int rc = allow_lds<k_attention_short_f32<D, R, WAVES>>(F::kLds);
+    if (rc != BRA_OK) return rc;
+    for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
+        const ProfScope scope(st, K_ATTENTION);
+        k_attention_short_f32<D, R, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
+    }
+    return BRA_OK;
+}
+
 template <class E, int D>
 int run(const Sizes &S, const Call &A, hipStream_t st)
 {
     constexpr bool f32 = sizeof(E) == 4;
+    constexpr int kFits = D <= 32 ? 256 : D <= 64 ? 128 : 64;
     int rc;
+    if constexpr (f32) {
+        const int keys = short_keys(S);
+        if (keys == kFits) return waves(S) == 2 ? launch_short<D, kFits, 2>(A, st) : launch_short<D, kFits, 4>(A, st);
+        if constexpr (D <= 64) {
+            if (keys) return waves(S) == 2 ? launch_short<D, kFits / 2, 2>(A, st) : launch_short<D, kFits / 2, 4>(A, st);
+        }
+    }
     if (few(S)) rc = launch<E, D, 32, (f32 && D > 64 ? 2 : 4), true>(A, st);
     else rc = waves(S) == 2 ? launch_rows<E, D, 2>(A, st) : launch_rows<E, D, 4>(A, st);
     if (rc == BRA_OK && A.splits > 1) rc = join<E, D>(A, (long)S.B * S.Hk, st);
@@ -438,7 +527,7 @@ using namespace att;
 size_t attention_workspace_bytes(const Sizes &S)
 {
     const long splits = splits_of(S), rows = S.rows() * S.B * S.Hk;
-    return (S.f32 && !few(S) ? terms_bytes(S, false) : 0) + (splits > 1 ? align256(sizeof(float) * splits * rows * S.width()) + align256(2 * sizeof(float) * splits * rows) : 0);
+    return (S.f32 && !few(S) && !short_keys(S) ? terms_bytes(S, false) : 0) + (splits > 1 ? align256(sizeof(float) * splits * rows * S.width()) + align256(2 * sizeof(float) * splits * rows) : 0);
 }
 
 int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &V, const Rows &O, float *lse, void *ws, hipStream_t st)
@@ -450,7 +539,7 @@ int attention_forward(const Sizes &S, const Rows &Q, const Rows &K, const Rows &
     A.O = O;
     A.lse = lse;
     set_grid(A, (long)S.B * S.Hk, row_tiles(S), splits_of(S));
-    if (S.f32 && !few(S)) {
+    if (S.f32 && !few(S) && !short_keys(S)) {
         const int rc = make_terms(S, A, false, ws, st);
         if (rc != BRA_OK) return rc;
         ws = (char *)ws + terms_bytes(S, false);

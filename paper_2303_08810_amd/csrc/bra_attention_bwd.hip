@@ -475,31 +475,6 @@ struct Short {
     typedef Slots<G, T, kPlane> S;
 };
 
-// A head's rows, which lie at place(row), to LDS; zeros behind `rows`.
-template <class E, class F, class P>
-__device__ __forceinline__ void load_short(char *tile, int rows, int pieces, P place)
-{
-    typedef typename F::G G;
-    constexpr int kLoads = F::kPlane / 16, L = (kLoads + F::kThreads - 1) / F::kThreads;
-    const unsigned at = lds_address(tile) + 1024 * __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-#pragma unroll
-    for (int u = 0; u < L; ++u) {
-        const int i = threadIdx.x + F::kThreads * u, row = i / G::kPieces, piece = i % G::kPieces ^ G::turn(row);
-        if (kLoads % F::kThreads != 0 && i >= kLoads) break;         // (whole wavefronts)
-        const bool there = row < rows && piece < pieces;
-        const char *p = there ? place(row) + (int)sizeof(E) * 8 * piece : (const char *)zeros;
-        if constexpr (F::T == 1) load_to_lds_untracked((const bf16_t *)p, at + 16 * F::kThreads * u);
-        else {
-            const f32x4 v0 = *(const f32x4 *)p, v1 = *(const f32x4 *)(there ? p + 16 : p);
-            const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            bf16x8 t[3];
-            split3(v, t);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) *(bf16x8 *)(tile + k * F::kPlane + 16 * i) = t[k];
-        }
-    }
-}
-
 template <class E, int D, int R>
 __global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 : 2) void k_short_grads(Call A)
 {
