@@ -12,23 +12,23 @@ namespace bra {
 namespace att {
 namespace {
 
-// KT keys a tile.
-template <class E, int D, int KT, int WAVES, bool FEW>
-struct Forward {
+// Few rows, tiles of 32 keys.
+template <class E, int D, int WAVES>
+struct Few {
     typedef Geometry<E, D> G;
-    static constexpr int kThreads = 64 * WAVES, kLoaders = FEW ? 64 : kThreads, kRows = FEW ? 32 : 32 * WAVES;
-    static constexpr int kTile = KT * G::kPitch, kBuffer = 2 * kTile, kKeyTile = KT;
-    static constexpr int kRings = 2 * kBuffer * (FEW ? WAVES : 1);
+    static constexpr int KT = 32, kThreads = 64 * WAVES, kRows = 32;
+    static constexpr int kTile = KT * G::kPitch, kBuffer = 2 * kTile, kRings = 2 * kBuffer * WAVES;
     static constexpr int kColumn = D + 4;       // floats of a column's sums: the lanes of a wavefront begin in different banks
-    static constexpr int kJoin = FEW ? WAVES * 32 * (kColumn + 2) * 4 : 0;
+    static constexpr int kJoin = WAVES * 32 * (kColumn + 2) * 4;
     static constexpr int kLds = kRings > kJoin ? kRings : kJoin;
-    typedef Stage<G, KT, kLoaders> Loads;
+    typedef Stage<G, KT, 64> Loads;
 };
 
 // O (or its share before the division) and the statistics of one row.
 template <class E, class G>
-__device__ __forceinline__ void finish(const Call &A, int b, int hk, int split, int row, int h, const f32x16 (&acc)[G::NT], float m, float l)
+__device__ __forceinline__ void finish(const Call &A, int b, int hk, int split, int row, int h, f32x16 (&acc)[G::NT], float m, float l)
 {
+    if (l == 0.f) clear(acc);               // no weight: zeros, also where the values that others see are not finite
     const int query = row_query(A, row), head = hk * A.G + row - query * A.G;
     if (A.splits > 1) {
         const long at = ((long)(b * A.Hk + hk) * A.splits + split) * A.rows + row;
@@ -43,27 +43,24 @@ __device__ __forceinline__ void finish(const Call &A, int b, int hk, int split, 
     if (A.lse && h == 0) A.lse[((long)b * A.Hk * A.G + head) * A.Nq + query] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <class E, int D, int KT, int WAVES, bool FEW>
-__global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D > 96) ? 1 : 2) void k_attention(Call A)
+template <class E, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_few(Call A)
 {
-    typedef Forward<E, D, KT, WAVES, FEW> F;
+    typedef Few<E, D, WAVES> F;
     typedef typename F::G G;
+    constexpr int KT = F::KT;
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 32, c = lane % 32;
-    const Place place(A, A.first + blockIdx.x, A.tiles * A.splits);
-    const int tile = A.tiles - 1 - place.inner % A.tiles, split = place.inner / A.tiles;     // those of a causal mask's long rows first
-    const int hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
+    const Place place(A, A.first + blockIdx.x, A.splits);
+    const int split = place.inner, hb = place.head, b = hb / A.Hk, hk = hb % A.Hk;
     const Sequence seq(A, b);
     const int pieces = A.d * (int)sizeof(E) / 16;
 
-    const int first_row = tile * F::kRows, row = first_row + (FEW ? 0 : 32 * wave) + c;
+    const int row = c;
     const bool valid = row < A.rows;
-    const int query = row_query(A, min(row, A.rows - 1)), limit = valid ? seq.limit(query) : 0;
-    const int least = columns_min(limit);
-    // keys that any row of the workgroup sees
-    int end = 0;
-    if (row_query(A, first_row) < seq.nq) end = seq.limit(min(row_query(A, min(first_row + F::kRows, A.rows) - 1), seq.nq - 1));
-    const int all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, last = min(all, (split + 1) * share);
+    const int query = row_query(A, min(row, A.rows - 1)), limit = valid ? seq.limit(query) : 0, least = columns_min(limit);
+    // keys that any row sees
+    const int end = columns_max(limit), all = (end + KT - 1) / KT, share = (all + A.splits - 1) / A.splits, last = min(all, (split + 1) * share);
 
     typename G::Piece x[G::kSteps];
     {
@@ -71,65 +68,49 @@ __global__ __launch_bounds__(64 * WAVES, (FEW && D > 64) || (sizeof(E) == 4 && D
         load_columns<G>(A.Q.p + b * A.Q.batch + query * A.Q.token + head * A.Q.head, limit > 0, pieces, h, x);
     }
     const char *keys = A.K.p + b * A.K.batch + hk * A.K.head, *values = A.V.p + b * A.V.batch + hk * A.V.head;
-    char *ring = lds + (FEW ? wave * 2 * F::kBuffer : 0);
+    char *ring = lds + wave * 2 * F::kBuffer;
     const unsigned ring_at = lds_address(ring);
-    const int thread = FEW ? lane : threadIdx.x;
     auto request = [&](bool value, int t, int buffer) {
         const long token = value ? A.V.token : A.K.token;
         const int k0 = t * KT;
         const char *from = (value ? values : keys) + k0 * token;
-        F::Loads::request([&](int r) { return from + r * token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + (value ? F::kTile : 0), thread);
+        F::Loads::request([&](int r) { return from + r * token; }, seq.nk - k0, pieces, ring_at + buffer * F::kBuffer + (value ? F::kTile : 0), lane);
     };
 
     f32x16 acc[G::NT];
     clear(acc);
     Running run(limit > 0);
-    const char *kt = ring, *vt = ring + F::kTile;
-    f32x16 s[KT / 32];
-    auto scores = [&](int k0) {
-        clear(s);
-#pragma unroll
-        for (int i = 0; i < KT / 32; ++i) multiply_rows<G>(s[i], kt, 32 * i, x, lane);
+    // Each wavefront for itself, two tiles ahead: keys (values) are asked for as soon as those two tiles before them have been read (8 caches of up to 32768
+    // keys of 8 heads of 128 one tile ahead 126 us, two 122).
+    constexpr int L = F::Loads::L;
+    int t = split * share + wave;
+    for (int n = 0; n < 2; ++n)
+        if (t + n * WAVES < last) {
+            request(false, t + n * WAVES, n);
+            request(true, t + n * WAVES, n);
+        }
+    arrived<G>(x);
+    for (int buffer = 0; t < last; t += WAVES, buffer ^= 1) {
+        const bool one = t + WAVES < last, two = t + 2 * WAVES < last;
+        const char *kt = ring + buffer * F::kBuffer, *vt = kt + F::kTile;
+        const int k0 = t * KT;
+        if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(L) : "memory");
+        f32x16 s{};
+        multiply_rows<G>(s, kt, 0, x, lane);
         if (k0 + KT > least) {
 #pragma unroll
-            for (int i = 0; i < KT / 32; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[i][r] = k0 + 32 * i + result_row(r, h) < limit ? s[i][r] : -INFINITY;
+            for (int r = 0; r < 16; ++r) s[r] = k0 + result_row(r, h) < limit ? s[r] : -INFINITY;
         }
-    };
-    auto outputs = [&] {
-#pragma unroll
-        for (int i = 0; i < KT / 32; ++i) multiply_columns<G>(acc, vt, 32 * i, s[i], lane);
-    };
-    if constexpr (FEW) {
-        // Each wavefront for itself, two tiles ahead: keys (values) are asked for as soon as those two tiles before them have been read.
-        // One tile ahead the loads' latency was in the way: 604 MB of keys and values for one token each 146 us.
-        constexpr int L = F::Loads::L;
-        int t = split * share + wave;
-        for (int n = 0; n < 2; ++n)
-            if (t + n * WAVES < last) {
-                request(false, t + n * WAVES, n);
-                request(true, t + n * WAVES, n);
-            }
-        arrived<G>(x);
-        for (int buffer = 0; t < last; t += WAVES, buffer ^= 1) {
-            const bool one = t + WAVES < last, two = t + 2 * WAVES < last;
-            kt = ring + buffer * F::kBuffer;
-            vt = kt + F::kTile;
-            if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
-            else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(L) : "memory");
-            scores(t * KT);
-            lds_reads_done();
-            if (two) request(false, t + 2 * WAVES, buffer);
-#pragma unroll
-            for (int i = 0; i < KT / 32; ++i) run.weights(s[i], A.c, acc);
-            if (two) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
-            else if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * L) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            outputs();
-            lds_reads_done();
-            if (two) request(true, t + 2 * WAVES, buffer);
-        }
+        lds_reads_done();
+        if (two) request(false, t + 2 * WAVES, buffer);
+        run.weights(s, A.c, acc);
+        if (two) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * L) : "memory");
+        else if (one) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * L) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        multiply_columns<G>(acc, vt, 0, s, lane);
+        lds_reads_done();
+        if (two) request(true, t + 2 * WAVES, buffer);
     }
 
     // the wavefronts' shares: [wave][column][kColumn] sums, then [wave][column] m and l; every wavefront puts some of the channels together
@@ -411,15 +392,15 @@ int splits_of(const Sizes &S)
     return (int)std::max(1L, std::min({want / blocks, tiles / least, 64L}));
 }
 
-template <class E, int D, int KT, int WAVES, bool FEW>
-int launch(Call A, hipStream_t st)
+template <class E, int D, int WAVES>
+int launch_few(Call A, hipStream_t st)
 {
-    typedef Forward<E, D, KT, WAVES, FEW> F;
-    const int rc = allow_lds<k_attention<E, D, KT, WAVES, FEW>>(F::kLds);
+    typedef Few<E, D, WAVES> F;
+    const int rc = allow_lds<k_attention_few<E, D, WAVES>>(F::kLds);
     if (rc != BRA_OK) return rc;
     for (A.first = 0; A.first < A.blocks; A.first += kMaxBlocks) {
         const ProfScope scope(st, K_ATTENTION);
-        k_attention<E, D, KT, WAVES, FEW><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
+        k_attention_few<E, D, WAVES><<<(unsigned)std::min(kMaxBlocks, A.blocks - A.first), F::kThreads, F::kLds, st>>>(A);
         if (hipGetLastError() != hipSuccess) return BRA_ERR_LAUNCH;
     }
     return BRA_OK;
@@ -482,7 +463,7 @@ int run(const Sizes &S, const Call &A, hipStream_t st)
             if (keys) return waves(S) == 2 ? launch_short<D, kFits / 2, 2>(A, st) : launch_short<D, kFits / 2, 4>(A, st);
         }
     }
-    if (few(S)) rc = launch<E, D, 32, (f32 && D > 64 ? 2 : 4), true>(A, st);
+    if (few(S)) rc = launch_few<E, D, (f32 && D > 64 ? 2 : 4)>(A, st);
     else rc = waves(S) == 2 ? launch_rows<E, D, 2>(A, st) : launch_rows<E, D, 4>(A, st);
     if (rc == BRA_OK && A.splits > 1) rc = join<E, D>(A, (long)S.B * S.Hk, st);
     return rc;

@@ -113,6 +113,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
         if (t + 1 < last) body(std::integral_constant<int, 1>{}, t + 1);
     }
     if (!valid) return;
+    if (limit == 0) clear(acc);             // it sees nothing: zeros, also where the keys that others see are not finite
     if (A.splits > 1) store_columns<float, G>((char *)(A.part + (((long)hb * A.splits + split) * A.rows + row) * D), acc, A.scale, A.d, h);
     else store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
 }
@@ -131,14 +132,14 @@ struct Backward {
 };
 
 // A wavefront's registers over the subtiles.
-template <class G, bool KEYS>
+template <class G>
 struct Pipe {
     typedef Slots<G, 1, 0> S;
     typedef typename S::Columns X;
-    static constexpr int kColumns = (KEYS ? 2 : 1) * S::kColumns, kReadAhead = 2 * S::kRows < 8 ? 2 * S::kRows : 8;
+    static constexpr int kColumns = 2 * S::kColumns, kReadAhead = 2 * S::kRows < 8 ? 2 * S::kRows : 8;
     f32x16 s[2];                                // scores and dP of a subtile
     typename S::Weights p, ds;                  // of the subtile before
-    f32x16 sum[KEYS ? 2 : 1][G::NT];            // dV and dK, or dQ
+    f32x16 sum[2][G::NT];                       // dV and dK
 
     // s of a subtile
     __device__ __forceinline__ void scores(const char *t0, const char *t1, const Reader<G> &R, const X &x, const X &g)
@@ -154,14 +155,12 @@ struct Pipe {
     template <int F>
     __device__ __forceinline__ void read_column(typename S::Operand &o, const char *t0, const char *t1, const Reader<G> &R)
     {
-        S::read_columns(o, KEYS && F % 2 == 0 ? t1 : t0, R, KEYS ? F / 2 : F);
+        S::read_columns(o, F % 2 ? t0 : t1, R, F / 2);
     }
     template <int F>
     __device__ __forceinline__ void product(const typename S::Operand &o)
     {
-        if constexpr (!KEYS) S::columns(sum[0], o, ds, F);
-        else if constexpr (F % 2 == 0) S::columns(sum[0], o, p, F / 2);
-        else S::columns(sum[1], o, ds, F / 2);
+        S::columns(sum[F % 2], o, F % 2 ? ds : p, F / 2);
     }
     __device__ __forceinline__ void sums(const char *t0, const char *t1, const Reader<G> &R)
     {
@@ -195,13 +194,13 @@ struct Pipe {
                 s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], c, minus_lse));
                 s[1][r] = s[0][r] * (s[1][r] - delta);
                 if constexpr (r % 2) {
-                    if (KEYS) S::keep(np, s[0], r);
+                    S::keep(np, s[0], r);
                     S::keep(nds, s[1], r);
                 }
             });
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (KEYS) p = np;
+        p = np;
         ds = nds;
         s[0] = s[1] = f32x16{};
         unrolled<2 * S::kRows>([&](auto i) __attribute__((always_inline)) {
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     const float *row_sums = (h ? A.row_delta : A.row_lse) + (long)hb * A.rows;
 
     const Reader<G> reader(lane);
-    Pipe<G, true> pipe;
+    Pipe<G> pipe;
     clear(pipe.sum[0]);
     clear(pipe.sum[1]);
     auto slot = [&](int j) __attribute__((always_inline)) {
@@ -555,6 +554,7 @@ __global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 :
                     S::columns(acc, o, w, f);
                 });
             }
+            if (limit == 0) clear(acc);
             if (row < A.rows) store_columns<E, G>(A.dQ.p + b * A.dQ.batch + query * A.dQ.token + head * A.dQ.head, acc, A.scale, A.d, h);
             if (F::kGroups == F::kSide || group + F::kSide >= F::kGroups) return;
         }

@@ -229,3 +229,25 @@ def test_graphs_and_streams(Nq, Nk, dtype):
     for i, got in results:
         for a, b in zip(got, want[i]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Nq,Nk", [(3, 40), (3, 3000), (60, 60), (60, 3000), (150, 300)])
+def test_rows_that_see_nothing_are_zero_whatever_the_values_hold(Nq, Nk, dtype):
+    """NaN and infinities among the values (and keys) that other rows see: rows behind the length, and those that a causal mask leaves without a key, stay zero, and so do the
+    gradients there and of keys behind the length."""
+    Q, K, V, dO = make(2, Nq, Nk, 2, 1, 64, dtype)
+    lens = torch.tensor([Nq - 2, Nq], dtype=torch.int32, device="cuda")
+    k_lens = torch.tensor([Nk - 1, 1], dtype=torch.int32, device="cuda")
+    V[0, 1, 0, 3], K[0, 2, 0, 5], V[1, 0, 0, 0] = math.nan, math.nan, math.inf
+    rule = dict(causal=True, q_lens=lens, k_lens=k_lens)
+    O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True, **rule)
+    dQ, dK, dV = bra.bra_attention_backward(Q, K, V, O, lse, dO, **rule)
+    empty = torch.zeros(2, Nq, dtype=torch.bool, device="cuda")
+    empty[0, Nq - 2:] = True
+    empty[1, :Nq - 1] = True                    # one key: the last query alone sees it
+    for t in (O, dQ):
+        assert not t[empty].any() and not t[empty].isnan().any()
+    assert bool((lse.transpose(1, 2)[empty] == -math.inf).all())
+    for t in (dK, dV):
+        assert not t[0, Nk - 1:].any() and not t[1, 1:].any()
