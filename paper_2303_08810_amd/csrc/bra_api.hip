@@ -130,7 +130,7 @@ static int make_attention_sizes(const bra_attention_shape *s, att::Sizes &S)
     if (!s) return BRA_ERR_NULL;
     constexpr int kMost = 1 << 28;
     if (s->B < 0 || s->Nq < 0 || s->Nk < 0 || s->B > kMost || s->Nq > kMost || s->Nk > kMost || s->kv_heads < 1 || s->heads < s->kv_heads || s->heads % s->kv_heads || s->heads > 65536 ||
-        s->d < 1 || !std::isfinite(s->scale))
+        s->d < 1 || !std::isfinite(s->scale) || s->scale > 1e38f)
         return BRA_ERR_SHAPE;
     if ((long)s->B * s->heads > (1L << 30) || (long)s->Nq * s->heads > (1L << 30)) return BRA_ERR_SHAPE;
     if ((long)s->B * s->heads > (1L << 40) / std::max({s->Nq, s->Nk, 1})) return BRA_ERR_SHAPE;

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_few(Ca
     for (int piece = 2 * wave + h; piece < D / 8; piece += 2 * WAVES) {
         if (8 * piece >= A.d) break;
         float v[8] = {};
-        if (limit > 0)
+        if (l != 0.f)
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float *from = sums + (w * 32 + c) * F::kColumn + 8 * piece;
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 #pragma unroll 4
         for (int s = group; s < A.splits; s += groups) {
             const long p = at + (long)s * A.rows;
-            if (A.part_ml[2 * p] == -INFINITY) continue;
+            if (A.part_ml[2 * p + 1] == 0.f) continue;          // (not the maximum: sums that are NaN have none)
             const f32x4 v0 = *(const f32x4 *)(A.part + p * D + ch), v1 = *(const f32x4 *)(A.part + p * D + ch + 4);
             const f32x2 ml = *(const f32x2 *)(A.part_ml + 2 * p);
             const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};

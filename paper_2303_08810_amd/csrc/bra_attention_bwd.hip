@@ -396,11 +396,9 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     S::arrived(g);
 
     const Reader<G> reader(lane);
-    struct {
-        f32x16 sum[2][G::NT];           // dV and dK
-    } pipe;
-    clear(pipe.sum[0]);
-    clear(pipe.sum[1]);
+    f32x16 sum[2][G::NT];           // dV and dK
+    clear(sum[0]);
+    clear(sum[1]);
     auto body = [&](auto B, int t) __attribute__((always_inline)) {
         constexpr int kMine = decltype(B)::value * F::kSlot, kOther = F::kSlot - kMine;
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -442,7 +440,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
         unrolled<2 * S::kColumns>([&](auto f) __attribute__((always_inline)) {
             typename S::Operand o;
             S::read_columns(o, f % 2 ? qt : gt, reader, f / 2);
-            S::columns(pipe.sum[f % 2], o, f % 2 ? ds : p, f / 2);
+            S::columns(sum[f % 2], o, f % 2 ? ds : p, f / 2);
         });
     };
     for (int t = first; t < last; t += 2) {
@@ -451,16 +449,16 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
     }
     if (key >= A.Nk) return;
     if (!live) {
-        clear(pipe.sum[0]);
-        clear(pipe.sum[1]);
+        clear(sum[0]);
+        clear(sum[1]);
     }
     if (A.splits > 1) {
         float *part = A.part + ((((long)hb * A.splits + split) * A.Nk + key) * 2) * D;
-        store_columns<float, G>((char *)part, pipe.sum[1], A.scale, A.d, h);
-        store_columns<float, G>((char *)(part + D), pipe.sum[0], 1.f, A.d, h);
+        store_columns<float, G>((char *)part, sum[1], A.scale, A.d, h);
+        store_columns<float, G>((char *)(part + D), sum[0], 1.f, A.d, h);
     } else {
-        store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, pipe.sum[1], A.scale, A.d, h);
-        store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, pipe.sum[0], 1.f, A.d, h);
+        store_columns<E, G>(A.dK.p + b * A.dK.batch + key * A.dK.token + hk * A.dK.head, sum[1], A.scale, A.d, h);
+        store_columns<E, G>(A.dV.p + b * A.dV.batch + key * A.dV.token + hk * A.dV.head, sum[0], 1.f, A.d, h);
     }
 }
 

@@ -33,7 +33,7 @@ def attention(s, backward, ws=FAKE, ws_bytes=1 << 50, lse=FAKE, q_lens=None, k_l
 @pytest.mark.parametrize("backward", [False, True])
 def test_attention_refusals(backward):
     assert attention(None, backward) == -1
-    for bad in (shape(B=-1), shape(Nq=-1), shape(Nk=-1), shape(kv=0), shape(heads=3), shape(heads=0, kv=1), shape(heads=1, kv=2), shape(d=0), shape(scale=NAN), shape(scale=INF),
+    for bad in (shape(B=-1), shape(Nq=-1), shape(Nk=-1), shape(kv=0), shape(heads=3), shape(heads=0, kv=1), shape(heads=1, kv=2), shape(d=0), shape(scale=NAN), shape(scale=3e38), shape(scale=INF),
                 shape(Nq=(1 << 28) + 1), shape(Nk=(1 << 28) + 1), shape(B=(1 << 28) + 1), shape(heads=65538), shape(B=1 << 28, heads=8), shape(Nq=1 << 28, heads=8),
                 shape(B=1 << 14, Nk=1 << 28)):
         assert attention(bad, backward) == -2

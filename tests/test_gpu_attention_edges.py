@@ -251,3 +251,19 @@ def test_rows_that_see_nothing_are_zero_whatever_the_values_hold(Nq, Nk, dtype):
     assert bool((lse.transpose(1, 2)[empty] == -math.inf).all())
     for t in (dK, dV):
         assert not t[0, Nk - 1:].any() and not t[1, 1:].any()
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32), ids=("bf16", "f32"))
+@pytest.mark.parametrize("Nq,Nk", ((3, 40), (3, 3000), (60, 60), (60, 3000), (150, 300)))
+def test_what_is_not_a_number_reaches_every_row_that_sees_it(Nq, Nk, dtype):
+    """A NaN in a key that all rows see, one after the other through the sequence: no split's sums go missing."""
+    for key in (0, Nk // 2, Nk - 1):
+        Q, K, V, _ = make(2, Nq, Nk, 2, 1, 64, dtype)
+        want, want_lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+        K[0, key, 0, 9] = math.nan
+        O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+        assert bool(O[0].isnan().all()) and bool(lse[0].isnan().all())
+        assert torch.equal(O[1], want[1]) and torch.equal(lse[1], want_lse[1])
+        K[0, :, 0, 9] = math.nan
+        O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
+        assert bool(O[0].isnan().all()) and bool(lse[0].isnan().all()) and torch.equal(O[1], want[1])
