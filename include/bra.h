@@ -351,7 +351,7 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
  * finite, or above 3.3e38, makes NaN of what depends on it), up to 32 rows (queries times heads / kv_heads) forward the float32 matrix instruction.
  * scale <= 0 selects 1 / sqrt(d).  No atomic adds: a repeat gives the same bits.  Nothing else than `ws` is needed; its size depends on the shape and
  * may be 0.
- * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite, negative
+ * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite or above 1e38, negative
  * strides, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; LAUNCH. */
 typedef struct bra_attention_shape {
     int32_t B, Nq, Nk;        /* sequences; queries and keys of each, at most */
@@ -410,7 +410,7 @@ int bra_qk_norm_forward(const bra_qk_norm_shape *shape, const bra_rows *Q, const
                         const bra_qk_norm_params *params, const bra_rows *Qout, const bra_rows *Kout_opt, void *hip_stream);
 
 /* Gradients of it.  Q, K: its inputs (not read without gammas); gQ, gK: what came back to its outputs.  dQ, dK have the inputs' dtype; dq_gamma and
- * dk_gamma [d] float32 or NULL, summed over tokens and heads, OVERWRITTEN.  dQ may be gQ or Q, dK may be gK or K.  No atomic adds: a repeat gives the
+ * dk_gamma [d] float32 or NULL, summed over tokens and heads, OVERWRITTEN.  dQ may be gQ or Q, dK may be gK or K.  With eps = 0 a head of zeros is NaN, as the formula has it.  No atomic adds: a repeat gives the
  * same bits.  Errors as above, and WORKSPACE. */
 int bra_qk_norm_backward_workspace_bytes(const bra_qk_norm_shape *shape, size_t *out_bytes);
 int bra_qk_norm_backward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K_opt, const bra_qk_norm_params *params,

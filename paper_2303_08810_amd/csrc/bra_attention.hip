@@ -388,6 +388,8 @@ int splits_of(const Sizes &S)
     if (blocks == 0) return 1;
     // A split is worth its join (5 us and more) where enough tiles are left to it (us without / with: 1024 tokens of 12 heads of 64 16.7 / 17.8, 2 x 512 of 8
     // heads 13.0 / 15.1; 2048 causal of 16 / 4 heads of 128 46.8 / 44.5; float32 3 x 667 of 6 heads of 40 37.7 / 30.4).
+    // Workgroups at least (single tokens, us with 512 / 1024 / 2048: 8 caches of up to 32768 keys of 8 heads of 128 119 / 119 / 134, 4 of up to 16384 46 / 54 / 75, 32 of
+    // up to 4096 69 / 66 / 84, float32, 4 of 8192 of 12 heads of 64 62 / 78 / 83).
     const long want = 512, least = few(S) ? 2 * waves(S) : S.f32 ? 5 : 12;
     return (int)std::max(1L, std::min({want / blocks, tiles / least, 64L}));
 }
