@@ -213,38 +213,59 @@ struct Pipe {
 };
 
 // A workgroup's subtiles [0, n), of which this wavefront works on [from, to).  Turn j has the subtiles j - 1 to j + 1 in LDS; before it, what was asked
-// for in turn j - 3 has arrived everywhere, and then subtile j + kRing - 2 is asked for, where j - 2 lay.  `own`: this wavefront's
-// loads of a subtile.
+// for in turn j - 2 has arrived everywhere, and then subtile j + 3 is asked for, where j - 2 lay.  `loads`: whether this wavefront loads.
 template <class F, class Scores, class Weights, class Sums, class Request>
-__device__ __forceinline__ void take_turns(int n, int from, int to, bool one_more, bool loads, Scores scores, Weights weights, Sums sums, Request request)
+__device__ __forceinline__ void take_turns(int n, int from, int to, bool loads, Scores scores, Weights weights, Sums sums, Request request)
 {
+    static_assert(F::kRing == 5, "three subtiles that are worked on, two on their way");
     if (n <= 0) return;
-    for (int j = 0; j < min(n, F::kRing - 3); ++j) request(j);
-    auto turn = [&](int j) __attribute__((always_inline)) {
+    // where the subtiles j - 1 .. j + 3 lie, which go round
+    unsigned before = 3 * F::kSlot, here = 4 * F::kSlot, next = 0, then = F::kSlot, asked = 2 * F::kSlot;
+    request(0, next);
+    if (n > 1) request(1, then);
+    int j = -1;
+    auto turn = [&]() __attribute__((always_inline)) {
         // (fewer loads than this are on their way in the last turns: all of them are waited for)
         if (j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        else if (one_more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L + 1) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L + 1) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (j + F::kRing - 2 < n) request(j + F::kRing - 2);
+        if (j + 3 < n) request(j + 3, asked);
+    };
+    auto turned = [&]() __attribute__((always_inline)) {
+        const unsigned last = before;
+        before = here;
+        here = next;
+        next = then;
+        then = asked;
+        asked = last;
+        ++j;
     };
     // every wavefront meets the others at n + 2 barriers; what it does between them differs at its ends alone, so that its sums stay where they are
-    int j = -1;
     if (from < to) {
-        for (; j < from - 1; ++j) turn(j);
-        turn(j++);
-        scores(from);
-        turn(j++);
-        weights(std::false_type{}, from);
-        for (; j < to; ++j) {
-            turn(j);
-            weights(std::true_type{}, j);
+        while (j < from - 1) {
+            turn();
+            turned();
         }
-        turn(j++);
-        sums(to - 1);
+        turn();
+        scores(next);
+        turned();
+        turn();
+        weights(std::false_type{}, j, before, here, next);
+        turned();
+        while (j < to) {
+            turn();
+            weights(std::true_type{}, j, before, here, next);
+            turned();
+        }
+        turn();
+        sums(before);
+        turned();
     }
-    for (; j <= n; ++j) turn(j);
+    while (j <= n) {
+        turn();
+        turned();
+    }
 }
 
 template <int D, int WAVES>
@@ -291,44 +312,42 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     Pipe<G> pipe;
     clear(pipe.sum[0]);
     clear(pipe.sum[1]);
-    auto slot = [&](int j) __attribute__((always_inline)) {
-        unsigned o = (unsigned)j % F::kRing * F::kSlot;
-        asm("" : "+s"(o));          // (a scalar, or the compiler forms it again for every lane and read)
-        return o;
-    };
+    const bool loads = wave < F::Loads::kLoaders, steady = queries.whole && queries.step && grads.step;
     take_turns<F>(
-        n, max(least / 32 - first, 0), wave_key < seq.nk ? n : 0, wave == 0, wave < F::Loads::kLoaders,
-        [&](int j) __attribute__((always_inline)) { pipe.scores(lds + slot(j), lds + slot(j) + F::kTile, reader, x, g); },
-        [&](auto columns, int j) __attribute__((always_inline)) {
+        n, max(least / 32 - first, 0), wave_key < seq.nk ? n : 0, loads,
+        [&](unsigned next) __attribute__((always_inline)) { pipe.scores(lds + next, lds + next + F::kTile, reader, x, g); },
+        [&](auto columns, int j, unsigned before, unsigned here, unsigned next) __attribute__((always_inline)) {
+            // (behind the last subtile: what is there, whose scores nobody uses)
+            const float *mine = (const float *)(lds + here + 2 * F::kTile) + 4 * h;
+            f32x4 l[4], d[2];
+            unrolled<4>([&](auto q) __attribute__((always_inline)) { l[q] = *(const f32x4 *)(mine + 8 * q); });
+            d[0] = *(const f32x4 *)(mine + 32);
+            // rows that do not see this lane's key have no weight: masks change these numbers, not the products' results, which would move between registers for it
             const int r0 = row0 + 32 * j;
             if (r0 < most || r0 + 32 > end) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int i = r0 + result_row(r, h);
-                    const bool see = i >= begin && i < end;
-                    pipe.s[0][r] = see ? pipe.s[0][r] : -INFINITY;
-                    pipe.s[1][r] = see ? pipe.s[1][r] : 0.f;
+                    l[r / 4][r % 4] = i >= begin && i < end ? l[r / 4][r % 4] : INFINITY;
                 }
             }
-            const char *before = lds + slot(j + F::kRing - 1), *next = lds + slot(j + 1);        // (behind the last one: what is there, whose scores nobody uses)
-            const float *mine = (const float *)(lds + slot(j) + 2 * F::kTile) + 4 * h;
-            f32x4 l[2], d[2];
-            l[0] = *(const f32x4 *)mine;
-            d[0] = *(const f32x4 *)(mine + 32);
-            pipe.template step<decltype(columns)::value>(before, before + F::kTile, next, next + F::kTile, reader, x, g, A.c, [&](auto r, float &ml, float &dl) __attribute__((always_inline)) {
-                if constexpr (r % 4 == 0 && r < 12) {
-                    l[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 8);
-                    d[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 40);
-                }
-                ml = -l[r / 4 % 2][r % 4];
+            pipe.template step<decltype(columns)::value>(lds + before, lds + before + F::kTile, lds + next, lds + next + F::kTile, reader, x, g, A.c, [&](auto r, float &ml, float &dl) __attribute__((always_inline)) {
+                if constexpr (r % 4 == 0 && r < 12) d[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 40);
+                ml = -l[r / 4][r % 4];
                 dl = d[r / 4 % 2][r % 4];
             });
         },
-        [&](int j) __attribute__((always_inline)) { pipe.sums(lds + slot(j), lds + slot(j) + F::kTile, reader); },
-        [&](int j) __attribute__((always_inline)) {
-            queries.request(at + slot(j), pieces, threadIdx.x, query_at);
-            grads.request(at + slot(j) + F::kTile, pieces, threadIdx.x, grad_at);
-            if (wave == 0) load4_to_lds_untracked(row_sums + min(row0 + 32 * j + c, A.rows - 1), at + slot(j) + 2 * F::kTile);
+        [&](unsigned before) __attribute__((always_inline)) { pipe.sums(lds + before, lds + before + F::kTile, reader); },
+        [&](int j, unsigned to) __attribute__((always_inline)) {
+            if (!loads) return;
+            load4_to_lds_untracked(row_sums + min(row0 + 32 * j + c, A.rows - 1), at + to + 2 * F::kTile);
+            if (steady && row0 + 32 * j + 32 <= end) {
+                queries.request_whole(at + to);
+                grads.request_whole(at + to + F::kTile);
+            } else {
+                queries.request(at + to, pieces, threadIdx.x, query_at);
+                grads.request(at + to + F::kTile, pieces, threadIdx.x, grad_at);
+            }
         });
     if (key >= A.Nk) return;
     if (!live) {

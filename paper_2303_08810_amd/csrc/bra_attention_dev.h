@@ -495,19 +495,22 @@ struct Tiles {
     __device__ __forceinline__ void request(unsigned lds, int pieces, int thread, F at)
     {
         const unsigned to = lds + 1024 * wave;
-        if (wave < kLoaders) {
-            if (whole && row + ROWS <= end) {
 #pragma unroll
-                for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)place[u], to + 16 * THREADS * u);
-            } else {
-#pragma unroll
-                for (int u = 0; u < L; ++u)
-                    load_to_lds_untracked((const bf16_t *)(row + row_of(u, thread) < end && piece_of(u, thread) < pieces ? place[u] : (const char *)zeros), to + 16 * THREADS * u);
-            }
-        }
+        for (int u = 0; u < L; ++u)
+            load_to_lds_untracked((const bf16_t *)(row + row_of(u, thread) < end && piece_of(u, thread) < pieces ? place[u] : (const char *)zeros), to + 16 * THREADS * u);
         row += ROWS;
 #pragma unroll
         for (int u = 0; u < L; ++u) place[u] = step ? place[u] + step : at(row + row_of(u, thread)) + 16 * piece_of(u, thread);
+    }
+    // the same where the tile and its rows are whole and places go on by `step`
+    __device__ __forceinline__ void request_whole(unsigned lds)
+    {
+        const unsigned to = lds + 1024 * wave;
+#pragma unroll
+        for (int u = 0; u < L; ++u) load_to_lds_untracked((const bf16_t *)place[u], to + 16 * THREADS * u);
+        row += ROWS;
+#pragma unroll
+        for (int u = 0; u < L; ++u) place[u] += step;
     }
 };
 
