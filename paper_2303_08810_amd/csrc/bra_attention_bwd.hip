@@ -136,16 +136,17 @@ template <class G>
 struct Pipe {
     typedef Slots<G, 1, 0> S;
     typedef typename S::Columns X;
-    static constexpr int kColumns = 2 * S::kColumns, kReadAhead = 2 * S::kRows < 8 ? 2 * S::kRows : 8;
+    static constexpr int kColumns = 2 * S::kColumns, kScores = 2 * S::kRows, kAhead = kScores < 8 ? kScores : 8;
     f32x16 s[2];                                // scores and dP of a subtile
     typename S::Weights p, ds;                  // of the subtile before
     f32x16 sum[2][G::NT];                       // dV and dK
+    typename S::Operand ahead[kAhead];          // the first operands of the sums of the subtile before
 
     // s of a subtile
     __device__ __forceinline__ void scores(const char *t0, const char *t1, const Reader<G> &R, const X &x, const X &g)
     {
         s[0] = s[1] = f32x16{};
-        unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+        unrolled<kScores>([&](auto f) __attribute__((always_inline)) {
             typename S::Operand o;
             S::read_rows(o, f % 2 ? t1 : t0, R, f / 2);
             S::rows(s[f % 2], o, f % 2 ? g : x, f / 2);
@@ -166,26 +167,30 @@ struct Pipe {
     {
         unrolled<kColumns>([&](auto f) __attribute__((always_inline)) {
             typename S::Operand o;
-            this->template read_column<f>(o, t0, t1, R);
+            if constexpr (f < kAhead) o = ahead[f];
+            else this->template read_column<f>(o, t0, t1, R);
             this->template product<f>(o);
         });
     }
-    // s -> p, ds; with COLUMNS the sums of the subtile before, in b0, b1, on the way; then s of the next one, in n0, n1.  weights(r): value r's
-    // -lse log2 e and delta.  Operands are read kBefore products ahead.
-    template <bool COLUMNS, class W>
-    __device__ __forceinline__ void step(const char *b0, const char *b1, const char *n0, const char *n1, const Reader<G> &R, const X &x, const X &g, float c, W weights)
+    // s -> p, ds; with COLUMNS the sums of the subtile before, in b0, b1, on the way; then s of the next one, in n0, n1, of which nothing is read before
+    // arrive().  weights(r): value r's -lse log2 e and delta.  Operands are read kAhead products ahead, also those of the next step, which
+    // come from this subtile, in h0, h1.
+    template <bool COLUMNS, class W, class Arrive>
+    __device__ __forceinline__ void step(const char *b0, const char *b1, const char *h0, const char *h1, const char *n0, const char *n1, const Reader<G> &R, const X &x, const X &g, float c,
+                                         W weights, Arrive arrive)
     {
-        constexpr int N = COLUMNS ? kColumns : 1, all = N + 2 * S::kRows, kBefore = kReadAhead;
+        constexpr int N = COLUMNS ? kColumns : kAhead, all = N + kScores;
         typename S::Operand o[all];
         typename S::Weights np, nds;
         auto read = [&](auto f) __attribute__((always_inline)) {
-            if constexpr (f >= N) S::read_rows(o[f], (f - N) % 2 ? n1 : n0, R, (f - N) / 2);
+            if constexpr (f >= all) this->template read_column<f - all>(ahead[f - all], h0, h1, R);
+            else if constexpr (f >= N) S::read_rows(o[f], (f - N) % 2 ? n1 : n0, R, (f - N) / 2);
             else if constexpr (COLUMNS) this->template read_column<f>(o[f], b0, b1, R);
         };
-        unrolled<kBefore>(read);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (COLUMNS) unrolled<kAhead>([&](auto f) __attribute__((always_inline)) { o[f] = ahead[f]; });
         unrolled<N>([&](auto f) __attribute__((always_inline)) {
-            if constexpr (f + kBefore < all) read(std::integral_constant<int, f + kBefore>{});
+            if constexpr (f + kAhead == N) arrive();
+            read(std::integral_constant<int, f + kAhead>{});
             if constexpr (COLUMNS) this->template product<f>(o[f]);
             unrolled<16 * (f + 1) / N - 16 * f / N>([&](auto i) __attribute__((always_inline)) {
                 constexpr int r = 16 * f / N + i;
@@ -196,6 +201,12 @@ struct Pipe {
                 if constexpr (r % 2) {
                     S::keep(np, s[0], r);
                     S::keep(nds, s[1], r);
+                    if constexpr (N > kAhead) {         // formed here, not in the block behind arrive()
+                        unsigned a = np.v[0][r / 8][r % 8 / 2], b = nds.v[0][r / 8][r % 8 / 2];
+                        asm volatile("" : "+v"(a), "+v"(b));
+                        np.v[0][r / 8][r % 8 / 2] = a;
+                        nds.v[0][r / 8][r % 8 / 2] = b;
+                    }
                 }
             });
             __builtin_amdgcn_sched_barrier(0);
@@ -203,17 +214,17 @@ struct Pipe {
         p = np;
         ds = nds;
         s[0] = s[1] = f32x16{};
-        unrolled<2 * S::kRows>([&](auto i) __attribute__((always_inline)) {
+        unrolled<kScores>([&](auto i) __attribute__((always_inline)) {
             constexpr int f = N + i;
-            if constexpr (f + kBefore < all) read(std::integral_constant<int, f + kBefore>{});
+            read(std::integral_constant<int, f + kAhead>{});
             S::rows(s[i % 2], o[f], i % 2 ? g : x, i / 2);
             __builtin_amdgcn_sched_barrier(0);
         });
     }
 };
 
-// A workgroup's subtiles [0, n), of which this wavefront works on [from, to).  Turn j has the subtiles j - 1 to j + 1 in LDS; before it, what was asked
-// for in turn j - 2 has arrived everywhere, and then subtile j + 3 is asked for, where j - 2 lay.  `loads`: whether this wavefront loads.
+// A workgroup's subtiles [0, n), of which this wavefront works on [from, to).  Turn j makes sure that subtile j + 1 has arrived and that nobody reads j - 2 any
+// more, in whose place it asks for j + 3.  `loads`: whether this wavefront loads.
 template <class F, class Scores, class Weights, class Sums, class Request>
 __device__ __forceinline__ void take_turns(int n, int from, int to, bool loads, Scores scores, Weights weights, Sums sums, Request request)
 {
@@ -226,8 +237,8 @@ __device__ __forceinline__ void take_turns(int n, int from, int to, bool loads, 
     int j = -1;
     auto turn = [&]() __attribute__((always_inline)) {
         // (fewer loads than this are on their way in the last turns: all of them are waited for)
-        if (j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * F::Loads::L + 1) : "memory");
+        if (j + 2 >= n || !loads) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * F::Loads::L + 1) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (j + 3 < n) request(j + 3, asked);
@@ -250,16 +261,15 @@ __device__ __forceinline__ void take_turns(int n, int from, int to, bool loads, 
         turn();
         scores(next);
         turned();
-        turn();
-        weights(std::false_type{}, j, before, here, next);
+        weights(std::false_type{}, j, before, here, next, turn);
         turned();
         while (j < to) {
-            turn();
-            weights(std::true_type{}, j, before, here, next);
+            weights(std::true_type{}, j, before, here, next, turn);
             turned();
         }
-        turn();
         sums(before);
+        lds_reads_done();
+        turn();
         turned();
     }
     while (j <= n) {
@@ -316,7 +326,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
     take_turns<F>(
         n, max(least / 32 - first, 0), wave_key < seq.nk ? n : 0, loads,
         [&](unsigned next) __attribute__((always_inline)) { pipe.scores(lds + next, lds + next + F::kTile, reader, x, g); },
-        [&](auto columns, int j, unsigned before, unsigned here, unsigned next) __attribute__((always_inline)) {
+        [&](auto columns, int j, unsigned before, unsigned here, unsigned next, auto arrive) __attribute__((always_inline)) {
             // (behind the last subtile: what is there, whose scores nobody uses)
             const float *mine = (const float *)(lds + here + 2 * F::kTile) + 4 * h;
             f32x4 l[4], d[2];
@@ -331,11 +341,14 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_key_grads(Call A
                     l[r / 4][r % 4] = i >= begin && i < end ? l[r / 4][r % 4] : INFINITY;
                 }
             }
-            pipe.template step<decltype(columns)::value>(lds + before, lds + before + F::kTile, lds + next, lds + next + F::kTile, reader, x, g, A.c, [&](auto r, float &ml, float &dl) __attribute__((always_inline)) {
-                if constexpr (r % 4 == 0 && r < 12) d[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 40);
-                ml = -l[r / 4][r % 4];
-                dl = d[r / 4 % 2][r % 4];
-            });
+            pipe.template step<decltype(columns)::value>(
+                lds + before, lds + before + F::kTile, lds + here, lds + here + F::kTile, lds + next, lds + next + F::kTile, reader, x, g, A.c,
+                [&](auto r, float &ml, float &dl) __attribute__((always_inline)) {
+                    if constexpr (r % 4 == 0 && r < 12) d[(r / 4 + 1) % 2] = *(const f32x4 *)(mine + 2 * r + 40);
+                    ml = -l[r / 4][r % 4];
+                    dl = d[r / 4 % 2][r % 4];
+                },
+                arrive);
         },
         [&](unsigned before) __attribute__((always_inline)) { pipe.sums(lds + before, lds + before + F::kTile, reader); },
         [&](int j, unsigned to) __attribute__((always_inline)) {
