@@ -226,6 +226,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : sizeof(E
         unrolled<KT / 32>([&](auto i) __attribute__((always_inline)) {
             s[i] = f32x16{};
             unrolled<S::kRows>([&](auto f) __attribute__((always_inline)) {
+                if (S::kLeaves && f == S::kRows - 1 && 16 * f >= A.d) return;
                 typename S::Operand o;
                 S::read_rows(o, lds + kMine + i * F::kSub, reader, f);
                 S::rows(s[i], o, x, f);
@@ -297,6 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_short_
     for (int i = 0; 32 * i < most; ++i) {
         f32x16 s{};
         unrolled<S::kRows>([&](auto f) __attribute__((always_inline)) {
+            if (S::kLeaves && f == S::kRows - 1 && 16 * f >= A.d) return;
             typename S::Operand o;
             S::read_rows(o, kt + i * F::kSub, reader, f);
             S::rows(s, o, x, f);

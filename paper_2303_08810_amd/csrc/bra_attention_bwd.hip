@@ -87,6 +87,7 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
             const char *kt = lds + kMine + i * F::kSub, *vt = kt + F::kTile;
             f32x16 s{}, d{};
             unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+                if (S::kLeaves && f / 2 == S::kRows - 1 && 16 * (f / 2) >= A.d) return;
                 typename S::Operand o;
                 S::read_rows(o, f % 2 ? vt : kt, reader, f / 2);
                 S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
@@ -443,6 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
         const float *ls = (const float *)(gt + F::kTile) + 4 * h;
         f32x16 s{}, d{};
         unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+            if (S::kLeaves && f / 2 == S::kRows - 1 && 16 * (f / 2) >= A.d) return;
             typename S::Operand o;
             S::read_rows(o, f % 2 ? gt : qt, reader, f / 2);
             S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
@@ -552,6 +554,7 @@ __global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 :
     auto scores = [&](f32x16 &s, f32x16 &d, const char *t0, const char *t1, const typename S::Columns &x, const typename S::Columns &g) __attribute__((always_inline)) {
         s = d = f32x16{};
         unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
+            if (S::kLeaves && f / 2 == S::kRows - 1 && 16 * (f / 2) >= A.d) return;
             typename S::Operand o;
             S::read_rows(o, f % 2 ? t1 : t0, reader, f / 2);
             S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);

@@ -272,6 +272,7 @@ __device__ __forceinline__ void unrolled(F f)
 template <class G, int T, int PLANE>
 struct Slots {
     static constexpr int kRows = G::kSteps, kColumns = 2 * G::NT;
+    static constexpr bool kLeaves = T == 3;         // the last step of rows is left out where heads have no channels there: six products for a branch
     struct Operand {
         u32x4 v[T];
     };
