@@ -542,16 +542,16 @@ __device__ __forceinline__ int columns_max(int v)
     return __builtin_amdgcn_readfirstlane(v);
 }
 
-// Softmax statistics of a column, in powers of two: m, from which its weights are taken (a whole number, the same in both of its lanes), l this lane's
-// share of their sum.
+// Softmax statistics of a column, in powers of two: m, from which its weights are taken (the same in both of its lanes), l this lane's share of their
+// sum.
 struct Running {
     float m, base, bar, l = 0.f;        // base: m, or 0 where there is none yet; bar: what a lane's weights of 32 keys may sum up to
     // `sees`: whether any key is visible to the column; one that sees none needs no m
     __device__ __forceinline__ explicit Running(bool sees) : m(sees ? -INFINITY : 0.f), base(0.f), bar(sees ? -1.f : kMost) {}
     static constexpr float kMost = 8192.f;
     // S -> P of 32 keys.  Weights are taken from the m that there is; only where a lane's sum shows that one has grown too large, or where there is none
-    // yet, the maximum is looked for, and m raised to it: what is in acc follows by a power of two, so that nothing is rounded.  Sums are float32
-    // and stay below 2^13 a step.  The maximum of every tile took a sixth of the vector instructions, which bound heads of 64 channels.
+    // yet, the maximum is looked for, and m raised to it.  Sums are float32 and stay below 2^13 a step.  The largest weight of a row's first tile is
+    // one, which bf16 holds: a row of one key is that key's value, and in rows of few keys the weight that counts most is not rounded.  The maximum of every tile took a sixth of the vector instructions, which bound heads of 64 channels.
     template <int NT>
     __device__ __forceinline__ void weights(f32x16 &s, float c, f32x16 (&acc)[NT])
     {
@@ -566,7 +566,7 @@ struct Running {
             float top = fmaxf(s[0], s[1]);
 #pragma unroll
             for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
-            const float next = fmaxf(m, ceilf(pair_max(top) * c)), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+            const float next = fmaxf(m, pair_max(top) * c), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
             m = next;
             base = next == -INFINITY ? 0.f : next;
             bar = next == -INFINITY ? -1.f : kMost;

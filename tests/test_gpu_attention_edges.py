@@ -267,3 +267,19 @@ def test_what_is_not_a_number_reaches_every_row_that_sees_it(Nq, Nk, dtype):
         K[0, :, 0, 9] = math.nan
         O, lse = bra.bra_attention_forward(Q, K, V, want_lse=True)
         assert bool(O[0].isnan().all()) and bool(lse[0].isnan().all()) and torch.equal(O[1], want[1])
+
+
+@pytest.mark.parametrize("want_lse", (False, True))
+@pytest.mark.parametrize("d", (8, 64, 128))
+@pytest.mark.parametrize("Nq,Nk", ((1, 1), (50, 1), (50, 600), (700, 1), (300, 5000)))
+def test_a_row_of_one_key_is_its_value(Nq, Nk, d, want_lse):
+    """Its weight is 2^x with |x| below 2^-24 |S| log2 e, S below 64 here: one in bf16, and within 2^-17 of one in the sum that divides it, which the rounding of the
+    quotient to bf16 takes back.  Whether lse is asked for changes nothing."""
+    Q, K, V, _ = make(2, Nq, Nk, 4, 2, d, torch.bfloat16)
+    k_lens = torch.ones(2, dtype=torch.int32, device="cuda")
+    O = bra.bra_attention_forward(Q, K, V, k_lens=k_lens, want_lse=want_lse)
+    O = O[0] if want_lse else O
+    assert torch.equal(O, V[:, :1].repeat_interleave(2, 2).expand(-1, Nq, -1, -1))
+    if Nk > 1:
+        O, lse = bra.bra_attention_forward(Q, K, V, causal=True, want_lse=True)
+        assert torch.equal(O, bra.bra_attention_forward(Q, K, V, causal=True))
