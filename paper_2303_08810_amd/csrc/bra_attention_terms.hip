@@ -16,7 +16,7 @@ struct Tensors {
     int n;
 };
 
-// A workgroup has 128 pieces of 8 channels of a head.  2 x 1295 tokens of 8 / 2 heads of 72 among others: K, V, Q and dO 7 us.
+// A workgroup has 128 pieces of 8 channels of a head.  2 x 1295 tokens of 8 / 2 heads of 72: K, V, Q and dO 9 us, 40 MB written.
 template <int P>
 __global__ __launch_bounds__(128) void k_attention_terms(Call A, Tensors X, unsigned first)
 {
