@@ -283,3 +283,18 @@ def test_a_row_of_one_key_is_its_value(Nq, Nk, d, want_lse):
     if Nk > 1:
         O, lse = bra.bra_attention_forward(Q, K, V, causal=True, want_lse=True)
         assert torch.equal(O, bra.bra_attention_forward(Q, K, V, causal=True))
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32), ids=("bf16", "f32"))
+@pytest.mark.parametrize("B,Nk,kv,kind", ((2, 6000, 3, "one long"), (8, 2000, 1, "even"), (70, 1500, 2, "uneven"), (130, 1000, 1, "uneven"), (256, 600, 1, "one long"), (5, 3000, 7, "none")))
+def test_caches_of_very_different_lengths(B, Nk, kv, kind, dtype):
+    """Single tokens over caches of very different lengths: every key of every sequence counts once."""
+    d = 32
+    Q, K, V, _ = make(B, 1, Nk, 2 * kv, kv, d, dtype)
+    lens = {"one long": [Nk if b == B // 2 else b % 3 for b in range(B)], "even": [Nk] * B, "uneven": [(37 * b * b + 1) % (Nk + 1) for b in range(B)], "none": [0] * B}[kind]
+    lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ref = Attention(Q, K, V, k_lens=lens)
+    O_ref, lse_ref, O_off, lse_off = ref.forward()
+    O, lse = bra.bra_attention_forward(Q, K, V, k_lens=lens, want_lse=True)
+    check(O, O_ref, O_off, "O")
+    check(lse, lse_ref, lse_off, "lse")
