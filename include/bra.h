@@ -375,6 +375,8 @@ int bra_attention_forward(const bra_attention_shape *shape, const bra_rows *Q, c
  *     P = exp(S - lse),  delta_i = dO[i] . O[i],  dS = P (dO V^T - delta),
  *     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO, dK and dV summed over the heads that share a key head.
  * dQ, dK, dV have the inputs' dtype, and are OVERWRITTEN, with zeros from nq (nk) on.  bf16: P and dS are rounded to bf16 before the products.
+ * A row that sees one key, whose weight is one, has O = V and adds nothing to dQ and dK: dS is set to zero, where |log2 P| < 2^-16 (1 + |lse| log2 e), and not left
+ * to the rounding of two sums.  (With lse and O of a longer sequence, of whose keys a call has some, P is less and dS is what the formula gives.)
  * Errors as above. */
 int bra_attention_backward_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes);
 int bra_attention_backward(const bra_attention_shape *shape, const bra_rows *Q, const bra_rows *K, const bra_rows *V,

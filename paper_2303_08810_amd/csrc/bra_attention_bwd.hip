@@ -95,6 +95,11 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(E) == 4 && D > 64 ? 1 : 2) void 
                 S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
             });
             if (masked) {
+                if (i == 0 && k0 == 0 && limit == 1 && all_weight(s[0], A.c, lse)) {
+                    // dS = 0 here; the key side, whose dO V has the same bits, subtracts it from itself
+                    lse = INFINITY;
+                    if (h == 0) A.row_delta[(long)hb * A.rows + row] = d[0];
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = k0 + 32 * i + result_row(r, h) < limit ? s[r] : -INFINITY;
             }
@@ -451,7 +456,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 32 ? 1 : 2) void k_key_grads_f32(Ca
             if (S::kLeaves && f / 2 == S::kRows - 1 && 16 * (f / 2) >= A.d) return;
             typename S::Operand o;
             S::read_rows(o, f % 2 ? gt : qt, reader, f / 2);
-            S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
+            S::template rows<true>(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
         });
         if (r0 < most || r0 + 32 > end) {
 #pragma unroll
@@ -556,29 +561,41 @@ __global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 :
 #pragma unroll
             for (int ks = 0; ks < G::kSteps; ++ks) x.v[t][ks] = *(const bf16x8 *)(tile + t * F::kPlane + reader.row[ks]);
     };
-    auto scores = [&](f32x16 &s, f32x16 &d, const char *t0, const char *t1, const typename S::Columns &x, const typename S::Columns &g) __attribute__((always_inline)) {
+    auto scores = [&](auto mirror, f32x16 &s, f32x16 &d, const char *t0, const char *t1, const typename S::Columns &x, const typename S::Columns &g) __attribute__((always_inline)) {
         s = d = f32x16{};
         unrolled<2 * S::kRows>([&](auto f) __attribute__((always_inline)) {
             if (S::kLeaves && f / 2 == S::kRows - 1 && 16 * (f / 2) >= A.d) return;
             typename S::Operand o;
             S::read_rows(o, f % 2 ? t1 : t0, reader, f / 2);
-            S::rows(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
+            S::template rows<decltype(mirror)::value>(f % 2 ? d : s, o, f % 2 ? g : x, f / 2);
         });
     };
     typename S::Columns x, g;
     f32x16 s, d;
+    if (seq.nk == 1) {              // (as in k_query_grads: the key side subtracts its dO V from itself)
+        for (int group = wave; wave < F::kSide && group < F::kGroups; group += F::kSide) {
+            const int row = 32 * group + c, limit = row < A.rows ? seq.limit(row_query(A, row)) : 0;
+            keep(x, qt + group * F::kSub);
+            keep(g, gt + group * F::kSub);
+            scores(std::false_type{}, s, d, kt, vt, x, g);
+            if (limit == 1 && h == 0 && all_weight(s[0], A.c, sums[row])) sums[R + row] = d[0];
+        }
+        __syncthreads();
+    }
     if (wave < F::kSide) {
         for (int group = wave;; group += F::kSide) {
             const int row = 32 * group + c, some = min(row, A.rows - 1), query = row_query(A, some), head = hk * A.G + some - query * A.G;
             if (32 * group >= A.rows) return;
             const int limit = row < A.rows ? seq.limit(query) : 0, most = columns_max(limit);
-            const float lse = sums[row], delta = sums[R + row];
+            const float delta = sums[R + row];
+            float lse = sums[row];
             keep(x, qt + group * F::kSub);
             keep(g, gt + group * F::kSub);
             f32x16 acc[G::NT];
             clear(acc);
             for (int i = 0; 32 * i < most; ++i) {
-                scores(s, d, kt + i * F::kSub, vt + i * F::kSub, x, g);
+                scores(std::false_type{}, s, d, kt + i * F::kSub, vt + i * F::kSub, x, g);
+                if (i == 0 && limit == 1 && all_weight(s[0], A.c, lse)) lse = INFINITY;
                 typename S::Weights w;
                 unrolled<16>([&](auto e) __attribute__((always_inline)) {
                     constexpr int r = e;
@@ -608,7 +625,7 @@ __global__ __launch_bounds__((Short<E, D, R>::kThreads), D > 64 && R < 128 ? 1 :
         clear(dk);
         clear(dv);
         for (int i = columns_min(begin) / 32; 32 * i < end; ++i) {
-            scores(s, d, qt + i * F::kSub, gt + i * F::kSub, x, g);
+            scores(std::true_type{}, s, d, qt + i * F::kSub, gt + i * F::kSub, x, g);
             const float *mine = sums + 32 * i + 4 * h;
             typename S::Weights p, ds;
             unrolled<4>([&](auto q) __attribute__((always_inline)) {

@@ -282,9 +282,11 @@ struct Slots {
     struct Weights {            // 32 values of the contraction
         u32x4 v[T][2];
     };
+    // MIRROR: the terms' products in the order in which they come with the operands exchanged, so that both sides of a gradient have the same bits of a score.
+    template <bool MIRROR = false>
     __device__ static __forceinline__ f32x16 product(const Operand &a, const bf16x8 (&b)[T], f32x16 c)
     {
-        auto one = [&](int i, int j) __attribute__((always_inline)) { c = mfma32(__builtin_bit_cast(bf16x8, a.v[i]), b[j], c); };
+        auto one = [&](int i, int j) __attribute__((always_inline)) { c = mfma32(__builtin_bit_cast(bf16x8, a.v[MIRROR ? j : i]), b[MIRROR ? i : j], c); };
         if constexpr (T == 3) {
             one(2, 0);
             one(0, 2);
@@ -311,12 +313,13 @@ struct Slots {
             o.v[t] = u32x4{r[0][0], r[0][1], r[1][0], r[1][1]};
         }
     }
+    template <bool MIRROR = false>
     __device__ static __forceinline__ void rows(f32x16 &s, const Operand &o, const Columns &x, int f)
     {
         bf16x8 b[T];
 #pragma unroll
         for (int t = 0; t < T; ++t) b[t] = x.v[t][f];
-        s = product(o, b, s);
+        s = product<MIRROR>(o, b, s);
     }
     __device__ static __forceinline__ void columns(f32x16 (&acc)[G::NT], const Operand &o, const Weights &p, int f)
     {
@@ -514,6 +517,11 @@ struct Tiles {
         for (int u = 0; u < L; ++u) place[u] += step;
     }
 };
+
+// Whether the one key that a row sees has all of its weight, as far as the roundings of its score and of lse (both in powers of two) tell: O is that key's value then, and
+// dS = dO V - dO O is zero.  What float32 leaves of the difference of the two sums would be all that dQ, and dK of a sequence of one key, consist of.  The score
+// is asked, not the number of keys alone: with the lse of a longer sequence, of whose keys a call has one, the weight is less and dS is what the formula gives.
+__device__ __forceinline__ bool all_weight(float s, float c, float lse) { return fabsf(fmaf(s, c, -lse)) < 0x1p-16f * (1.f + fabsf(lse)); }
 
 // Of the two lanes of a column.
 __device__ __forceinline__ float pair_max(float v)
