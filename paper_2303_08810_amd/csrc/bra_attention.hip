@@ -325,6 +325,23 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_short_
     if (valid) finish<E, G>(A, b, hk, 0, row, h, acc, run.m, pair_sum(run.l));
 }
 
+// What a thread of k_attention_join has: 8 channels from ch on of row `slot` of a workgroup's, every groups-th split from `group` on.  Pieces and groups that do not divide 256
+// leave threads over, which have no row; the first group takes the others' sums from LDS rows thread + CH, thread + 2 CH ...
+struct JoinPlace {
+    int per, ch, group, slot;
+    constexpr JoinPlace(int thread, int CH, int groups) : per(256 / (CH * groups)), ch(8 * (thread % CH)), group(thread / CH % groups), slot(thread / (CH * groups)) {}
+    constexpr bool has_row() const { return slot < per; }
+};
+constexpr bool join_stays_in_lds(int CH)
+{
+    for (int groups = 1; CH * groups <= 256; groups *= 2)
+        for (int t = 0; t < 256; ++t) {
+            const JoinPlace P(t, CH, groups);
+            if (P.has_row() && P.group == 0 && t + (groups - 1) * CH >= 256) return false;
+        }
+    return true;
+}
+
 // The splits' sums put together.  A thread has 8 channels of a row and every `groups`-th of its splits (one after another they took 26 us for
 // 32 splits of 256 rows, this way 6); the groups meet in LDS.
 template <class E, int D>
@@ -332,9 +349,11 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
 {
     constexpr int CH = D / 8;
     __shared__ float lds[256][11];
-    const int per = 256 / (CH * groups), ch = 8 * (threadIdx.x % CH), group = threadIdx.x / CH % groups, slot = threadIdx.x / (CH * groups);
-    const long r = (A.first + blockIdx.x) * per + slot, rows = A.blocks * A.rows;           // here blocks: sequences x key heads
-    const bool valid = slot < per && r < rows;
+    static_assert(join_stays_in_lds(CH), "rows of lds");
+    const JoinPlace P(threadIdx.x, CH, groups);
+    const int ch = P.ch, group = P.group;
+    const long r = (A.first + blockIdx.x) * P.per + P.slot, rows = A.blocks * A.rows;           // here blocks: sequences x key heads
+    const bool valid = P.has_row() && r < rows;
     const int row = valid ? (int)(r % A.rows) : 0, hb = valid ? (int)(r / A.rows) : 0, b = hb / A.Hk, hk = hb % A.Hk;
     const long at = (long)hb * A.splits * A.rows + row;
     float top = -INFINITY, l = 0.f, o[8] = {};
@@ -361,7 +380,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Call A, int groups)
         lds[threadIdx.x][8] = top;
         lds[threadIdx.x][9] = l;
         __syncthreads();
-        if (group) return;
+        if (group || !valid) return;        // (threads without a row have none in lds behind them either)
         for (int g = 1; g < groups; ++g) {
             const float *from = lds[threadIdx.x + g * CH];
             const float v[8] = {from[0], from[1], from[2], from[3], from[4], from[5], from[6], from[7]};
