@@ -70,7 +70,7 @@ enum {
     BRA_ERR_UNSUPPORTED = -6, /* valid shape outside what the kernels are built for */
     BRA_ERR_LAUNCH = -7,      /* the HIP runtime reported an error at enqueue time */
     BRA_ERR_TOO_LARGE = -8,   /* bra_forward_static: the shape needs more than BRA_STATIC_SCRATCH_BYTES */
-    BRA_ERR_OVERLAP = -10,    /* bra_adamw_step: parameters that share memory */
+    BRA_ERR_OVERLAP = -10,    /* bra_adamw_step: parameters that share memory; bra_attention_*, bra_qk_norm_*: what is written shares memory */
     BRA_ERR_ALIGN = -9        /* bra_ffn_*, bra_norm_*, bra_adamw_step, bra_attention_*, bra_qk_norm_*: a pointer (or stride) is not aligned as its entry point asks */
 };
 
@@ -345,14 +345,16 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
  * on, queries and what comes back from nq on are not read; what is read beyond a causal mask's edge must be finite.
  * A tensor [B, N, heads, d] is given by a bra_rows: its element (b, n, h, c) lies at data + b batch + n token + h head + c, in elements, so that
  * parts of one buffer, or a cache with the heads outside, are taken as they lie.  Pointers, and strides in bytes, are multiples of 16 (the stride
- * of a dimension of one entry is not looked at); inputs may have strides of 0.  What is written overlaps neither itself nor an input.
+ * of a dimension of one entry is not looked at); inputs may have strides of 0.  What is written overlaps neither itself nor
+ * anything else of the call (OVERLAP: places are compared exactly, but for tensors whose dimensions run through each other, which count as overlapping where 4096 steps do not
+ * tell); the workspace is memory of its own.
  * d: a multiple of 8 up to 128 (heads that are no multiple of 32 wide take the time of the next one).  bf16 tensors: P is rounded to bf16 before its product
  * with V, everything else is float32.  float32 tensors: products of three bf16 terms per operand (relative error of a product 2^-23; a value that is not
  * finite, or above 3.3e38, makes NaN of what depends on it), up to 32 rows (queries times heads / kv_heads) forward the float32 matrix instruction.
  * scale <= 0 selects 1 / sqrt(d).  No atomic adds: a repeat gives the same bits.  Nothing else than `ws` is needed; its size depends on the shape and
  * may be 0.
  * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite or above 1e38, negative
- * strides, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; LAUNCH. */
+ * strides, places 2^56 bytes from data and further, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; OVERLAP; LAUNCH. */
 typedef struct bra_attention_shape {
     int32_t B, Nq, Nk;        /* sequences; queries and keys of each, at most */
     int32_t heads, kv_heads;  /* heads of the queries, of keys and values */
@@ -390,9 +392,10 @@ int bra_attention_backward(const bra_attention_shape *shape, const bra_rows *Q, 
  *                                                         (BRA_PAIRS_HALVES) or (2 p, 2 p + 1) (BRA_PAIRS_NEIGHBOURS); the others stay
  * with cos, sin [table_rows, turned / 2] float32 at row positions[b N + n] (int32, clamped to the table), or n where positions is NULL.
  * Q [B, N, heads, d] and K [B, N, kv_heads, d] as bra_rows (see above); K NULL with kv_heads = 0: queries alone.  q_gamma and k_gamma [d] float32, both or
- * neither.  The outputs have the inputs' dtype, rounded once; Qout may be Q, Kout may be K.
+ * neither.  The outputs have the inputs' dtype, rounded once; Qout may be Q, Kout may be K,
+ * at the same places; apart from that what is written shares no memory with anything else of the call.
  * Errors: NULL; SHAPE (B, N < 0, heads < 1, kv_heads < 0, B N (heads + kv_heads) above 2^30, turned odd or outside 0 .. d, table_rows < 1, or < N without
- * positions, where turned > 0, eps < 0, negative strides); DTYPE (dtype or pairs); UNSUPPORTED (d no multiple of 8 or above 128); ALIGN; LAUNCH. */
+ * positions, where turned > 0, eps < 0, strides as above); DTYPE (dtype or pairs); UNSUPPORTED (d no multiple of 8 or above 128); ALIGN; OVERLAP; LAUNCH. */
 enum { BRA_PAIRS_HALVES = 0, BRA_PAIRS_NEIGHBOURS = 1 };    /* bra_qk_norm_shape.pairs */
 typedef struct bra_qk_norm_shape {
     int32_t B, N, heads, kv_heads, d;
@@ -412,7 +415,7 @@ int bra_qk_norm_forward(const bra_qk_norm_shape *shape, const bra_rows *Q, const
                         const bra_qk_norm_params *params, const bra_rows *Qout, const bra_rows *Kout_opt, void *hip_stream);
 
 /* Gradients of it.  Q, K: its inputs (not read without gammas); gQ, gK: what came back to its outputs.  dQ, dK have the inputs' dtype; dq_gamma and
- * dk_gamma [d] float32 or NULL, summed over tokens and heads, OVERWRITTEN.  dQ may be gQ or Q, dK may be gK or K.  With eps = 0 a head of zeros is NaN, as the formula has it.  No atomic adds: a repeat gives the
+ * dk_gamma [d] float32 or NULL, summed over tokens and heads, OVERWRITTEN.  dQ may be gQ or Q, dK may be gK or K, at the same places.  With eps = 0 a head of zeros is NaN, as the formula has it.  No atomic adds: a repeat gives the
  * same bits.  Errors as above, and WORKSPACE. */
 int bra_qk_norm_backward_workspace_bytes(const bra_qk_norm_shape *shape, size_t *out_bytes);
 int bra_qk_norm_backward(const bra_qk_norm_shape *shape, const bra_rows *Q, const bra_rows *K_opt, const bra_qk_norm_params *params,

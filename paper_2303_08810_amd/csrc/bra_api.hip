@@ -4,6 +4,7 @@
 #include "bra_ffn.h"
 #include "bra_norm.h"
 #include "bra_attention.h"
+#include "bra_overlap.h"
 #include "bra_qk_norm.h"
 
 #include <math.h>
@@ -147,10 +148,37 @@ static int make_rows(const bra_rows *r, long B, long N, long heads, size_t eleme
     if (B == 0 || N == 0 || heads == 0) return BRA_OK;
     if (!r || !r->data) return BRA_ERR_NULL;
     const long e = (long)element;
-    R = att::Rows{(char *)r->data, B > 1 ? r->batch * e : 0, N > 1 ? r->token * e : 0, heads > 1 ? r->head * e : 0};
+    // (what lies further away than 2^56 bytes is no tensor)
+    constexpr long far = 1L << 56;
+    if ((B > 1 && r->batch > far / e / (B - 1)) || (N > 1 && r->token > far / e / (N - 1)) || (heads > 1 && r->head > far / e / (heads - 1))) return BRA_ERR_SHAPE;
     if ((B > 1 && r->batch < 0) || (N > 1 && r->token < 0) || (heads > 1 && r->head < 0)) return BRA_ERR_SHAPE;
+    R = att::Rows{(char *)r->data, B > 1 ? r->batch * e : 0, N > 1 ? r->token * e : 0, heads > 1 ? r->head * e : 0};
     if ((uintptr_t)R.p % 16 || R.batch % 16 || R.token % 16 || R.head % 16) return BRA_ERR_ALIGN;
     return BRA_OK;
+}
+
+// Where a call's tensors lie.  What is written may be what it is given as (`same`, at the same places), and meets nothing else of the call.
+static Pieces pieces_of(const att::Rows &R, long B, long N, long heads, long bytes) { return Pieces{R.p, bytes, {B, N, heads}, {R.batch, R.token, R.head}}; }
+static Pieces pieces_of(const void *p, size_t bytes) { return Pieces{(const char *)p, (long)bytes, {1, 1, 1}, {0, 0, 0}}; }
+struct Written {
+    Pieces at;
+    const Pieces *same[2];
+};
+static bool meet(std::initializer_list<Written> written, std::initializer_list<const Pieces *> read)
+{
+    for (const Written &w : written) {
+        if (!w.at.any()) continue;
+        if (meets_itself(w.at)) return true;
+        const uintptr_t from = (uintptr_t)w.at.p, to = from + w.at.last() + w.at.bytes;
+        for (const Written *o = written.begin(); o != &w; ++o)
+            if (share_memory(w.at, o->at)) return true;
+        for (const Pieces *r : read) {
+            if ((uintptr_t)r->p >= to || (uintptr_t)r->p + r->last() + r->bytes <= from) continue;      // (nearly always)
+            const bool allowed = r == w.same[0] || r == w.same[1];
+            if (!(allowed && same_place(w.at, *r)) && share_memory(w.at, *r)) return true;
+        }
+    }
+    return false;
 }
 
 static int make_qk_norm_sizes(const bra_qk_norm_shape *s, QkNormSizes &S)
@@ -511,6 +539,20 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
     return adamw_step(tensors, count, *a, (hipStream_t)hip_stream);
 }
 
+// Where they lie.
+struct QkNormVectors {
+    Pieces at[5];
+    QkNormVectors(const QkNormSizes &S, const QkNormIn &I)
+    {
+        const size_t gamma = 4 * (size_t)S.d, table = 4 * (size_t)S.table_rows * (S.turned / 2);
+        at[0] = pieces_of(I.q_gamma, gamma);
+        at[1] = pieces_of(I.k_gamma, gamma);
+        at[2] = pieces_of(S.turned ? I.cos : nullptr, table);
+        at[3] = pieces_of(S.turned ? I.sin : nullptr, table);
+        at[4] = pieces_of(S.turned ? I.positions : nullptr, 4 * (size_t)S.tokens);
+    }
+};
+
 int bra_attention_workspace_bytes(const bra_attention_shape *shape, size_t *out_bytes)
 {
     if (!out_bytes) return BRA_ERR_NULL;
@@ -536,6 +578,9 @@ int bra_attention_forward(const bra_attention_shape *shape, const bra_rows *Q, c
     if (S.B == 0 || S.Nq == 0) return BRA_OK;
     const size_t need = attention_workspace_bytes(S);
     if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    const long row = (long)e * S.d;
+    const Pieces in[] = {pieces_of(q, S.B, S.Nq, S.H, row), pieces_of(k, S.B, S.Nk, S.Hk, row), pieces_of(v, S.B, S.Nk, S.Hk, row), pieces_of(q_lens, 4 * (size_t)S.B), pieces_of(k_lens, 4 * (size_t)S.B)};
+    if (meet({{pieces_of(o, S.B, S.Nq, S.H, row), {}}, {pieces_of(lse, 4 * (size_t)S.B * S.H * S.Nq), {}}}, {&in[0], &in[1], &in[2], &in[3], &in[4]})) return BRA_ERR_OVERLAP;
     S.q_lens = q_lens;
     S.k_lens = k_lens;
     return attention_forward(S, q, k, v, o, lse, ws, (hipStream_t)hip_stream);
@@ -568,6 +613,11 @@ int bra_attention_backward(const bra_attention_shape *shape, const bra_rows *Q, 
     if (S.B == 0 || (S.Nq == 0 && S.Nk == 0)) return BRA_OK;
     const size_t need = attention_backward_workspace_bytes(S);
     if (need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    const long row = (long)e * S.d;
+    auto queries = [&](const att::Rows &R) { return pieces_of(R, S.B, S.Nq, S.H, row); };
+    auto keys = [&](const att::Rows &R) { return pieces_of(R, S.B, S.Nk, S.Hk, row); };
+    const Pieces in[] = {queries(q), keys(k), keys(v), queries(o), queries(go), pieces_of(lse, 4 * (size_t)S.B * S.H * S.Nq), pieces_of(q_lens, 4 * (size_t)S.B), pieces_of(k_lens, 4 * (size_t)S.B)};
+    if (meet({{queries(dq), {}}, {keys(dk), {}}, {keys(dv), {}}}, {&in[0], &in[1], &in[2], &in[3], &in[4], &in[5], &in[6], &in[7]})) return BRA_ERR_OVERLAP;
     S.q_lens = q_lens;
     S.k_lens = k_lens;
     return attention_backward(S, q, k, v, o, lse, go, dq, dk, dv, ws, (hipStream_t)hip_stream);
@@ -586,6 +636,12 @@ int bra_qk_norm_forward(const bra_qk_norm_shape *shape, const bra_rows *Q, const
     if ((rc = make_rows(Q, shape->B, S.N, S.heads, e, I.Q)) || (rc = make_rows(K, shape->B, S.N, S.kv_heads, e, I.K)) || (rc = make_rows(Qout, shape->B, S.N, S.heads, e, q)) ||
         (rc = make_rows(Kout, shape->B, S.N, S.kv_heads, e, k)))
         return rc;
+    const long row = (long)e * S.d, B = shape->B;
+    const QkNormVectors vectors(S, I);
+    const Pieces in[] = {pieces_of(I.Q, B, S.N, S.heads, row), pieces_of(I.K, B, S.N, S.kv_heads, row)};
+    if (meet({{pieces_of(q, B, S.N, S.heads, row), {&in[0]}}, {pieces_of(k, B, S.N, S.kv_heads, row), {&in[1]}}},
+             {&in[0], &in[1], &vectors.at[0], &vectors.at[1], &vectors.at[2], &vectors.at[3], &vectors.at[4]}))
+        return BRA_ERR_OVERLAP;
     return qk_norm_forward(S, I, q, k, (hipStream_t)hip_stream);
 }
 
@@ -616,6 +672,15 @@ int bra_qk_norm_backward(const bra_qk_norm_shape *shape, const bra_rows *Q, cons
     if (!aligned(4, {dq_gamma, dk_gamma})) return BRA_ERR_ALIGN;
     const size_t need = qk_norm_backward_workspace_bytes(S);
     if (I.q_gamma && need && !ws_ok(ws, ws_bytes, need)) return BRA_ERR_WORKSPACE;
+    const long row = (long)e * S.d, B = shape->B;
+    auto queries = [&](const att::Rows &R) { return pieces_of(R, B, S.N, S.heads, row); };
+    auto keys = [&](const att::Rows &R) { return pieces_of(R, B, S.N, S.kv_heads, row); };
+    const QkNormVectors vectors(S, I);
+    const Pieces in[] = {queries(I.Q), keys(I.K), queries(gq), keys(gk)};
+    const size_t sums = I.q_gamma ? 4 * (size_t)S.d : 0;
+    if (meet({{queries(dq), {&in[0], &in[2]}}, {keys(dk), {&in[1], &in[3]}}, {pieces_of(dq_gamma, sums), {}}, {pieces_of(dk_gamma, sums), {}}},
+             {&in[0], &in[1], &in[2], &in[3], &vectors.at[0], &vectors.at[1], &vectors.at[2], &vectors.at[3], &vectors.at[4]}))
+        return BRA_ERR_OVERLAP;
     return qk_norm_backward(S, I, gq, gk, dq, dk, dq_gamma, dk_gamma, ws, (hipStream_t)hip_stream);
 }
 
@@ -631,7 +696,7 @@ const char *bra_strerror(int code)
     case BRA_ERR_UNSUPPORTED: return "shape not supported by the requested kernel family";
     case BRA_ERR_LAUNCH: return "HIP runtime error while enqueueing";
     case BRA_ERR_TOO_LARGE: return "shape needs more scratch memory than the library's built-in buffer holds";
-    case BRA_ERR_OVERLAP: return "parameters or their copies share memory";
+    case BRA_ERR_OVERLAP: return "what is written shares memory with another part of itself or of the call";
     case BRA_ERR_ALIGN: return "a tensor is not aligned as its entry point asks";
     default: return "unknown error code";
     }

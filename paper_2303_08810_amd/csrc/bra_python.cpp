@@ -5,7 +5,6 @@
 // Functions here take every argument by position; the Python functions of the package give them their names and
 // defaults.  No kernel lives here and nothing is computed.
 #include <ATen/ATen.h>
-#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -718,16 +717,16 @@ bra_rows rows_of(const at::Tensor &t, const at::Tensor &X, at::IntArrayRef sizes
     return r;
 }
 
-// What is written: no two elements in one place, and not where something that is read or written lies (as far as views of one buffer tell).
-void own_memory(const at::Tensor &t, std::initializer_list<const at::Tensor *> others)
+// As run(); what is written sharing memory is a ValueError.
+template <typename F>
+void run_rows(F call)
 {
-    if (!t.numel()) return;
-    if (at::has_internal_overlap(t) == at::MemOverlap::Yes) value_error("an output overlaps itself");
-    for (const at::Tensor *o : others) {
-        if (!o || !o->numel()) continue;
-        const auto status = at::get_overlap_status(t, *o);
-        if (t.data_ptr() == o->data_ptr() || status == at::MemOverlapStatus::Full || status == at::MemOverlapStatus::Partial) value_error("an output shares memory with another tensor of the call");
-    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = call();
+    Py_END_ALLOW_THREADS;
+    if (rc == BRA_ERR_OVERLAP) value_error("an output overlaps itself or shares memory with another tensor of the call");
+    check(rc);
 }
 
 // Attention's operands: Q [B, Nq, heads, d], K and V [B, Nk, kv_heads, d].
@@ -778,14 +777,13 @@ PyObject *py_attention_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const c10::DeviceGuard guard(Q.device());
         at::Tensor own, lse, O = out ? *out : at::empty(Q.sizes(), Q.options());
         const bra_rows o = rows_of(O, Q, Q.sizes(), "out must be a tensor of Q's shape and dtype on its GPU, channels next to each other and every row on 16 bytes");
-        if (out) own_memory(*out, {&Q, &K, &V});
         const bool want_lse = PyObject_IsTrue(a[7]);
         if (want_lse) lse = at::empty({Q.size(0), Q.size(2), Q.size(1)}, Q.options().dtype(at::kFloat));
         size_t bytes = 0;
         check(bra_attention_workspace_bytes(&c.s, &bytes));
         const at::Tensor *ws = workspace_if(tensor(a[8]), bytes, Q, own);
         void *st = stream_of(Q);
-        run([&] {
+        run_rows([&] {
             return bra_attention_forward(&c.s, &c.Q, &c.K, &c.V, c.q_lens, c.k_lens, &o, want_lse ? (float *)lse.data_ptr() : nullptr, data(ws), ws ? (size_t)ws->numel() : 0, st);
         });
         PyObject *r;
@@ -819,13 +817,11 @@ PyObject *py_attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (!given) grads[i] = at::empty(like_of.sizes(), Q.options());
             d[i] = rows_of(grads[i], Q, like_of.sizes(), "out must be tensors of Q's, K's and V's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes");
         }
-        if (given)
-            for (int i = 0; i < 3; ++i) own_memory(grads[i], {&Q, &K, &V, &O, &dO, &grads[(i + 1) % 3], &grads[(i + 2) % 3]});
         size_t bytes = 0;
         check(bra_attention_backward_workspace_bytes(&c.s, &bytes));
         const at::Tensor *ws = workspace_if(tensor(a[10]), bytes, Q, own);
         void *st = stream_of(Q);
-        run([&] {
+        run_rows([&] {
             return bra_attention_backward(&c.s, &c.Q, &c.K, &c.V, &o, (const float *)lse.data_ptr(), &go, c.q_lens, c.k_lens, &d[0], &d[1], &d[2], data(ws), ws ? (size_t)ws->numel() : 0, st);
         });
         for (int i = 0; i < 3; ++i) objects[i] = wrap(grads[i]);        // (the caller's own object where it gave one)
@@ -875,7 +871,6 @@ QkNormCall qk_norm_call(const at::Tensor &Q, const at::Tensor *K, PyObject *q_ga
 struct Pair {
     at::Tensor Q, K;
     bra_rows q{}, k{};
-    bool given = false;
     Pair(PyObject *out, const at::Tensor &likeQ, const at::Tensor *likeK)
     {
         if (out == Py_None) {
@@ -886,27 +881,10 @@ struct Pair {
             if (outs.n != 2) value_error("out must be two tensors");
             Q = need(outs[0]);
             if (likeK) K = need(outs[1]);
-            given = true;
         }
         const char *text = "out must be tensors of Q's and K's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes";
         q = rows_of(Q, likeQ, likeQ.sizes(), text);
         if (likeK) k = rows_of(K, likeQ, likeK->sizes(), text);
-    }
-    // An output may be an input of its own kind, at the same places.
-    void check_memory(std::initializer_list<const at::Tensor *> ofQ, std::initializer_list<const at::Tensor *> ofK)
-    {
-        auto same = [](const at::Tensor &t, const at::Tensor *o) { return o && o->data_ptr() == t.data_ptr() && o->strides().equals(t.strides()) && o->sizes().equals(t.sizes()); };
-        if (!given) return;
-        for (const at::Tensor *o : ofQ) {
-            if (!same(Q, o)) own_memory(Q, {o});
-            if (K.defined()) own_memory(K, {o});
-        }
-        for (const at::Tensor *o : ofK) {
-            if (K.defined() && !same(K, o)) own_memory(K, {o});
-            own_memory(Q, {o});
-        }
-        own_memory(Q, {});
-        if (K.defined()) own_memory(K, {&Q});
     }
     PyObject *take(int i) { return wrap(i ? K : Q); }      // (the caller's own object where it gave one)
 };
@@ -925,9 +903,8 @@ PyObject *py_qk_norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const QkNormCall c = qk_norm_call(Q, K, a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
         const c10::DeviceGuard guard(Q.device());
         Pair out(a[9], Q, K);
-        out.check_memory({&Q}, {K});
         void *st = stream_of(Q);
-        run([&] { return bra_qk_norm_forward(&c.s, &c.Q, K ? &c.K : nullptr, &c.p, &out.q, K ? &out.k : nullptr, st); });
+        run_rows([&] { return bra_qk_norm_forward(&c.s, &c.Q, K ? &c.K : nullptr, &c.p, &out.q, K ? &out.k : nullptr, st); });
         return tuple({out.take(0), K ? out.take(1) : none()});
     });
 }
@@ -944,7 +921,6 @@ PyObject *py_qk_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (K) gk = rows_of(*gK, Q, K->sizes(), "dQ and dK must be tensors of Q's and K's shapes and dtype on their GPU, channels next to each other and every row on 16 bytes");
         const c10::DeviceGuard guard(Q.device());
         Pair out(a[12], Q, K);
-        out.check_memory({&Q, &gQ}, {K, gK});
         const bool norm = c.p.q_gamma != nullptr;
         at::Tensor own, dq_gamma, dk_gamma;
         const at::Tensor *ws = nullptr;
@@ -956,7 +932,7 @@ PyObject *py_qk_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
             ws = workspace(tensor(a[11]), bytes, Q, own);
         }
         void *st = stream_of(Q);
-        run([&] {
+        run_rows([&] {
             return bra_qk_norm_backward(&c.s, &c.Q, K ? &c.K : nullptr, &c.p, &gq, K ? &gk : nullptr, &out.q, K ? &out.k : nullptr, norm ? (float *)dq_gamma.data_ptr() : nullptr,
                                         norm && K ? (float *)dk_gamma.data_ptr() : nullptr, data(ws), ws ? (size_t)ws->numel() : 0, st);
         });
