@@ -75,6 +75,14 @@ double real(PyObject *o)
     return v;
 }
 
+// what `if` asks for; an object may have an exception of its own for it
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v;
+}
+
 float scale_of(PyObject *o) { return o == Py_None ? 0.f : (float)real(o); }
 
 int dtype_of(const at::Tensor &X)
@@ -195,6 +203,7 @@ PyObject *py_init(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyObject *py_route(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 8, [&]() -> PyObject * {
+        const bool want_ar = truth(a[5]);
         const at::Tensor &X = need(a[0]), &Wqkv = need(a[1]);
         const bra_shape s = layer_shape(X, Wqkv, nullptr, nullptr, integer(a[2]), integer(a[3]), integer(a[4]), Py_None, a[6]);
         at::Tensor own;
@@ -205,7 +214,6 @@ PyObject *py_route(PyObject *, PyObject *const *a, Py_ssize_t n)
             own = scratch(bytes, X);
             ws = &own;
         }
-        const bool want_ar = PyObject_IsTrue(a[5]);
         at::Tensor Ir = new_index(s, X), Ar;
         const int64_t R = (int64_t)s.S * s.S;
         if (want_ar) Ar = at::empty({s.B, R, R}, X.options().dtype(at::kFloat));
@@ -222,6 +230,7 @@ PyObject *py_route(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyObject *py_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 13, [&]() -> PyObject * {
+        const bool want_ir = truth(a[9]);
         const at::Tensor &X = need(a[0]), &Wqkv = need(a[1]), &Wo = need(a[2]), &Wlce = need(a[3]);
         const bra_shape s = layer_shape(X, Wqkv, &Wo, &Wlce, integer(a[4]), integer(a[5]), integer(a[6]), a[7], a[10]);
         const at::Tensor *Ir_in = tensor(a[8]), *ws = tensor(a[11]), *out = tensor(a[12]);
@@ -233,7 +242,6 @@ PyObject *py_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
             ws = &own;
         }
         Y = out ? *out : at::empty_like(X);
-        const bool want_ir = PyObject_IsTrue(a[9]);
         if (want_ir) Ir = new_index(s, X);
         check_index(Ir_in, s, "Ir_in must be a contiguous int32 [B, S*S, k] device tensor");
         void *st = stream_of(X);
@@ -274,12 +282,12 @@ PyObject *py_forward_static(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyObject *py_forward_padded(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 11, [&]() -> PyObject * {
+        const bool want_ir = truth(a[9]);
         const at::Tensor &X = need(a[0]), &Wqkv = need(a[1]), &Wo = need(a[2]), &Wlce = need(a[3]);
         const bra_shape s = layer_shape(X, Wqkv, &Wo, &Wlce, integer(a[4]), integer(a[5]), integer(a[6]), a[7], a[10]);
         size_t bytes = 0;
         check(bra_padded_workspace_bytes(&s, &bytes));
         at::Tensor ws = scratch(bytes, X), Y = at::empty_like(X), Ir;
-        const bool want_ir = PyObject_IsTrue(a[9]);
         if (want_ir) Ir = new_index(s, X);
         const at::Tensor *Ir_in = tensor(a[8]);
         check_index(Ir_in, s, "Ir_in must be a contiguous int32 [B, S*S, k] device tensor");
@@ -331,6 +339,7 @@ PyObject *py_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyObject *py_block_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 12, [&]() -> PyObject * {
+        const bool want_ir = truth(a[8]);
         const at::Tensor &X = need(a[0]);
         if (X.dim() != 4) value_error("X must be [B, H, W, C]");
         if (!(X.is_cuda() && X.is_contiguous())) value_error("X must be a contiguous device tensor");
@@ -367,7 +376,6 @@ PyObject *py_block_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
             ws = &own;
         }
         Xout = out ? *out : at::empty_like(X);
-        const bool want_ir = PyObject_IsTrue(a[8]);
         if (want_ir) Ir = new_index(s, X);
         check_index(Ir_in, s, "Ir_in must be a contiguous int32 [B, S*S, k] device tensor");
         const bra_block_params bp = {p[0]->data_ptr(), (const float *)p[1]->data_ptr(), (const float *)p[2]->data_ptr(),
@@ -429,6 +437,7 @@ bra_ffn_shape ffn_shape(const at::Tensor &X, const at::Tensor &W1, const at::Ten
 PyObject *py_ffn_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 9, [&]() -> PyObject * {
+        const bool want_pre = truth(a[6]);
         const at::Tensor &X = need(a[0]), &W1 = need(a[1]), &W2 = need(a[2]);
         const at::Tensor *b1 = tensor(a[3]), *b2 = tensor(a[4]), *out = tensor(a[8]);
         const bra_ffn_shape s = ffn_shape(X, W1, W2, b1, b2, a[5]);
@@ -438,7 +447,6 @@ PyObject *py_ffn_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         check(bra_ffn_workspace_bytes(&s, &bytes));
         at::Tensor own, Y = out ? *out : at::empty_like(X), pre;
         const at::Tensor *ws = workspace(tensor(a[7]), bytes, X, own);
-        const bool want_pre = PyObject_IsTrue(a[6]);
         if (want_pre) {
             auto sizes = X.sizes().vec();
             sizes.back() = 2 * (int64_t)s.hidden;
@@ -460,6 +468,7 @@ PyObject *py_ffn_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyObject *py_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 10, [&]() -> PyObject * {
+        const bool biases = truth(a[7]);
         const at::Tensor &X = need(a[0]), &W1 = need(a[1]), &W2 = need(a[2]), &dY = need(a[3]);
         const at::Tensor *b1 = tensor(a[4]), *pre = tensor(a[5]);
         const bra_ffn_shape s = ffn_shape(X, W1, W2, b1, nullptr, a[6]);
@@ -472,7 +481,6 @@ PyObject *py_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         check(bra_ffn_backward_workspace_bytes(&s, &bytes));
         const int asked = integer(a[8]), kind = asked < 0 ? s.dtype : asked;
         const auto options = X.options().dtype(kind == BRA_F32 ? at::kFloat : at::kBFloat16);
-        const bool biases = PyObject_IsTrue(a[7]);
         at::Tensor own, dX = at::empty_like(X), dW1 = at::empty(W1.sizes(), options), dW2 = at::empty(W2.sizes(), options), db1, db2;
         if (biases) {
             db1 = at::empty({2 * (int64_t)s.hidden}, options);
@@ -737,15 +745,14 @@ struct AttentionCall {
 };
 AttentionCall attention_call(const at::Tensor &Q, const at::Tensor &K, const at::Tensor &V, PyObject *causal, PyObject *q_lens, PyObject *k_lens, PyObject *scale)
 {
+    const bool masked = truth(causal);
     if (Q.dim() != 4 || K.dim() != 4) value_error("Q must be [B, Nq, heads, d], K and V [B, Nk, kv_heads, d]");
     const int dtype = dtype_of(Q);
     for (int d = 0; d < 4; ++d)
         if (Q.size(d) > INT32_MAX || K.size(d) > INT32_MAX) check(BRA_ERR_SHAPE);
     if (K.size(0) != Q.size(0) || K.size(3) != Q.size(3)) value_error("Q must be [B, Nq, heads, d], K and V [B, Nk, kv_heads, d]");
     AttentionCall c{};
-    const int truth = PyObject_IsTrue(causal);
-    if (truth < 0) throw Raised{};
-    c.s = bra_attention_shape{(int32_t)Q.size(0), (int32_t)Q.size(1), (int32_t)K.size(1), (int32_t)Q.size(2), (int32_t)K.size(2), (int32_t)Q.size(3), dtype, truth, scale_of(scale)};
+    c.s = bra_attention_shape{(int32_t)Q.size(0), (int32_t)Q.size(1), (int32_t)K.size(1), (int32_t)Q.size(2), (int32_t)K.size(2), (int32_t)Q.size(3), dtype, masked, scale_of(scale)};
     size_t bytes;
     check(bra_attention_workspace_bytes(&c.s, &bytes));       // the shape before the strides
     const char *text = "Q, K and V must be on one GPU, of one dtype, [B, N, heads, d] with channels next to each other and every row on 16 bytes";
@@ -771,13 +778,13 @@ const at::Tensor *workspace_if(const at::Tensor *ws, size_t bytes, const at::Ten
 PyObject *py_attention_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 10, [&]() -> PyObject * {
+        const bool want_lse = truth(a[7]);
         const at::Tensor &Q = need(a[0]), &K = need(a[1]), &V = need(a[2]);
         const AttentionCall c = attention_call(Q, K, V, a[3], a[4], a[5], a[6]);
         const at::Tensor *out = tensor(a[9]);
         const c10::DeviceGuard guard(Q.device());
         at::Tensor own, lse, O = out ? *out : at::empty(Q.sizes(), Q.options());
         const bra_rows o = rows_of(O, Q, Q.sizes(), "out must be a tensor of Q's shape and dtype on its GPU, channels next to each other and every row on 16 bytes");
-        const bool want_lse = PyObject_IsTrue(a[7]);
         if (want_lse) lse = at::empty({Q.size(0), Q.size(2), Q.size(1)}, Q.options().dtype(at::kFloat));
         size_t bytes = 0;
         check(bra_attention_workspace_bytes(&c.s, &bytes));
