@@ -403,7 +403,8 @@ def bra_attention_backward(Q, K, V, O, lse, dO, *, causal=False, q_lens=None, k_
 
 def rotary_table(H, W=None, channels=64, base=10000.0, device=None):
     """(cos, sin) [positions, channels / 2] float32 for bra_qk_norm_forward, angles formed in 64 bits: position n turns pair p by n base^(-2 p / channels).
-    With W for a map of H x W tokens: the first half of the pairs by a token's row, the second by its column, each as a table of channels / 2."""
+    With W for a map of H x W tokens: the first half of the pairs by a token's row, the second by its column, each as a table of channels / 2.
+    device: where the table is made (None: torch's default, the host as a rule); bra_qk_norm_forward takes it on the queries' GPU."""
     if channels < 0 or channels % (2 if W is None else 4):
         raise ValueError("channels must be a multiple of 2, of 4 for a map")
     at = lambda n, c: torch.arange(n, dtype=torch.float64, device=device)[:, None] * base ** (-torch.arange(0, c, 2, dtype=torch.float64, device=device) / max(c, 1))
