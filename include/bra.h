@@ -342,19 +342,22 @@ int bra_adamw_step(const bra_adamw_tensor *tensors, int32_t count, const bra_ada
  *     P = exp(S - max S) on the visible keys,  O_a[i] = sum_j P[i,j] V[j] / sum_j P[i,j],  lse_a[i] = log sum_j exp S[i,j]
  * nq, nk: Nq and Nk, or q_lens[b] and k_lens[b] (int32 [B] on the device, read when the kernel runs and clamped to 0 .. Nq and 0 .. Nk) where given.
  * A query with no visible key (or none of finite score) has O = 0 and lse = -infinity; so do the queries from nq on.  Keys and values from nk
- * on, queries and what comes back from nq on are not read; what is read beyond a causal mask's edge must be finite.
+ * on, queries and what comes back from nq on are not read; what is read beyond a causal mask's edge must be finite, and so must its products
+ * (S, and dO V backward) in float32.
  * A tensor [B, N, heads, d] is given by a bra_rows: its element (b, n, h, c) lies at data + b batch + n token + h head + c, in elements, so that
  * parts of one buffer, or a cache with the heads outside, are taken as they lie.  Pointers, and strides in bytes, are multiples of 16 (the stride
  * of a dimension of one entry is not looked at); inputs may have strides of 0.  What is written overlaps neither itself nor
  * anything else of the call (OVERLAP: places are compared exactly, but for tensors whose dimensions run through each other, which count as overlapping where 4096 steps do not
  * tell); the workspace is memory of its own.
- * d: a multiple of 8 up to 128 (heads that are no multiple of 32 wide take the time of the next one).  bf16 tensors: P is rounded to bf16 before its product
+ * d: a multiple of 8 up to 128.  A width takes the time of the next of 32, 64, 96 and 128, or up to a tenth more where it is not 32, 64 or 128; gradients in bf16 with a number of
+ * heads to a key head that does not divide 32 run up to a quarter below the rate of the powers of two beside it.  bf16 tensors: P is rounded to bf16 before its product
  * with V, everything else is float32.  float32 tensors: products of three bf16 terms per operand (relative error of a product 2^-23; a value that is not
  * finite, or above 3.3e38, makes NaN of what depends on it), up to 32 rows (queries times heads / kv_heads) forward the float32 matrix instruction.
  * scale <= 0 selects 1 / sqrt(d).  No atomic adds: a repeat gives the same bits.  Nothing else than `ws` is needed; its size depends on the shape and
  * may be 0.
  * Errors: NULL; SHAPE (B, Nq, Nk < 0 or above 2^28, kv_heads < 1 or not a divisor of heads, heads above 65536, d < 1, a scale that is not finite or above 1e38, negative
- * strides, places 2^56 bytes from data and further, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d); WORKSPACE; ALIGN; OVERLAP; LAUNCH. */
+ * strides, places 2^56 bytes from data and further, B heads or Nq heads above 2^30, B heads Nq or B heads Nk above 2^40); DTYPE; UNSUPPORTED (d; float32 tensors
+ * that need 2^32 workgroups for their terms, 26 TB of workspace); WORKSPACE; ALIGN; OVERLAP; LAUNCH. */
 typedef struct bra_attention_shape {
     int32_t B, Nq, Nk;        /* sequences; queries and keys of each, at most */
     int32_t heads, kv_heads;  /* heads of the queries, of keys and values */

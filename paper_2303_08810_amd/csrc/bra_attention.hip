@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * WAVES, D > 64 ? 1 : 2) void k_attention_few(Ca
 }
 
 // Many rows: the wavefronts of a workgroup have 32 rows each and share tiles of KT keys and values, the next of which is on its way.  Heads of 128 are bound by
-// the matrix cores at the clock that the card's power leaves them (1.8 GHz): 8192 causal tokens of 32 / 8 heads 520 to 540 us, 1.02 to 1.06 PFLOP/s, where a large
+// the matrix cores at the clock that the card's power leaves them (1.8 GHz): 8192 causal tokens of 32 / 8 heads 520 to 555 us, 0.99 to 1.06 PFLOP/s by the card, where a large
 // product of the library reaches 1.15.  Heads of 64 by the vector instructions, 16 exponentials of 16 cycles and 40 others of 4 to 256 cycles of products:
 // 32 x 1024 tokens of 12 heads 130 us, 2 x 8192 of 16 heads 563 us, 0.98 PFLOP/s.  float32: six products for one, 8 x 1000 of 8 heads of 64 98 us with the
 // terms, 168 TFLOP/s (the float32 instruction has 154 at most).

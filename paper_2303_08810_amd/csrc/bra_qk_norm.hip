@@ -135,8 +135,9 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (
     }
 }
 
-// Both passes at what a copy reaches, about 5 TB/s: 32 x 1024 tokens of 12 + 12 heads of 64 40 us (201 MB); backward 2 x 8192 of 32 + 8 heads of 128 113 us
-// (506 MB in 99 at that rate; its sums keep it at two workgroups to a compute unit).  One token: 6 us, the call on the host; the kernel 2.8.
+// Bound by memory, near what a copy reaches (5.1 TB/s): 32 x 1024 tokens of 12 + 12 heads of 64 41 to 44 us, 4.6 to 4.9 TB/s; backward 2 x 8192 of 32 + 8 heads of 128 114 us,
+// 4.4 TB/s (its sums keep it at two workgroups to a compute unit).  Backward in float32, 6475 tokens of 6 + 6 heads of 40: 13 us where the bytes take 7: the 512 workgroups take three
+// turns for 2.37 turns' rows, and three of a team's eight lanes have no channels.  One token: 6 us, the call on the host; the kernel 2.8.
 template <class E, int V, int RPT, bool BACK>
 __global__ __launch_bounds__(kThreads) void k_qk_norm(Work W)
 {
